@@ -340,6 +340,62 @@ int32_t gspmd_resharded_dot(const gspmd_mesh* mesh, const gspmd_dot_dims* dims,
                             const int64_t* lhs_fill, int32_t epilogue,
                             void* workspace, int64_t workspace_bytes, void* hip_stream);
 
+/* Losses over a vocabulary that is split on the mesh: what a partitioned language model ends in.
+ *
+ * Activations x [T, M] (dimension 0 split over a mesh dimension or whole) and the vocabulary matrix w, [V, M] (vocab_dim 0) or [M, V]
+ * (vocab_dim 1), its vocabulary dimension split over another mesh dimension or whole, M whole in both, have logits z[t, v] = sum_m x[t, m] w[v, m].  The
+ * calls compute, per token, a loss on them, and on request the gradients of sum_t weight[t] * loss[t] with respect to x and w, for ALL partitions of the mesh:
+ *   lse[t]  = log sum_v exp(z[t, v] / tau)                               (the AllReduce of a maximum and a sum over the vocabulary's mesh dimension)
+ *   D[t, v] = weight[t] / tau * (exp(z[t, v] / tau - lse[t]) - p[t, v])   p: the targets' shares, below
+ *   dx = D w,  dw = D^T x                                                (summed over the vocabulary's and the tokens' mesh dimension, as an AllReduce)
+ * The logits of all tokens are never held: tokens go through the workspace in pieces of at most 1 GiB of logits (less where the workspace is smaller).
+ * Operands are bf16 or f32; logits, maxima, sums and losses are fp32; D is rounded once to the operands' type, as an operand of the
+ * products that make the gradients, which accumulate in fp32 and are stored in that type.  A weight of 0 makes a token's D zero whatever its logits are; its x still
+ * enters dw's sums, times 0, so x must be finite there (padding beyond the valid lengths may hold anything).  Logits that are NaN, +infinity or -infinity throughout give NaN. */
+#define GSPMD_MAX_TARGETS 1024
+
+/* One partition's arrays per token (device memory, dense, of the static token count of x's shard; padding may hold anything in the inputs and is written as 0 in
+ * loss and lse).  Partitions of the same tokens may pass the same pointers (loss and lse are then written once). */
+typedef struct {
+  const int32_t* ids;     /* [tokens, targets]: vocabulary entries (0 .. V - 1); any other value: no target there */
+  const void* logits;     /* [tokens, targets]: the teacher's logits of these entries (gspmd_softmax_distill), ignored elsewhere */
+  int32_t logits_dtype;   /* gspmd_dtype of `logits`, the same for all partitions */
+  const float* weights;   /* [tokens], NULL: all 1 */
+  float* loss;            /* [tokens], out: without the weight */
+  float* lse;             /* [tokens], out; NULL: not wanted */
+} gspmd_token_buf;
+
+/* Bytes of device workspace for these losses: `bytes` for the fewest pieces that they are computed in, `least` (nullable) the least that a call accepts.
+ * dtype: of the operands; gradients: whether dx or dw will be asked for.  Pure host work. */
+int32_t gspmd_softmax_workspace_bytes(const gspmd_mesh* mesh, const gspmd_sharding* x_sh, const gspmd_sharding* w_sh,
+                                      int32_t vocab_dim, int32_t dtype, int32_t gradients, int64_t* bytes, int64_t* least);
+
+/* Softmax cross entropy: one label per token (ids [tokens]), loss[t] = lse[t] - z[t, label], tau = 1, p one at the label.  A token without
+ * a label (an id outside 0 .. V - 1) has loss 0 and takes no part in the gradients.
+ * x_shards, w_shards, tokens, dx_shards, dw_shards: host arrays of P entries indexed by partition id; the gradients' shards have the shapes and type of x's and w's, each
+ * array may be NULL (that gradient is not computed), partitions that hold the same data may share a buffer (the same one with the same row stride) and others
+ * receive it each; padding is written as 0.  Gradients must not overlap the operands.
+ * The call enqueues kernels only, and may be recorded into a HIP graph, up to 32 pairs of a token shard and a vocabulary shard.  Equal calls (workspace size included)
+ * give equal bits.  GSPMD_ERR_NEEDS_RESHARD if M is split, or tokens and vocabulary over one mesh dimension; GSPMD_ERR_BAD_DOT_DIMS for shapes that do not belong together. */
+int32_t gspmd_softmax_xent(const gspmd_mesh* mesh,
+                           const gspmd_shard_buf* x_shards, const gspmd_sharding* x_sh,
+                           const gspmd_shard_buf* w_shards, const gspmd_sharding* w_sh, int32_t vocab_dim,
+                           const gspmd_token_buf* tokens,
+                           const gspmd_shard_buf* dx_shards, const gspmd_shard_buf* dw_shards,
+                           void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* Distillation from a teacher's top logits: `targets` (1 .. GSPMD_MAX_TARGETS) entries per token, ids and logits [tokens, targets]; an entry whose id is outside
+ * 0 .. V - 1 is absent.  With tau = temperature (positive, finite) and p = softmax over a token's entries of logits / tau,
+ *   loss[t] = sum_k p_k (log p_k - (z[t, id_k] / tau - lse[t])),   0 log 0 = 0:
+ * the divergence of the student's distribution from the teacher's over its entries.  An id given twice counts twice.  A token without entries (or with logits of -infinity only) has loss 0
+ * and takes no part in the gradients.  (A loss scaled by tau^2 is one with weights scaled by it.)  Other arguments as gspmd_softmax_xent. */
+int32_t gspmd_softmax_distill(const gspmd_mesh* mesh,
+                              const gspmd_shard_buf* x_shards, const gspmd_sharding* x_sh,
+                              const gspmd_shard_buf* w_shards, const gspmd_sharding* w_sh, int32_t vocab_dim,
+                              const gspmd_token_buf* tokens, int32_t targets, float temperature,
+                              const gspmd_shard_buf* dx_shards, const gspmd_shard_buf* dw_shards,
+                              void* workspace, int64_t workspace_bytes, void* hip_stream);
+
 /* Utility (no counterpart in the paper; a profiling aid for the MFMA contraction kernel).  While a record buffer is
  * set, every later Dot launch of this process (any entry point, any stream) makes workgroup b < n_records of its
  * MFMA kernel write record b: eight 64-bit words of the GPU's 100 MHz constant-rate counter at kernel entry (bits

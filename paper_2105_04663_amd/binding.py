@@ -22,8 +22,10 @@ EXPORTED_SYMBOLS = (
     "gspmd_shard_assemble", "gspmd_plan_dot", "gspmd_infer_out_sharding", "gspmd_reshard_workspace_bytes", "gspmd_reshard",
     "gspmd_compatible_operand_shardings", "gspmd_resharded_dot_workspace_bytes", "gspmd_resharded_dot",
     "gspmd_grouped_dot_noalloc", "gspmd_set_tile_timeline",
+    "gspmd_softmax_workspace_bytes", "gspmd_softmax_xent", "gspmd_softmax_distill",
 )
 TILE_TIMELINE_WORDS = 8
+MAX_TARGETS = 1024
 NOALLOC_MAX_WORKSPACE_BYTES = 32 * 1024 * 1024
 
 
@@ -53,6 +55,11 @@ class _CShardBuf(C.Structure):
 # what _bufs writes its words by
 if (sys.byteorder, C.sizeof(_CShardBuf), _CShardBuf.data.offset, _CShardBuf.dtype.offset, _CShardBuf.row_stride.offset) != ("little", 24, 0, 8, 16):
     raise ImportError("unexpected layout of gspmd_shard_buf")
+
+
+class _CTokenBuf(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("logits", C.c_void_p), ("logits_dtype", C.c_int32), ("weights", C.c_void_p), ("loss", C.c_void_p),
+                ("lse", C.c_void_p)]
 
 
 class _CGemmDesc(C.Structure):
@@ -102,6 +109,9 @@ def load_library():
     lib.gspmd_resharded_dot.argtypes = [pm, pd, pbs, ps, pbs, ps, pbs, ps, pi64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
     lib.gspmd_plan_dot.argtypes = [pm, pd, ps, ps, ps, C.c_int64, C.c_int64, C.c_int64, C.c_int64, pi64,
                                    C.POINTER(_CGemmDesc), C.c_int64, pi64]
+    lib.gspmd_softmax_workspace_bytes.argtypes = [pm, ps, ps, C.c_int32, C.c_int32, C.c_int32, pi64, pi64]
+    lib.gspmd_softmax_xent.argtypes = [pm, pbs, ps, pbs, ps, C.c_int32, pbs, pbs, pbs, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.gspmd_softmax_distill.argtypes = [pm, pbs, ps, pbs, ps, C.c_int32, pbs, C.c_int32, C.c_float, pbs, pbs, C.c_void_p, C.c_int64, C.c_void_p]
     lib.gspmd_set_tile_timeline.argtypes = [C.c_void_p, C.c_int64]
     for name in EXPORTED_SYMBOLS[1:]:
         getattr(lib, name).restype = C.c_int32
@@ -444,3 +454,54 @@ def shard_assemble(mesh: Mesh, sharding: Sharding, partition_id: int, shard: Sha
 def set_tile_timeline(device_records: int, n_records: int) -> None:
     """gspmd_set_tile_timeline: device_records = address of n_records * 64 bytes of cleared device memory, or 0 to switch off."""
     _check(load_library().gspmd_set_tile_timeline(C.c_void_p(int(device_records) or None), int(n_records)), "gspmd_set_tile_timeline")
+
+
+@dataclass
+class TokenBuf:
+    """One partition's arrays per token: addresses in device memory (0 = none), dense, of the static token count of x's shard."""
+    ids: int               # int32 [tokens, targets]
+    loss: int              # float32 [tokens]
+    lse: int = 0           # float32 [tokens]
+    weights: int = 0       # float32 [tokens]
+    logits: int = 0        # [tokens, targets], the teacher's
+    logits_dtype: int = F32
+
+
+def _token_bufs(tokens: Sequence[TokenBuf]):
+    return (_CTokenBuf * max(1, len(tokens)))(*[_CTokenBuf(b.ids or None, b.logits or None, b.logits_dtype, b.weights or None, b.loss or None, b.lse or None)
+                                                for b in tokens])
+
+
+def softmax_workspace_bytes(mesh: Mesh, x_sh: Sharding, w_sh: Sharding, vocab_dim: int, dtype: int, gradients: bool, least: bool = False) -> int:
+    """Bytes of workspace for softmax_xent and softmax_distill in the fewest pieces, or (`least`) the least that they accept."""
+    m, a, b = mesh._c(), x_sh._c(), w_sh._c()
+    n, few = C.c_int64(0), C.c_int64(0)
+    _check(load_library().gspmd_softmax_workspace_bytes(C.byref(m), C.byref(a), C.byref(b), int(vocab_dim), int(dtype), int(gradients), C.byref(n), C.byref(few)),
+           "gspmd_softmax_workspace_bytes")
+    return few.value if least else n.value
+
+
+def _loss_shards(mesh: Mesh, x_shards, w_shards, tokens, dx_shards, dw_shards):
+    if any(s is not None and len(s) != mesh.n_partitions for s in (x_shards, w_shards, tokens, dx_shards, dw_shards)):
+        raise ValueError("one shard buffer per partition is required")
+    return [None if s is None else _bufs(s) for s in (x_shards, w_shards, dx_shards, dw_shards)]
+
+
+def softmax_xent(mesh: Mesh, x_shards: Sequence[ShardBuf], x_sh: Sharding, w_shards: Sequence[ShardBuf], w_sh: Sharding, tokens: Sequence[TokenBuf],
+                 vocab_dim: int = 0, dx_shards: Optional[Sequence[ShardBuf]] = None, dw_shards: Optional[Sequence[ShardBuf]] = None,
+                 workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Softmax cross entropy over the split vocabulary, per token, and on request its gradients (gspmd_softmax_xent)."""
+    m, a, b = mesh._c(), x_sh._c(), w_sh._c()
+    xs, ws, dxs, dws = _loss_shards(mesh, x_shards, w_shards, tokens, dx_shards, dw_shards)
+    _check(load_library().gspmd_softmax_xent(C.byref(m), xs, C.byref(a), ws, C.byref(b), int(vocab_dim), _token_bufs(tokens), dxs, dws,
+                                             C.c_void_p(workspace), int(workspace_bytes), C.c_void_p(stream)), "gspmd_softmax_xent")
+
+
+def softmax_distill(mesh: Mesh, x_shards: Sequence[ShardBuf], x_sh: Sharding, w_shards: Sequence[ShardBuf], w_sh: Sharding, tokens: Sequence[TokenBuf],
+                    targets: int, temperature: float = 1.0, vocab_dim: int = 0, dx_shards: Optional[Sequence[ShardBuf]] = None,
+                    dw_shards: Optional[Sequence[ShardBuf]] = None, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Distillation from a teacher's top logits, per token, and on request its gradients (gspmd_softmax_distill)."""
+    m, a, b = mesh._c(), x_sh._c(), w_sh._c()
+    xs, ws, dxs, dws = _loss_shards(mesh, x_shards, w_shards, tokens, dx_shards, dw_shards)
+    _check(load_library().gspmd_softmax_distill(C.byref(m), xs, C.byref(a), ws, C.byref(b), int(vocab_dim), _token_bufs(tokens), int(targets), float(temperature),
+                                                dxs, dws, C.c_void_p(workspace), int(workspace_bytes), C.c_void_p(stream)), "gspmd_softmax_distill")

@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "../../include/gspmd.h"
+#include "dots.h"
 #include "kernels_basic.h"
 #include "kernels_f32.h"
 #include "launch.h"
@@ -23,8 +24,6 @@ using namespace gspmd;
 static_assert(kF32Tile == kGenTile && kF32Threads == 256, "dot_f32_kernel and dot_fallback_kernel share their tiles and launch");
 
 namespace {
-
-constexpr int64_t kWsAlign = 256;
 
 // Workspace of gspmd_grouped_dot_noalloc: one copy per GPU the library is loaded on, held until the process ends.  In
 // host code the array's name is only a handle: its device address is looked up once per device (scratch_address).
@@ -724,6 +723,29 @@ int32_t launch_reduce_scatter(const gspmd_mesh* mesh, const gspmd_sharding* out_
 }
 
 }  // namespace
+
+namespace gspmd {
+
+int32_t run_dots(std::vector<Problem>& ps, int32_t layout, int32_t in_dtype, int32_t out_dtype, void* tables, int64_t table_bytes, hipStream_t stream) {
+  return launch_problems(ps, layout, in_dtype, out_dtype, GSPMD_EPILOGUE_NONE, false, tables, table_bytes, stream);
+}
+
+int32_t run_sum(const std::vector<float*>& partials, int64_t rows, int64_t cols, int64_t ld_in, void* out, int64_t ld_out, int32_t out_dtype, hipStream_t stream) {
+  if (t_pin.dry_run) return GSPMD_OK;
+  const float* some[kMaxPartials];
+  some[0] = partials[0];
+  for (size_t next = 1;;) {
+    int n = 1;
+    while (n < kMaxPartials && next < partials.size()) some[n++] = partials[next++];
+    const bool last = next == partials.size();
+    const int32_t st = launch_reduce(some, n, rows, cols, ld_in, last ? out : partials[0], last ? ld_out : ld_in, last ? out_dtype : GSPMD_F32, stream);
+    if (st != GSPMD_OK || last) return st;
+  }
+}
+
+bool launches_are_dry() { return t_pin.dry_run != 0; }
+
+}  // namespace gspmd
 
 extern "C" {
 

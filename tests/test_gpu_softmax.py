@@ -1,0 +1,199 @@
+"""Softmax cross entropy and distillation over a split vocabulary against float64, element by element, at the sizes, meshes and targets where they can go wrong."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2105_04663_amd as g
+from tests.losses import Problem
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab_dim", [0, 1])
+@pytest.mark.parametrize("T,M,V", [(1, 1, 1), (1, 8, 2), (2, 65, 7), (33, 64, 90), (65, 130, 257), (300, 72, 1025), (5, 257, 8200)])
+def test_xent(dtype, vocab_dim, T, M, V):
+    Problem(T, M, V, dtype, vocab_dim=vocab_dim, pad=(T + V) % 2 == 0).stage().call().check()
+
+
+# rows of every variant of the row kernel, at and beside the sizes where one takes over from another
+@pytest.mark.parametrize("V", [1023, 1024, 1025, 8191, 8192, 8193, 32768, 32769, 49152, 49153, 70001])
+@pytest.mark.parametrize("dtype,K", [("bf16", None), ("bf16", 5), ("f32", 5)])
+def test_rows(V, dtype, K):
+    Problem(3, 16, V, dtype, K=K, tau=1.5 if K else 1.0, missing=0.0).stage().call().check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K,tau,logits_dtype", [(1, 1.0, "f32"), (3, 2.0, "bf16"), (64, 0.5, "f32"), (100, 3.0, "bf16"), (1024, 1.0, "f32")])
+def test_distill(dtype, K, tau, logits_dtype):
+    Problem(37, 48, 1500, dtype, K=K, tau=tau, logits_dtype=logits_dtype).stage().call().check()
+
+
+MESHES = [dict(mesh=(1, 4)), dict(mesh=(3, 1)), dict(mesh=(2, 4), ids_order=(5, 2, 7, 0, 3, 1, 6, 4)), dict(mesh=(2, 2, 3), x_map=(2, -1), v_axis=0),
+          dict(mesh=(2, 2, 3), x_map=(2, -1), v_axis=0, share=False), dict(mesh=(8, 2)), dict(mesh=(2, 3), x_map=(-1, -1), v_axis=-1, share=False),
+          dict(mesh=(4, 1, 2), x_map=(0, 1), v_axis=2)]
+
+
+@pytest.mark.parametrize("where", MESHES, ids=lambda m: "x".join(map(str, m["mesh"])) + ("" if m.get("share", True) else "_own"))
+@pytest.mark.parametrize("dtype,K,vocab_dim,pad", [("bf16", None, 0, True), ("bf16", 7, 1, False), ("f32", None, 1, True)])
+def test_meshes(where, dtype, K, vocab_dim, pad):
+    Problem(41, 24, 203, dtype, K=K, vocab_dim=vocab_dim, pad=pad, **where).stage().call().check()
+
+
+@pytest.mark.parametrize("T,V,mesh", [(5, 9, (4, 4)), (1, 3, (3, 8)), (9, 65, (4, 5)), (2, 1, (2, 2)), (40, 300, (40, 1)), (70, 40, (66, 1)), (20, 130, (3, 17))])
+def test_partitions_without_tokens_or_entries(T, V, mesh):
+    for dtype, vocab_dim in (("bf16", 0), ("f32", 1)):
+        Problem(T, 24, V, dtype, vocab_dim=vocab_dim, mesh=mesh).stage().call().check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_tokens_and_no_hidden_dimension(dtype):
+    p = Problem(0, 24, 50, dtype, mesh=(1, 2)).stage().call()
+    assert not p.results()["dw"].any()
+    p = Problem(6, 0, 50, dtype).stage((False, False)).call()
+    got = p.results()
+    assert np.allclose(got["lse"], np.log(50.0), atol=1e-6)
+    assert np.allclose(got["loss"], np.where(p.ids[:, 0] >= 0, np.log(50.0), 0.0), atol=1e-6)
+
+
+@pytest.mark.parametrize("grad", [(False, False), (True, False), (False, True)])
+@pytest.mark.parametrize("K", [None, 4])
+def test_fewer_gradients(grad, K):
+    full = Problem(70, 40, 333, K=K).stage().call().results()
+    some = Problem(70, 40, 333, K=K).stage(grad).call().check()
+    for name in some:
+        if name in ("dx", "dw"):
+            assert np.array_equal(some[name], full[name])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_targets(dtype):
+    """Labels outside the vocabulary are none: loss 0, nothing in the gradients, bits of zero in all of them if no token has one."""
+    p = Problem(20, 16, 77, dtype, missing=0.0)
+    p.ids[:] = np.array([-1, 77, 78, 2 ** 31 - 1, -2 ** 31] * 4, dtype=np.int64).astype(np.int32)[:, None]
+    got = p.stage().call().check()
+    assert not got["loss"].any() and not got["dx"].any() and not got["dw"].any()
+    q = Problem(20, 16, 77, dtype, K=6, missing=1.0)
+    q.logits_t[:] = float("nan")                       # of entries that are absent
+    got = q.stage().call().results()
+    assert not got["loss"].any() and not got["dx"].any() and not got["dw"].any()
+
+
+def test_teachers_logits_at_the_ends():
+    p = Problem(6, 16, 77, K=4, missing=0.0)
+    p.ids[3] = [5, 5, 5, 9]                             # one entry given three times
+    for a in (p.logits, p.logits_t):
+        a[0, 1:] = -np.inf                              # one entry
+        a[1, :] = -np.inf                               # none
+        a[2, 0] = -3e38                                 # the type's lowest
+        a[4, 2] = 200.0                                 # all of it on one entry
+    got = p.stage().call().check()
+    assert got["loss"][1] == 0.0 and not got["dx"][1].any()
+
+
+def test_one_bad_token_leaves_the_others():
+    """A NaN among a token's teacher's logits, or in its activations, is a NaN in its own results; a weight of 0 keeps it out of D."""
+    ref = Problem(9, 16, 300, K=3, missing=0.0).stage((True, False)).call().results()
+    p = Problem(9, 16, 300, K=3, missing=0.0)
+    p.logits_t[2, 1] = float("nan")
+    p.logits_t[3, 0] = float("inf")
+    p.xt[5, 3] = float("nan")
+    p.weights[6] = 0.0
+    p.xt[6, 2] = float("inf")
+    got = p.stage((True, False)).call().results()
+    assert np.isnan(got["loss"][[2, 3, 5, 6]]).all() and np.isnan(got["dx"][[2, 3, 5]]).all()
+    assert not got["dx"][6].any()
+    for t in (0, 1, 4, 7, 8):
+        assert got["loss"][t] == ref["loss"][t] and np.array_equal(got["dx"][t], ref["dx"][t])
+
+
+def test_large_logits():
+    """Far beyond what exp takes: the maximum is subtracted."""
+    for dtype in ("bf16", "f32"):
+        p = Problem(17, 64, 500, dtype, wscale=40.0)
+        got = p.stage().call().check()
+        assert np.isfinite(got["loss"]).all() and np.abs(got["lse"]).max() > 500
+
+
+@pytest.mark.parametrize("dtype,K", [("bf16", None), ("bf16", 9), ("f32", None)])
+@pytest.mark.parametrize("mesh", [(1, 1), (2, 3)])
+def test_pieces(dtype, K, mesh):
+    """Less workspace: more pieces, down to one row of every token shard, the same results within their bounds; one byte less than the least is refused."""
+    p = Problem(75, 40, 600, dtype, K=K, mesh=mesh).stage()
+    p.call()
+    for n in (p.least, p.least + (p.bytes - p.least) // 3, max(p.least, p.bytes - 1), p.bytes, p.bytes + 100000):
+        for s in (p.dxs, p.dws):
+            for b in s:
+                b[1].fill_(float("nan"))
+        p.call(n).check()
+    with pytest.raises(g.GspmdError) as e:
+        p.call(p.least - 1)
+    assert e.value.status == 8
+
+
+def test_equal_calls_give_equal_bits():
+    for kw in (dict(), dict(mesh=(2, 4)), dict(dtype="f32", K=5)):
+        a, b = (Problem(200, 96, 1111, **kw).stage().call().results() for _ in range(2))
+        for name in a:
+            assert np.array_equal(a[name], b[name]), name
+
+
+@pytest.mark.parametrize("vocab_dim", [0, 1])
+def test_gradients_against_differences(vocab_dim):
+    """float32: the loss along a direction.  Its third derivative is below 8 |s|^3 (s: the largest change of a logit), a loss is 2^-20 off at most, so with h s = 0.05 a
+    central difference is within 8 * 0.05^2 s / 6 + 2^-20 T / h of the derivative."""
+    rng = np.random.default_rng(5)
+    for K in (None, 4):
+        p = Problem(6, 12, 40, "f32", K=K, vocab_dim=vocab_dim, weights=False)
+        got = p.stage().call().results()
+        for which in ("x", "w"):
+            base, grad = getattr(p, which), got["d" + which]
+            direction = rng.standard_normal(base.shape)
+            s = np.abs(direction @ p.w.T if which == "x" else p.x @ direction.T).max()
+            h = 0.05 / s
+            at = []
+            for sign in (1, -1):
+                q = Problem(6, 12, 40, "f32", K=K, vocab_dim=vocab_dim, weights=False)
+                t = torch.from_numpy((base + sign * h * direction).astype(np.float32))
+                setattr(q, which + "t", t)
+                at.append((q.stage((False, False)).call().results()["loss"].sum(), t.double().numpy()))
+            step = at[0][1] - at[1][1]                  # as the type holds it
+            assert abs((at[0][0] - at[1][0]) / (2 * h) - (grad * step).sum() / (2 * h)) <= 6 * (8 * 0.05 ** 2 * s / 6) + 6 * 2.0 ** -20 / h
+
+
+def test_another_stream_and_a_graph():
+    p = Problem(130, 64, 700, mesh=(2, 2)).stage()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    p.call(stream=stream.cuda_stream)
+    stream.synchronize()
+    ref = p.check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.call(stream=torch.cuda.current_stream().cuda_stream)
+    for turn in range(4):
+        for s in (p.dxs, p.dws):
+            for b in s:
+                b[1].fill_(float(turn))
+        p.xs[0][1][:3].mul_(-1.0)                       # other inputs for every replay
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [b[1].clone() for b in p.dxs + p.dws] + [t[1]["loss"].clone() for t in p.ts]
+        p.call()
+        torch.cuda.synchronize()
+        for a, b in zip(replayed, [b[1] for b in p.dxs + p.dws] + [t[1]["loss"] for t in p.ts]):
+            assert torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0))
+    assert np.isfinite(ref["loss"]).all()
+
+
+def test_random_problems():
+    """Sizes, meshes and layouts drawn together."""
+    rng = np.random.default_rng(77)
+    for n in range(40):
+        T, M, V = (int(np.exp(rng.uniform(0, np.log(hi)))) for hi in (400, 300, 3000))
+        K = None if rng.random() < 0.5 else int(rng.integers(1, 40))
+        p = Problem(T, M, V, "bf16" if rng.random() < 0.7 else "f32", K=K, tau=float(rng.choice([0.7, 1.0, 2.5])) if K else 1.0, seed=n, vocab_dim=int(rng.integers(0, 2)),
+                    mesh=(int(rng.integers(1, 5)), int(rng.integers(1, 7))), pad=bool(rng.integers(0, 2)), share=bool(rng.integers(0, 2)), weights=bool(rng.integers(0, 2)))
+        print(n, T, M, V, p.dtype, K, p.mesh.shape, p.vocab_dim, p.pad, flush=True)
+        p.stage().call().check()
