@@ -373,7 +373,7 @@ int32_t gspmd_softmax_workspace_bytes(const gspmd_mesh* mesh, const gspmd_shardi
 /* Softmax cross entropy: one label per token (ids [tokens]), loss[t] = lse[t] - z[t, label], tau = 1, p one at the label.  A token without
  * a label (an id outside 0 .. V - 1) has loss 0 and takes no part in the gradients.
  * x_shards, w_shards, tokens, dx_shards, dw_shards: host arrays of P entries indexed by partition id; the gradients' shards have the shapes and type of x's and w's, each
- * array may be NULL (that gradient is not computed), partitions that hold the same data may share a buffer (the same one with the same row stride) and others
+ * array may be NULL (that gradient is not computed); all shards of one tensor have one row stride; partitions that hold the same data may share a buffer, others
  * receive it each; padding is written as 0.  Gradients must not overlap the operands.
  * The call enqueues kernels only, and may be recorded into a HIP graph, up to 32 pairs of a token shard and a vocabulary shard.  Equal calls (workspace size included)
  * give equal bits.  GSPMD_ERR_NEEDS_RESHARD if M is split, or tokens and vocabulary over one mesh dimension; GSPMD_ERR_BAD_DOT_DIMS for shapes that do not belong together. */

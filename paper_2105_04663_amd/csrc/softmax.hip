@@ -1,8 +1,9 @@
 // Losses over a split vocabulary (include/gspmd.h: gspmd_softmax_xent, gspmd_softmax_distill).
 //
-// The logits of a piece of tokens (some rows of every token shard, all of the vocabulary) go to the workspace as float32, one product per pair of token shard and vocabulary
-// shard; softmax_rows_kernel makes of each row the token's loss and, in place, D, the gradient with respect to the logits; two more products make of D the piece's rows of dx
-// and its share of dw.  Sums over shards (dx over the vocabulary's, dw over the tokens') and over pieces (dw) are float32 partials, added up in ascending order.
+// Tokens are taken in pieces, in the order of all shards together.  A piece's logits go to the workspace as float32; softmax_rows_kernel makes of each row the token's loss
+// and, in place, D, the gradient with respect to the logits; two more products make of D the piece's rows of dx and its share of dw.
+// dx is a sum over the vocabulary.  Where the tokens give it too few output tiles to fill the chip, or the vocabulary's shards lie apart, its ranges are products of their own, float32 partials
+// that add_up_kernel adds in ascending order.  dw is a sum over the tokens: x from several shards is put together first (it is small beside w), and pieces add up in float32.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -19,9 +20,11 @@
 namespace gspmd {
 namespace {
 
-// Logits of a piece, at most (float32; at least one row of every token shard): what the workspace query provides for.
+// Logits of a piece, at most (float32; at least one token's): what the workspace query provides for.
 constexpr int64_t kPieceBytes = int64_t(1) << 30;
 constexpr int64_t kColumnAlign = 64;
+// Up to so many tokens what D's rounding to bfloat16 loses takes part in the products, as rows of its own: these are bound by w and dw then.
+constexpr int64_t kFewTokens = 64;
 
 struct Loss {
   const gspmd_mesh* mesh = nullptr;
@@ -33,24 +36,40 @@ struct Loss {
   int32_t dtype = 0;
   bool dx = false, dw = false;
   int64_t esize() const { return dtype == GSPMD_BF16 ? 2 : 4; }
-  int64_t valid_t(int64_t i) const { return std::max<int64_t>(0, std::min(ts, T - i * ts)); }
   int64_t valid_v(int64_t j) const { return std::max<int64_t>(0, std::min(vs, V - j * vs)); }
-  // logits: the vocabulary shards that hold any entry, one after the other
-  int64_t shards_v() const { return vs > 0 ? (V + vs - 1) / vs : 0; }
-  int64_t per_cols() const { return round_up(std::max<int64_t>(vs, 1), kColumnAlign); }
-  int64_t ldz() const { return std::max<int64_t>(shards_v(), 1) * per_cols(); }
-  int64_t dw_rows() const { return vocab_dim == 0 ? vs : M; }
-  int64_t dw_cols() const { return vocab_dim == 0 ? M : vs; }
-  // fp32 partials: dx of each vocabulary shard, dw of each token shard and (several pieces) of the pieces before
-  bool parts_dx() const { return dx && nb > 1; }
-  int64_t dw_partials(bool pieces) const { return dw && (na > 1 || pieces) ? na + (pieces ? 1 : 0) : 0; }
-  int64_t row_bytes() const {                // workspace per row of a token shard
-    return na * (ldz() * 4 + (parts_dx() ? nb * round_up(M, 4) * 4 : 0));
+  // a row of logits: the vocabulary shards that hold any entry, one after the other
+  int64_t windows() const { return (V + vs - 1) / vs; }
+  int64_t per_cols() const { return round_up(vs, kColumnAlign); }
+  int64_t cols() const { return (windows() - 1) * per_cols() + valid_v(windows() - 1); }
+  int64_t ldz() const { return windows() * per_cols(); }
+  int64_t w_rows() const { return vocab_dim == 0 ? vs : M; }
+  int64_t w_cols() const { return vocab_dim == 0 ? M : vs; }
+  // both parts of D
+  bool with_lost() const { return (dx || dw) && dtype == GSPMD_BF16 && T <= kFewTokens; }
+  int64_t parts() const { return with_lost() ? 2 : 1; }
+  int64_t ldx() const { return round_up(std::max<int64_t>(M, 1), kColumnAlign); }        // of x put together
+  int64_t ld_sum() const { return round_up(std::max<int64_t>(M, 1), 4); }                // of dx's partials
+  // ranges of a window whose products make dx, for pieces of `rows` tokens
+  int64_t ranges(int64_t rows) const {
+    if (!dx || rows == 0) return 1;
+    const int64_t few = rows * parts() <= 128, edge = dtype == GSPMD_F32 || few ? 64 : 256;
+    const int64_t tiles = ((rows * parts() + edge - 1) / edge) * ((M + edge - 1) / edge), want = dtype == GSPMD_F32 ? 1024 : few ? 512 : 256;
+    const int64_t least = dtype == GSPMD_F32 || few ? 512 : 2048;                        // entries of a range
+    return std::max<int64_t>(1, std::min({want / std::max<int64_t>(tiles, 1), vs / least, 32 / windows(), int64_t(16)}));
   }
-  int64_t dw_bytes(bool pieces) const { return dw_partials(pieces) * nb * round_up(dw_rows() * round_up(dw_cols(), 4) * 4, kWsAlign); }
-  int64_t table_bytes() const { return round_up((na * nb * 2 + 1) * kTableBytesPerProblem, kWsAlign); }
-  int64_t fixed_bytes(bool pieces) const { return table_bytes() + dw_bytes(pieces) + 4 * kWsAlign; }
-  int64_t whole_rows() const { return std::min<int64_t>(ts, std::max<int64_t>(T, 0)); }
+  bool adds_up(int64_t rows) const { return dx && (windows() * ranges(rows) > 1 || with_lost()); }
+  int64_t most_rows() const { return std::min(T, std::max<int64_t>(1, kPieceBytes / (ldz() * 4))); }
+  // Copies of operands whose rows are not padded to 16 bytes, which the products read several times slower than they are copied once: from this many rows of products on.
+  bool packing_pays() const { return dtype == GSPMD_BF16 && T * (dx || dw ? 3 : 1) >= 1024; }
+  int64_t packed_w_bytes() const { return round_up((vocab_dim == 0 ? ldz() * ldx() : std::max<int64_t>(M, 1) * ldz()) * esize(), kWsAlign); }
+  // ---- the workspace, for pieces of `rows` tokens
+  int64_t table_bytes() const { return round_up((na * nb + 32 + nb) * kTableBytesPerProblem, kWsAlign); }
+  int64_t x_bytes(int64_t rows) const { return round_up(rows * parts() * ldx() * esize(), kWsAlign); }
+  int64_t z_bytes(int64_t rows) const { return round_up(rows * parts() * ldz() * 4, kWsAlign); }
+  int64_t sum_bytes(int64_t rows) const { return adds_up(rows) ? round_up(windows() * ranges(rows) * parts() * rows * ld_sum() * 4, kWsAlign) : 0; }
+  int64_t dw_size() const { return round_up(w_rows() * round_up(w_cols(), 4) * 4, kWsAlign) / 4; }                 // float32 elements of a shard's partial
+  int64_t dw_bytes(int64_t rows) const { return dw && rows < T ? 2 * nb * dw_size() * 4 : 0; }
+  int64_t bytes(int64_t rows) const { return table_bytes() + x_bytes(rows) + z_bytes(rows) + sum_bytes(rows) + dw_bytes(rows); }
 };
 
 // Shapes, shardings and the extents that follow from them.
@@ -78,7 +97,7 @@ int32_t analyse(const gspmd_mesh* mesh, const gspmd_sharding* x_sh, const gspmd_
   l->ts = (l->T + l->na - 1) / l->na;
   l->vs = (l->V + l->nb - 1) / l->nb;
   constexpr int64_t kMost = INT32_MAX >> 2;                  // of a padded row of logits as of every extent
-  if (l->T > kMost || l->M > kMost || l->ldz() > kMost || l->na * l->nb > kMaxProblems / 2) return GSPMD_ERR_UNSUPPORTED;
+  if (l->T > kMost || l->M > kMost || l->V > kMost || l->ldz() > kMost || l->na * l->nb > kMaxProblems / 2) return GSPMD_ERR_UNSUPPORTED;
   return GSPMD_OK;
 }
 
@@ -87,16 +106,15 @@ struct Buffers {                             // the distinct ones of one positio
   std::vector<gspmd_shard_buf> others;
 };
 
-int32_t add_buffer(std::vector<Buffers>& at, int64_t pos, bool seen, const gspmd_shard_buf& b) {
+void add_buffer(std::vector<Buffers>& at, int64_t pos, bool seen, const gspmd_shard_buf& b) {
   Buffers& here = at[static_cast<size_t>(pos)];
   if (!seen) {
     here.first = b;
-    return GSPMD_OK;
+    return;
   }
-  if (b.data == here.first.data) return b.row_stride == here.first.row_stride ? GSPMD_OK : GSPMD_ERR_BAD_BUFFER;
-  for (const auto& o : here.others) if (o.data == b.data) return GSPMD_OK;
+  if (b.data == here.first.data) return;
+  for (const auto& o : here.others) if (o.data == b.data) return;
   here.others.push_back(b);
-  return GSPMD_OK;
 }
 
 // A shard's row stride in elements, or -1.
@@ -105,59 +123,40 @@ int64_t stride_of(const gspmd_shard_buf& b, int64_t cols) {
   return ld < cols || ld > INT32_MAX ? -1 : std::max<int64_t>(ld, 1);
 }
 
-// A group of products that add up to one output block.
-struct Sum {
-  std::vector<Problem> members;              // same valid output extents where they have any K; C is set by run_sums
-  void* out;
-  int32_t ld_out, rows, cols;                // static extents
-  float* earlier = nullptr;                  // what pieces before have added up (dense, ld of the partials), and goes on in
-  float* partials = nullptr;                 // room for the members, ld of the partials
-};
+bool padded(const gspmd_shard_buf& b, int64_t ld) { return !(reinterpret_cast<uintptr_t>(b.data) & 15) && !(ld & 7); }
 
-int32_t run_sums(std::vector<Sum>& sums, int32_t layout, int32_t dtype, bool first, bool last, void* tables, int64_t table_bytes, hipStream_t stream) {
-  std::vector<Problem> launch;
-  size_t most = 0;
-  for (auto& s : sums) most = std::max(most, static_cast<size_t>(std::count_if(s.members.begin(), s.members.end(), [](const Problem& p) { return p.Kv > 0; })));
-  const bool direct = most <= 1 && first && last;
-  auto add = [&](Problem p, void* c, int64_t ldc, const Sum& s) {
-    p.C = c;
-    p.ldc = static_cast<int32_t>(ldc);
-    p.Ms = s.rows;
-    p.Ns = s.cols;
-    if (p.Mv == 0 || p.Nv == 0 || p.Kv == 0) p.Mv = p.Nv = p.Kv = 0;
-    launch.push_back(p);
-  };
-  for (auto& s : sums) {
-    std::stable_partition(s.members.begin(), s.members.end(), [](const Problem& p) { return p.Kv > 0; });
-    const int64_t ld = round_up(s.cols, 4), size = static_cast<int64_t>(s.rows) * ld;
-    if (direct) {
-      add(s.members[0], s.out, s.ld_out, s);
-    } else {
-      for (size_t m = 0; m < s.members.size(); ++m)
-        if (m == 0 || s.members[m].Kv > 0) add(s.members[m], s.partials + static_cast<int64_t>(m) * size, ld, s);
-    }
-  }
-  int32_t st = run_dots(launch, layout, dtype, direct ? dtype : static_cast<int32_t>(GSPMD_F32), tables, table_bytes, stream);
-  if (st != GSPMD_OK || direct) return st;
-  for (auto& s : sums) {
-    const int64_t ld = round_up(s.cols, 4), size = static_cast<int64_t>(s.rows) * ld;
-    std::vector<float*> parts;
-    if (!first) parts.push_back(s.earlier);
-    for (size_t m = 0; m < s.members.size(); ++m)
-      if (m == 0 || s.members[m].Kv > 0) parts.push_back(s.partials + static_cast<int64_t>(m) * size);
-    if ((st = run_sum(parts, s.rows, s.cols, ld, last ? s.out : s.earlier, last ? s.ld_out : ld, last ? dtype : static_cast<int32_t>(GSPMD_F32), stream)) != GSPMD_OK) return st;
-  }
-  return GSPMD_OK;
-}
-
-template <typename T, bool GRAD>
+template <typename T, bool GRAD, bool LOST>
 void launch_rows_as(const SoftmaxRows& a, unsigned rows, hipStream_t stream) {
   const size_t lds = static_cast<size_t>(a.targets) * 12;
-  if (a.cols <= 64 * 4 * 4) hipLaunchKernelGGL((softmax_rows_kernel<T, 64, 4, false, GRAD>), dim3(rows), dim3(64), lds, stream, a);
-  else if (a.cols <= 256 * 4 * 8) hipLaunchKernelGGL((softmax_rows_kernel<T, 256, 8, false, GRAD>), dim3(rows), dim3(256), lds, stream, a);
-  else if (a.cols <= 1024 * 4 * 8) hipLaunchKernelGGL((softmax_rows_kernel<T, 1024, 8, false, GRAD>), dim3(rows), dim3(1024), lds, stream, a);
-  else if (a.cols <= 1024 * 4 * 12) hipLaunchKernelGGL((softmax_rows_kernel<T, 1024, 12, false, GRAD>), dim3(rows), dim3(1024), lds, stream, a);
-  else hipLaunchKernelGGL((softmax_rows_kernel<T, 1024, 8, true, GRAD>), dim3(rows), dim3(1024), lds, stream, a);
+  if (a.cols <= 64 * 4 * 4) hipLaunchKernelGGL((softmax_rows_kernel<T, 64, 4, false, GRAD, LOST>), dim3(rows), dim3(64), lds, stream, a);
+  else if (a.cols <= 256 * 4 * 8) hipLaunchKernelGGL((softmax_rows_kernel<T, 256, 8, false, GRAD, LOST>), dim3(rows), dim3(256), lds, stream, a);
+  else if (a.cols <= 512 * 4 * 8) hipLaunchKernelGGL((softmax_rows_kernel<T, 512, 8, false, GRAD, LOST>), dim3(rows), dim3(512), lds, stream, a);
+  else if (a.cols <= 1024 * 4 * 8) hipLaunchKernelGGL((softmax_rows_kernel<T, 1024, 8, false, GRAD, LOST>), dim3(rows), dim3(1024), lds, stream, a);
+  else if (a.cols <= 1024 * 4 * 12) hipLaunchKernelGGL((softmax_rows_kernel<T, 1024, 12, false, GRAD, LOST>), dim3(rows), dim3(1024), lds, stream, a);
+  else hipLaunchKernelGGL((softmax_rows_kernel<T, 1024, 8, true, GRAD, LOST>), dim3(rows), dim3(1024), lds, stream, a);
+}
+
+int32_t launched() { return hipGetLastError() == hipSuccess ? GSPMD_OK : GSPMD_ERR_DEVICE; }
+
+int32_t launch_rows(const SoftmaxRows& a, const Loss& l, int64_t rows, hipStream_t stream) {
+  const unsigned n = static_cast<unsigned>(rows);
+  if (!l.dx && !l.dw) launch_rows_as<float, false, false>(a, n, stream);
+  else if (l.dtype == GSPMD_F32) launch_rows_as<float, true, false>(a, n, stream);
+  else if (l.with_lost()) launch_rows_as<bf16_bits, true, true>(a, n, stream);
+  else launch_rows_as<bf16_bits, true, false>(a, n, stream);
+  return launched();
+}
+
+dim3 rows_grid(int64_t vectors, int64_t rows) {
+  return dim3(static_cast<unsigned>((vectors + 255) / 256), static_cast<unsigned>(std::min<int64_t>(rows, 32768)));
+}
+
+int32_t launch_pack(const PackRows& a, int32_t dtype, hipStream_t stream) {
+  if (a.rows == 0 || a.chunks == 0) return GSPMD_OK;
+  const dim3 grid = rows_grid(a.chunks, a.rows);
+  if (dtype == GSPMD_BF16) hipLaunchKernelGGL((pack_rows_kernel<uint16_t>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((pack_rows_kernel<uint32_t>), grid, dim3(256), 0, stream, a);
+  return launched();
 }
 
 int32_t copy_rows(const gspmd_shard_buf& from, const gspmd_shard_buf& to, int64_t rows, int64_t cols, int64_t ld_from, int64_t ld_to, hipStream_t stream) {
@@ -165,7 +164,7 @@ int32_t copy_rows(const gspmd_shard_buf& from, const gspmd_shard_buf& to, int64_
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>((cols + 255) / 256, 64)), static_cast<unsigned>(std::min<int64_t>(rows, 4096)));
   if (from.dtype == GSPMD_BF16) hipLaunchKernelGGL((copy_rows_kernel<uint16_t>), grid, dim3(256), 0, stream, static_cast<const uint16_t*>(from.data), static_cast<uint16_t*>(to.data), rows, cols, ld_from, ld_to);
   else hipLaunchKernelGGL((copy_rows_kernel<uint32_t>), grid, dim3(256), 0, stream, static_cast<const uint32_t*>(from.data), static_cast<uint32_t*>(to.data), rows, cols, ld_from, ld_to);
-  return hipGetLastError() == hipSuccess ? GSPMD_OK : GSPMD_ERR_DEVICE;
+  return launched();
 }
 
 int32_t check_shard(const gspmd_shard_buf& b, int32_t dtype, int64_t rows, int64_t cols) {
@@ -174,6 +173,25 @@ int32_t check_shard(const gspmd_shard_buf& b, int32_t dtype, int64_t rows, int64
   if (!b.data && rows > 0 && cols > 0) return GSPMD_ERR_NULL;
   if (reinterpret_cast<uintptr_t>(b.data) & (dtype == GSPMD_BF16 ? 1 : 3)) return GSPMD_ERR_BAD_BUFFER;
   return GSPMD_OK;
+}
+
+Problem product(const void* a, int64_t lda, const void* b, int64_t ldb, void* c, int64_t ldc, int64_t m, int64_t n, int64_t k, int64_t m_static, int64_t n_static) {
+  Problem p;
+  std::memset(&p, 0, sizeof(p));
+  p.A = a;
+  p.B = b;
+  p.C = c;
+  p.lda = static_cast<int32_t>(lda);
+  p.ldb = static_cast<int32_t>(ldb);
+  p.ldc = static_cast<int32_t>(ldc);
+  p.Ms = static_cast<int32_t>(m_static);
+  p.Ns = static_cast<int32_t>(n_static);
+  if (m > 0 && n > 0 && k > 0) {               // all or none: without a term to sum the output is its zero fill
+    p.Mv = static_cast<int32_t>(m);
+    p.Nv = static_cast<int32_t>(n);
+    p.Kv = static_cast<int32_t>(k);
+  }
+  return p;
 }
 
 int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const gspmd_sharding* x_sh, const gspmd_shard_buf* w_shards, const gspmd_sharding* w_sh, int32_t vocab_dim,
@@ -195,15 +213,20 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   std::vector<Buffers> x(static_cast<size_t>(l.na)), w(static_cast<size_t>(l.nb)), dx(x), dw(w);
   std::vector<std::vector<gspmd_token_buf>> token(static_cast<size_t>(l.na));
   std::vector<char> seen_t(static_cast<size_t>(l.na), 0), seen_v(static_cast<size_t>(l.nb), 0);
-  const int64_t w_rows = l.dw_rows(), w_cols = l.dw_cols();
+  const int64_t w_rows = l.w_rows(), w_cols = l.w_cols();
   for (int64_t at = 0; at < l.P; ++at) {
     const int64_t p = mesh->device_ids[at];
-    int64_t coords[kMaxRank];
-    if ((st = mesh_coords(mesh, p, coords)) != GSPMD_OK) return st;
+    int64_t coords[kMaxRank], rest = at;
+    for (int a = mesh->rank - 1; a >= 0; --a) {
+      coords[a] = rest % mesh->shape[a];
+      rest /= mesh->shape[a];
+    }
     const int64_t i = l.axis_t >= 0 ? coords[l.axis_t] : 0, j = l.axis_v >= 0 ? coords[l.axis_v] : 0;
     if ((st = check_shard(x_shards[p], l.dtype, l.ts, l.M)) != GSPMD_OK || (st = check_shard(w_shards[p], l.dtype, w_rows, w_cols)) != GSPMD_OK) return st;
     if (l.dx && (st = check_shard(dx_shards[p], l.dtype, l.ts, l.M)) != GSPMD_OK) return st;
     if (l.dw && (st = check_shard(dw_shards[p], l.dtype, w_rows, w_cols)) != GSPMD_OK) return st;
+    if (x_shards[p].row_stride != x_shards[0].row_stride || w_shards[p].row_stride != w_shards[0].row_stride || (l.dx && dx_shards[p].row_stride != dx_shards[0].row_stride) ||
+        (l.dw && dw_shards[p].row_stride != dw_shards[0].row_stride)) return GSPMD_ERR_BAD_BUFFER;
     const gspmd_token_buf& tb = tokens[p];
     if (l.ts > 0 && (!tb.ids || !tb.loss || (teacher && !tb.logits))) return GSPMD_ERR_NULL;
     if (teacher && tb.logits_dtype != GSPMD_F32 && tb.logits_dtype != GSPMD_BF16) return GSPMD_ERR_UNSUPPORTED;
@@ -211,94 +234,168 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
     const bool ts = seen_t[static_cast<size_t>(i)], vs = seen_v[static_cast<size_t>(j)];
     if (!ts) x[static_cast<size_t>(i)].first = x_shards[p];
     if (!vs) w[static_cast<size_t>(j)].first = w_shards[p];
-    if (l.dx && (st = add_buffer(dx, i, ts, dx_shards[p])) != GSPMD_OK) return st;
-    if (l.dw && (st = add_buffer(dw, j, vs, dw_shards[p])) != GSPMD_OK) return st;
+    if (l.dx) add_buffer(dx, i, ts, dx_shards[p]);
+    if (l.dw) add_buffer(dw, j, vs, dw_shards[p]);
     auto& mine = token[static_cast<size_t>(i)];
     const bool known = std::any_of(mine.begin(), mine.end(), [&](const gspmd_token_buf& o) { return o.loss == tb.loss && o.lse == tb.lse; });
     if (!known) mine.push_back(tb);
     seen_t[static_cast<size_t>(i)] = seen_v[static_cast<size_t>(j)] = 1;
   }
-
   // (the first of a shard's is what the kernel writes: one with an lse, if any has)
   for (auto& list : token) std::stable_partition(list.begin(), list.end(), [](const gspmd_token_buf& tb) { return tb.lse != nullptr; });
 
-  // ---- pieces: as many rows of every token shard as the workspace holds
-  const int64_t whole = l.whole_rows();
+  // ---- pieces: as many tokens as the workspace holds (more than the query asks for is not used)
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & (kWsAlign - 1))) return GSPMD_ERR_WORKSPACE;
-  const int64_t in_piece = std::max<int64_t>(1, kPieceBytes / (l.na * l.ldz() * 4));       // (more workspace than the query asks for is not used)
-  int64_t rows = std::min(whole, in_piece);
-  if (l.fixed_bytes(rows < whole) + rows * l.row_bytes() > workspace_bytes)
-    rows = std::min(rows, (workspace_bytes - l.fixed_bytes(true)) / l.row_bytes());
-  if (whole > 0 && rows < 1) return GSPMD_ERR_WORKSPACE;
-  if (l.fixed_bytes(false) > workspace_bytes) return GSPMD_ERR_WORKSPACE;
-  int64_t pieces = whole > 0 ? (whole + rows - 1) / rows : 1;
-  if (pieces > 1) {                           // even ones, in whole tiles where that does not make more of them
-    rows = (whole + pieces - 1) / pieces;
-    const int64_t up = round_up(rows, 256);
-    if (l.fixed_bytes(true) + up * l.row_bytes() <= workspace_bytes && up <= in_piece) rows = up;
-    pieces = (whole + rows - 1) / rows;
+  int64_t rows = l.most_rows();
+  if (l.bytes(rows) > workspace_bytes) {
+    int64_t fit = 0;                            // the most that fit (bytes() does not grow evenly: ranges fall as rows grow, so every size is looked at by halves)
+    for (int64_t step = rows; step > 0; step /= 2)
+      while (fit + step < rows && l.bytes(fit + step) <= workspace_bytes) fit += step;
+    if (fit == 0 && l.T > 0) return GSPMD_ERR_WORKSPACE;
+    rows = fit;
+  }
+  int64_t pieces = rows > 0 ? (l.T + rows - 1) / rows : 1;
+  if (pieces > 1) {                             // even ones, in whole tiles where that makes no more of them
+    const int64_t even = (l.T + pieces - 1) / pieces, up = round_up(even, 256), next = up < rows ? up : even;
+    if (l.bytes(next) <= workspace_bytes) rows = next;
+    pieces = (l.T + rows - 1) / rows;
   }
   char* ws = static_cast<char*>(workspace);
   auto take = [&](int64_t bytes) {
     char* at = ws;
-    ws += round_up(bytes, kWsAlign);
+    ws += bytes;
     return at;
   };
   void* const tables = take(l.table_bytes());
-  const int64_t ldz = l.ldz(), per_cols = l.per_cols(), zs = l.shards_v();
-  const int64_t dw_size = round_up(w_rows * round_up(w_cols, 4) * 4, kWsAlign) / 4;          // float32 elements of a partial
-  float* const dw_parts = reinterpret_cast<float*>(take(l.dw_bytes(pieces > 1)));
-  float* const z = reinterpret_cast<float*>(take(l.na * rows * ldz * 4));
-  float* const dx_parts = l.parts_dx() ? reinterpret_cast<float*>(take(l.na * rows * l.nb * round_up(l.M, 4) * 4)) : nullptr;
-  const int64_t e = l.esize(), ldd = ldz * 4 / e;
-  const bool grad = l.dx || l.dw;
+  char* const x_all = take(l.x_bytes(rows));
+  float* const z = reinterpret_cast<float*>(take(l.z_bytes(rows)));
+  float* const sums = reinterpret_cast<float*>(take(l.sum_bytes(rows)));
+  float* const dw_sums = reinterpret_cast<float*>(take(l.dw_bytes(rows)));
+  char* const w_all = ws;
+  const int64_t room_w = workspace_bytes - (ws - static_cast<char*>(workspace));
+  const int64_t e = l.esize(), ldz = l.ldz(), ldd = ldz * 4 / e, per_cols = l.per_cols(), nw = l.windows(), vec = 16 / e;
+  const bool dry = launches_are_dry(), lost = l.with_lost();
+  const int64_t ldx_in = stride_of(x_shards[0], l.M), ldw = stride_of(w_shards[0], w_cols);
+  const int64_t lddx = l.dx ? stride_of(dx_shards[0], l.M) : 0, lddw = l.dw ? stride_of(dw_shards[0], w_cols) : 0;
+
+  // ---- the vocabulary matrix: shard by shard, or in one padded copy of all of them (zeros between)
+  struct Window { const char* data; int64_t ld, col, entries; };
+  std::vector<Window> windows;
+  bool w_padded = true, x_padded = true;
+  for (int64_t j = 0; j < nw; ++j) w_padded = w_padded && padded(w[static_cast<size_t>(j)].first, ldw);
+  for (int64_t i = 0; i < l.na; ++i) x_padded = x_padded && padded(x[static_cast<size_t>(i)].first, ldx_in);
+  if (!w_padded && l.packing_pays() && room_w >= l.packed_w_bytes() && l.M > 0) {
+    const int64_t ld = vocab_dim == 0 ? l.ldx() : ldz, chunks = ld / vec;
+    for (int64_t from = 0; from < nw && !dry; from += kInlineTokenShards) {
+      const int64_t n = std::min<int64_t>(kInlineTokenShards, nw - from);
+      PackRows a;
+      std::memset(&a, 0, sizeof(a));
+      for (int64_t j = 0; j < n; ++j) a.from[j] = w[static_cast<size_t>(from + j)].first.data;
+      a.ld = ld;
+      a.ld_from = ldw;
+      a.copies = 1;
+      a.per_cols = static_cast<int32_t>(per_cols);
+      a.per = static_cast<int32_t>(l.vs);
+      if (vocab_dim == 0) {                     // a shard's rows are per_cols apart
+        for (int64_t j = 0; j < n; ++j) {
+          a.from[0] = w[static_cast<size_t>(from + j)].first.data;
+          a.to = w_all + (from + j) * per_cols * ld * e;
+          a.rows = static_cast<int32_t>(per_cols);
+          a.chunks = static_cast<int32_t>(chunks);
+          a.tokens = static_cast<int32_t>(l.valid_v(from + j));
+          a.per_row = static_cast<int32_t>(per_cols);
+          a.cols = static_cast<int32_t>(l.M);
+          if ((st = launch_pack(a, l.dtype, stream)) != GSPMD_OK) return st;
+        }
+      } else {
+        a.to = w_all + from * per_cols * e;
+        a.rows = static_cast<int32_t>(l.M);
+        a.chunks = static_cast<int32_t>(n * per_cols / vec);
+        a.by_columns = 1;
+        a.cols = static_cast<int32_t>(l.V - from * l.vs);
+        if ((st = launch_pack(a, l.dtype, stream)) != GSPMD_OK) return st;
+      }
+    }
+    windows.push_back(Window{w_all, ld, 0, l.cols()});
+  } else {
+    for (int64_t j = 0; j < nw; ++j) windows.push_back(Window{static_cast<const char*>(w[static_cast<size_t>(j)].first.data), ldw, j * per_cols, l.valid_v(j)});
+  }
+  // x put together: where dw sums over tokens of several shards, or over both parts of D, and where rows are not padded
+  const bool pack_x = l.M > 0 && ((l.dw && (l.na > 1 || lost)) || (!x_padded && l.packing_pays()));
 
   for (int64_t piece = 0; piece < pieces; ++piece) {
-    const int64_t first = piece * rows, held = std::min(rows, std::max<int64_t>(l.ts - first, 0));
-    auto valid = [&](int64_t i) { return std::max<int64_t>(0, std::min(rows, l.valid_t(i) - first)); };
-    auto z_at = [&](int64_t i, int64_t j, int64_t size) { return reinterpret_cast<char*>(z + i * rows * ldz) + j * per_cols * size; };
-    auto x_at = [&](int64_t i) { return static_cast<char*>(x[static_cast<size_t>(i)].first.data) + first * stride_of(x[static_cast<size_t>(i)].first, l.M) * e; };
-    auto problem = [](const void* a, int64_t lda, const void* b, int64_t ldb, int64_t m, int64_t n, int64_t k) {
-      Problem p;
-      std::memset(&p, 0, sizeof(p));
-      p.A = a;
-      p.B = b;
-      p.lda = static_cast<int32_t>(lda);
-      p.ldb = static_cast<int32_t>(ldb);
-      p.Mv = static_cast<int32_t>(m);
-      p.Nv = static_cast<int32_t>(n);
-      p.Kv = static_cast<int32_t>(k);
-      return p;
+    const int64_t first = piece * rows, n = std::min(rows, l.T - first);       // tokens
+    const bool last = piece == pieces - 1;
+    const int64_t end = last ? l.na * l.ts : first + n;                        // .. and with the last ones the padding of all shards
+    // the token shards that rows first .. end of all of them lie in: (shard, first row in it, rows)
+    auto each_shard = [&](auto&& go) {
+      for (int64_t at = first; at < end;) {
+        const int64_t i = at / l.ts, stop = std::min(end, (i + 1) * l.ts);
+        if (const int32_t s = go(i, at - i * l.ts, stop - at, at - first); s != GSPMD_OK) return s;
+        at = stop;
+      }
+      return static_cast<int32_t>(GSPMD_OK);
     };
+    // launches whose tables hold so many shards: (first row of all, rows, first shard, shards)
+    auto by_tables = [&](auto&& go) {
+      for (int64_t at = first; at < end && !dry;) {
+        const int64_t i = at / l.ts, shards = std::min<int64_t>(kInlineTokenShards, l.na - i), stop = std::min(end, (i + shards) * l.ts);
+        if (const int32_t s = go(at, stop - at, i, shards); s != GSPMD_OK) return s;
+        at = stop;
+      }
+      return static_cast<int32_t>(GSPMD_OK);
+    };
+    if (pack_x)
+      st = by_tables([&](int64_t at, int64_t count, int64_t i0, int64_t shards) -> int32_t {
+        PackRows a;
+        std::memset(&a, 0, sizeof(a));
+        for (int64_t i = 0; i < shards; ++i) a.from[i] = x[static_cast<size_t>(i0 + i)].first.data;
+        a.ld_from = ldx_in;
+        a.to = x_all + (at - first) * l.ldx() * e;
+        a.ld = l.ldx();
+        a.rows = static_cast<int32_t>(std::min(count, first + n - at));
+        a.chunks = static_cast<int32_t>(l.ldx() / vec);
+        a.first = static_cast<int32_t>(at);
+        a.tokens = static_cast<int32_t>(l.T);
+        a.per_row = static_cast<int32_t>(l.ts);
+        a.first_shard = static_cast<int32_t>(i0);
+        a.cols = static_cast<int32_t>(l.M);
+        a.copies = lost ? 2 : 1;
+        return a.rows > 0 ? launch_pack(a, l.dtype, stream) : static_cast<int32_t>(GSPMD_OK);
+      });
+    if (st != GSPMD_OK) return st;
     // ---- logits
     std::vector<Problem> ps;
-    for (int64_t i = 0; i < l.na; ++i)
-      for (int64_t j = 0; j < zs; ++j) {
-        const gspmd_shard_buf &xb = x[static_cast<size_t>(i)].first, &wb = w[static_cast<size_t>(j)].first;
-        Problem p = problem(x_at(i), stride_of(xb, l.M), wb.data, stride_of(wb, w_cols), valid(i), l.valid_v(j), l.M);
-        p.C = z_at(i, j, 4);
-        p.ldc = static_cast<int32_t>(ldz);
-        p.Ms = p.Mv;
-        p.Ns = p.Nv;
-        if (p.Kv == 0) p.Mv = p.Nv = 0;       // no hidden dimension: logits of 0, by the zero fill
-        if (p.Ms > 0) ps.push_back(p);
-      }
+    auto logits = [&](const char* from, int64_t ld, int64_t row, int64_t count) {
+      for (const Window& v : windows)
+        ps.push_back(product(from, ld, v.data, v.ld, z + row * ldz + v.col, ldz, count, v.entries, l.M, count, v.entries));
+    };
+    if (pack_x) {
+      logits(x_all, l.ldx(), 0, n);
+    } else {
+      each_shard([&](int64_t i, int64_t at, int64_t count, int64_t row) -> int32_t {
+        const int64_t valid = std::min(count, n - row);
+        if (valid > 0) logits(static_cast<const char*>(x[static_cast<size_t>(i)].first.data) + at * ldx_in * e, ldx_in, row, valid);
+        return GSPMD_OK;
+      });
+    }
     if ((st = run_dots(ps, vocab_dim == 0 ? GSPMD_LAYOUT_RHS_K_CONTIGUOUS : 0, l.dtype, GSPMD_F32, tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
     // ---- rows
-    for (int64_t from = 0; held > 0 && from < l.na && !launches_are_dry(); from += kInlineTokenShards) {
-      const int64_t n = std::min<int64_t>(kInlineTokenShards, l.na - from);
+    st = by_tables([&](int64_t at, int64_t count, int64_t i0, int64_t shards) {
       SoftmaxRows a;
       std::memset(&a, 0, sizeof(a));
-      for (int64_t i = 0; i < n; ++i) {
-        const gspmd_token_buf& tb = token[static_cast<size_t>(from + i)][0];
-        a.shard[i] = TokenShard{tb.ids, teacher ? tb.logits : nullptr, tb.weights, tb.loss, tb.lse, static_cast<int32_t>(l.valid_t(from + i)), 0};
+      for (int64_t i = 0; i < shards; ++i) {
+        const gspmd_token_buf& tb = token[static_cast<size_t>(i0 + i)][0];
+        a.shard[i] = TokenShard{tb.ids, teacher ? tb.logits : nullptr, tb.weights, tb.loss, tb.lse};
       }
-      a.z = z + from * rows * ldz;
+      a.z = z + (at - first) * ldz;
       a.ldz = ldz;
-      a.rows_per = static_cast<int32_t>(rows);
-      a.first = static_cast<int32_t>(first);
-      a.tokens = static_cast<int32_t>(l.ts);
-      a.cols = static_cast<int32_t>((zs - 1) * per_cols + l.valid_v(zs - 1));
+      a.lost = n;
+      a.first = static_cast<int32_t>(at);
+      a.tokens = static_cast<int32_t>(l.T);
+      a.per_shard = static_cast<int32_t>(l.ts);
+      a.first_shard = static_cast<int32_t>(i0);
+      a.cols = static_cast<int32_t>(l.cols());
       a.vocab = static_cast<int32_t>(l.V);
       a.per = static_cast<int32_t>(l.vs);
       a.per_cols = static_cast<int32_t>(per_cols);
@@ -306,62 +403,96 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
       a.targets = targets;
       a.inv_tau = 1.f / tau;
       a.logits_bf16 = teacher && tokens[0].logits_dtype == GSPMD_BF16;
-      const unsigned blocks = static_cast<unsigned>(n * rows);
-      if (!grad) launch_rows_as<float, false>(a, blocks, stream);
-      else if (l.dtype == GSPMD_BF16) launch_rows_as<bf16_bits, true>(a, blocks, stream);
-      else launch_rows_as<float, true>(a, blocks, stream);
-      if (hipGetLastError() != hipSuccess) return GSPMD_ERR_DEVICE;
-    }
-    // ---- dx: the piece's rows, summed over the vocabulary's shards
-    if (l.dx && held > 0) {
-      std::vector<Sum> sums(static_cast<size_t>(l.na));
-      for (int64_t i = 0; i < l.na; ++i) {
-        Sum& s = sums[static_cast<size_t>(i)];
-        const gspmd_shard_buf& ob = dx[static_cast<size_t>(i)].first;
-        s.ld_out = static_cast<int32_t>(stride_of(ob, l.M));
-        s.out = static_cast<char*>(ob.data) + first * s.ld_out * e;
-        s.rows = static_cast<int32_t>(held);
-        s.cols = static_cast<int32_t>(l.M);
-        s.partials = dx_parts ? dx_parts + i * rows * l.nb * round_up(l.M, 4) : nullptr;
-        for (int64_t j = 0; j < zs; ++j) {
-          const gspmd_shard_buf& wb = w[static_cast<size_t>(j)].first;
-          s.members.push_back(problem(z_at(i, j, e), ldd, wb.data, stride_of(wb, w_cols), valid(i), l.M, valid(i) > 0 ? l.valid_v(j) : 0));
-        }
+      return launch_rows(a, l, count, stream);
+    });
+    if (st != GSPMD_OK) return st;
+    const char* const d = reinterpret_cast<const char*>(z);
+    // ---- dx: the piece's rows
+    const int32_t dx_layout = vocab_dim == 0 ? 0 : GSPMD_LAYOUT_RHS_K_CONTIGUOUS;
+    auto w_from = [&](const Window& v, int64_t entry) { return v.data + (vocab_dim == 0 ? entry * v.ld : entry) * e; };
+    if (l.dx && !(l.adds_up(rows) && (lost || windows.size() * l.ranges(rows) > 1))) {
+      ps.clear();
+      const Window& v = windows[0];
+      each_shard([&](int64_t i, int64_t at, int64_t count, int64_t row) -> int32_t {
+        const gspmd_shard_buf& o = dx[static_cast<size_t>(i)].first;
+        ps.push_back(product(d + row * ldz * 4, ldd, v.data, v.ld, static_cast<char*>(o.data) + at * lddx * e, lddx, std::min(count, n - row), l.M, v.entries, count, l.M));
+        return GSPMD_OK;
+      });
+      if ((st = run_dots(ps, dx_layout, l.dtype, l.dtype, tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
+    } else if (l.dx && l.M > 0) {
+      ps.clear();
+      const int64_t both = n * l.parts(), size = both * l.ld_sum(), ranges = l.ranges(rows);
+      for (const Window& v : windows) {
+        const int64_t each = round_up((v.entries + ranges - 1) / ranges, 256);
+        for (int64_t from = 0; from < v.entries; from += each)
+          ps.push_back(product(d + (v.col + from) * e, ldd, w_from(v, from), v.ld, sums + static_cast<int64_t>(ps.size()) * size, l.ld_sum(), both, l.M,
+                               std::min(each, v.entries - from), both, l.M));
       }
-      if ((st = run_sums(sums, vocab_dim == 0 ? 0 : GSPMD_LAYOUT_RHS_K_CONTIGUOUS, l.dtype, true, true, tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
+      const int64_t count_all = static_cast<int64_t>(ps.size()) * l.parts();
+      if (n > 0 && (st = run_dots(ps, dx_layout, l.dtype, GSPMD_F32, tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
+      st = by_tables([&](int64_t at, int64_t count, int64_t i0, int64_t shards) {
+        AddUp a;
+        std::memset(&a, 0, sizeof(a));
+        uintptr_t bits = 0;
+        for (int64_t i = 0; i < shards; ++i) {
+          a.to[i] = dx[static_cast<size_t>(i0 + i)].first.data;
+          bits |= reinterpret_cast<uintptr_t>(a.to[i]);
+        }
+        a.partials = sums + (at - first) * l.ld_sum();
+        a.stride = n * l.ld_sum();
+        a.ld_in = l.ld_sum();
+        a.ld_out = lddx;
+        a.count = static_cast<int32_t>(count_all);
+        a.rows = static_cast<int32_t>(count);
+        a.cols = static_cast<int32_t>(l.M);
+        a.first = static_cast<int32_t>(at);
+        a.tokens = static_cast<int32_t>(l.T);
+        a.per_row = static_cast<int32_t>(l.ts);
+        a.first_shard = static_cast<int32_t>(i0);
+        const bool four = !(l.M & 3) && !(a.ld_out & 3) && !(bits & static_cast<uintptr_t>(4 * e - 1));
+        const dim3 grid = rows_grid(four ? l.M / 4 : l.M, count);
+        if (l.dtype == GSPMD_BF16) {
+          if (four) hipLaunchKernelGGL((add_up_kernel<bf16_bits, 4>), grid, dim3(256), 0, stream, a);
+          else hipLaunchKernelGGL((add_up_kernel<bf16_bits, 1>), grid, dim3(256), 0, stream, a);
+        } else {
+          if (four) hipLaunchKernelGGL((add_up_kernel<float, 4>), grid, dim3(256), 0, stream, a);
+          else hipLaunchKernelGGL((add_up_kernel<float, 1>), grid, dim3(256), 0, stream, a);
+        }
+        return launched();
+      });
+      if (st != GSPMD_OK) return st;
     }
-    // ---- dw: summed over the tokens' shards and the pieces
+    // ---- dw: straight into its shards, or over several pieces in float32
     if (l.dw) {
-      std::vector<Sum> sums(static_cast<size_t>(l.nb));
+      const char* const from = pack_x ? x_all : static_cast<const char*>(x[0].first.data) + first * ldx_in * e;
+      const int64_t ldx = pack_x ? l.ldx() : ldx_in, k = n * l.parts(), ld_part = round_up(w_cols, 4);
+      ps.clear();
       for (int64_t j = 0; j < l.nb; ++j) {
-        Sum& s = sums[static_cast<size_t>(j)];
-        const gspmd_shard_buf& ob = dw[static_cast<size_t>(j)].first;
-        s.out = ob.data;
-        s.ld_out = static_cast<int32_t>(stride_of(ob, w_cols));
-        s.rows = static_cast<int32_t>(w_rows);
-        s.cols = static_cast<int32_t>(w_cols);
-        s.partials = dw_parts + j * l.dw_partials(pieces > 1) * dw_size;
-        s.earlier = pieces > 1 ? s.partials + l.na * dw_size : nullptr;
-        for (int64_t i = 0; i < l.na; ++i) {
-          const gspmd_shard_buf& xb = x[static_cast<size_t>(i)].first;
-          const int64_t k = l.valid_v(j) > 0 ? valid(i) : 0, ldx = stride_of(xb, l.M);
-          s.members.push_back(vocab_dim == 0 ? problem(z_at(i, j, e), ldd, x_at(i), ldx, l.valid_v(j), l.M, k)
-                                             : problem(x_at(i), ldx, z_at(i, j, e), ldd, l.M, l.valid_v(j), k));
-        }
+        const gspmd_shard_buf& o = dw[static_cast<size_t>(j)].first;
+        void* const c = pieces == 1 ? o.data : dw_sums + (j * 2 + (piece > 0 ? 1 : 0)) * l.dw_size();
+        const int64_t ldc = pieces == 1 ? lddw : ld_part, entries = l.valid_v(j);
+        const char* const dj = d + j * per_cols * e;
+        ps.push_back(vocab_dim == 0 ? product(dj, ldd, from, ldx, c, ldc, entries, l.M, k, w_rows, w_cols) : product(from, ldx, dj, ldd, c, ldc, l.M, entries, k, w_rows, w_cols));
       }
-      if ((st = run_sums(sums, GSPMD_LAYOUT_LHS_K_MAJOR, l.dtype, piece == 0, piece == pieces - 1, tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
+      if ((st = run_dots(ps, GSPMD_LAYOUT_LHS_K_MAJOR, l.dtype, pieces == 1 ? l.dtype : static_cast<int32_t>(GSPMD_F32), tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
+      for (int64_t j = 0; piece > 0 && j < l.nb; ++j) {
+        const gspmd_shard_buf& o = dw[static_cast<size_t>(j)].first;
+        float* const sum = dw_sums + j * 2 * l.dw_size();
+        if ((st = run_sum({sum, sum + l.dw_size()}, w_rows, w_cols, ld_part, last ? o.data : sum, last ? lddw : ld_part, last ? l.dtype : static_cast<int32_t>(GSPMD_F32),
+                          stream)) != GSPMD_OK) return st;
+      }
     }
   }
   // ---- partitions that hold the same results in buffers of their own
-  if (launches_are_dry()) return GSPMD_OK;
-  auto spread = [&](const std::vector<Buffers>& at, int64_t r, int64_t c) {
+  if (dry) return GSPMD_OK;
+  auto spread = [&](const std::vector<Buffers>& at, int64_t r, int64_t c, int64_t ld) {
     for (const auto& b : at)
       for (const auto& o : b.others)
-        if ((st = copy_rows(b.first, o, r, c, stride_of(b.first, c), stride_of(o, c), stream)) != GSPMD_OK) return st;
+        if ((st = copy_rows(b.first, o, r, c, ld, ld, stream)) != GSPMD_OK) return st;
     return static_cast<int32_t>(GSPMD_OK);
   };
-  if (l.dx && (st = spread(dx, l.ts, l.M)) != GSPMD_OK) return st;
-  if (l.dw && (st = spread(dw, w_rows, w_cols)) != GSPMD_OK) return st;
+  if (l.dx && (st = spread(dx, l.ts, l.M, lddx)) != GSPMD_OK) return st;
+  if (l.dw && (st = spread(dw, w_rows, w_cols, lddw)) != GSPMD_OK) return st;
   for (const auto& list : token)
     for (size_t k = 1; k < list.size(); ++k) {
       auto one = [&](float* from, float* to) {
@@ -389,9 +520,9 @@ int32_t gspmd_softmax_workspace_bytes(const gspmd_mesh* mesh, const gspmd_shardi
   if (st != GSPMD_OK) return st;
   l.dtype = dtype;
   l.dx = l.dw = gradients != 0;
-  const int64_t whole = l.whole_rows(), rows = std::min(whole, std::max<int64_t>(1, kPieceBytes / (l.na * l.ldz() * 4)));
-  *bytes = l.fixed_bytes(rows < whole) + rows * l.row_bytes();
-  if (least) *least = std::min(*bytes, l.fixed_bytes(whole > 1) + std::min<int64_t>(whole, 1) * l.row_bytes());
+  const int64_t rows = l.most_rows();
+  *bytes = l.bytes(rows) + (l.packing_pays() ? l.packed_w_bytes() : 0);
+  if (least) *least = std::min(*bytes, l.bytes(std::min<int64_t>(l.T, 1)));
   return GSPMD_OK;
 } catch (...) { return GSPMD_ERR_HOST_MEMORY; }
 
