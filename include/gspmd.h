@@ -348,7 +348,7 @@ int32_t gspmd_resharded_dot(const gspmd_mesh* mesh, const gspmd_dot_dims* dims,
  *   lse[t]  = log sum_v exp(z[t, v] / tau)                               (the AllReduce of a maximum and a sum over the vocabulary's mesh dimension)
  *   D[t, v] = weight[t] / tau * (exp(z[t, v] / tau - lse[t]) - p[t, v])   p: the targets' shares, below
  *   dx = D w,  dw = D^T x                                                (summed over the vocabulary's and the tokens' mesh dimension, as an AllReduce)
- * The logits of all tokens are never held: tokens go through the workspace in pieces of at most 1 GiB of logits (less where the workspace is smaller).
+ * The logits of all tokens are never held: tokens go through the workspace in pieces of at most 2 GiB of logits (less where the workspace is smaller).
  * Operands are bf16 or f32; logits, maxima, sums and losses are fp32; D is rounded once to the operands' type, as an operand of the
  * products that make the gradients, which accumulate in fp32 and are stored in that type.  A weight of 0 makes a token's D zero whatever its logits are; its x still
  * enters dw's sums, times 0, so x must be finite there (padding beyond the valid lengths may hold anything).  Logits that are NaN, +infinity or -infinity throughout give NaN. */

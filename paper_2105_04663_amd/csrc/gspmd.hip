@@ -13,6 +13,7 @@
 #include "dots.h"
 #include "kernels_basic.h"
 #include "kernels_f32.h"
+#include "kernels_stats.h"
 #include "launch.h"
 #include "mfma_common.h"
 #include "plan.h"
@@ -728,6 +729,30 @@ namespace gspmd {
 
 int32_t run_dots(std::vector<Problem>& ps, int32_t layout, int32_t in_dtype, int32_t out_dtype, void* tables, int64_t table_bytes, hipStream_t stream) {
   return launch_problems(ps, layout, in_dtype, out_dtype, GSPMD_EPILOGUE_NONE, false, tables, table_bytes, stream);
+}
+
+bool takes_stats(const std::vector<Problem>& ps, int32_t layout) {
+  if (ps.empty() || (layout & GSPMD_LAYOUT_LHS_K_MAJOR)) return false;
+  const KernelPath path = kernel_path(ps, GSPMD_BF16, layout);
+  return path == kPathMfmaDirect && pick_kernel(ps, path, layout, false).kernel == kMfmaBig;
+}
+
+int32_t run_stats(std::vector<Problem>& ps, int32_t layout, const SoftmaxFinish& finish, void* tables, int64_t table_bytes, hipStream_t stream) {
+  const int64_t tiles = assign_tiles(ps, kMfmaBM, kMfmaBN), bytes = static_cast<int64_t>(ps.size()) * sizeof(Problem);
+  if (tiles < 0) return GSPMD_ERR_UNSUPPORTED;
+  if (t_pin.dry_run) return GSPMD_OK;
+  InlineProblems inl;
+  std::memset(&inl, 0, sizeof(inl));
+  const bool inline_table = ps.size() <= static_cast<size_t>(kInlineProblems);
+  if (inline_table) {
+    std::memcpy(inl.p, ps.data(), static_cast<size_t>(bytes));
+  } else {
+    if (bytes > table_bytes) return GSPMD_ERR_WORKSPACE;
+    if (hipMemcpyAsync(tables, ps.data(), static_cast<size_t>(bytes), hipMemcpyHostToDevice, stream) != hipSuccess) return GSPMD_ERR_DEVICE;
+  }
+  const MfmaLaunch l{&inl, inline_table ? nullptr : static_cast<const Problem*>(tables), static_cast<int>(ps.size()), static_cast<int>(tiles), GSPMD_EPILOGUE_NONE, nullptr, nullptr, nullptr, 0};
+  const bool ok = layout == 0 ? launch_dot_stats_layout<0>(l, finish, stream) : launch_dot_stats_layout<GSPMD_LAYOUT_RHS_K_CONTIGUOUS>(l, finish, stream);
+  return ok ? GSPMD_OK : GSPMD_ERR_DEVICE;
 }
 
 int32_t run_sum(const std::vector<float*>& partials, int64_t rows, int64_t cols, int64_t ld_in, void* out, int64_t ld_out, int32_t out_dtype, hipStream_t stream) {

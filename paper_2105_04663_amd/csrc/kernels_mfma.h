@@ -32,6 +32,7 @@
 #include <type_traits>
 
 #include "kernels_basic.h"
+#include "kernels_stats.h"
 #include "launch.h"
 #include "mainloop_asm.h"
 #include "mfma_common.h"
@@ -85,10 +86,12 @@ __device__ __forceinline__ void zero_rows_below(TOut* __restrict__ C, int ldc, i
 // partials of 2048 x 4096 and their sum: 122.3 to 123.0, and 124.3 to 124.8 with 0 or 14).  So they are aligned to 16 KiB and come first
 // in a compiled source (launch_dot_mfma_layout), which puts them 32 KiB into one whatever the sizes of the other kernels.
 constexpr int kMfmaCodeAlign = 16384;
-template <typename TOut, int LAYOUT, bool STAGED>
+// `finish`: what becomes of a tile's accumulators instead of the epilogue, in a launch without joined problems.
+struct NoFinish {};
+template <typename TOut, int LAYOUT, bool STAGED, typename Finish>
 __global__ __attribute__((aligned(kMfmaCodeAlign))) __launch_bounds__(kMfmaThreads) void dot_mfma_kernel(const InlineProblems inl, const Problem* __restrict__ tab, int n_prob, int epilogue,
                                                                 float* __restrict__ join_partials, uint32_t* __restrict__ join_counters,
-                                                                unsigned long long* __restrict__ timeline, int timeline_records) {
+                                                                unsigned long long* __restrict__ timeline, int timeline_records, const Finish finish) {
   constexpr bool AKM = (LAYOUT & GSPMD_LAYOUT_LHS_K_MAJOR) != 0, BKC = (LAYOUT & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) != 0;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int t = threadIdx.x, lane = t & 63;
@@ -471,6 +474,9 @@ __global__ __attribute__((aligned(kMfmaCodeAlign))) __launch_bounds__(kMfmaThrea
     }   // !STAGED
   }
 
+  if constexpr (!std::is_same_v<Finish, NoFinish>) {
+    finish(acc, P, own, n0, smem);
+  } else {
   // ---- joined problems (a contracting dimension split over partitions, Section 4.2, or one K range cut in pieces):
   // every contribution to an output tile is written to its slot of the workspace as fp32, in the accumulators' own
   // lane order (each wave-instruction stores 1 KiB of consecutive addresses); the workgroup that arrives last at the
@@ -730,6 +736,7 @@ __global__ __attribute__((aligned(kMfmaCodeAlign))) __launch_bounds__(kMfmaThrea
     GSPMD_WAIT_ALL();
     timeline_stamp(rec, 7, t);
   }
+  }   // NoFinish
 }
 
 // The kernel needs all 160 KiB of LDS as dynamic shared memory: raised once per instantiation and device.  Callable
@@ -741,13 +748,13 @@ inline bool launch_dot_mfma_as(const MfmaLaunch& l, hipStream_t stream) {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return false;
   std::call_once(once[dev], [dev] {
-    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_mfma_kernel<TOut, LAYOUT, STAGED>),
+    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_mfma_kernel<TOut, LAYOUT, STAGED, NoFinish>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, kMfmaLds) == hipSuccess;
   });
   if (!ok[dev]) return false;
   const dim3 grid(static_cast<unsigned>(l.tiles)), block(kMfmaThreads);
-  hipLaunchKernelGGL((dot_mfma_kernel<TOut, LAYOUT, STAGED>), grid, block, kMfmaLds, stream, *l.inl, l.tab, l.n_prob, l.epilogue, l.join_partials,
-                     l.join_counters, l.timeline, l.timeline_records);
+  hipLaunchKernelGGL((dot_mfma_kernel<TOut, LAYOUT, STAGED, NoFinish>), grid, block, kMfmaLds, stream, *l.inl, l.tab, l.n_prob, l.epilogue, l.join_partials,
+                     l.join_counters, l.timeline, l.timeline_records, NoFinish{});
   return hipGetLastError() == hipSuccess;
 }
 
@@ -756,5 +763,23 @@ bool launch_dot_mfma_layout(const MfmaLaunch& l, int32_t out_dtype, bool staged,
   if (!staged) return out_dtype == GSPMD_F32 ? launch_dot_mfma_as<float, LAYOUT, false>(l, stream) : launch_dot_mfma_as<bf16_bits, LAYOUT, false>(l, stream);
   return out_dtype == GSPMD_F32 ? launch_dot_mfma_as<float, LAYOUT, true>(l, stream) : launch_dot_mfma_as<bf16_bits, LAYOUT, true>(l, stream);
 }
+
+#if GSPMD_TU_LAYOUT == 0 || GSPMD_TU_LAYOUT == 2
+template <int LAYOUT>
+bool launch_dot_stats_layout(const MfmaLaunch& l, const SoftmaxFinish& finish, hipStream_t stream) {
+  static std::once_flag once[kMaxDevices];
+  static bool ok[kMaxDevices];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return false;
+  std::call_once(once[dev], [dev] {
+    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_mfma_kernel<float, LAYOUT, false, SoftmaxFinish>),
+                                  hipFuncAttributeMaxDynamicSharedMemorySize, kMfmaLds) == hipSuccess;
+  });
+  if (!ok[dev]) return false;
+  hipLaunchKernelGGL((dot_mfma_kernel<float, LAYOUT, false, SoftmaxFinish>), dim3(static_cast<unsigned>(l.tiles)), dim3(kMfmaThreads), kMfmaLds, stream, *l.inl, l.tab, l.n_prob,
+                     GSPMD_EPILOGUE_NONE, nullptr, nullptr, nullptr, 0, finish);
+  return hipGetLastError() == hipSuccess;
+}
+#endif
 
 }  // namespace gspmd

@@ -65,6 +65,39 @@ __device__ __forceinline__ float over_block(float v, float* shared, Op op) {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
+// The teacher's logit of a target; of a label 0.
+__device__ __forceinline__ float teachers_logit(const GSPMD_KERNARG TokenShard& s, int is_bf16, int64_t at) {
+  if (s.logits == nullptr) return 0.f;
+  return is_bf16 ? bf16_to_float(static_cast<const bf16_bits*>(s.logits)[at]) : static_cast<const float*>(s.logits)[at];
+}
+
+// A token's targets, by one wave: shares p_k = softmax of q_k (-infinity: no target), given to `keep`, and sum_k p_k (log p_k - u_k).
+// A NaN among the teacher's logits stays: the shares, the loss and the gradient of its token are NaN.
+struct TargetSums {
+  bool any;
+  float sum;
+};
+template <typename Q, typename U, typename Keep>
+__device__ __forceinline__ TargetSums over_targets(int K, Q q_of, U u_of, Keep keep) {
+  const int lane = threadIdx.x & 63;
+  auto most = [](float x, float y) { return x != x ? x : y != y ? y : fmaxf(x, y); };
+  auto plus = [](float x, float y) { return x + y; };
+  float q_most = -INFINITY;
+  for (int k = lane; k < K; k += 64) q_most = most(q_most, q_of(k));
+  q_most = over_wave(q_most, most);
+  if (q_most == -INFINITY) return TargetSums{false, 0.f};
+  float total = 0.f, sum = 0.f;
+  for (int k = lane; k < K; k += 64) total += __builtin_amdgcn_exp2f((q_of(k) - q_most) * kLog2e);
+  total = over_wave(total, plus);
+  const float log_total = logf(total);
+  for (int k = lane; k < K; k += 64) {
+    const float q = q_of(k) - q_most, p = __builtin_amdgcn_exp2f(q * kLog2e) / total;
+    if (p != 0.f) sum += p * ((q - log_total) - u_of(k));
+    keep(k, p);
+  }
+  return TargetSums{true, over_wave(sum, plus)};
+}
+
 // Bound by memory: reads 4 bytes a logit, writes 2 (4 in float32).  A workgroup takes a row and keeps it in registers between the maximum and D, so that it is read once (LONG,
 // beyond 48 K columns: twice, the second time mostly from the caches).  The row's loads go first: what a token's targets need, two accesses one after the other, comes while they are under way.
 // T: the operands' type.  A thread holds VECS vectors of 4 logits; LONG: rows of more than THREADS * VECS * 4, taken in several rounds.
@@ -118,44 +151,19 @@ __global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 5) void softmax
   auto plus = [](float x, float y) { return x + y; };
 
   // ---- the targets, by the first wave: their logits (before D takes the logits' place), shares, and what the loss takes from them
-  const bool teacher = s.logits != nullptr;
   float of_targets = 0.f;                       // sum_k p_k (log p_k - u_k)
   if (t < 64) {
-    // (a NaN among the teacher's logits stays: the shares, the loss and the gradient of its token are NaN)
-    auto most = [](float x, float y) { return x != x ? x : y != y ? y : fmaxf(x, y); };
-    float q_most = -INFINITY;
     for (int k = t; k < K; k += 64) {
       const int64_t at = static_cast<int64_t>(token) * K + k;
       int id = s.ids[at];
       if (id < 0 || id >= a.vocab) id = -1;
-      float u = 0.f, q = -INFINITY;
-      if (id >= 0) {
-        u = z[column(id)] * inv_tau;
-        q = !teacher ? 0.f : (a.logits_bf16 ? bf16_to_float(static_cast<const bf16_bits*>(s.logits)[at]) : static_cast<const float*>(s.logits)[at]) * inv_tau;
-        q_most = most(q_most, q);
-      }
-      u_of[k] = u;
-      p_of[k] = q;
+      u_of[k] = id >= 0 ? z[column(id)] * inv_tau : 0.f;
+      p_of[k] = id >= 0 ? teachers_logit(s, a.logits_bf16, at) * inv_tau : -INFINITY;
       id_of[k] = id;
     }
-    q_most = over_wave(q_most, most);
-    const bool some = q_most != -INFINITY;
-    if (some) {
-      float q_total = 0.f;
-      for (int k = t; k < K; k += 64) {
-        p_of[k] -= q_most;
-        q_total += __builtin_amdgcn_exp2f(p_of[k] * kLog2e);
-      }
-      q_total = over_wave(q_total, plus);
-      const float log_q = logf(q_total);
-      for (int k = t; k < K; k += 64) {
-        const float p = __builtin_amdgcn_exp2f(p_of[k] * kLog2e) / q_total;
-        if (p != 0.f) of_targets += p * ((p_of[k] - log_q) - u_of[k]);
-        p_of[k] = p;
-      }
-      of_targets = over_wave(of_targets, plus);
-    }
-    if (t == 0) any_target = some;
+    const TargetSums of = over_targets(K, [&](int k) { return p_of[k]; }, [&](int k) { return u_of[k]; }, [&](int k, float p) { p_of[k] = p; });
+    of_targets = of.sum;
+    if (t == 0) any_target = of.any;
   }
 
   // ---- maximum and total
@@ -259,6 +267,101 @@ __global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 5) void softmax
           d[column(id)] = v;
         }
       }
+  }
+}
+
+// ---- logits that are not kept (kernels_stats.h): the targets' columns before the products, and what their tiles leave put together after them.
+struct SoftmaxMerge {
+  SoftmaxRows rows;              // z: the table of pairs [group][ldz rows], `cols` its groups
+  int32_t* columns;              // [rows][targets]
+  float* logits;                 // [rows][targets]
+  int32_t count;                 // rows of the launch (for the columns: tokens)
+};
+static_assert(sizeof(SoftmaxMerge) <= 4096, "kernel arguments");
+
+__device__ __forceinline__ int target_column(int id, int vocab, int per, int per_cols) {
+  if (id < 0 || id >= vocab) return -1;
+  const int j = id / per;
+  return j * per_cols + (id - j * per);
+}
+
+__global__ __launch_bounds__(256) static void target_columns_kernel(const SoftmaxMerge args) {
+  const GSPMD_KERNARG SoftmaxRows& a = first_kernel_argument<SoftmaxMerge>()->rows;
+  const int K = a.targets;
+  int32_t* const columns = first_kernel_argument<SoftmaxMerge>()->columns;
+  const int64_t total = static_cast<int64_t>(first_kernel_argument<SoftmaxMerge>()->count) * K;
+  for (int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; n < total; n += static_cast<int64_t>(gridDim.x) * 256) {
+    const int row = static_cast<int>(n / K), g = a.first + row, i = g / a.per_shard;
+    columns[n] = target_column(a.shard[i - a.first_shard].ids[static_cast<int64_t>(g - i * a.per_shard) * K + (n - static_cast<int64_t>(row) * K)], a.vocab, a.per, a.per_cols);
+  }
+}
+
+// TOKENS tokens a workgroup (16, whose pairs are whole lines, or with few tokens 4): the threads go through the groups of 64 columns, then a wave takes a token's targets.
+constexpr int kMergeThreads = 1024;
+constexpr int32_t kStatsTargets = 128;           // of a token, at most
+template <int TOKENS>
+__global__ __launch_bounds__(kMergeThreads) void softmax_merge_kernel(const SoftmaxMerge args) {
+  constexpr int kMergeTokens = TOKENS, kSides = kMergeThreads / TOKENS;
+  const GSPMD_KERNARG SoftmaxRows& a = first_kernel_argument<SoftmaxMerge>()->rows;
+  typedef __attribute__((ext_vector_type(2))) float float2_t;
+  __shared__ float2_t part[kSides][kMergeTokens];
+  const int count = first_kernel_argument<SoftmaxMerge>()->count;
+  const int t = threadIdx.x, r = t & (kMergeTokens - 1), row0 = blockIdx.x * kMergeTokens;
+  const float inv_tau = a.inv_tau, c = inv_tau * kLog2e;
+  GSPMD_GLOBAL const float2_t* const pairs = (GSPMD_GLOBAL const float2_t*)a.z;
+  auto join = [&](float2_t p, float2_t q) {
+    const float m = fmaxf(p.x, q.x), from = m == -INFINITY ? 0.f : m;
+    return float2_t{m, p.y * __builtin_amdgcn_exp2f((p.x - from) * c) + q.y * __builtin_amdgcn_exp2f((q.x - from) * c)};
+  };
+  // this wave's token and its targets, two a lane: on their way first
+  const int wave = t >> 6, lane = t & 63, g = a.first + row0 + wave, i = g / a.per_shard, token = g - i * a.per_shard, K = a.targets;
+  const bool has_row = wave < kMergeTokens && row0 + wave < count, has_token = has_row && g < a.tokens;
+  const GSPMD_KERNARG TokenShard& s = a.shard[has_row ? i - a.first_shard : 0];
+  const int64_t at = static_cast<int64_t>(row0 + wave) * K;
+  float q[2], u[2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const int k = n * 64 + lane;
+    q[n] = -INFINITY;
+    u[n] = 0.f;
+    if (has_token && k < K && ((GSPMD_GLOBAL const int32_t*)first_kernel_argument<SoftmaxMerge>()->columns)[at + k] >= 0) {
+      q[n] = teachers_logit(s, a.logits_bf16, static_cast<int64_t>(token) * K + k) * inv_tau;
+      u[n] = ((GSPMD_GLOBAL const float*)first_kernel_argument<SoftmaxMerge>()->logits)[at + k] * inv_tau;
+    }
+  }
+  float2_t mine = {-INFINITY, 0.f};
+  if (row0 + r < count && a.first + row0 + r < a.tokens)
+    for (int group = t / kMergeTokens; group < a.cols; group += 4 * kSides) {
+      float2_t next[4];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const int at = group + n * kSides;
+        next[n] = float2_t{-INFINITY, 0.f};
+        if (at < a.cols) next[n] = pairs[static_cast<int64_t>(at) * a.ldz + row0 + r];
+      }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) mine = join(mine, next[n]);
+    }
+  part[t / kMergeTokens][r] = mine;
+  __syncthreads();
+  if (!has_row) return;
+  if (!has_token) {                             // padding of the last shards
+    if (lane == 0) {
+      s.loss[token] = 0.f;
+      if (s.lse) s.lse[token] = 0.f;
+    }
+    return;
+  }
+  mine = part[lane][wave];
+#pragma unroll
+  for (int n = 64; n < kSides; n += 64) mine = join(mine, part[n + lane][wave]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) mine = join(mine, float2_t{__shfl_xor(mine.x, d), __shfl_xor(mine.y, d)});
+  const float u_most = mine.x * inv_tau, log_total = logf(mine.y);
+  const TargetSums of = over_targets(K, [&](int k) { return q[k >> 6]; }, [&](int k) { return u[k >> 6]; }, [](int, float) {});
+  if (lane == 0) {
+    s.loss[token] = of.any ? of.sum + u_most + log_total : 0.f;
+    if (s.lse) s.lse[token] = u_most + log_total;
   }
 }
 

@@ -39,6 +39,11 @@ inline bool launch_dot_mfma(const MfmaLaunch& l, int32_t layout, int32_t out_dty
 }
 #endif
 
+// One launch of dot_mfma_kernel whose tiles end in SoftmaxFinish; layouts with a K-contiguous lhs, direct loads, no joined problems.
+struct SoftmaxFinish;
+template <int LAYOUT>
+bool launch_dot_stats_layout(const MfmaLaunch& l, const SoftmaxFinish& finish, hipStream_t stream);
+
 // One launch of dot_split_kernel in tiles of 16 * row_blocks rows (1, 2 or 4 blocks) x 16 * col_blocks columns (4; 2 with 1 or 2 row blocks; no joined
 // problems).
 constexpr int kSplitWaves = 8, kSplitThreads = 64 * kSplitWaves;

@@ -15,13 +15,14 @@
 #include "../../include/gspmd.h"
 #include "dots.h"
 #include "kernels_softmax.h"
+#include "kernels_stats.h"
 #include "plan.h"
 
 namespace gspmd {
 namespace {
 
 // Logits of a piece, at most (float32; at least one token's): what the workspace query provides for.
-constexpr int64_t kPieceBytes = int64_t(1) << 30;
+constexpr int64_t kPieceBytes = int64_t(1) << 31;
 constexpr int64_t kColumnAlign = 64;
 // Up to so many tokens what D's rounding to bfloat16 loses takes part in the products, as rows of its own: these are bound by w and dw then.
 constexpr int64_t kFewTokens = 64;
@@ -49,15 +50,17 @@ struct Loss {
   int64_t parts() const { return with_lost() ? 2 : 1; }
   int64_t ldx() const { return round_up(std::max<int64_t>(M, 1), kColumnAlign); }        // of x put together
   int64_t ld_sum() const { return round_up(std::max<int64_t>(M, 1), 4); }                // of dx's partials
-  // ranges of a window whose products make dx, for pieces of `rows` tokens
+  // Ranges of the vocabulary whose products make dx, for pieces of `rows` tokens: of all of it where it lies in one matrix, and of one of its shards.
   int64_t ranges(int64_t rows) const {
     if (!dx || rows == 0) return 1;
-    const int64_t few = rows * parts() <= 128, edge = dtype == GSPMD_F32 || few ? 64 : 256;
-    const int64_t tiles = ((rows * parts() + edge - 1) / edge) * ((M + edge - 1) / edge), want = dtype == GSPMD_F32 ? 1024 : few ? 512 : 256;
-    const int64_t least = dtype == GSPMD_F32 || few ? 512 : 2048;                        // entries of a range
-    return std::max<int64_t>(1, std::min({want / std::max<int64_t>(tiles, 1), vs / least, 32 / windows(), int64_t(16)}));
+    const bool few = rows * parts() <= 128, small = dtype == GSPMD_F32 || few;
+    const int64_t edge = small ? 64 : 256, tiles = ((rows * parts() + edge - 1) / edge) * ((M + edge - 1) / edge);
+    const int64_t want = dtype == GSPMD_F32 ? 1024 : few ? 512 : 256, least = small ? 512 : 2048;         // workgroups; entries of a range
+    return std::max<int64_t>(1, std::min({want / std::max<int64_t>(tiles, 1), V / least, int64_t(16)}));
   }
-  bool adds_up(int64_t rows) const { return dx && (windows() * ranges(rows) > 1 || with_lost()); }
+  int64_t ranges_of_shard(int64_t rows) const { return std::max<int64_t>(1, std::min(ranges(rows), int64_t(32)) / windows()); }
+  int64_t most_ranges(int64_t rows) const { return std::max(ranges(rows), windows() * ranges_of_shard(rows)); }
+  bool adds_up(int64_t rows) const { return dx && (most_ranges(rows) > 1 || with_lost()); }
   int64_t most_rows() const { return std::min(T, std::max<int64_t>(1, kPieceBytes / (ldz() * 4))); }
   // Copies of operands whose rows are not padded to 16 bytes, which the products read several times slower than they are copied once: from this many rows of products on.
   bool packing_pays() const { return dtype == GSPMD_BF16 && T * (dx || dw ? 3 : 1) >= 1024; }
@@ -66,7 +69,7 @@ struct Loss {
   int64_t table_bytes() const { return round_up((na * nb + 32 + nb) * kTableBytesPerProblem, kWsAlign); }
   int64_t x_bytes(int64_t rows) const { return round_up(rows * parts() * ldx() * esize(), kWsAlign); }
   int64_t z_bytes(int64_t rows) const { return round_up(rows * parts() * ldz() * 4, kWsAlign); }
-  int64_t sum_bytes(int64_t rows) const { return adds_up(rows) ? round_up(windows() * ranges(rows) * parts() * rows * ld_sum() * 4, kWsAlign) : 0; }
+  int64_t sum_bytes(int64_t rows) const { return adds_up(rows) ? round_up(most_ranges(rows) * parts() * rows * ld_sum() * 4, kWsAlign) : 0; }
   int64_t dw_size() const { return round_up(w_rows() * round_up(w_cols(), 4) * 4, kWsAlign) / 4; }                 // float32 elements of a shard's partial
   int64_t dw_bytes(int64_t rows) const { return dw && rows < T ? 2 * nb * dw_size() * 4 : 0; }
   int64_t bytes(int64_t rows) const { return table_bytes() + x_bytes(rows) + z_bytes(rows) + sum_bytes(rows) + dw_bytes(rows); }
@@ -320,6 +323,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   } else {
     for (int64_t j = 0; j < nw; ++j) windows.push_back(Window{static_cast<const char*>(w[static_cast<size_t>(j)].first.data), ldw, j * per_cols, l.valid_v(j)});
   }
+  auto w_from = [&](const Window& v, int64_t entry) { return v.data + (vocab_dim == 0 ? entry * v.ld : entry) * e; };
   // x put together: where dw sums over tokens of several shards, or over both parts of D, and where rows are not padded
   const bool pack_x = l.M > 0 && ((l.dw && (l.na > 1 || lost)) || (!x_padded && l.packing_pays()));
 
@@ -364,11 +368,14 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
         return a.rows > 0 ? launch_pack(a, l.dtype, stream) : static_cast<int32_t>(GSPMD_OK);
       });
     if (st != GSPMD_OK) return st;
-    // ---- logits
+    // ---- logits: one product per segment of rows and vocabulary shard (also where these lie in one copy, whose gaps are no entries)
     std::vector<Problem> ps;
     auto logits = [&](const char* from, int64_t ld, int64_t row, int64_t count) {
-      for (const Window& v : windows)
-        ps.push_back(product(from, ld, v.data, v.ld, z + row * ldz + v.col, ldz, count, v.entries, l.M, count, v.entries));
+      for (int64_t j = 0; j < nw; ++j) {
+        const Window& v = windows.size() == 1 ? windows[0] : windows[static_cast<size_t>(j)];
+        const char* const b = w_from(v, windows.size() == 1 ? j * per_cols : 0);
+        ps.push_back(product(from, ld, b, v.ld, z + row * ldz + j * per_cols, ldz, count, l.valid_v(j), l.M, count, l.valid_v(j)));
+      }
     };
     if (pack_x) {
       logits(x_all, l.ldx(), 0, n);
@@ -379,38 +386,86 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
         return GSPMD_OK;
       });
     }
-    if ((st = run_dots(ps, vocab_dim == 0 ? GSPMD_LAYOUT_RHS_K_CONTIGUOUS : 0, l.dtype, GSPMD_F32, tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
+    const int32_t logits_layout = vocab_dim == 0 ? GSPMD_LAYOUT_RHS_K_CONTIGUOUS : 0;
+    auto rows_args = [&](SoftmaxRows* a, int64_t at, int64_t i0, int64_t shards) {
+      std::memset(a, 0, sizeof(*a));
+      for (int64_t i = 0; i < shards; ++i) {
+        const gspmd_token_buf& tb = token[static_cast<size_t>(i0 + i)][0];
+        a->shard[i] = TokenShard{tb.ids, teacher ? tb.logits : nullptr, tb.weights, tb.loss, tb.lse};
+      }
+      a->z = z + (at - first) * ldz;
+      a->ldz = ldz;
+      a->lost = n;
+      a->first = static_cast<int32_t>(at);
+      a->tokens = static_cast<int32_t>(l.T);
+      a->per_shard = static_cast<int32_t>(l.ts);
+      a->first_shard = static_cast<int32_t>(i0);
+      a->cols = static_cast<int32_t>(l.cols());
+      a->vocab = static_cast<int32_t>(l.V);
+      a->per = static_cast<int32_t>(l.vs);
+      a->per_cols = static_cast<int32_t>(per_cols);
+      a->by_cols = fast_div(static_cast<uint32_t>(per_cols));
+      a->targets = targets;
+      a->inv_tau = 1.f / tau;
+      a->logits_bf16 = teacher && tokens[0].logits_dtype == GSPMD_BF16;
+    };
+    // Without gradients the logits need not be kept: their tiles end in what the losses need of them.
+    const int64_t groups = (l.cols() + 63) / 64, pair_bytes = round_up(groups * n * 8, kWsAlign), target_bytes = round_up(n * targets * 4, kWsAlign);
+    if (!l.dx && !l.dw && l.dtype == GSPMD_BF16 && l.M > 0 && n > 0 && targets <= kStatsTargets && pair_bytes + 2 * target_bytes <= l.z_bytes(rows) && takes_stats(ps, logits_layout)) {
+      char* const base = reinterpret_cast<char*>(z);
+      int32_t* const columns = reinterpret_cast<int32_t*>(base + pair_bytes);
+      float* const of_targets = reinterpret_cast<float*>(base + pair_bytes + target_bytes);
+      for (Problem& p : ps) {
+        const int64_t at = static_cast<float*>(p.C) - z;
+        p.join_first = static_cast<int32_t>(at / ldz);
+        p.join_slot = static_cast<int32_t>(at % ldz);
+        p.C = z;
+        p.ldc = static_cast<int32_t>(n);
+      }
+      auto merge_args = [&](SoftmaxMerge* m, int64_t at, int64_t i0, int64_t shards) {
+        rows_args(&m->rows, at, i0, shards);
+        m->rows.z = z + (at - first) * 2;
+        m->rows.ldz = n;
+        m->rows.cols = static_cast<int32_t>(groups);
+        m->columns = columns + (at - first) * targets;
+        m->logits = of_targets + (at - first) * targets;
+      };
+      st = by_tables([&](int64_t at, int64_t count, int64_t i0, int64_t shards) -> int32_t {
+        SoftmaxMerge m;
+        merge_args(&m, at, i0, shards);
+        m.count = static_cast<int32_t>(std::max<int64_t>(0, std::min(count, first + n - at)));
+        const int64_t total = m.count * static_cast<int64_t>(targets);
+        if (total == 0) return GSPMD_OK;
+        hipLaunchKernelGGL(target_columns_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((total + 255) / 256, 4096))), dim3(256), 0, stream, m);
+        return launched();
+      });
+      if (st != GSPMD_OK) return st;
+      const SoftmaxFinish finish{columns, of_targets, targets, kLog2e / tau};
+      if ((st = run_stats(ps, logits_layout, finish, tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
+      st = by_tables([&](int64_t at, int64_t count, int64_t i0, int64_t shards) -> int32_t {
+        SoftmaxMerge m;
+        merge_args(&m, at, i0, shards);
+        m.count = static_cast<int32_t>(count);
+        if (count >= 4096) hipLaunchKernelGGL((softmax_merge_kernel<16>), dim3(static_cast<unsigned>((count + 15) / 16)), dim3(kMergeThreads), 0, stream, m);
+        else hipLaunchKernelGGL((softmax_merge_kernel<4>), dim3(static_cast<unsigned>((count + 3) / 4)), dim3(kMergeThreads), 0, stream, m);
+        return launched();
+      });
+      if (st != GSPMD_OK) return st;
+      continue;
+    }
+    if ((st = run_dots(ps, logits_layout, l.dtype, GSPMD_F32, tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
     // ---- rows
     st = by_tables([&](int64_t at, int64_t count, int64_t i0, int64_t shards) {
       SoftmaxRows a;
-      std::memset(&a, 0, sizeof(a));
-      for (int64_t i = 0; i < shards; ++i) {
-        const gspmd_token_buf& tb = token[static_cast<size_t>(i0 + i)][0];
-        a.shard[i] = TokenShard{tb.ids, teacher ? tb.logits : nullptr, tb.weights, tb.loss, tb.lse};
-      }
-      a.z = z + (at - first) * ldz;
-      a.ldz = ldz;
-      a.lost = n;
-      a.first = static_cast<int32_t>(at);
-      a.tokens = static_cast<int32_t>(l.T);
-      a.per_shard = static_cast<int32_t>(l.ts);
-      a.first_shard = static_cast<int32_t>(i0);
-      a.cols = static_cast<int32_t>(l.cols());
-      a.vocab = static_cast<int32_t>(l.V);
-      a.per = static_cast<int32_t>(l.vs);
-      a.per_cols = static_cast<int32_t>(per_cols);
-      a.by_cols = fast_div(static_cast<uint32_t>(per_cols));
-      a.targets = targets;
-      a.inv_tau = 1.f / tau;
-      a.logits_bf16 = teacher && tokens[0].logits_dtype == GSPMD_BF16;
+      rows_args(&a, at, i0, shards);
       return launch_rows(a, l, count, stream);
     });
     if (st != GSPMD_OK) return st;
     const char* const d = reinterpret_cast<const char*>(z);
     // ---- dx: the piece's rows
     const int32_t dx_layout = vocab_dim == 0 ? 0 : GSPMD_LAYOUT_RHS_K_CONTIGUOUS;
-    auto w_from = [&](const Window& v, int64_t entry) { return v.data + (vocab_dim == 0 ? entry * v.ld : entry) * e; };
-    if (l.dx && !(l.adds_up(rows) && (lost || windows.size() * l.ranges(rows) > 1))) {
+    const int64_t ranges = windows.size() == 1 ? l.ranges(rows) : l.ranges_of_shard(rows);
+    if (l.dx && !lost && windows.size() == 1 && ranges == 1) {
       ps.clear();
       const Window& v = windows[0];
       each_shard([&](int64_t i, int64_t at, int64_t count, int64_t row) -> int32_t {
@@ -421,7 +476,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
       if ((st = run_dots(ps, dx_layout, l.dtype, l.dtype, tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
     } else if (l.dx && l.M > 0) {
       ps.clear();
-      const int64_t both = n * l.parts(), size = both * l.ld_sum(), ranges = l.ranges(rows);
+      const int64_t both = n * l.parts(), size = both * l.ld_sum();
       for (const Window& v : windows) {
         const int64_t each = round_up((v.entries + ranges - 1) / ranges, 256);
         for (int64_t from = 0; from < v.entries; from += each)

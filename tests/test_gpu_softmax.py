@@ -5,6 +5,7 @@ import torch
 
 import paper_2105_04663_amd as g
 from tests.losses import Problem
+from tests.pin import MFMA, pinned
 
 pytestmark = pytest.mark.gpu
 
@@ -185,6 +186,50 @@ def test_another_stream_and_a_graph():
         for a, b in zip(replayed, [b[1] for b in p.dxs + p.dws] + [t[1]["loss"] for t in p.ts]):
             assert torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0))
     assert np.isfinite(ref["loss"]).all()
+
+
+@pytest.fixture
+def big_tiles():
+    """The calls of a test through dot_mfma_kernel, whose tiles reduce the logits of a call without gradients where they are."""
+    with pinned(MFMA):
+        yield
+
+
+@pytest.mark.parametrize("vocab_dim", [0, 1])
+@pytest.mark.parametrize("T,M,V,K", [(1, 64, 64, None), (17, 72, 65, None), (256, 64, 256, 1), (300, 130, 1025, 3), (513, 96, 700, 33), (40, 1000, 3000, 128), (33, 64, 500, 129)])
+def test_logits_that_are_not_kept(big_tiles, vocab_dim, T, M, V, K):
+    Problem(T, M, V, K=K, vocab_dim=vocab_dim).stage((False, False)).call().check()
+
+
+@pytest.mark.parametrize("mesh,T,V", [((1, 4), 50, 901), ((2, 3), 600, 1300), ((5, 7), 33, 100), ((66, 2), 70, 300), ((3, 8), 1, 9)])
+def test_logits_that_are_not_kept_on_meshes(big_tiles, mesh, T, V):
+    for K, vocab_dim in ((None, 0), (5, 1)):
+        Problem(T, 80, V, K=K, vocab_dim=vocab_dim, mesh=mesh, tau=1.7 if K else 1.0).stage((False, False)).call().check()
+
+
+def test_targets_of_one_tile(big_tiles):
+    """All of 256 tokens' 128 targets in one tile: more than it looks at between two barriers."""
+    p = Problem(300, 64, 2000, K=128, missing=0.3)
+    p.ids[:] = np.where(p.ids >= 0, 512 + p.ids % 256, -1)
+    p.stage((False, False)).call().check()
+
+
+def test_logits_that_are_not_kept_in_pieces(big_tiles):
+    p = Problem(700, 64, 900, K=3, mesh=(2, 2)).stage((False, False))
+    for n in (p.least + (p.bytes - p.least) // 3, p.bytes):
+        p.call(n).check()
+
+
+def test_logits_that_are_not_kept_at_their_ends(big_tiles):
+    p = Problem(40, 64, 300, wscale=30.0).stage((False, False)).call()
+    assert np.abs(p.check()["lse"]).max() > 300
+    p = Problem(20, 64, 300, missing=1.0).stage((False, False)).call()
+    assert not p.check()["loss"].any()
+    p = Problem(20, 64, 300, K=2, missing=0.0)
+    p.logits_t[3, 0] = float("nan")
+    p.xt[5, 1] = float("nan")
+    got = p.stage((False, False)).call().results()
+    assert np.isnan(got["loss"][[3, 5]]).all() and np.isfinite(np.delete(got["loss"], [3, 5])).all()
 
 
 def test_random_problems():
