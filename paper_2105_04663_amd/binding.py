@@ -52,7 +52,7 @@ class _CShardBuf(C.Structure):
     _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("row_stride", C.c_int64)]
 
 
-# what _bufs writes its words by
+# what _bufs and _token_bufs write their words by
 if (sys.byteorder, C.sizeof(_CShardBuf), _CShardBuf.data.offset, _CShardBuf.dtype.offset, _CShardBuf.row_stride.offset) != ("little", 24, 0, 8, 16):
     raise ImportError("unexpected layout of gspmd_shard_buf")
 
@@ -60,6 +60,10 @@ if (sys.byteorder, C.sizeof(_CShardBuf), _CShardBuf.data.offset, _CShardBuf.dtyp
 class _CTokenBuf(C.Structure):
     _fields_ = [("ids", C.c_void_p), ("logits", C.c_void_p), ("logits_dtype", C.c_int32), ("weights", C.c_void_p), ("loss", C.c_void_p),
                 ("lse", C.c_void_p)]
+
+
+if (C.sizeof(_CTokenBuf), _CTokenBuf.logits_dtype.offset, _CTokenBuf.weights.offset, _CTokenBuf.lse.offset) != (48, 16, 24, 40):
+    raise ImportError("unexpected layout of gspmd_token_buf")
 
 
 class _CGemmDesc(C.Structure):
@@ -468,8 +472,14 @@ class TokenBuf:
 
 
 def _token_bufs(tokens: Sequence[TokenBuf]):
-    return (_CTokenBuf * max(1, len(tokens)))(*[_CTokenBuf(b.ids or None, b.logits or None, b.logits_dtype, b.weights or None, b.loss or None, b.lse or None)
-                                                for b in tokens])
+    """Array of _CTokenBuf, written as the six 64-bit words of each."""
+    words = []
+    for b in tokens:
+        words += b.ids, b.logits, b.logits_dtype, b.weights, b.loss, b.lse
+    try:
+        return struct.pack("%dq" % len(words), *words)
+    except struct.error:                                    # None for no array, addresses beyond 63 bits
+        return (C.c_int64 * max(6, len(words)))(*[w or 0 for w in words])
 
 
 def softmax_workspace_bytes(mesh: Mesh, x_sh: Sharding, w_sh: Sharding, vocab_dim: int, dtype: int, gradients: bool, least: bool = False) -> int:
@@ -482,9 +492,10 @@ def softmax_workspace_bytes(mesh: Mesh, x_sh: Sharding, w_sh: Sharding, vocab_di
 
 
 def _loss_shards(mesh: Mesh, x_shards, w_shards, tokens, dx_shards, dw_shards):
-    if any(s is not None and len(s) != mesh.n_partitions for s in (x_shards, w_shards, tokens, dx_shards, dw_shards)):
+    P = mesh.n_partitions
+    if not (len(x_shards) == len(w_shards) == len(tokens) == P) or (dx_shards is not None and len(dx_shards) != P) or (dw_shards is not None and len(dw_shards) != P):
         raise ValueError("one shard buffer per partition is required")
-    return [None if s is None else _bufs(s) for s in (x_shards, w_shards, dx_shards, dw_shards)]
+    return _bufs(x_shards), _bufs(w_shards), None if dx_shards is None else _bufs(dx_shards), None if dw_shards is None else _bufs(dw_shards)
 
 
 def softmax_xent(mesh: Mesh, x_shards: Sequence[ShardBuf], x_sh: Sharding, w_shards: Sequence[ShardBuf], w_sh: Sharding, tokens: Sequence[TokenBuf],

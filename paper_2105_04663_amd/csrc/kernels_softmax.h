@@ -438,8 +438,16 @@ __global__ __launch_bounds__(256) void add_up_kernel(const AddUp args) {
     in_vec sum{};
     if (g < a.tokens) {
       GSPMD_GLOBAL const float* from = (GSPMD_GLOBAL const float*)a.partials + static_cast<int64_t>(row) * a.ld_in + col;
-      sum = *(GSPMD_GLOBAL const in_vec*)from;
-      for (int p = 1; p < a.count; ++p) sum += *(GSPMD_GLOBAL const in_vec*)(from + static_cast<int64_t>(p) * a.stride);
+      // eight on their way at a time: one after the other, 32 of them took 9 us
+      in_vec next[8];
+      for (int p = 0; p < a.count; p += 8) {
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+          if (p + n < a.count) next[n] = *(GSPMD_GLOBAL const in_vec*)(from + static_cast<int64_t>(p + n) * a.stride);
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+          if (p + n < a.count) sum = p + n == 0 ? next[n] : sum + next[n];
+      }
     }
     GSPMD_GLOBAL T* const to = (GSPMD_GLOBAL T*)a.to[i - a.first_shard] + static_cast<int64_t>(at) * a.ld_out + col;
     typedef T out_vec __attribute__((ext_vector_type(V)));

@@ -26,6 +26,7 @@ constexpr int64_t kPieceBytes = int64_t(1) << 31;
 constexpr int64_t kColumnAlign = 64;
 // Up to so many tokens what D's rounding to bfloat16 loses takes part in the products, as rows of its own: these are bound by w and dw then.
 constexpr int64_t kFewTokens = 64;
+constexpr int64_t kFewRows = 256;            // less than a tile
 
 struct Loss {
   const gspmd_mesh* mesh = nullptr;
@@ -62,8 +63,10 @@ struct Loss {
   int64_t most_ranges(int64_t rows) const { return std::max(ranges(rows), windows() * ranges_of_shard(rows)); }
   bool adds_up(int64_t rows) const { return dx && (most_ranges(rows) > 1 || with_lost()); }
   int64_t most_rows() const { return std::min(T, std::max<int64_t>(1, kPieceBytes / (ldz() * 4))); }
-  // Copies of operands whose rows are not padded to 16 bytes, which the products read several times slower than they are copied once: from this many rows of products on.
+  // A padded copy of operands whose rows are not padded to 16 bytes, which the products read several times slower than they are copied once: from this many rows of products on ..
   bool packing_pays() const { return dtype == GSPMD_BF16 && T * (dx || dw ? 3 : 1) >= 1024; }
+  // .. and of a vocabulary in many shards, where dx's partials, one for each, would be more than that copy (4085 tokens, 2834 x 2393 on 3 x 8: 439 us without).
+  bool joining_pays() const { return dx && windows() > 1 && 2 * T * windows() >= V; }
   int64_t packed_w_bytes() const { return round_up((vocab_dim == 0 ? ldz() * ldx() : std::max<int64_t>(M, 1) * ldz()) * esize(), kWsAlign); }
   // ---- the workspace, for pieces of `rows` tokens
   int64_t table_bytes() const { return round_up((na * nb + 32 + nb) * kTableBytesPerProblem, kWsAlign); }
@@ -287,7 +290,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   bool w_padded = true, x_padded = true;
   for (int64_t j = 0; j < nw; ++j) w_padded = w_padded && padded(w[static_cast<size_t>(j)].first, ldw);
   for (int64_t i = 0; i < l.na; ++i) x_padded = x_padded && padded(x[static_cast<size_t>(i)].first, ldx_in);
-  if (!w_padded && l.packing_pays() && room_w >= l.packed_w_bytes() && l.M > 0) {
+  if (((!w_padded && l.packing_pays()) || l.joining_pays()) && room_w >= l.packed_w_bytes() && l.M > 0) {
     const int64_t ld = vocab_dim == 0 ? l.ldx() : ldz, chunks = ld / vec;
     for (int64_t from = 0; from < nw && !dry; from += kInlineTokenShards) {
       const int64_t n = std::min<int64_t>(kInlineTokenShards, nw - from);
@@ -324,8 +327,9 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
     for (int64_t j = 0; j < nw; ++j) windows.push_back(Window{static_cast<const char*>(w[static_cast<size_t>(j)].first.data), ldw, j * per_cols, l.valid_v(j)});
   }
   auto w_from = [&](const Window& v, int64_t entry) { return v.data + (vocab_dim == 0 ? entry * v.ld : entry) * e; };
-  // x put together: where dw sums over tokens of several shards, or over both parts of D, and where rows are not padded
-  const bool pack_x = l.M > 0 && ((l.dw && (l.na > 1 || lost)) || (!x_padded && l.packing_pays()));
+  // x put together: where dw sums over tokens of several shards, or over both parts of D, where shards have so few tokens that each would read the vocabulary matrix for
+  // itself (15 tokens in two shards, 8099 x 124058: 690 us so), and where rows are not padded
+  const bool pack_x = l.M > 0 && ((l.dw && (l.na > 1 || lost)) || (l.na > 1 && l.ts < kFewRows) || (!x_padded && l.packing_pays()));
 
   for (int64_t piece = 0; piece < pieces; ++piece) {
     const int64_t first = piece * rows, n = std::min(rows, l.T - first);       // tokens
@@ -368,25 +372,36 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
         return a.rows > 0 ? launch_pack(a, l.dtype, stream) : static_cast<int32_t>(GSPMD_OK);
       });
     if (st != GSPMD_OK) return st;
-    // ---- logits: one product per segment of rows and vocabulary shard (also where these lie in one copy, whose gaps are no entries)
+    // ---- logits.  Where they need not be kept (without gradients) their tiles end in what the losses need of them.
+    const int64_t groups = (l.cols() + 63) / 64, pair_bytes = round_up(groups * n * 8, kWsAlign), target_bytes = round_up(n * targets * 4, kWsAlign);
+    bool stats = !l.dx && !l.dw && l.dtype == GSPMD_BF16 && l.M > 0 && n > 0 && targets <= kStatsTargets && pair_bytes + 2 * target_bytes <= l.z_bytes(rows);
+    const int32_t logits_layout = vocab_dim == 0 ? GSPMD_LAYOUT_RHS_K_CONTIGUOUS : 0;
     std::vector<Problem> ps;
     auto logits = [&](const char* from, int64_t ld, int64_t row, int64_t count) {
-      for (int64_t j = 0; j < nw; ++j) {
-        const Window& v = windows.size() == 1 ? windows[0] : windows[static_cast<size_t>(j)];
-        const char* const b = w_from(v, windows.size() == 1 ? j * per_cols : 0);
-        ps.push_back(product(from, ld, b, v.ld, z + row * ldz + j * per_cols, ldz, count, l.valid_v(j), l.M, count, l.valid_v(j)));
+      const bool one = windows.size() == 1;                  // one copy of all shards, zeros between: one product; but what lies between is no entry of the vocabulary
+      for (int64_t j = 0; j < (one && !stats ? 1 : nw); ++j) {
+        const Window& v = windows[one ? 0 : static_cast<size_t>(j)];
+        const int64_t entries = one && !stats ? v.entries : l.valid_v(j);
+        ps.push_back(product(from, ld, w_from(v, one ? j * per_cols : 0), v.ld, z + row * ldz + j * per_cols, ldz, count, entries, l.M, count, entries));
       }
     };
-    if (pack_x) {
-      logits(x_all, l.ldx(), 0, n);
-    } else {
+    auto all_logits = [&] {
+      ps.clear();
+      if (pack_x) {
+        logits(x_all, l.ldx(), 0, n);
+        return;
+      }
       each_shard([&](int64_t i, int64_t at, int64_t count, int64_t row) -> int32_t {
         const int64_t valid = std::min(count, n - row);
         if (valid > 0) logits(static_cast<const char*>(x[static_cast<size_t>(i)].first.data) + at * ldx_in * e, ldx_in, row, valid);
         return GSPMD_OK;
       });
+    };
+    all_logits();
+    if (stats && !takes_stats(ps, logits_layout)) {
+      stats = false;
+      all_logits();
     }
-    const int32_t logits_layout = vocab_dim == 0 ? GSPMD_LAYOUT_RHS_K_CONTIGUOUS : 0;
     auto rows_args = [&](SoftmaxRows* a, int64_t at, int64_t i0, int64_t shards) {
       std::memset(a, 0, sizeof(*a));
       for (int64_t i = 0; i < shards; ++i) {
@@ -409,9 +424,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
       a->inv_tau = 1.f / tau;
       a->logits_bf16 = teacher && tokens[0].logits_dtype == GSPMD_BF16;
     };
-    // Without gradients the logits need not be kept: their tiles end in what the losses need of them.
-    const int64_t groups = (l.cols() + 63) / 64, pair_bytes = round_up(groups * n * 8, kWsAlign), target_bytes = round_up(n * targets * 4, kWsAlign);
-    if (!l.dx && !l.dw && l.dtype == GSPMD_BF16 && l.M > 0 && n > 0 && targets <= kStatsTargets && pair_bytes + 2 * target_bytes <= l.z_bytes(rows) && takes_stats(ps, logits_layout)) {
+    if (stats) {
       char* const base = reinterpret_cast<char*>(z);
       int32_t* const columns = reinterpret_cast<int32_t*>(base + pair_bytes);
       float* const of_targets = reinterpret_cast<float*>(base + pair_bytes + target_bytes);
@@ -576,7 +589,7 @@ int32_t gspmd_softmax_workspace_bytes(const gspmd_mesh* mesh, const gspmd_shardi
   l.dtype = dtype;
   l.dx = l.dw = gradients != 0;
   const int64_t rows = l.most_rows();
-  *bytes = l.bytes(rows) + (l.packing_pays() ? l.packed_w_bytes() : 0);
+  *bytes = l.bytes(rows) + (l.packing_pays() || l.joining_pays() ? l.packed_w_bytes() : 0);
   if (least) *least = std::min(*bytes, l.bytes(std::min<int64_t>(l.T, 1)));
   return GSPMD_OK;
 } catch (...) { return GSPMD_ERR_HOST_MEMORY; }
