@@ -14,6 +14,7 @@
 
 #include "../../include/gspmd.h"
 #include "dots.h"
+#include "kernels_few.h"
 #include "kernels_softmax.h"
 #include "kernels_stats.h"
 #include "plan.h"
@@ -27,6 +28,8 @@ constexpr int64_t kColumnAlign = 64;
 // Up to so many tokens what D's rounding to bfloat16 loses takes part in the products, as rows of its own: these are bound by w and dw then.
 constexpr int64_t kFewTokens = 64;
 constexpr int64_t kFewRows = 256;            // less than a tile
+constexpr int64_t kFewWeights = int64_t(32) << 20;
+constexpr int64_t kFewWorkgroups = 3072;     // of the kernels for a handful of tokens
 
 struct Loss {
   const gspmd_mesh* mesh = nullptr;
@@ -75,6 +78,40 @@ struct Loss {
   int64_t sum_bytes(int64_t rows) const { return adds_up(rows) ? round_up(most_ranges(rows) * parts() * rows * ld_sum() * 4, kWsAlign) : 0; }
   int64_t dw_size() const { return round_up(w_rows() * round_up(w_cols(), 4) * 4, kWsAlign) / 4; }                 // float32 elements of a shard's partial
   int64_t dw_bytes(int64_t rows) const { return dw && rows < T ? 2 * nb * dw_size() * 4 : 0; }
+  // ---- a handful of tokens (kernels_few.h): as many as were measured faster there, all sizes of w from 0.6 to 262 MB together (us, a step with gradients, these kernels / the others;
+  // M x V): float32, [V, M], 1 token 640 x 10368 32 / 51, 2048 x 32000 182 / 225; 8 tokens 37 / 52, 185 / 237; 16 tokens 55 / 53, 242 / 239; [M, V], 4 tokens 40 / 52, 183 / 225;
+  // 8 tokens 50 / 53, 131 / 123 (2048 x 16000).  bfloat16, [V, M], 1 token 128 x 2304 27 / 34, 1024 x 16000 34 / 42, 2048 x 16000 55 / 57, 2048 x 32000 106 / 101; 3 tokens 24 / 32, 39 / 41,
+  // 63 / 58, 115 / 102; 8 tokens 640 x 10368 43 / 35; losses alone, 1 token 640 x 10368 15 / 16, 3 or more slower; [M, V], 3 tokens 640 x 10368 36 / 35, 2048 x 16000 84 / 59.
+  // bfloat16 beyond 32 MB of w: only where its rows are not padded, which the others read slowly (3 tokens, 4279 x 29599 in 4 shards 302).
+  bool few() const {
+    const int64_t most = dtype == GSPMD_F32 ? (vocab_dim == 0 ? 8 : 4) : vocab_dim == 0 && (dx || dw) ? 4 : 0;
+    return T > 0 && T <= most && M > 0 && nb <= kFewWindows && na <= kInlineTokenShards;
+  }
+  bool few_takes(bool w_padded) const { return few() && (dtype == GSPMD_F32 || !w_padded || V * M * 2 <= kFewWeights); }
+  int64_t few_lanes() const {                // [V, M]: of a row
+    int64_t lanes = 1;
+    while (lanes < 64 && lanes * 16 / esize() < M) lanes *= 2;
+    return lanes;
+  }
+  // Ranges of the vocabulary that dx has partials of: enough workgroups, as long as the partials are little beside w.
+  int64_t few_ranges(int64_t* each, int64_t* blocks) const {
+    if (vocab_dim == 1) {
+      *blocks = (vs + 1024 / esize() - 1) / (1024 / esize());
+      const int64_t y = std::max<int64_t>(1, std::min<int64_t>(kFewWorkgroups / std::max<int64_t>(nb * *blocks, 1), M / 32));
+      *each = round_up((M + y - 1) / y, 32);
+      return nb * *blocks;
+    }
+    const int64_t across = few_across(), sides = 4 * (64 / few_lanes());
+    const int64_t ranges = std::max<int64_t>(1, std::min({kFewWorkgroups / across, V * esize() / (32 * T), int64_t(512)}) / nb);
+    *each = round_up((vs + ranges - 1) / ranges, sides);
+    *blocks = (vs + *each - 1) / *each;
+    return nb * *blocks;
+  }
+  int64_t few_across() const { return (M + few_lanes() * 16 / esize() - 1) / (few_lanes() * 16 / esize()); }
+  int64_t few_bytes() const {
+    int64_t each, blocks;
+    return round_up(T * ldz() * 4, kWsAlign) + (dx ? few_ranges(&each, &blocks) * T * ld_sum() * 4 : 0);
+  }
   int64_t bytes(int64_t rows) const { return table_bytes() + x_bytes(rows) + z_bytes(rows) + sum_bytes(rows) + dw_bytes(rows); }
 };
 
@@ -200,6 +237,68 @@ Problem product(const void* a, int64_t lda, const void* b, int64_t ldb, void* c,
   return p;
 }
 
+// The calls' kernels for a handful of tokens: `a` and `rows` hold the arguments of both products and of the row kernel.
+template <typename T, int NT>
+int32_t launch_few_logits(const FewTokens& a, const Loss& l, hipStream_t stream) {
+  FewTokens b = a;
+  if (l.vocab_dim == 0) {
+    constexpr int kRows = NT >= 4 ? 4 : 8;
+    const int64_t per_block = 4 * (64 / a.lanes) * kRows;
+    b.blocks = static_cast<int32_t>((l.vs + per_block - 1) / per_block);
+    hipLaunchKernelGGL((few_logits_kernel<T, NT, kRows>), dim3(static_cast<unsigned>(l.windows() * b.blocks)), dim3(256), 0, stream, b);
+  } else if constexpr (sizeof(T) == 4 && NT <= 4) {
+    auto go = [&](auto side) {               // narrower where wide ones would leave compute units without one
+      constexpr int kSide = decltype(side)::value, kCols = kSide * few_vec<T>(), lds = std::max(512 * NT, (kFewAcross / 64) * NT * kCols) * 4;
+      b.blocks = static_cast<int32_t>((l.vs + kCols - 1) / kCols);
+      hipLaunchKernelGGL((few_logits_across_kernel<T, NT, kSide>), dim3(static_cast<unsigned>(l.windows() * b.blocks)), dim3(kFewAcross), lds, stream, b);
+    };
+    if (l.V >= 64 * 16 * few_vec<T>()) go(std::integral_constant<int, 16>{}); else go(std::integral_constant<int, 4>{});
+  }
+  return launched();
+}
+
+template <typename T, int NT>
+int32_t launch_few_gradients(const FewTokens& a, const Loss& l, int64_t ranges, hipStream_t stream) {
+  if (l.vocab_dim == 0)
+    hipLaunchKernelGGL((few_gradients_kernel<T, NT>), dim3(static_cast<unsigned>(l.few_across()), static_cast<unsigned>(ranges)), dim3(256), (few_gradients_lds<T, NT>(a.lanes)), stream, a);
+  else if constexpr (sizeof(T) == 4 && NT <= 4)
+    hipLaunchKernelGGL((few_gradients_across_kernel<T, NT>), dim3(static_cast<unsigned>(ranges), static_cast<unsigned>((l.M + a.each - 1) / a.each)), dim3(256), 256 * NT * 4, stream, a);
+  return launched();
+}
+
+template <typename T, typename Go>
+int32_t few_by_tokens(int64_t tokens, Go go) {
+  if (tokens <= 1) return go(std::integral_constant<int, 1>{});
+  if (tokens <= 2) return go(std::integral_constant<int, 2>{});
+  if constexpr (sizeof(T) == 4) if (tokens > 4) return go(std::integral_constant<int, 8>{});
+  return go(std::integral_constant<int, 4>{});
+}
+
+template <typename T>
+int32_t run_few(const Loss& l, FewTokens& a, const SoftmaxRows& rows, AddUp& sums, hipStream_t stream) {
+  int32_t st = few_by_tokens<T>(l.T, [&](auto nt) { return launch_few_logits<T, decltype(nt)::value>(a, l, stream); });
+  if (st != GSPMD_OK) return st;
+  const unsigned tokens = static_cast<unsigned>(l.na * l.ts);
+  if (l.dx || l.dw) launch_rows_as<float, true, false>(rows, tokens, stream); else launch_rows_as<float, false, false>(rows, tokens, stream);
+  if ((st = launched()) != GSPMD_OK || !(l.dx || l.dw)) return st;
+  int64_t each, blocks;
+  const int64_t ranges = l.few_ranges(&each, &blocks);
+  a.each = static_cast<int32_t>(each);
+  a.blocks = static_cast<int32_t>(blocks);
+  st = few_by_tokens<T>(l.T, [&](auto nt) { return launch_few_gradients<T, decltype(nt)::value>(a, l, ranges, stream); });
+  if (st != GSPMD_OK || !l.dx) return st;
+  sums.partials = a.sums;
+  sums.stride = l.T * l.ld_sum();
+  sums.ld_in = l.ld_sum();
+  sums.count = static_cast<int32_t>(ranges);
+  bool four = !(l.M & 3) && !(sums.ld_out & 3);
+  for (int64_t i = 0; i < l.na; ++i) four = four && !(reinterpret_cast<uintptr_t>(sums.to[i]) & (4 * sizeof(T) - 1));
+  const dim3 grid(static_cast<unsigned>((l.M + (four ? 63 : 15)) / (four ? 64 : 16)), static_cast<unsigned>(sums.rows));
+  if (four) hipLaunchKernelGGL((add_up_few_kernel<T, 4>), grid, dim3(256), 0, stream, sums);
+  else hipLaunchKernelGGL((add_up_few_kernel<T, 1>), grid, dim3(256), 0, stream, sums);
+  return launched();
+}
+
 int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const gspmd_sharding* x_sh, const gspmd_shard_buf* w_shards, const gspmd_sharding* w_sh, int32_t vocab_dim,
                  const gspmd_token_buf* tokens, int32_t targets, float tau, bool teacher, const gspmd_shard_buf* dx_shards, const gspmd_shard_buf* dw_shards, void* workspace,
                  int64_t workspace_bytes, void* hip_stream) {
@@ -250,8 +349,97 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   // (the first of a shard's is what the kernel writes: one with an lse, if any has)
   for (auto& list : token) std::stable_partition(list.begin(), list.end(), [](const gspmd_token_buf& tb) { return tb.lse != nullptr; });
 
-  // ---- pieces: as many tokens as the workspace holds (more than the query asks for is not used)
+  // partitions that hold the same results in buffers of their own
+  const bool dry = launches_are_dry();
+  const int64_t ldx_in = stride_of(x_shards[0], l.M), ldw = stride_of(w_shards[0], w_cols);
+  const int64_t lddx = l.dx ? stride_of(dx_shards[0], l.M) : 0, lddw = l.dw ? stride_of(dw_shards[0], w_cols) : 0;
+  auto spread_results = [&]() -> int32_t {
+    if (dry) return GSPMD_OK;
+    auto spread = [&](const std::vector<Buffers>& at, int64_t r, int64_t c, int64_t ld) {
+      for (const auto& b : at)
+        for (const auto& o : b.others)
+          if ((st = copy_rows(b.first, o, r, c, ld, ld, stream)) != GSPMD_OK) return st;
+      return static_cast<int32_t>(GSPMD_OK);
+    };
+    if (l.dx && (st = spread(dx, l.ts, l.M, lddx)) != GSPMD_OK) return st;
+    if (l.dw && (st = spread(dw, w_rows, w_cols, lddw)) != GSPMD_OK) return st;
+    for (const auto& list : token)
+      for (size_t k = 1; k < list.size(); ++k) {
+        auto one = [&](float* from, float* to) {
+          if (!from || !to || from == to) return static_cast<int32_t>(GSPMD_OK);
+          return copy_rows(gspmd_shard_buf{from, GSPMD_F32, 0}, gspmd_shard_buf{to, GSPMD_F32, 0}, 1, l.ts, l.ts, l.ts, stream);
+        };
+        if ((st = one(list[0].loss, list[k].loss)) != GSPMD_OK || (st = one(list[0].lse, list[k].lse)) != GSPMD_OK) return st;
+      }
+    return GSPMD_OK;
+  };
+
+  auto rows_args = [&](SoftmaxRows* a, float* z, int64_t at, int64_t i0, int64_t shards) {      // for rows of tokens `at` .. of all, the first of them in shard i0
+    std::memset(a, 0, sizeof(*a));
+    for (int64_t i = 0; i < shards; ++i) {
+      const gspmd_token_buf& tb = token[static_cast<size_t>(i0 + i)][0];
+      a->shard[i] = TokenShard{tb.ids, teacher ? tb.logits : nullptr, tb.weights, tb.loss, tb.lse};
+    }
+    a->z = z;
+    a->ldz = l.ldz();
+    a->first = static_cast<int32_t>(at);
+    a->tokens = static_cast<int32_t>(l.T);
+    a->per_shard = static_cast<int32_t>(l.ts);
+    a->first_shard = static_cast<int32_t>(i0);
+    a->cols = static_cast<int32_t>(l.cols());
+    a->vocab = static_cast<int32_t>(l.V);
+    a->per = static_cast<int32_t>(l.vs);
+    a->per_cols = static_cast<int32_t>(l.per_cols());
+    a->by_cols = fast_div(static_cast<uint32_t>(l.per_cols()));
+    a->targets = targets;
+    a->inv_tau = 1.f / tau;
+    a->logits_bf16 = teacher && tokens[0].logits_dtype == GSPMD_BF16;
+  };
+
+  // ---- a handful of tokens: kernels of their own, all tokens at once
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & (kWsAlign - 1))) return GSPMD_ERR_WORKSPACE;
+  bool w_padded = true;
+  for (int64_t j = 0; j < l.windows(); ++j) w_padded = w_padded && padded(w[static_cast<size_t>(j)].first, ldw);
+  if (l.few_takes(w_padded) && workspace_bytes >= l.few_bytes()) {
+    if (dry) return GSPMD_OK;
+    FewTokens a;
+    std::memset(&a, 0, sizeof(a));
+    AddUp sums;
+    std::memset(&sums, 0, sizeof(sums));
+    SoftmaxRows rows;
+    a.z = static_cast<float*>(workspace);
+    rows_args(&rows, a.z, 0, 0, l.na);
+    for (int64_t j = 0; j < l.nb; ++j) {
+      a.w[j] = w[static_cast<size_t>(j)].first.data;
+      a.dw[j] = l.dw ? dw[static_cast<size_t>(j)].first.data : nullptr;
+    }
+    for (int64_t n = 0; n < kFewMost; ++n) {
+      const int64_t t = std::min(n, l.T - 1);
+      a.x[n] = static_cast<const char*>(x[static_cast<size_t>(t / l.ts)].first.data) + t % l.ts * ldx_in * l.esize();
+    }
+    a.sums = l.dx ? a.z + round_up(l.T * l.ldz() * 4, kWsAlign) / 4 : nullptr;
+    a.ldz = l.ldz();
+    a.ldw = ldw;
+    a.lddw = lddw;
+    a.ld_sum = l.ld_sum();
+    a.tokens = static_cast<int32_t>(l.T);
+    a.M = static_cast<int32_t>(l.M);
+    a.vocab = static_cast<int32_t>(l.V);
+    a.per = static_cast<int32_t>(l.vs);
+    a.per_cols = static_cast<int32_t>(l.per_cols());
+    a.shards = static_cast<int32_t>(l.nb);
+    a.lanes = static_cast<int32_t>(l.few_lanes());
+    for (int64_t i = 0; l.dx && i < l.na; ++i) sums.to[i] = dx[static_cast<size_t>(i)].first.data;
+    sums.ld_out = lddx;
+    sums.rows = static_cast<int32_t>(l.na * l.ts);
+    sums.cols = a.M;
+    sums.tokens = a.tokens;
+    sums.per_row = static_cast<int32_t>(l.ts);
+    st = l.dtype == GSPMD_BF16 ? run_few<bf16_bits>(l, a, rows, sums, stream) : run_few<float>(l, a, rows, sums, stream);
+    return st != GSPMD_OK ? st : spread_results();
+  }
+
+  // ---- pieces: as many tokens as the workspace holds (more than the query asks for is not used)
   int64_t rows = l.most_rows();
   if (l.bytes(rows) > workspace_bytes) {
     int64_t fit = 0;                            // the most that fit (bytes() does not grow evenly: ranges fall as rows grow, so every size is looked at by halves)
@@ -280,15 +468,12 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   char* const w_all = ws;
   const int64_t room_w = workspace_bytes - (ws - static_cast<char*>(workspace));
   const int64_t e = l.esize(), ldz = l.ldz(), ldd = ldz * 4 / e, per_cols = l.per_cols(), nw = l.windows(), vec = 16 / e;
-  const bool dry = launches_are_dry(), lost = l.with_lost();
-  const int64_t ldx_in = stride_of(x_shards[0], l.M), ldw = stride_of(w_shards[0], w_cols);
-  const int64_t lddx = l.dx ? stride_of(dx_shards[0], l.M) : 0, lddw = l.dw ? stride_of(dw_shards[0], w_cols) : 0;
+  const bool lost = l.with_lost();
 
   // ---- the vocabulary matrix: shard by shard, or in one padded copy of all of them (zeros between)
   struct Window { const char* data; int64_t ld, col, entries; };
   std::vector<Window> windows;
-  bool w_padded = true, x_padded = true;
-  for (int64_t j = 0; j < nw; ++j) w_padded = w_padded && padded(w[static_cast<size_t>(j)].first, ldw);
+  bool x_padded = true;
   for (int64_t i = 0; i < l.na; ++i) x_padded = x_padded && padded(x[static_cast<size_t>(i)].first, ldx_in);
   if (((!w_padded && l.packing_pays()) || l.joining_pays()) && room_w >= l.packed_w_bytes() && l.M > 0) {
     const int64_t ld = vocab_dim == 0 ? l.ldx() : ldz, chunks = ld / vec;
@@ -402,28 +587,6 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
       stats = false;
       all_logits();
     }
-    auto rows_args = [&](SoftmaxRows* a, int64_t at, int64_t i0, int64_t shards) {
-      std::memset(a, 0, sizeof(*a));
-      for (int64_t i = 0; i < shards; ++i) {
-        const gspmd_token_buf& tb = token[static_cast<size_t>(i0 + i)][0];
-        a->shard[i] = TokenShard{tb.ids, teacher ? tb.logits : nullptr, tb.weights, tb.loss, tb.lse};
-      }
-      a->z = z + (at - first) * ldz;
-      a->ldz = ldz;
-      a->lost = n;
-      a->first = static_cast<int32_t>(at);
-      a->tokens = static_cast<int32_t>(l.T);
-      a->per_shard = static_cast<int32_t>(l.ts);
-      a->first_shard = static_cast<int32_t>(i0);
-      a->cols = static_cast<int32_t>(l.cols());
-      a->vocab = static_cast<int32_t>(l.V);
-      a->per = static_cast<int32_t>(l.vs);
-      a->per_cols = static_cast<int32_t>(per_cols);
-      a->by_cols = fast_div(static_cast<uint32_t>(per_cols));
-      a->targets = targets;
-      a->inv_tau = 1.f / tau;
-      a->logits_bf16 = teacher && tokens[0].logits_dtype == GSPMD_BF16;
-    };
     if (stats) {
       char* const base = reinterpret_cast<char*>(z);
       int32_t* const columns = reinterpret_cast<int32_t*>(base + pair_bytes);
@@ -436,8 +599,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
         p.ldc = static_cast<int32_t>(n);
       }
       auto merge_args = [&](SoftmaxMerge* m, int64_t at, int64_t i0, int64_t shards) {
-        rows_args(&m->rows, at, i0, shards);
-        m->rows.z = z + (at - first) * 2;
+        rows_args(&m->rows, z + (at - first) * 2, at, i0, shards);
         m->rows.ldz = n;
         m->rows.cols = static_cast<int32_t>(groups);
         m->columns = columns + (at - first) * targets;
@@ -470,7 +632,8 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
     // ---- rows
     st = by_tables([&](int64_t at, int64_t count, int64_t i0, int64_t shards) {
       SoftmaxRows a;
-      rows_args(&a, at, i0, shards);
+      rows_args(&a, z + (at - first) * ldz, at, i0, shards);
+      a.lost = n;
       return launch_rows(a, l, count, stream);
     });
     if (st != GSPMD_OK) return st;
@@ -551,25 +714,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
       }
     }
   }
-  // ---- partitions that hold the same results in buffers of their own
-  if (dry) return GSPMD_OK;
-  auto spread = [&](const std::vector<Buffers>& at, int64_t r, int64_t c, int64_t ld) {
-    for (const auto& b : at)
-      for (const auto& o : b.others)
-        if ((st = copy_rows(b.first, o, r, c, ld, ld, stream)) != GSPMD_OK) return st;
-    return static_cast<int32_t>(GSPMD_OK);
-  };
-  if (l.dx && (st = spread(dx, l.ts, l.M, lddx)) != GSPMD_OK) return st;
-  if (l.dw && (st = spread(dw, w_rows, w_cols, lddw)) != GSPMD_OK) return st;
-  for (const auto& list : token)
-    for (size_t k = 1; k < list.size(); ++k) {
-      auto one = [&](float* from, float* to) {
-        if (!from || !to || from == to) return static_cast<int32_t>(GSPMD_OK);
-        return copy_rows(gspmd_shard_buf{from, GSPMD_F32, 0}, gspmd_shard_buf{to, GSPMD_F32, 0}, 1, l.ts, l.ts, l.ts, stream);
-      };
-      if ((st = one(list[0].loss, list[k].loss)) != GSPMD_OK || (st = one(list[0].lse, list[k].lse)) != GSPMD_OK) return st;
-    }
-  return GSPMD_OK;
+  return spread_results();
 }
 
 }  // namespace
@@ -590,6 +735,7 @@ int32_t gspmd_softmax_workspace_bytes(const gspmd_mesh* mesh, const gspmd_shardi
   l.dx = l.dw = gradients != 0;
   const int64_t rows = l.most_rows();
   *bytes = l.bytes(rows) + (l.packing_pays() || l.joining_pays() ? l.packed_w_bytes() : 0);
+  if (l.few()) *bytes = std::max(*bytes, l.few_bytes());
   if (least) *least = std::min(*bytes, l.bytes(std::min<int64_t>(l.T, 1)));
   return GSPMD_OK;
 } catch (...) { return GSPMD_ERR_HOST_MEMORY; }

@@ -188,6 +188,27 @@ def test_another_stream_and_a_graph():
     assert np.isfinite(ref["loss"]).all()
 
 
+# a handful of tokens, which have kernels of their own: every number of them that these provide for, rows of fewer elements than a lane takes and of more than a workgroup's
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab_dim", [0, 1])
+@pytest.mark.parametrize("T,M,V", [(1, 1, 1), (1, 5, 700), (2, 64, 129), (3, 515, 1000), (4, 1030, 333), (5, 72, 5003), (8, 2100, 90), (8, 17, 40), (11, 300, 777), (16, 520, 1300)])
+def test_a_handful_of_tokens(dtype, vocab_dim, T, M, V):
+    for K, pad in ((None, True), (6, False)):
+        p = Problem(T, M, V, dtype, K=K, vocab_dim=vocab_dim, pad=pad, missing=0.1).stage()
+        p.call().check()
+        if p.least < p.bytes:                           # the other path
+            p.call(p.least).check()
+
+
+@pytest.mark.parametrize("vocab_dim", [0, 1])
+@pytest.mark.parametrize("mesh,T,V", [((2, 3), 7, 1000), ((5, 8), 3, 61), ((16, 2), 16, 300), ((1, 64), 2, 100), ((1, 65), 2, 100), ((3, 4), 8, 9)])
+def test_a_handful_of_tokens_on_meshes(mesh, T, V, vocab_dim):
+    for dtype, K, share in (("bf16", None, True), ("f32", 3, False)):
+        Problem(T, 96, V, dtype, K=K, vocab_dim=vocab_dim, mesh=mesh, pad=T % 2 == 0, share=share).stage().call().check()
+        for grad in ((True, False), (False, True), (False, False)):
+            Problem(T, 96, V, dtype, K=K, vocab_dim=vocab_dim, mesh=mesh, pad=T % 2 == 0, share=share).stage(grad).call().check()
+
+
 @pytest.fixture
 def big_tiles():
     """The calls of a test through dot_mfma_kernel, whose tiles reduce the logits of a call without gradients where they are."""
