@@ -420,39 +420,20 @@ __global__ __launch_bounds__(256) void few_gradients_across_kernel(const FewToke
   }
 }
 
-// Token shards of dx = the sum of `count` partials of few rows: 16 threads side by side (V columns each), 16 sharing the partials of each, whose sums meet in LDS in ascending order.
-template <typename T, int V>
+// Token shards of dx = the sum of `count` partials of few rows: 16 threads side by side (4 columns each), 16 sharing the partials of each, whose sums meet in LDS in ascending order.
+template <typename T>
 __global__ __launch_bounds__(256) void add_up_few_kernel(const AddUp args) {
   const GSPMD_KERNARG AddUp& a = *first_kernel_argument<AddUp>();
-  typedef float in_vec __attribute__((ext_vector_type(V)));
-  typedef T out_vec __attribute__((ext_vector_type(V)));
-  __shared__ in_vec parts[16][16];
-  const int x = threadIdx.x & 15, part = threadIdx.x >> 4, col = (blockIdx.x * 16 + x) * V, row = blockIdx.y;
-  const int g = a.first + row, i = g / a.per_row, at = g - i * a.per_row, each = (a.count + 15) / 16, begin = part * each, end = min(begin + each, a.count);
-  in_vec sum{};
-  if (col < a.cols && g < a.tokens) {
-    GSPMD_GLOBAL const float* from = (GSPMD_GLOBAL const float*)a.partials + static_cast<int64_t>(row) * a.ld_in + col;
-    in_vec next[8];
-    for (int p = begin; p < end; p += 8) {
-#pragma unroll
-      for (int n = 0; n < 8; ++n)
-        if (p + n < end) next[n] = *(GSPMD_GLOBAL const in_vec*)(from + static_cast<int64_t>(p + n) * a.stride);
-#pragma unroll
-      for (int n = 0; n < 8; ++n)
-        if (p + n < end) sum += next[n];
-    }
-  }
+  __shared__ f32x4 parts[16][16];
+  const int x = threadIdx.x & 15, part = threadIdx.x >> 4, col = (blockIdx.x * 16 + x) * 4, row = blockIdx.y;
+  const int g = a.first + row, i = g / a.per_row, at = g - i * a.per_row, each = (a.count + 15) / 16, begin = part * each;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  if (col < a.cols && g < a.tokens) sum = sum_partials((GSPMD_GLOBAL const float*)a.partials + static_cast<int64_t>(row) * a.ld_in + col, a.stride, begin, min(begin + each, a.count));
   parts[part][x] = sum;
   __syncthreads();
   if (part != 0 || col >= a.cols) return;
   for (int p = 1; p < 16; ++p) sum += parts[p][x];
-  out_vec o;
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    if constexpr (sizeof(T) == 2) o[e] = __builtin_bit_cast(bf16_bits, static_cast<__bf16>(sum[e]));
-    else o[e] = sum[e];
-  }
-  *(GSPMD_GLOBAL out_vec*)((GSPMD_GLOBAL T*)a.to[i - a.first_shard] + static_cast<int64_t>(at) * a.ld_out + col) = o;
+  store_sum<T>((GSPMD_GLOBAL T*)a.to[i - a.first_shard] + static_cast<int64_t>(at) * a.ld_out + col, sum, a.cols - col);
 }
 
 }  // namespace gspmd

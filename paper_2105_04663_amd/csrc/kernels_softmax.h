@@ -99,11 +99,11 @@ __device__ __forceinline__ TargetSums over_targets(int K, Q q_of, U u_of, Keep k
 }
 
 // Bound by memory: reads 4 bytes a logit, writes 2 (4 in float32).  A workgroup takes a row and keeps it in registers between the maximum and D, so that it is read once (LONG,
-// beyond 48 K columns: twice, the second time mostly from the caches).  The row's loads go first: what a token's targets need, two accesses one after the other, comes while they are under way.
+// beyond 64 K columns: twice, the second time mostly from the caches).  The row's loads go first: what a token's targets need, two accesses one after the other, comes while they are under way.
 // T: the operands' type.  A thread holds VECS vectors of 4 logits; LONG: rows of more than THREADS * VECS * 4, taken in several rounds.
 template <typename T, int THREADS, int VECS, bool LONG, bool GRAD, bool LOST>
-__global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 5) void softmax_rows_kernel(const SoftmaxRows args) {
-  extern __shared__ float targets_lds[];       // u, p (first: the teacher's logit / tau) and id of every target
+__global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 4) void softmax_rows_kernel(const SoftmaxRows args) {
+  extern __shared__ __attribute__((aligned(16))) float targets_lds[];       // u, p (first: the teacher's logit / tau) and id of every target, in fours
   __shared__ float shared[16];
   __shared__ bool any_target;
   const GSPMD_KERNARG SoftmaxRows& a = *first_kernel_argument<SoftmaxRows>();
@@ -118,10 +118,10 @@ __global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 5) void softmax
     return;
   }
   float* const z = a.z + static_cast<int64_t>(blockIdx.x) * a.ldz;
-  const int K = a.targets;
+  const int K = a.targets, K4 = (K + 3) & ~3;
   const float inv_tau = a.inv_tau, c = inv_tau * kLog2e;
-  float *const u_of = targets_lds, *const p_of = targets_lds + K;
-  int32_t* const id_of = reinterpret_cast<int32_t*>(targets_lds + 2 * K);
+  float *const u_of = targets_lds, *const p_of = targets_lds + K4;
+  int32_t* const id_of = reinterpret_cast<int32_t*>(targets_lds + 2 * K4);
   const FastDiv by_cols{a.by_cols.mul, a.by_cols.shift};
   auto column = [&](int id) {
     const int j = id / a.per;
@@ -161,6 +161,7 @@ __global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 5) void softmax
       p_of[k] = id >= 0 ? teachers_logit(s, a.logits_bf16, at) * inv_tau : -INFINITY;
       id_of[k] = id;
     }
+    if (t < K4 - K) id_of[K + t] = -1;
     const TargetSums of = over_targets(K, [&](int k) { return p_of[k]; }, [&](int k) { return u_of[k]; }, [&](int k, float p) { p_of[k] = p; });
     of_targets = of.sum;
     if (t == 0) any_target = of.any;
@@ -257,7 +258,13 @@ __global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 5) void softmax
         const int id = id_of[k];
         if (id < 0) continue;
         float p = 0.f;
-        for (int n = 0; n < K; ++n) p += id_of[n] == id ? p_of[n] : 0.f;
+        for (int n = 0; n < K4; n += 4) {
+          const int4 ids = *reinterpret_cast<const int4*>(id_of + n);
+          if (ids.x == id) p += p_of[n];
+          if (ids.y == id) p += p_of[n + 1];
+          if (ids.z == id) p += p_of[n + 2];
+          if (ids.w == id) p += p_of[n + 3];
+        }
         const float v = scale * (__builtin_amdgcn_exp2f(((u_of[k] - u_most) - log_total) * kLog2e) - p);
         if constexpr (sizeof(T) == 2) {
           const __bf16 r = static_cast<__bf16>(v);
@@ -372,10 +379,10 @@ struct PackRows {
   void* to;                      // first row of the launch
   int64_t ld, ld_from;           // elements
   int32_t rows, chunks;          // of the result; 16-byte chunks of a row
-  int32_t first, tokens, per_row;          // the result's first row is row `first` of all shards; rows that exist, and of a shard
+  int32_t first, total, per_row;           // row shards: the result's first row is row `first` of all, rows that exist in all, rows apart in the result
   int32_t first_shard;           // the table's first
   int32_t by_columns;            // column shards (one row shard) instead
-  int32_t per_cols, per, cols;   // column shards: columns apart in the result and wide, and columns that exist in all; else the row's `cols`
+  int32_t per_cols, per, cols;   // column shards: columns apart in the result; shards of either kind: rows or columns of one; columns that exist in all
   int32_t copies;                // the rows again, `rows` further on
 };
 static_assert(sizeof(PackRows) <= 4096, "kernel arguments");
@@ -399,7 +406,7 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const PackRows args) {
     } else {
       const int g = a.first + row, i = g / a.per_row, at = g - i * a.per_row;
       from = (GSPMD_GLOBAL const T*)a.from[i - a.first_shard] + static_cast<int64_t>(at) * a.ld_from + col;
-      n = g < a.tokens ? a.cols - col : 0;
+      n = at < a.per && i * a.per + at < a.total ? a.cols - col : 0;
     }
     vec v;
     if (n >= V) {
@@ -427,37 +434,49 @@ struct AddUp {
 };
 static_assert(sizeof(AddUp) <= 4096, "kernel arguments");
 
-template <typename T, int V>
+// Four columns a thread: partials' rows are padded to 16 bytes; the result is stored at its elements' alignment (column by column 8 partials of 1999 x 1001 took 26 us).
+template <typename T>
+__device__ __forceinline__ void store_sum(GSPMD_GLOBAL T* to, f32x4 sum, int n) {
+  typedef T out_vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  out_vec o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (sizeof(T) == 2) o[e] = __builtin_bit_cast(bf16_bits, static_cast<__bf16>(sum[e]));
+    else o[e] = sum[e];
+  }
+  if (n >= 4) {
+    *(GSPMD_GLOBAL out_vec*)to = o;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) to[e] = o[e];
+  }
+}
+
+// begin .. end of the partials of four columns, eight on their way at a time (one after the other, 32 of them took 9 us)
+__device__ __forceinline__ f32x4 sum_partials(GSPMD_GLOBAL const float* from, int64_t stride, int begin, int end) {
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f}, next[8];
+  for (int p = begin; p < end; p += 8) {
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+      if (p + n < end) next[n] = *(GSPMD_GLOBAL const f32x4*)(from + static_cast<int64_t>(p + n) * stride);
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+      if (p + n < end) sum = p + n == begin ? next[n] : sum + next[n];
+  }
+  return sum;
+}
+
+template <typename T>
 __global__ __launch_bounds__(256) void add_up_kernel(const AddUp args) {
   const GSPMD_KERNARG AddUp& a = *first_kernel_argument<AddUp>();
-  typedef float in_vec __attribute__((ext_vector_type(V)));
+  const int col = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (col >= a.cols) return;
   for (int row = blockIdx.y; row < a.rows; row += gridDim.y) {
-    const int col = (blockIdx.x * 256 + threadIdx.x) * V;
-    if (col >= a.cols) continue;
     const int g = a.first + row, i = g / a.per_row, at = g - i * a.per_row;
-    in_vec sum{};
-    if (g < a.tokens) {
-      GSPMD_GLOBAL const float* from = (GSPMD_GLOBAL const float*)a.partials + static_cast<int64_t>(row) * a.ld_in + col;
-      // eight on their way at a time: one after the other, 32 of them took 9 us
-      in_vec next[8];
-      for (int p = 0; p < a.count; p += 8) {
-#pragma unroll
-        for (int n = 0; n < 8; ++n)
-          if (p + n < a.count) next[n] = *(GSPMD_GLOBAL const in_vec*)(from + static_cast<int64_t>(p + n) * a.stride);
-#pragma unroll
-        for (int n = 0; n < 8; ++n)
-          if (p + n < a.count) sum = p + n == 0 ? next[n] : sum + next[n];
-      }
-    }
-    GSPMD_GLOBAL T* const to = (GSPMD_GLOBAL T*)a.to[i - a.first_shard] + static_cast<int64_t>(at) * a.ld_out + col;
-    typedef T out_vec __attribute__((ext_vector_type(V)));
-    out_vec o;
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      if constexpr (sizeof(T) == 2) o[e] = __builtin_bit_cast(bf16_bits, static_cast<__bf16>(sum[e]));
-      else o[e] = sum[e];
-    }
-    *(GSPMD_GLOBAL out_vec*)to = o;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (g < a.tokens) sum = sum_partials((GSPMD_GLOBAL const float*)a.partials + static_cast<int64_t>(row) * a.ld_in + col, a.stride, 0, a.count);
+    store_sum<T>((GSPMD_GLOBAL T*)a.to[i - a.first_shard] + static_cast<int64_t>(at) * a.ld_out + col, sum, a.cols - col);
   }
 }
 

@@ -28,6 +28,7 @@ constexpr int64_t kColumnAlign = 64;
 // Up to so many tokens what D's rounding to bfloat16 loses takes part in the products, as rows of its own: these are bound by w and dw then.
 constexpr int64_t kFewTokens = 64;
 constexpr int64_t kFewRows = 256;            // less than a tile
+constexpr int64_t kSmallSum = int64_t(1) << 20;      // elements of a partial of dx that are hardly noticed
 constexpr int64_t kFewWeights = int64_t(32) << 20;
 constexpr int64_t kFewWorkgroups = 3072;     // of the kernels for a handful of tokens
 
@@ -59,7 +60,7 @@ struct Loss {
     if (!dx || rows == 0) return 1;
     const bool few = rows * parts() <= 128, small = dtype == GSPMD_F32 || few;
     const int64_t edge = small ? 64 : 256, tiles = ((rows * parts() + edge - 1) / edge) * ((M + edge - 1) / edge);
-    const int64_t want = dtype == GSPMD_F32 ? 1024 : few ? 512 : 256, least = small ? 512 : 2048;         // workgroups; entries of a range
+    const int64_t want = dtype == GSPMD_F32 ? 1024 : few ? 512 : 256, least = small || rows * M <= kSmallSum ? 512 : 2048;         // workgroups; entries of a range
     return std::max<int64_t>(1, std::min({want / std::max<int64_t>(tiles, 1), V / least, int64_t(16)}));
   }
   int64_t ranges_of_shard(int64_t rows) const { return std::max<int64_t>(1, std::min(ranges(rows), int64_t(32)) / windows()); }
@@ -84,7 +85,7 @@ struct Loss {
   // 63 / 58, 115 / 102; 8 tokens 640 x 10368 43 / 35; losses alone, 1 token 640 x 10368 15 / 16, 3 or more slower; [M, V], 3 tokens 640 x 10368 36 / 35, 2048 x 16000 84 / 59.
   // bfloat16 beyond 32 MB of w: only where its rows are not padded, which the others read slowly (3 tokens, 4279 x 29599 in 4 shards 302).
   bool few() const {
-    const int64_t most = dtype == GSPMD_F32 ? (vocab_dim == 0 ? 8 : 4) : vocab_dim == 0 && (dx || dw) ? 4 : 0;
+    const int64_t most = dtype == GSPMD_F32 ? (vocab_dim == 0 || V * M * 4 <= kFewWeights ? 8 : 4) : vocab_dim == 0 && (dx || dw) ? 4 : 0;
     return T > 0 && T <= most && M > 0 && nb <= kFewWindows && na <= kInlineTokenShards;
   }
   bool few_takes(bool w_padded) const { return few() && (dtype == GSPMD_F32 || !w_padded || V * M * 2 <= kFewWeights); }
@@ -170,12 +171,12 @@ bool padded(const gspmd_shard_buf& b, int64_t ld) { return !(reinterpret_cast<ui
 
 template <typename T, bool GRAD, bool LOST>
 void launch_rows_as(const SoftmaxRows& a, unsigned rows, hipStream_t stream) {
-  const size_t lds = static_cast<size_t>(a.targets) * 12;
+  const size_t lds = static_cast<size_t>((a.targets + 3) & ~3) * 12;
   if (a.cols <= 64 * 4 * 4) hipLaunchKernelGGL((softmax_rows_kernel<T, 64, 4, false, GRAD, LOST>), dim3(rows), dim3(64), lds, stream, a);
   else if (a.cols <= 256 * 4 * 8) hipLaunchKernelGGL((softmax_rows_kernel<T, 256, 8, false, GRAD, LOST>), dim3(rows), dim3(256), lds, stream, a);
   else if (a.cols <= 512 * 4 * 8) hipLaunchKernelGGL((softmax_rows_kernel<T, 512, 8, false, GRAD, LOST>), dim3(rows), dim3(512), lds, stream, a);
   else if (a.cols <= 1024 * 4 * 8) hipLaunchKernelGGL((softmax_rows_kernel<T, 1024, 8, false, GRAD, LOST>), dim3(rows), dim3(1024), lds, stream, a);
-  else if (a.cols <= 1024 * 4 * 12) hipLaunchKernelGGL((softmax_rows_kernel<T, 1024, 12, false, GRAD, LOST>), dim3(rows), dim3(1024), lds, stream, a);
+  else if (a.cols <= 1024 * 4 * 16) hipLaunchKernelGGL((softmax_rows_kernel<T, 1024, 16, false, GRAD, LOST>), dim3(rows), dim3(1024), lds, stream, a);
   else hipLaunchKernelGGL((softmax_rows_kernel<T, 1024, 8, true, GRAD, LOST>), dim3(rows), dim3(1024), lds, stream, a);
 }
 
@@ -246,7 +247,7 @@ int32_t launch_few_logits(const FewTokens& a, const Loss& l, hipStream_t stream)
     const int64_t per_block = 4 * (64 / a.lanes) * kRows;
     b.blocks = static_cast<int32_t>((l.vs + per_block - 1) / per_block);
     hipLaunchKernelGGL((few_logits_kernel<T, NT, kRows>), dim3(static_cast<unsigned>(l.windows() * b.blocks)), dim3(256), 0, stream, b);
-  } else if constexpr (sizeof(T) == 4 && NT <= 4) {
+  } else if constexpr (sizeof(T) == 4) {
     auto go = [&](auto side) {               // narrower where wide ones would leave compute units without one
       constexpr int kSide = decltype(side)::value, kCols = kSide * few_vec<T>(), lds = std::max(512 * NT, (kFewAcross / 64) * NT * kCols) * 4;
       b.blocks = static_cast<int32_t>((l.vs + kCols - 1) / kCols);
@@ -261,7 +262,7 @@ template <typename T, int NT>
 int32_t launch_few_gradients(const FewTokens& a, const Loss& l, int64_t ranges, hipStream_t stream) {
   if (l.vocab_dim == 0)
     hipLaunchKernelGGL((few_gradients_kernel<T, NT>), dim3(static_cast<unsigned>(l.few_across()), static_cast<unsigned>(ranges)), dim3(256), (few_gradients_lds<T, NT>(a.lanes)), stream, a);
-  else if constexpr (sizeof(T) == 4 && NT <= 4)
+  else if constexpr (sizeof(T) == 4)
     hipLaunchKernelGGL((few_gradients_across_kernel<T, NT>), dim3(static_cast<unsigned>(ranges), static_cast<unsigned>((l.M + a.each - 1) / a.each)), dim3(256), 256 * NT * 4, stream, a);
   return launched();
 }
@@ -291,11 +292,7 @@ int32_t run_few(const Loss& l, FewTokens& a, const SoftmaxRows& rows, AddUp& sum
   sums.stride = l.T * l.ld_sum();
   sums.ld_in = l.ld_sum();
   sums.count = static_cast<int32_t>(ranges);
-  bool four = !(l.M & 3) && !(sums.ld_out & 3);
-  for (int64_t i = 0; i < l.na; ++i) four = four && !(reinterpret_cast<uintptr_t>(sums.to[i]) & (4 * sizeof(T) - 1));
-  const dim3 grid(static_cast<unsigned>((l.M + (four ? 63 : 15)) / (four ? 64 : 16)), static_cast<unsigned>(sums.rows));
-  if (four) hipLaunchKernelGGL((add_up_few_kernel<T, 4>), grid, dim3(256), 0, stream, sums);
-  else hipLaunchKernelGGL((add_up_few_kernel<T, 1>), grid, dim3(256), 0, stream, sums);
+  hipLaunchKernelGGL((add_up_few_kernel<T>), dim3(static_cast<unsigned>((l.M + 63) / 64), static_cast<unsigned>(sums.rows)), dim3(256), 0, stream, sums);
   return launched();
 }
 
@@ -488,24 +485,20 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
       a.per_cols = static_cast<int32_t>(per_cols);
       a.per = static_cast<int32_t>(l.vs);
       if (vocab_dim == 0) {                     // a shard's rows are per_cols apart
-        for (int64_t j = 0; j < n; ++j) {
-          a.from[0] = w[static_cast<size_t>(from + j)].first.data;
-          a.to = w_all + (from + j) * per_cols * ld * e;
-          a.rows = static_cast<int32_t>(per_cols);
-          a.chunks = static_cast<int32_t>(chunks);
-          a.tokens = static_cast<int32_t>(l.valid_v(from + j));
-          a.per_row = static_cast<int32_t>(per_cols);
-          a.cols = static_cast<int32_t>(l.M);
-          if ((st = launch_pack(a, l.dtype, stream)) != GSPMD_OK) return st;
-        }
+        a.to = w_all + from * per_cols * ld * e;
+        a.rows = static_cast<int32_t>(n * per_cols);
+        a.chunks = static_cast<int32_t>(chunks);
+        a.total = static_cast<int32_t>(l.V - from * l.vs);
+        a.per_row = static_cast<int32_t>(per_cols);
+        a.cols = static_cast<int32_t>(l.M);
       } else {
         a.to = w_all + from * per_cols * e;
         a.rows = static_cast<int32_t>(l.M);
         a.chunks = static_cast<int32_t>(n * per_cols / vec);
         a.by_columns = 1;
         a.cols = static_cast<int32_t>(l.V - from * l.vs);
-        if ((st = launch_pack(a, l.dtype, stream)) != GSPMD_OK) return st;
       }
+      if ((st = launch_pack(a, l.dtype, stream)) != GSPMD_OK) return st;
     }
     windows.push_back(Window{w_all, ld, 0, l.cols()});
   } else {
@@ -549,8 +542,8 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
         a.rows = static_cast<int32_t>(std::min(count, first + n - at));
         a.chunks = static_cast<int32_t>(l.ldx() / vec);
         a.first = static_cast<int32_t>(at);
-        a.tokens = static_cast<int32_t>(l.T);
-        a.per_row = static_cast<int32_t>(l.ts);
+        a.total = static_cast<int32_t>(l.T);
+        a.per_row = a.per = static_cast<int32_t>(l.ts);
         a.first_shard = static_cast<int32_t>(i0);
         a.cols = static_cast<int32_t>(l.M);
         a.copies = lost ? 2 : 1;
@@ -664,11 +657,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
       st = by_tables([&](int64_t at, int64_t count, int64_t i0, int64_t shards) {
         AddUp a;
         std::memset(&a, 0, sizeof(a));
-        uintptr_t bits = 0;
-        for (int64_t i = 0; i < shards; ++i) {
-          a.to[i] = dx[static_cast<size_t>(i0 + i)].first.data;
-          bits |= reinterpret_cast<uintptr_t>(a.to[i]);
-        }
+        for (int64_t i = 0; i < shards; ++i) a.to[i] = dx[static_cast<size_t>(i0 + i)].first.data;
         a.partials = sums + (at - first) * l.ld_sum();
         a.stride = n * l.ld_sum();
         a.ld_in = l.ld_sum();
@@ -680,15 +669,9 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
         a.tokens = static_cast<int32_t>(l.T);
         a.per_row = static_cast<int32_t>(l.ts);
         a.first_shard = static_cast<int32_t>(i0);
-        const bool four = !(l.M & 3) && !(a.ld_out & 3) && !(bits & static_cast<uintptr_t>(4 * e - 1));
-        const dim3 grid = rows_grid(four ? l.M / 4 : l.M, count);
-        if (l.dtype == GSPMD_BF16) {
-          if (four) hipLaunchKernelGGL((add_up_kernel<bf16_bits, 4>), grid, dim3(256), 0, stream, a);
-          else hipLaunchKernelGGL((add_up_kernel<bf16_bits, 1>), grid, dim3(256), 0, stream, a);
-        } else {
-          if (four) hipLaunchKernelGGL((add_up_kernel<float, 4>), grid, dim3(256), 0, stream, a);
-          else hipLaunchKernelGGL((add_up_kernel<float, 1>), grid, dim3(256), 0, stream, a);
-        }
+        const dim3 grid = rows_grid((l.M + 3) / 4, count);
+        if (l.dtype == GSPMD_BF16) hipLaunchKernelGGL((add_up_kernel<bf16_bits>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((add_up_kernel<float>), grid, dim3(256), 0, stream, a);
         return launched();
       });
       if (st != GSPMD_OK) return st;
