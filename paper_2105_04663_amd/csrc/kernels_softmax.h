@@ -39,6 +39,10 @@ struct SoftmaxRows {
   FastDiv by_cols;               // by per_cols
   float inv_tau;
   int32_t logits_bf16;
+  const bf16_bits* x;            // with D in two parts: the tokens' activations (of one shard), put together beside them, or null
+  bf16_bits* x_copies;           // two of them, `lost` rows apart
+  int64_t ldx, ld_copy;
+  int32_t x_cols;
 };
 static_assert(sizeof(SoftmaxRows) <= 4096, "kernel arguments");
 
@@ -148,6 +152,14 @@ __global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 4) void softmax
     }
   };
   load_round(0);
+  if constexpr (LOST)
+    if (a.x)
+      for (int m = t; m < a.x_cols; m += THREADS) {
+        const bf16_bits v = a.x[static_cast<int64_t>(token) * a.ldx + m];
+        bf16_bits* const to = a.x_copies + static_cast<int64_t>(blockIdx.x) * a.ld_copy + m;
+        to[0] = v;
+        to[a.lost * a.ld_copy] = v;
+      }
   auto plus = [](float x, float y) { return x + y; };
 
   // ---- the targets, by the first wave: their logits (before D takes the logits' place), shares, and what the loss takes from them
@@ -280,9 +292,10 @@ __global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 4) void softmax
 // ---- logits that are not kept (kernels_stats.h): the targets' columns before the products, and what their tiles leave put together after them.
 struct SoftmaxMerge {
   SoftmaxRows rows;              // z: the table of pairs [group][ldz rows], `cols` its groups
-  int32_t* columns;              // [rows][targets]
+  int32_t* columns;              // [rows][targets]; of one shard of tokens and one of the vocabulary the targets' own ids
   float* logits;                 // [rows][targets]
   int32_t count;                 // rows of the launch (for the columns: tokens)
+  int32_t end;                   // columns of a row of logits: others are none
 };
 static_assert(sizeof(SoftmaxMerge) <= 4096, "kernel arguments");
 
@@ -331,7 +344,8 @@ __global__ __launch_bounds__(kMergeThreads) void softmax_merge_kernel(const Soft
     const int k = n * 64 + lane;
     q[n] = -INFINITY;
     u[n] = 0.f;
-    if (has_token && k < K && ((GSPMD_GLOBAL const int32_t*)first_kernel_argument<SoftmaxMerge>()->columns)[at + k] >= 0) {
+    const int column = has_token && k < K ? ((GSPMD_GLOBAL const int32_t*)first_kernel_argument<SoftmaxMerge>()->columns)[at + k] : -1;
+    if (column >= 0 && column < first_kernel_argument<SoftmaxMerge>()->end) {
       q[n] = teachers_logit(s, a.logits_bf16, static_cast<int64_t>(token) * K + k) * inv_tau;
       u[n] = ((GSPMD_GLOBAL const float*)first_kernel_argument<SoftmaxMerge>()->logits)[at + k] * inv_tau;
     }
@@ -453,17 +467,16 @@ __device__ __forceinline__ void store_sum(GSPMD_GLOBAL T* to, f32x4 sum, int n) 
   }
 }
 
-// begin .. end of the partials of four columns, eight on their way at a time (one after the other, 32 of them took 9 us)
+// begin .. end of the partials of four columns, four on their way at a time (one after the other, 32 of them took 9 us)
 __device__ __forceinline__ f32x4 sum_partials(GSPMD_GLOBAL const float* from, int64_t stride, int begin, int end) {
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f}, next[8];
-  for (int p = begin; p < end; p += 8) {
-#pragma unroll
-    for (int n = 0; n < 8; ++n)
-      if (p + n < end) next[n] = *(GSPMD_GLOBAL const f32x4*)(from + static_cast<int64_t>(p + n) * stride);
-#pragma unroll
-    for (int n = 0; n < 8; ++n)
-      if (p + n < end) sum = p + n == begin ? next[n] : sum + next[n];
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  int p = begin;
+  auto at = [&](int n) { return *(GSPMD_GLOBAL const f32x4*)(from + static_cast<int64_t>(n) * stride); };
+  for (; p + 4 <= end; p += 4) {
+    const f32x4 a = at(p), b = at(p + 1), c = at(p + 2), d = at(p + 3);
+    sum = (((sum + a) + b) + c) + d;
   }
+  for (; p < end; ++p) sum += at(p);
   return sum;
 }
 

@@ -14,7 +14,7 @@ namespace gspmd {
 // What the launch's problems stand for: join_first is the problem's first row among the piece's, join_slot the column of a row of logits where its columns start (a multiple of
 // 64); C the table of pairs [column / 64][row], ldc its rows.
 struct SoftmaxFinish {
-  const int32_t* columns;        // [rows][targets]: the target's column in a row of logits, or -1
+  const int32_t* columns;        // [rows][targets]: the target's column in a row of logits; what is none is no target
   float* logits;                 // [rows][targets], out
   int32_t targets;
   float c;                       // log2(e) / tau

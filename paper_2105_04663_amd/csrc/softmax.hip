@@ -26,7 +26,7 @@ namespace {
 constexpr int64_t kPieceBytes = int64_t(1) << 31;
 constexpr int64_t kColumnAlign = 64;
 // Up to so many tokens what D's rounding to bfloat16 loses takes part in the products, as rows of its own: these are bound by w and dw then.
-constexpr int64_t kFewTokens = 64;
+constexpr int64_t kFewTokens = 128;
 constexpr int64_t kFewRows = 256;            // less than a tile
 constexpr int64_t kSmallSum = int64_t(1) << 20;      // elements of a partial of dx that are hardly noticed
 constexpr int64_t kFewWeights = int64_t(32) << 20;
@@ -507,7 +507,8 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   auto w_from = [&](const Window& v, int64_t entry) { return v.data + (vocab_dim == 0 ? entry * v.ld : entry) * e; };
   // x put together: where dw sums over tokens of several shards, or over both parts of D, where shards have so few tokens that each would read the vocabulary matrix for
   // itself (15 tokens in two shards, 8099 x 124058: 690 us so), and where rows are not padded
-  const bool pack_x = l.M > 0 && ((l.dw && (l.na > 1 || lost)) || (l.na > 1 && l.ts < kFewRows) || (!x_padded && l.packing_pays()));
+  const bool copied_x = lost && l.dw && l.na == 1;           // by the row kernel, beside D: only dw needs it
+  const bool pack_x = l.M > 0 && !copied_x && ((l.dw && l.na > 1) || (l.na > 1 && l.ts < kFewRows) || (!x_padded && l.packing_pays()));
 
   for (int64_t piece = 0; piece < pieces; ++piece) {
     const int64_t first = piece * rows, n = std::min(rows, l.T - first);       // tokens
@@ -546,7 +547,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
         a.per_row = a.per = static_cast<int32_t>(l.ts);
         a.first_shard = static_cast<int32_t>(i0);
         a.cols = static_cast<int32_t>(l.M);
-        a.copies = lost ? 2 : 1;
+        a.copies = lost && l.dw ? 2 : 1;
         return a.rows > 0 ? launch_pack(a, l.dtype, stream) : static_cast<int32_t>(GSPMD_OK);
       });
     if (st != GSPMD_OK) return st;
@@ -582,7 +583,8 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
     }
     if (stats) {
       char* const base = reinterpret_cast<char*>(z);
-      int32_t* const columns = reinterpret_cast<int32_t*>(base + pair_bytes);
+      const bool own_ids = l.na == 1 && nw == 1;             // they are the columns
+      int32_t* const columns = own_ids ? const_cast<int32_t*>(token[0][0].ids) + first * targets : reinterpret_cast<int32_t*>(base + pair_bytes);
       float* const of_targets = reinterpret_cast<float*>(base + pair_bytes + target_bytes);
       for (Problem& p : ps) {
         const int64_t at = static_cast<float*>(p.C) - z;
@@ -596,9 +598,10 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
         m->rows.ldz = n;
         m->rows.cols = static_cast<int32_t>(groups);
         m->columns = columns + (at - first) * targets;
+        m->end = static_cast<int32_t>(l.cols());
         m->logits = of_targets + (at - first) * targets;
       };
-      st = by_tables([&](int64_t at, int64_t count, int64_t i0, int64_t shards) -> int32_t {
+      if (!own_ids) st = by_tables([&](int64_t at, int64_t count, int64_t i0, int64_t shards) -> int32_t {
         SoftmaxMerge m;
         merge_args(&m, at, i0, shards);
         m.count = static_cast<int32_t>(std::max<int64_t>(0, std::min(count, first + n - at)));
@@ -627,6 +630,13 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
       SoftmaxRows a;
       rows_args(&a, z + (at - first) * ldz, at, i0, shards);
       a.lost = n;
+      if (copied_x) {
+        a.x = static_cast<const bf16_bits*>(x[0].first.data);
+        a.x_copies = reinterpret_cast<bf16_bits*>(x_all);
+        a.ldx = ldx_in;
+        a.ld_copy = l.ldx();
+        a.x_cols = static_cast<int32_t>(l.M);
+      }
       return launch_rows(a, l, count, stream);
     });
     if (st != GSPMD_OK) return st;
@@ -678,8 +688,8 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
     }
     // ---- dw: straight into its shards, or over several pieces in float32
     if (l.dw) {
-      const char* const from = pack_x ? x_all : static_cast<const char*>(x[0].first.data) + first * ldx_in * e;
-      const int64_t ldx = pack_x ? l.ldx() : ldx_in, k = n * l.parts(), ld_part = round_up(w_cols, 4);
+      const char* const from = pack_x || copied_x ? x_all : static_cast<const char*>(x[0].first.data) + first * ldx_in * e;
+      const int64_t ldx = pack_x || copied_x ? l.ldx() : ldx_in, k = n * l.parts(), ld_part = round_up(w_cols, 4);
       ps.clear();
       for (int64_t j = 0; j < l.nb; ++j) {
         const gspmd_shard_buf& o = dw[static_cast<size_t>(j)].first;
