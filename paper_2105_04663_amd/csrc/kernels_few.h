@@ -214,13 +214,13 @@ __global__ __launch_bounds__(256) void few_gradients_kernel(const FewTokens args
   };
   for (int chunk = begin; chunk < end; chunk += kChunk) {
     __syncthreads();
-    for (int i = t0; i < kChunk * NT; i += 256) {
-      const int t = i / kChunk, v = chunk + i % kChunk;
-      lds[(i % kChunk) * NT + t] = t < a.tokens && v < valid && v < end ? a.z[t * a.ldz + j * a.per_cols + v] : 0.f;
+    const int stop = min(chunk + kChunk, end), full = min(stop, valid) - chunk;
+    for (int i = t0; i < (stop - chunk) * NT; i += 256) {
+      const int t = i % NT, v = chunk + i / NT;
+      lds[i] = t < a.tokens && v < valid ? a.z[t * a.ldz + j * a.per_cols + v] : 0.f;
     }
     __syncthreads();
     if (room <= 0) continue;
-    const int stop = min(chunk + kChunk, end), full = min(stop, valid) - chunk;
     int r0 = side;
     if (whole)
       for (; r0 + (kAhead - 1) * sides < full; r0 += sides * kAhead) take(std::true_type{}, std::true_type{}, chunk, stop, r0);
@@ -295,13 +295,10 @@ __global__ __launch_bounds__(kFewAcross) void few_logits_across_kernel(const Few
   };
   for (int chunk = 0; chunk < a.M; chunk += kChunk) {
     __syncthreads();
-    for (int i = t0; i < kChunk * NT; i += THREADS) {
-      const int t = i / kChunk, m = chunk + i % kChunk;
-      lds[(i % kChunk) * NT + t] = t < a.tokens && m < a.M ? load_as_float(static_cast<const T*>(a.x[t]) + m) : 0.f;
-    }
+    const int rows = min(kChunk, a.M - chunk);
+    for (int i = t0; i < rows * NT; i += THREADS) lds[i] = load_as_float(static_cast<const T*>(a.x[i % NT]) + chunk + i / NT);
     __syncthreads();
     if (room <= 0) continue;
-    const int rows = min(kChunk, a.M - chunk);
     int r0 = side;
     if (whole)
       for (; r0 + (kAhead - 1) * kRows < rows; r0 += kRows * kAhead) take(std::true_type{}, std::true_type{}, chunk, r0, rows);
@@ -347,10 +344,20 @@ __global__ __launch_bounds__(256) void few_gradients_across_kernel(const FewToke
   for (int t = 0; t < NT; ++t) {
 #pragma unroll
     for (int e = 0; e < V; ++e) d[t][e] = 0.f;
-    if (t < a.tokens)
+    if (t >= a.tokens) continue;
+    GSPMD_GLOBAL const float* const from_d = (GSPMD_GLOBAL const float*)a.z + t * a.ldz + j * a.per_cols + at;
+    if (whole) {
+#pragma unroll
+      for (int e = 0; e < V; e += 4) {
+        const float4_t four = *(GSPMD_GLOBAL const float4_t*)(from_d + e);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) d[t][e + n] = four[n];
+      }
+    } else {
 #pragma unroll
       for (int e = 0; e < V; ++e)
-        if (e < room) d[t][e] = a.z[t * a.ldz + j * a.per_cols + at + e];
+        if (e < room) d[t][e] = from_d[e];
+    }
   }
   GSPMD_GLOBAL const T* const w = (GSPMD_GLOBAL const T*)a.w[j] + at;
   GSPMD_GLOBAL T* const dw = (GSPMD_GLOBAL T*)a.dw[j] + at;
@@ -394,12 +401,9 @@ __global__ __launch_bounds__(256) void few_gradients_across_kernel(const FewToke
   };
   for (int chunk = begin; chunk < end; chunk += kChunk) {
     __syncthreads();
-    for (int i = t0; i < kChunk * NT; i += 256) {
-      const int t = i / kChunk, m = chunk + i % kChunk;
-      lds[(i % kChunk) * NT + t] = t < a.tokens && m < end ? load_as_float(static_cast<const T*>(a.x[t]) + m) : 0.f;
-    }
-    __syncthreads();
     const int rows = min(kChunk, end - chunk);
+    for (int i = t0; i < rows * NT; i += 256) lds[i] = load_as_float(static_cast<const T*>(a.x[i % NT]) + chunk + i / NT);
+    __syncthreads();
     int r0 = wave * ROWS;
     if (whole && r0 + ROWS <= rows) {             // the next rows are on their way while these are taken
       const std::true_type yes{};
