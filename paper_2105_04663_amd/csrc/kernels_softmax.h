@@ -204,6 +204,7 @@ __global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 4) void softmax
   }
   const float own = m;
   m = over_block<THREADS>(m, shared, [](float p, float q) { return fmaxf(p, q); });
+  const float finite_m = m == -INFINITY ? 0.f : m;               // a row of -infinity: total 0, lse -infinity
   if constexpr (LONG) {
     total = own == -INFINITY ? total : total * __builtin_amdgcn_exp2f((own - m) * c);
   } else {
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 4) void softmax
     for (int n = 0; n < VECS; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        x[n][e] = __builtin_amdgcn_exp2f((x[n][e] - m) * c);
+        x[n][e] = __builtin_amdgcn_exp2f((x[n][e] - finite_m) * c);
         total += x[n][e];
       }
   }
@@ -254,7 +255,7 @@ __global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 4) void softmax
         for (int n = 0; n < VECS; ++n) {
           cut(first + (n * THREADS + t) * 4, x[n]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[n][e] = __builtin_amdgcn_exp2f((x[n][e] - m) * c);
+          for (int e = 0; e < 4; ++e) x[n][e] = __builtin_amdgcn_exp2f((x[n][e] - finite_m) * c);
         }
       }
       __syncthreads();

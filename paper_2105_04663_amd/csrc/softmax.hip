@@ -30,7 +30,7 @@ constexpr int64_t kFewTokens = 128;
 constexpr int64_t kFewRows = 256;            // less than a tile
 constexpr int64_t kSmallSum = int64_t(1) << 20;      // elements of a partial of dx that are hardly noticed
 constexpr int64_t kFewWeights = int64_t(32) << 20;
-constexpr int64_t kFewWorkgroups = 3072;     // of the kernels for a handful of tokens
+constexpr int64_t kFewWorkgroups = 12 * 256;     // of the kernels for a handful of tokens
 
 struct Loss {
   const gspmd_mesh* mesh = nullptr;

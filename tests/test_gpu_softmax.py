@@ -263,3 +263,19 @@ def test_random_problems():
                     mesh=(int(rng.integers(1, 5)), int(rng.integers(1, 7))), pad=bool(rng.integers(0, 2)), share=bool(rng.integers(0, 2)), weights=bool(rng.integers(0, 2)))
         print(n, T, M, V, p.dtype, K, p.mesh.shape, p.vocab_dim, p.pad, flush=True)
         p.stage().call().check()
+
+
+@pytest.mark.parametrize("T,V,dtype,grad,K", [(2, 300, "f32", True, None), (9, 300, "bf16", True, None), (200, 300, "bf16", False, 3), (9, 70000, "bf16", True, None), (3, 3000, "bf16", False, None)])
+def test_logits_of_minus_infinity_throughout(T, V, dtype, grad, K):
+    """A token without any probability: lse is -infinity, its loss and gradient NaN, by every path; other tokens are as ever."""
+    p = Problem(T, 16, V, dtype, K=K, missing=0.0)
+    p.xt[:, 0] = 0.0
+    ref = p.stage((grad, False)).call().results()
+    p.xt[1, 0] = 3e38
+    p.wt[:, 0] = -100.0
+    got = p.stage((grad, False)).call().results()
+    assert got["lse"][1] == -np.inf and np.isnan(got["loss"][1])
+    if grad:
+        assert np.isnan(got["dx"][1]).all()
+    others = np.arange(T) != 1
+    assert np.array_equal(got["lse"][others], ref["lse"][others]) and np.array_equal(got["loss"][others], ref["loss"][others])
