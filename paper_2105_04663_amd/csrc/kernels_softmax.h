@@ -438,14 +438,17 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const PackRows args) {
   }
 }
 
-// Token shards of dx = the sum of `count` partials (fp32, one after the other) in ascending order; a launch's rows are tokens first .. of all shards, padding is written as zeros.
+// Shards = the sum of `count` partials (fp32, one after the other) in ascending order; a launch's rows are rows first .. of all shards (dx: tokens; dw: entries), padding is written as zeros.
+// Or the shards are beside each other, `apart` columns each, in every row.
 struct AddUp {
   void* to[kInlineTokenShards];
   const float* partials;         // [count][rows][cols]
   int64_t stride;                // elements from one partial to the next
   int64_t ld_in, ld_out;
   int32_t count, rows, cols;
-  int32_t first, tokens, per_row, first_shard;
+  int32_t first, tokens, per_row, first_shard;     // tokens: rows (columns) that exist in all; per_row: of a shard
+  int32_t apart;                 // rows (columns) from one shard to the next in the partials
+  int32_t by_columns;
 };
 static_assert(sizeof(AddUp) <= 4096, "kernel arguments");
 
@@ -487,9 +490,20 @@ __global__ __launch_bounds__(256) void add_up_kernel(const AddUp args) {
   const int col = (blockIdx.x * 256 + threadIdx.x) * 4;
   if (col >= a.cols) return;
   for (int row = blockIdx.y; row < a.rows; row += gridDim.y) {
-    const int g = a.first + row, i = g / a.per_row, at = g - i * a.per_row;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    if (g < a.tokens) sum = sum_partials((GSPMD_GLOBAL const float*)a.partials + static_cast<int64_t>(row) * a.ld_in + col, a.stride, 0, a.count);
+    if (a.by_columns) {
+      const int i = col / a.apart, at = col - i * a.apart, g = a.first + i * a.per_row + at;      // (beyond what exists: zeros, as D's columns are; of a shard without entries there are none)
+      if (at >= a.per_row) continue;
+      if (g < a.tokens) sum = sum_partials((GSPMD_GLOBAL const float*)a.partials + static_cast<int64_t>(row) * a.ld_in + col, a.stride, 0, a.count);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (g + e >= a.tokens) sum[e] = 0.f;
+      store_sum<T>((GSPMD_GLOBAL T*)a.to[i] + static_cast<int64_t>(row) * a.ld_out + at, sum, a.per_row - at);
+      continue;
+    }
+    const int g = a.first + row, i = g / a.per_row, at = g - i * a.per_row;
+    const int64_t from = row + static_cast<int64_t>(i - a.first_shard) * (a.apart - a.per_row);
+    if (g < a.tokens) sum = sum_partials((GSPMD_GLOBAL const float*)a.partials + from * a.ld_in + col, a.stride, 0, a.count);
     store_sum<T>((GSPMD_GLOBAL T*)a.to[i - a.first_shard] + static_cast<int64_t>(at) * a.ld_out + col, sum, a.cols - col);
   }
 }

@@ -29,6 +29,8 @@ constexpr int64_t kColumnAlign = 64;
 constexpr int64_t kFewTokens = 128;
 constexpr int64_t kFewRows = 256;            // less than a tile
 constexpr int64_t kSmallSum = int64_t(1) << 20;      // elements of a partial of dx that are hardly noticed
+constexpr int64_t kNarrow = 128;
+constexpr double kNarrowWork = 2e9;
 constexpr int64_t kFewWeights = int64_t(32) << 20;
 constexpr int64_t kFewWorkgroups = 12 * 256;     // of the kernels for a handful of tokens
 
@@ -45,9 +47,10 @@ struct Loss {
   int64_t valid_v(int64_t j) const { return std::max<int64_t>(0, std::min(vs, V - j * vs)); }
   // a row of logits: the vocabulary shards that hold any entry, one after the other
   int64_t windows() const { return (V + vs - 1) / vs; }
-  int64_t per_cols() const { return round_up(vs, kColumnAlign); }
+  // Shards start on whole lines, unless that would make rows much longer (16000 x 110 logits in 8 shards, 8000 wide: 3147 us float32), and on 64 columns where their products may end in statistics.
+  int64_t per_cols() const { return round_up(vs, windows() == 1 || vs >= 1024 || (vs >= kNarrow && !dx && !dw && dtype == GSPMD_BF16) ? kColumnAlign : 8); }
   int64_t cols() const { return (windows() - 1) * per_cols() + valid_v(windows() - 1); }
-  int64_t ldz() const { return windows() * per_cols(); }
+  int64_t ldz() const { return round_up(windows() * per_cols(), kColumnAlign); }
   int64_t w_rows() const { return vocab_dim == 0 ? vs : M; }
   int64_t w_cols() const { return vocab_dim == 0 ? M : vs; }
   // both parts of D
@@ -66,11 +69,23 @@ struct Loss {
   int64_t ranges_of_shard(int64_t rows) const { return std::max<int64_t>(1, std::min(ranges(rows), int64_t(32)) / windows()); }
   int64_t most_ranges(int64_t rows) const { return std::max(ranges(rows), windows() * ranges_of_shard(rows)); }
   bool adds_up(int64_t rows) const { return dx && (most_ranges(rows) > 1 || with_lost()); }
+  // Ranges of the tokens whose products make dw together, in one matrix of all shards ..
+  int64_t dw_ranges() const {
+    if (!dw || T == 0) return 1;
+    const int64_t edge = dtype == GSPMD_F32 ? 64 : 256, tiles = ((cols() + edge - 1) / edge) * ((M + edge - 1) / edge);
+    const int64_t want = dtype == GSPMD_F32 ? 1024 : 256, least = dtype == GSPMD_F32 ? 512 : 1024;
+    return std::max<int64_t>(1, std::min({want / std::max<int64_t>(tiles, 1), T / least, int64_t(16)}));
+  }
+  bool narrow() const { return nb > 1 && vs < kNarrow && static_cast<double>(T) * static_cast<double>(M) * static_cast<double>(V) >= kNarrowWork; }         // shards of less than a tile, in products that are worth another launch
+  bool joins_dw() const { return dw && M > 0 && (dw_ranges() > 1 || narrow()); }
+  int64_t ld_dw() const { return vocab_dim == 0 ? ld_sum() : ldz(); }
+  int64_t dw_part() const { return (vocab_dim == 0 ? ldz() : M) * ld_dw(); }
+  int64_t joined_dw_bytes() const { return joins_dw() ? round_up(dw_ranges() * dw_part() * 4, kWsAlign) : 0; }
   int64_t most_rows() const { return std::min(T, std::max<int64_t>(1, kPieceBytes / (ldz() * 4))); }
   // A padded copy of operands whose rows are not padded to 16 bytes, which the products read several times slower than they are copied once: from this many rows of products on ..
   bool packing_pays() const { return dtype == GSPMD_BF16 && T * (dx || dw ? 3 : 1) >= 1024; }
   // .. and of a vocabulary in many shards, where dx's partials, one for each, would be more than that copy (4085 tokens, 2834 x 2393 on 3 x 8: 439 us without).
-  bool joining_pays() const { return dx && windows() > 1 && 2 * T * windows() >= V; }
+  bool joining_pays() const { return windows() > 1 && ((dx && 2 * T * windows() >= V) || narrow()); }
   int64_t packed_w_bytes() const { return round_up((vocab_dim == 0 ? ldz() * ldx() : std::max<int64_t>(M, 1) * ldz()) * esize(), kWsAlign); }
   // ---- the workspace, for pieces of `rows` tokens
   int64_t table_bytes() const { return round_up((na * nb + 32 + nb) * kTableBytesPerProblem, kWsAlign); }
@@ -200,6 +215,13 @@ int32_t launch_pack(const PackRows& a, int32_t dtype, hipStream_t stream) {
   const dim3 grid = rows_grid(a.chunks, a.rows);
   if (dtype == GSPMD_BF16) hipLaunchKernelGGL((pack_rows_kernel<uint16_t>), grid, dim3(256), 0, stream, a);
   else hipLaunchKernelGGL((pack_rows_kernel<uint32_t>), grid, dim3(256), 0, stream, a);
+  return launched();
+}
+
+int32_t launch_add_up(const AddUp& a, int32_t dtype, hipStream_t stream) {
+  const dim3 grid = rows_grid((a.cols + 3) / 4, a.rows);
+  if (dtype == GSPMD_BF16) hipLaunchKernelGGL((add_up_kernel<bf16_bits>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((add_up_kernel<float>), grid, dim3(256), 0, stream, a);
   return launched();
 }
 
@@ -462,8 +484,11 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   float* const z = reinterpret_cast<float*>(take(l.z_bytes(rows)));
   float* const sums = reinterpret_cast<float*>(take(l.sum_bytes(rows)));
   float* const dw_sums = reinterpret_cast<float*>(take(l.dw_bytes(rows)));
+  int64_t room = workspace_bytes - (ws - static_cast<char*>(workspace));
+  const bool join_dw = pieces == 1 && l.joins_dw() && room >= l.joined_dw_bytes();
+  float* const dw_parts = reinterpret_cast<float*>(take(join_dw ? l.joined_dw_bytes() : 0));
+  room -= join_dw ? l.joined_dw_bytes() : 0;
   char* const w_all = ws;
-  const int64_t room_w = workspace_bytes - (ws - static_cast<char*>(workspace));
   const int64_t e = l.esize(), ldz = l.ldz(), ldd = ldz * 4 / e, per_cols = l.per_cols(), nw = l.windows(), vec = 16 / e;
   const bool lost = l.with_lost();
 
@@ -472,7 +497,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   std::vector<Window> windows;
   bool x_padded = true;
   for (int64_t i = 0; i < l.na; ++i) x_padded = x_padded && padded(x[static_cast<size_t>(i)].first, ldx_in);
-  if (((!w_padded && l.packing_pays()) || l.joining_pays()) && room_w >= l.packed_w_bytes() && l.M > 0) {
+  if (((!w_padded && l.packing_pays()) || l.joining_pays()) && room >= l.packed_w_bytes() && l.M > 0) {
     const int64_t ld = vocab_dim == 0 ? l.ldx() : ldz, chunks = ld / vec;
     for (int64_t from = 0; from < nw && !dry; from += kInlineTokenShards) {
       const int64_t n = std::min<int64_t>(kInlineTokenShards, nw - from);
@@ -553,7 +578,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
     if (st != GSPMD_OK) return st;
     // ---- logits.  Where they need not be kept (without gradients) their tiles end in what the losses need of them.
     const int64_t groups = (l.cols() + 63) / 64, pair_bytes = round_up(groups * n * 8, kWsAlign), target_bytes = round_up(n * targets * 4, kWsAlign);
-    bool stats = !l.dx && !l.dw && l.dtype == GSPMD_BF16 && l.M > 0 && n > 0 && targets <= kStatsTargets && pair_bytes + 2 * target_bytes <= l.z_bytes(rows);
+    bool stats = !l.dx && !l.dw && l.dtype == GSPMD_BF16 && l.M > 0 && n > 0 && per_cols % 64 == 0 && targets <= kStatsTargets && pair_bytes + 2 * target_bytes <= l.z_bytes(rows);
     const int32_t logits_layout = vocab_dim == 0 ? GSPMD_LAYOUT_RHS_K_CONTIGUOUS : 0;
     std::vector<Problem> ps;
     auto logits = [&](const char* from, int64_t ld, int64_t row, int64_t count) {
@@ -677,17 +702,46 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
         a.cols = static_cast<int32_t>(l.M);
         a.first = static_cast<int32_t>(at);
         a.tokens = static_cast<int32_t>(l.T);
-        a.per_row = static_cast<int32_t>(l.ts);
+        a.per_row = a.apart = static_cast<int32_t>(l.ts);
         a.first_shard = static_cast<int32_t>(i0);
-        const dim3 grid = rows_grid((l.M + 3) / 4, count);
-        if (l.dtype == GSPMD_BF16) hipLaunchKernelGGL((add_up_kernel<bf16_bits>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((add_up_kernel<float>), grid, dim3(256), 0, stream, a);
-        return launched();
+        return launch_add_up(a, l.dtype, stream);
       });
       if (st != GSPMD_OK) return st;
     }
-    // ---- dw: straight into its shards, or over several pieces in float32
-    if (l.dw) {
+    // ---- dw: straight into its shards, over several pieces in float32, or over ranges of the tokens in float32 for all shards together
+    if (join_dw) {
+      const char* const from = pack_x || copied_x ? x_all : static_cast<const char*>(x[0].first.data);
+      const int64_t ldx = pack_x || copied_x ? l.ldx() : ldx_in, k = n * l.parts(), parts = l.dw_ranges(), each = round_up((k + parts - 1) / parts, 64), entries = l.cols();
+      ps.clear();
+      for (int64_t at = 0; at < k; at += each) {
+        const int64_t here = std::min(each, k - at);
+        const char *const dr = d + at * ldd * e, *const xr = from + at * ldx * e;
+        float* const c = dw_parts + static_cast<int64_t>(ps.size()) * l.dw_part();
+        ps.push_back(vocab_dim == 0 ? product(dr, ldd, xr, ldx, c, l.ld_dw(), entries, l.M, here, entries, l.M) : product(xr, ldx, dr, ldd, c, l.ld_dw(), l.M, entries, here, l.M, entries));
+      }
+      const int32_t count_all = static_cast<int32_t>(ps.size());
+      if ((st = run_dots(ps, GSPMD_LAYOUT_LHS_K_MAJOR, l.dtype, GSPMD_F32, tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
+      for (int64_t from_shard = 0; from_shard < l.nb && !dry; from_shard += kInlineTokenShards) {
+        const int64_t shards = std::min<int64_t>(kInlineTokenShards, l.nb - from_shard), before = from_shard * per_cols;
+        AddUp a;
+        std::memset(&a, 0, sizeof(a));
+        for (int64_t j = 0; j < shards; ++j) a.to[j] = dw[static_cast<size_t>(from_shard + j)].first.data;
+        a.partials = dw_parts + (vocab_dim == 0 ? before * l.ld_dw() : before);
+        a.stride = l.dw_part();
+        a.ld_in = l.ld_dw();
+        a.ld_out = lddw;
+        a.count = count_all;
+        a.apart = static_cast<int32_t>(per_cols);
+        a.per_row = static_cast<int32_t>(l.vs);
+        a.first = static_cast<int32_t>(from_shard * l.vs);
+        a.first_shard = static_cast<int32_t>(from_shard);
+        a.tokens = static_cast<int32_t>(l.V);
+        a.by_columns = vocab_dim;
+        a.rows = static_cast<int32_t>(vocab_dim == 0 ? shards * l.vs : l.M);
+        a.cols = static_cast<int32_t>(vocab_dim == 0 ? l.M : shards * per_cols);
+        if ((st = launch_add_up(a, l.dtype, stream)) != GSPMD_OK) return st;
+      }
+    } else if (l.dw) {
       const char* const from = pack_x || copied_x ? x_all : static_cast<const char*>(x[0].first.data) + first * ldx_in * e;
       const int64_t ldx = pack_x || copied_x ? l.ldx() : ldx_in, k = n * l.parts(), ld_part = round_up(w_cols, 4);
       ps.clear();
@@ -727,7 +781,7 @@ int32_t gspmd_softmax_workspace_bytes(const gspmd_mesh* mesh, const gspmd_shardi
   l.dtype = dtype;
   l.dx = l.dw = gradients != 0;
   const int64_t rows = l.most_rows();
-  *bytes = l.bytes(rows) + (l.packing_pays() || l.joining_pays() ? l.packed_w_bytes() : 0);
+  *bytes = l.bytes(rows) + (l.packing_pays() || l.joining_pays() ? l.packed_w_bytes() : 0) + (rows == l.T ? l.joined_dw_bytes() : 0);
   if (l.few()) *bytes = std::max(*bytes, l.few_bytes());
   if (least) *least = std::min(*bytes, l.bytes(std::min<int64_t>(l.T, 1)));
   return GSPMD_OK;

@@ -279,3 +279,20 @@ def test_logits_of_minus_infinity_throughout(T, V, dtype, grad, K):
         assert np.isnan(got["dx"][1]).all()
     others = np.arange(T) != 1
     assert np.array_equal(got["lse"][others], ref["lse"][others]) and np.array_equal(got["loss"][others], ref["loss"][others])
+
+
+@pytest.mark.parametrize("T,M,V,dtype,mesh", [(1100, 40, 300, "f32", (1, 1)), (1301, 33, 301, "f32", (2, 3)), (1100, 17, 9, "f32", (1, 8)), (2100, 40, 300, "bf16", (3, 1)), (4133, 77, 1003, "bf16", (2, 2)),
+                                              (2600, 8200, 101, "bf16", (2, 8)), (2600, 8200, 101, "f32", (1, 8))])
+@pytest.mark.parametrize("vocab_dim", [0, 1])
+@pytest.mark.parametrize("pad", [True, False])
+def test_dw_over_ranges_of_the_tokens(T, M, V, dtype, mesh, vocab_dim, pad):
+    """Long sums into few outputs, and narrow shards of the vocabulary: dw made for all shards together; with less workspace as everywhere else."""
+    p = Problem(T, M, V, dtype, mesh=mesh, vocab_dim=vocab_dim, pad=pad, K=3 if T % 2 else None).stage()
+    p.call().check()
+    if M < 100:
+        p.call(p.least + (p.bytes - p.least) // 2).check()
+
+
+@pytest.mark.parametrize("T,M,V,dtype", [(2600, 8200, 101, "bf16"), (2600, 8200, 101, "f32"), (16500, 700, 202, "bf16")])
+def test_losses_alone_over_narrow_shards(T, M, V, dtype):
+    Problem(T, M, V, dtype, mesh=(2, 8)).stage((False, False)).call().check()
