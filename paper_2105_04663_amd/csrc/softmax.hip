@@ -77,10 +77,13 @@ struct Loss {
     return std::max<int64_t>(1, std::min({want / std::max<int64_t>(tiles, 1), T / least, int64_t(16)}));
   }
   bool narrow() const { return nb > 1 && vs < kNarrow && static_cast<double>(T) * static_cast<double>(M) * static_cast<double>(V) >= kNarrowWork; }         // shards of less than a tile, in products that are worth another launch
-  bool joins_dw() const { return dw && M > 0 && (dw_ranges() > 1 || narrow()); }
+  // .. of each shard of tokens by itself, where the partials are less than x put together: no copy of x then.
+  bool ranges_by_shard() const { return dw && na > 1 && !with_lost() && ts >= kFewRows && na * V * 4 <= T * esize(); }
+  int64_t dw_parts() const { return ranges_by_shard() ? na * std::max<int64_t>(1, dw_ranges() / na) : dw_ranges(); }
+  bool joins_dw() const { return dw && M > 0 && (dw_parts() > 1 || narrow()); }
   int64_t ld_dw() const { return vocab_dim == 0 ? ld_sum() : ldz(); }
   int64_t dw_part() const { return (vocab_dim == 0 ? ldz() : M) * ld_dw(); }
-  int64_t joined_dw_bytes() const { return joins_dw() ? round_up(dw_ranges() * dw_part() * 4, kWsAlign) : 0; }
+  int64_t joined_dw_bytes() const { return joins_dw() ? round_up(dw_parts() * dw_part() * 4, kWsAlign) : 0; }
   int64_t most_rows() const { return std::min(T, std::max<int64_t>(1, kPieceBytes / (ldz() * 4))); }
   // A padded copy of operands whose rows are not padded to 16 bytes, which the products read several times slower than they are copied once: from this many rows of products on ..
   bool packing_pays() const { return dtype == GSPMD_BF16 && T * (dx || dw ? 3 : 1) >= 1024; }
@@ -533,7 +536,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   // x put together: where dw sums over tokens of several shards, or over both parts of D, where shards have so few tokens that each would read the vocabulary matrix for
   // itself (15 tokens in two shards, 8099 x 124058: 690 us so), and where rows are not padded
   const bool copied_x = lost && l.dw && l.na == 1;           // by the row kernel, beside D: only dw needs it
-  const bool pack_x = l.M > 0 && !copied_x && ((l.dw && l.na > 1) || (l.na > 1 && l.ts < kFewRows) || (!x_padded && l.packing_pays()));
+  const bool pack_x = l.M > 0 && !copied_x && ((l.dw && l.na > 1 && !(join_dw && l.ranges_by_shard())) || (l.na > 1 && l.ts < kFewRows) || (!x_padded && l.packing_pays()));
 
   for (int64_t piece = 0; piece < pieces; ++piece) {
     const int64_t first = piece * rows, n = std::min(rows, l.T - first);       // tokens
@@ -710,13 +713,15 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
     }
     // ---- dw: straight into its shards, over several pieces in float32, or over ranges of the tokens in float32 for all shards together
     if (join_dw) {
-      const char* const from = pack_x || copied_x ? x_all : static_cast<const char*>(x[0].first.data);
-      const int64_t ldx = pack_x || copied_x ? l.ldx() : ldx_in, k = n * l.parts(), parts = l.dw_ranges(), each = round_up((k + parts - 1) / parts, 64), entries = l.cols();
+      const bool put_together = pack_x || copied_x;
+      const int64_t ldx = put_together ? l.ldx() : ldx_in, k = n * l.parts(), entries = l.cols();
+      const int64_t span = l.ranges_by_shard() ? l.ts : std::max<int64_t>(k, 1), parts = l.ranges_by_shard() ? l.dw_parts() / l.na : l.dw_parts(), each = round_up((span + parts - 1) / parts, 64);
       ps.clear();
-      for (int64_t at = 0; at < k; at += each) {
-        const int64_t here = std::min(each, k - at);
-        const char *const dr = d + at * ldd * e, *const xr = from + at * ldx * e;
+      for (int64_t at = 0; at < k;) {
+        const int64_t i = at / span, here = std::min({each, k - at, (i + 1) * span - at});
+        const char *const dr = d + at * ldd * e, *const xr = put_together ? x_all + at * ldx * e : static_cast<const char*>(x[static_cast<size_t>(i)].first.data) + (at - i * span) * ldx * e;
         float* const c = dw_parts + static_cast<int64_t>(ps.size()) * l.dw_part();
+        at += here;
         ps.push_back(vocab_dim == 0 ? product(dr, ldd, xr, ldx, c, l.ld_dw(), entries, l.M, here, entries, l.M) : product(xr, ldx, dr, ldd, c, l.ld_dw(), l.M, entries, here, l.M, entries));
       }
       const int32_t count_all = static_cast<int32_t>(ps.size());
