@@ -16,8 +16,8 @@ int32_t run_dots(std::vector<Problem>& ps, int32_t layout, int32_t in_dtype, int
 
 struct SoftmaxFinish;
 // Products of bfloat16 operands that end in `finish` (kernels_stats.h) instead of outputs, for launches that takes_stats() names: those that go to 256 x 256 tiles with direct
-// loads anyhow.
-bool takes_stats(const std::vector<Problem>& ps, int32_t layout);
+// loads anyhow, and with long_outputs those whose outputs rather than products make them go to another kernel.
+bool takes_stats(const std::vector<Problem>& ps, int32_t layout, bool long_outputs);
 int32_t run_stats(std::vector<Problem>& ps, int32_t layout, const SoftmaxFinish& finish, void* tables, int64_t table_bytes, hipStream_t stream);
 
 // out[r, c] = partials[0][r, c] + partials[1][r, c] + .., ascending, in fp32; any number of partials (all but the first of 16 at a time add to
@@ -26,5 +26,7 @@ int32_t run_sum(const std::vector<float*>& partials, int64_t rows, int64_t cols,
 
 // A test has pinned this thread's calls to end before their launches (testing.h).
 bool launches_are_dry();
+// A test has pinned the kernel of this thread's products: there have to be some.
+bool a_product_is_pinned();
 
 }  // namespace gspmd

@@ -731,10 +731,12 @@ int32_t run_dots(std::vector<Problem>& ps, int32_t layout, int32_t in_dtype, int
   return launch_problems(ps, layout, in_dtype, out_dtype, GSPMD_EPILOGUE_NONE, false, tables, table_bytes, stream);
 }
 
-bool takes_stats(const std::vector<Problem>& ps, int32_t layout) {
+bool takes_stats(const std::vector<Problem>& ps, int32_t layout, bool long_outputs) {
   if (ps.empty() || (layout & GSPMD_LAYOUT_LHS_K_MAJOR)) return false;
   const KernelPath path = kernel_path(ps, GSPMD_BF16, layout);
-  return path == kPathMfmaDirect && pick_kernel(ps, path, layout, false).kernel == kMfmaBig;
+  if (path != kPathMfmaDirect) return false;
+  const MfmaKernel kernel = pick_kernel(ps, path, layout, false).kernel;
+  return kernel == kMfmaBig || (long_outputs && kernel == kMfmaPair);
 }
 
 int32_t run_stats(std::vector<Problem>& ps, int32_t layout, const SoftmaxFinish& finish, void* tables, int64_t table_bytes, hipStream_t stream) {
@@ -769,6 +771,8 @@ int32_t run_sum(const std::vector<float*>& partials, int64_t rows, int64_t cols,
 }
 
 bool launches_are_dry() { return t_pin.dry_run != 0; }
+
+bool a_product_is_pinned() { return t_pin.kernel != GSPMD_TESTING_BY_RULE; }
 
 }  // namespace gspmd
 

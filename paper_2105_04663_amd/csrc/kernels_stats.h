@@ -21,7 +21,7 @@ struct SoftmaxFinish {
 
   // Targets that a thread has in registers: the next ones are on their way while what is found among these is stored (a load and a barrier after the other, eight at a time: 1024 tokens of 100
   // targets, 1024 x 128000, 393 us).
-  static constexpr int kHeld = 32, kAtOnce = kHeld * 512;
+  static constexpr int kHeld = 56, kAtOnce = kHeld * 512;
 
   __device__ __forceinline__ void operator()(float16_t (&acc)[8], const Problem& P, TileRows own, int n0, unsigned char* smem) const {
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), wm = wave >> 2, wn = wave & 3;
@@ -72,8 +72,9 @@ struct SoftmaxFinish {
       __syncthreads();
 #pragma unroll
       for (int n = 0; n < kHeld; ++n) {
-        const int col = held[n] - tile_col;
-        if (held[n] < 0 || col < 0 || col >= cols) continue;
+        if (from + n * 512 >= total) break;
+        const int col = held[n] - tile_col;      // (of no target far below 0)
+        if (static_cast<uint32_t>(col) >= static_cast<uint32_t>(cols)) continue;
         const int i = from + n * 512 + t, row = i / targets;
         list[atomicAdd(count, 1u)] = static_cast<uint32_t>(row | col << 8 | (i - row * targets) << 16);
       }

@@ -15,6 +15,7 @@
 #include "../../include/gspmd.h"
 #include "dots.h"
 #include "kernels_few.h"
+#include "kernels_small.h"
 #include "kernels_softmax.h"
 #include "kernels_stats.h"
 #include "plan.h"
@@ -32,6 +33,13 @@ constexpr int64_t kSmallSum = int64_t(1) << 20;      // elements of a partial of
 constexpr int64_t kNarrow = 128;
 constexpr double kNarrowWork = 2e9;
 constexpr int64_t kFewWeights = int64_t(32) << 20;
+// Logits that caches do not hold: not kept, even by the kernel that is slower at their product (losses alone, us kept / not kept: 4096 x 64 x 32000 232 / 103, 7884 x 404 x 55589 1032 / 634;
+// 9670 x 96 x 2251, 87 MB, 61 / 65).
+constexpr int64_t kLongLogits = int64_t(128) << 20;
+// One launch for everything (kernels_small.h) against four to six, us a step with gradients, M x V: bfloat16 100 x 160, 4 tokens 18 / 31, 500 22 / 29, 4000 26 / 34; 256 x 256 (128 KB) 21 / 25, 27 / 28,
+// 31 / 34; 256 x 500 25 / 25, 33 / 31, 40 / 37; 512 x 512 33 / 26, 42 / 31, 57 / 39; float32 100 x 160 (64 KB) 19 / 26, 28 / 32, 34 / 39; 256 x 256 27 / 25, 40 / 35, 44 / 41.  Losses alone
+// (against two launches): 100 x 160 12 / 15.5; 256 x 256 bfloat16 12 / 15.5, float32 15 / 15, 500 tokens 18 / 15.
+constexpr int64_t kSmallMost = 4096, kSmallWeights = int64_t(128) << 10;
 constexpr int64_t kFewWorkgroups = 12 * 256;     // of the kernels for a handful of tokens
 
 struct Loss {
@@ -101,12 +109,13 @@ struct Loss {
   // M x V): float32, [V, M], 1 token 640 x 10368 32 / 51, 2048 x 32000 182 / 225; 8 tokens 37 / 52, 185 / 237; 16 tokens 55 / 53, 242 / 239; [M, V], 4 tokens 40 / 52, 183 / 225;
   // 8 tokens 50 / 53, 131 / 123 (2048 x 16000).  bfloat16, [V, M], 1 token 128 x 2304 27 / 34, 1024 x 16000 34 / 42, 2048 x 16000 55 / 57, 2048 x 32000 106 / 101; 3 tokens 24 / 32, 39 / 41,
   // 63 / 58, 115 / 102; 8 tokens 640 x 10368 43 / 35; losses alone, 1 token 640 x 10368 15 / 16, 3 or more slower; [M, V], 3 tokens 640 x 10368 36 / 35, 2048 x 16000 84 / 59.
-  // bfloat16 beyond 32 MB of w: only where its rows are not padded, which the others read slowly (3 tokens, 4279 x 29599 in 4 shards 302).
+  // bfloat16 beyond 32 MB of w: only where its rows are not whole lines, which the others read and write slowly (6390 x 116189 in 8 shards, rows of 6392: 1 token 1026 / 1357, 4 tokens 1058 / 1388;
+  // 904 x 50000, 4 tokens 84 / 97; whole lines: 3904 x 123392, 1 token 600 / 540, 4 tokens 612 / 548).
   bool few() const {
     const int64_t most = dtype == GSPMD_F32 ? (vocab_dim == 0 || V * M * 4 <= kFewWeights ? 8 : 4) : vocab_dim == 0 && (dx || dw) ? 4 : 0;
     return T > 0 && T <= most && M > 0 && nb <= kFewWindows && na <= kInlineTokenShards;
   }
-  bool few_takes(bool w_padded) const { return few() && (dtype == GSPMD_F32 || !w_padded || V * M * 2 <= kFewWeights); }
+  bool few_takes(bool w_lines) const { return few() && (dtype == GSPMD_F32 || !w_lines || V * M * 2 <= kFewWeights); }
   int64_t few_lanes() const {                // [V, M]: of a row
     int64_t lanes = 1;
     while (lanes < 64 && lanes * 16 / esize() < M) lanes *= 2;
@@ -130,6 +139,16 @@ struct Loss {
   int64_t few_bytes() const {
     int64_t each, blocks;
     return round_up(T * ldz() * 4, kWsAlign) + (dx ? few_ranges(&each, &blocks) * T * ld_sum() * 4 : 0);
+  }
+  // All in one workgroup for 16 tokens (kernels_small.h).
+  bool small() const { return T > 0 && T <= kSmallMost && M >= 8 && (vocab_dim == 0 || vs >= 8) && V * M * esize() <= kSmallWeights && ldz() <= kSmallColumns && na <= kSmallShards && nb <= kSmallShards; }
+  // workgroups for the same tokens: as many as have a part of dx's columns or of dw's tiles to make
+  int64_t small_slices() const {
+    const int64_t across = (M + 63) / 64, blocks = (na * ts + kSmallTokens - 1) / kSmallTokens;
+    int64_t want = 1;
+    if (dx) want = std::min<int64_t>(across, (across * ldz() + 1023) / 1024);
+    if (dw && T <= kSmallTokens) want = std::max(want, std::min<int64_t>(64, across * ldz() / 512));
+    return std::max<int64_t>(1, std::min(want, 256 / blocks));
   }
   int64_t bytes(int64_t rows) const { return table_bytes() + x_bytes(rows) + z_bytes(rows) + sum_bytes(rows) + dw_bytes(rows); }
 };
@@ -321,6 +340,14 @@ int32_t run_few(const Loss& l, FewTokens& a, const SoftmaxRows& rows, AddUp& sum
   return launched();
 }
 
+template <typename T>
+int32_t launch_small(const SmallLoss& a, const Loss& l, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>((l.na * l.ts + kSmallTokens - 1) / kSmallTokens), static_cast<unsigned>(l.small_slices()));
+  if (l.vocab_dim == 0) hipLaunchKernelGGL((small_loss_kernel<T, 0>), grid, dim3(kSmallThreads), 0, stream, a);
+  else hipLaunchKernelGGL((small_loss_kernel<T, 1>), grid, dim3(kSmallThreads), 0, stream, a);
+  return launched();
+}
+
 int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const gspmd_sharding* x_sh, const gspmd_shard_buf* w_shards, const gspmd_sharding* w_sh, int32_t vocab_dim,
                  const gspmd_token_buf* tokens, int32_t targets, float tau, bool teacher, const gspmd_shard_buf* dx_shards, const gspmd_shard_buf* dw_shards, void* workspace,
                  int64_t workspace_bytes, void* hip_stream) {
@@ -422,7 +449,8 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & (kWsAlign - 1))) return GSPMD_ERR_WORKSPACE;
   bool w_padded = true;
   for (int64_t j = 0; j < l.windows(); ++j) w_padded = w_padded && padded(w[static_cast<size_t>(j)].first, ldw);
-  if (l.few_takes(w_padded) && workspace_bytes >= l.few_bytes()) {
+  const bool may_be_small = l.small() && targets <= kSmallTargets && !a_product_is_pinned();
+  if (!(may_be_small && workspace_bytes >= l.bytes(l.T)) && l.few_takes(w_padded && ldw * l.esize() % 128 == 0) && workspace_bytes >= l.few_bytes()) {
     if (dry) return GSPMD_OK;
     FewTokens a;
     std::memset(&a, 0, sizeof(a));
@@ -493,14 +521,14 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   room -= join_dw ? l.joined_dw_bytes() : 0;
   char* const w_all = ws;
   const int64_t e = l.esize(), ldz = l.ldz(), ldd = ldz * 4 / e, per_cols = l.per_cols(), nw = l.windows(), vec = 16 / e;
-  const bool lost = l.with_lost();
+  const bool lost = l.with_lost(), small = may_be_small && pieces == 1;
 
   // ---- the vocabulary matrix: shard by shard, or in one padded copy of all of them (zeros between)
   struct Window { const char* data; int64_t ld, col, entries; };
   std::vector<Window> windows;
   bool x_padded = true;
   for (int64_t i = 0; i < l.na; ++i) x_padded = x_padded && padded(x[static_cast<size_t>(i)].first, ldx_in);
-  if (((!w_padded && l.packing_pays()) || l.joining_pays()) && room >= l.packed_w_bytes() && l.M > 0) {
+  if (!small && ((!w_padded && l.packing_pays()) || l.joining_pays()) && room >= l.packed_w_bytes() && l.M > 0) {
     const int64_t ld = vocab_dim == 0 ? l.ldx() : ldz, chunks = ld / vec;
     for (int64_t from = 0; from < nw && !dry; from += kInlineTokenShards) {
       const int64_t n = std::min<int64_t>(kInlineTokenShards, nw - from);
@@ -537,6 +565,96 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   // itself (15 tokens in two shards, 8099 x 124058: 690 us so), and where rows are not padded
   const bool copied_x = lost && l.dw && l.na == 1;           // by the row kernel, beside D: only dw needs it
   const bool pack_x = l.M > 0 && !copied_x && ((l.dw && l.na > 1 && !(join_dw && l.ranges_by_shard())) || (l.na > 1 && l.ts < kFewRows) || (!x_padded && l.packing_pays()));
+
+  // dw of a piece: straight into its shards, over several pieces in float32, or over ranges of the tokens in float32 for all shards together
+  auto make_dw = [&](int64_t piece, int64_t first, int64_t n, bool put_together) -> int32_t {
+    const bool last = piece == pieces - 1;
+    const char* const d = reinterpret_cast<const char*>(z);
+    std::vector<Problem> ps;
+    if (join_dw) {
+      const int64_t ldx = put_together ? l.ldx() : ldx_in, k = n * l.parts(), entries = l.cols();
+      const int64_t span = l.ranges_by_shard() ? l.ts : std::max<int64_t>(k, 1), parts = l.ranges_by_shard() ? l.dw_parts() / l.na : l.dw_parts(), each = round_up((span + parts - 1) / parts, 64);
+      ps.clear();
+      for (int64_t at = 0; at < k;) {
+        const int64_t i = at / span, here = std::min({each, k - at, (i + 1) * span - at});
+        const char *const dr = d + at * ldd * e, *const xr = put_together ? x_all + at * ldx * e : static_cast<const char*>(x[static_cast<size_t>(i)].first.data) + (at - i * span) * ldx * e;
+        float* const c = dw_parts + static_cast<int64_t>(ps.size()) * l.dw_part();
+        at += here;
+        ps.push_back(vocab_dim == 0 ? product(dr, ldd, xr, ldx, c, l.ld_dw(), entries, l.M, here, entries, l.M) : product(xr, ldx, dr, ldd, c, l.ld_dw(), l.M, entries, here, l.M, entries));
+      }
+      const int32_t count_all = static_cast<int32_t>(ps.size());
+      if ((st = run_dots(ps, GSPMD_LAYOUT_LHS_K_MAJOR, l.dtype, GSPMD_F32, tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
+      for (int64_t from_shard = 0; from_shard < l.nb && !dry; from_shard += kInlineTokenShards) {
+        const int64_t shards = std::min<int64_t>(kInlineTokenShards, l.nb - from_shard), before = from_shard * per_cols;
+        AddUp a;
+        std::memset(&a, 0, sizeof(a));
+        for (int64_t j = 0; j < shards; ++j) a.to[j] = dw[static_cast<size_t>(from_shard + j)].first.data;
+        a.partials = dw_parts + (vocab_dim == 0 ? before * l.ld_dw() : before);
+        a.stride = l.dw_part();
+        a.ld_in = l.ld_dw();
+        a.ld_out = lddw;
+        a.count = count_all;
+        a.apart = static_cast<int32_t>(per_cols);
+        a.per_row = static_cast<int32_t>(l.vs);
+        a.first = static_cast<int32_t>(from_shard * l.vs);
+        a.first_shard = static_cast<int32_t>(from_shard);
+        a.tokens = static_cast<int32_t>(l.V);
+        a.by_columns = vocab_dim;
+        a.rows = static_cast<int32_t>(vocab_dim == 0 ? shards * l.vs : l.M);
+        a.cols = static_cast<int32_t>(vocab_dim == 0 ? l.M : shards * per_cols);
+        if ((st = launch_add_up(a, l.dtype, stream)) != GSPMD_OK) return st;
+      }
+    } else if (l.dw) {
+      const char* const from = put_together ? x_all : static_cast<const char*>(x[0].first.data) + first * ldx_in * e;
+      const int64_t ldx = put_together ? l.ldx() : ldx_in, k = n * l.parts(), ld_part = round_up(w_cols, 4);
+      ps.clear();
+      for (int64_t j = 0; j < l.nb; ++j) {
+        const gspmd_shard_buf& o = dw[static_cast<size_t>(j)].first;
+        void* const c = pieces == 1 ? o.data : dw_sums + (j * 2 + (piece > 0 ? 1 : 0)) * l.dw_size();
+        const int64_t ldc = pieces == 1 ? lddw : ld_part, entries = l.valid_v(j);
+        const char* const dj = d + j * per_cols * e;
+        ps.push_back(vocab_dim == 0 ? product(dj, ldd, from, ldx, c, ldc, entries, l.M, k, w_rows, w_cols) : product(from, ldx, dj, ldd, c, ldc, l.M, entries, k, w_rows, w_cols));
+      }
+      if ((st = run_dots(ps, GSPMD_LAYOUT_LHS_K_MAJOR, l.dtype, pieces == 1 ? l.dtype : static_cast<int32_t>(GSPMD_F32), tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
+      for (int64_t j = 0; piece > 0 && j < l.nb; ++j) {
+        const gspmd_shard_buf& o = dw[static_cast<size_t>(j)].first;
+        float* const sum = dw_sums + j * 2 * l.dw_size();
+        if ((st = run_sum({sum, sum + l.dw_size()}, w_rows, w_cols, ld_part, last ? o.data : sum, last ? lddw : ld_part, last ? l.dtype : static_cast<int32_t>(GSPMD_F32),
+                          stream)) != GSPMD_OK) return st;
+      }
+    }
+    return GSPMD_OK;
+  };
+  // ---- all in one launch, but for dw's sum over more tokens than a workgroup's
+  if (small) {
+    const bool in_one = l.T <= kSmallTokens, dw_after = l.dw && !in_one;
+    const bool copies = dw_after && (lost || (l.na > 1 && !(join_dw && l.ranges_by_shard())) || (!x_padded && l.packing_pays()));
+    SmallLoss a;
+    std::memset(&a, 0, sizeof(a));
+    rows_args(&a.rows, dw_after ? z : nullptr, 0, 0, l.na);
+    a.rows.lost = l.T;
+    a.rows.ldx = ldx_in;
+    a.rows.x_copies = copies ? reinterpret_cast<bf16_bits*>(x_all) : nullptr;
+    a.rows.ld_copy = l.ldx();
+    for (int64_t j = 0; j < l.nb; ++j) {
+      a.w[j] = w[static_cast<size_t>(j)].first.data;
+      a.dw[j] = l.dw && in_one ? dw[static_cast<size_t>(j)].first.data : nullptr;
+    }
+    for (int64_t i = 0; i < l.na; ++i) {
+      a.x[i] = x[static_cast<size_t>(i)].first.data;
+      a.dx[i] = l.dx ? dx[static_cast<size_t>(i)].first.data : nullptr;
+    }
+    a.ldw = ldw;
+    a.lddw = lddw;
+    a.lddx = lddx;
+    a.M = static_cast<int32_t>(l.M);
+    a.shards = static_cast<int32_t>(l.nb);
+    a.token_shards = static_cast<int32_t>(l.na);
+    a.lost = lost;
+    if (!dry && (st = l.dtype == GSPMD_BF16 ? launch_small<bf16_bits>(a, l, stream) : launch_small<float>(a, l, stream)) != GSPMD_OK) return st;
+    if (dw_after && (st = make_dw(0, 0, l.T, copies)) != GSPMD_OK) return st;
+    return spread_results();
+  }
 
   for (int64_t piece = 0; piece < pieces; ++piece) {
     const int64_t first = piece * rows, n = std::min(rows, l.T - first);       // tokens
@@ -605,7 +723,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
       });
     };
     all_logits();
-    if (stats && !takes_stats(ps, logits_layout)) {
+    if (stats && !takes_stats(ps, logits_layout, n * ldz * 4 >= kLongLogits)) {
       stats = false;
       all_logits();
     }
@@ -711,60 +829,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
       });
       if (st != GSPMD_OK) return st;
     }
-    // ---- dw: straight into its shards, over several pieces in float32, or over ranges of the tokens in float32 for all shards together
-    if (join_dw) {
-      const bool put_together = pack_x || copied_x;
-      const int64_t ldx = put_together ? l.ldx() : ldx_in, k = n * l.parts(), entries = l.cols();
-      const int64_t span = l.ranges_by_shard() ? l.ts : std::max<int64_t>(k, 1), parts = l.ranges_by_shard() ? l.dw_parts() / l.na : l.dw_parts(), each = round_up((span + parts - 1) / parts, 64);
-      ps.clear();
-      for (int64_t at = 0; at < k;) {
-        const int64_t i = at / span, here = std::min({each, k - at, (i + 1) * span - at});
-        const char *const dr = d + at * ldd * e, *const xr = put_together ? x_all + at * ldx * e : static_cast<const char*>(x[static_cast<size_t>(i)].first.data) + (at - i * span) * ldx * e;
-        float* const c = dw_parts + static_cast<int64_t>(ps.size()) * l.dw_part();
-        at += here;
-        ps.push_back(vocab_dim == 0 ? product(dr, ldd, xr, ldx, c, l.ld_dw(), entries, l.M, here, entries, l.M) : product(xr, ldx, dr, ldd, c, l.ld_dw(), l.M, entries, here, l.M, entries));
-      }
-      const int32_t count_all = static_cast<int32_t>(ps.size());
-      if ((st = run_dots(ps, GSPMD_LAYOUT_LHS_K_MAJOR, l.dtype, GSPMD_F32, tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
-      for (int64_t from_shard = 0; from_shard < l.nb && !dry; from_shard += kInlineTokenShards) {
-        const int64_t shards = std::min<int64_t>(kInlineTokenShards, l.nb - from_shard), before = from_shard * per_cols;
-        AddUp a;
-        std::memset(&a, 0, sizeof(a));
-        for (int64_t j = 0; j < shards; ++j) a.to[j] = dw[static_cast<size_t>(from_shard + j)].first.data;
-        a.partials = dw_parts + (vocab_dim == 0 ? before * l.ld_dw() : before);
-        a.stride = l.dw_part();
-        a.ld_in = l.ld_dw();
-        a.ld_out = lddw;
-        a.count = count_all;
-        a.apart = static_cast<int32_t>(per_cols);
-        a.per_row = static_cast<int32_t>(l.vs);
-        a.first = static_cast<int32_t>(from_shard * l.vs);
-        a.first_shard = static_cast<int32_t>(from_shard);
-        a.tokens = static_cast<int32_t>(l.V);
-        a.by_columns = vocab_dim;
-        a.rows = static_cast<int32_t>(vocab_dim == 0 ? shards * l.vs : l.M);
-        a.cols = static_cast<int32_t>(vocab_dim == 0 ? l.M : shards * per_cols);
-        if ((st = launch_add_up(a, l.dtype, stream)) != GSPMD_OK) return st;
-      }
-    } else if (l.dw) {
-      const char* const from = pack_x || copied_x ? x_all : static_cast<const char*>(x[0].first.data) + first * ldx_in * e;
-      const int64_t ldx = pack_x || copied_x ? l.ldx() : ldx_in, k = n * l.parts(), ld_part = round_up(w_cols, 4);
-      ps.clear();
-      for (int64_t j = 0; j < l.nb; ++j) {
-        const gspmd_shard_buf& o = dw[static_cast<size_t>(j)].first;
-        void* const c = pieces == 1 ? o.data : dw_sums + (j * 2 + (piece > 0 ? 1 : 0)) * l.dw_size();
-        const int64_t ldc = pieces == 1 ? lddw : ld_part, entries = l.valid_v(j);
-        const char* const dj = d + j * per_cols * e;
-        ps.push_back(vocab_dim == 0 ? product(dj, ldd, from, ldx, c, ldc, entries, l.M, k, w_rows, w_cols) : product(from, ldx, dj, ldd, c, ldc, l.M, entries, k, w_rows, w_cols));
-      }
-      if ((st = run_dots(ps, GSPMD_LAYOUT_LHS_K_MAJOR, l.dtype, pieces == 1 ? l.dtype : static_cast<int32_t>(GSPMD_F32), tables, l.table_bytes(), stream)) != GSPMD_OK) return st;
-      for (int64_t j = 0; piece > 0 && j < l.nb; ++j) {
-        const gspmd_shard_buf& o = dw[static_cast<size_t>(j)].first;
-        float* const sum = dw_sums + j * 2 * l.dw_size();
-        if ((st = run_sum({sum, sum + l.dw_size()}, w_rows, w_cols, ld_part, last ? o.data : sum, last ? lddw : ld_part, last ? l.dtype : static_cast<int32_t>(GSPMD_F32),
-                          stream)) != GSPMD_OK) return st;
-      }
-    }
+    if ((st = make_dw(piece, first, n, pack_x || copied_x)) != GSPMD_OK) return st;
   }
   return spread_results();
 }

@@ -296,3 +296,35 @@ def test_dw_over_ranges_of_the_tokens(T, M, V, dtype, mesh, vocab_dim, pad):
 @pytest.mark.parametrize("T,M,V,dtype", [(2600, 8200, 101, "bf16"), (2600, 8200, 101, "f32"), (16500, 700, 202, "bf16")])
 def test_losses_alone_over_narrow_shards(T, M, V, dtype):
     Problem(T, M, V, dtype, mesh=(2, 8)).stage((False, False)).call().check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab_dim", [0, 1])
+@pytest.mark.parametrize("T,M,V,mesh", [(1, 8, 8, (1, 1)), (7, 9, 1280, (1, 1)), (16, 24, 1281, (1, 1)), (16, 65, 301, (1, 3)), (17, 66, 77, (2, 8)), (15, 67, 90, (3, 4)), (129, 130, 200, (2, 2)), (4096, 11, 40, (2, 2)),
+                                        (4097, 11, 40, (2, 2)), (3, 500, 60, (1, 6)), (33, 700, 33, (16, 2)), (12, 40, 81, (1, 9)), (260, 31, 512, (3, 16))])
+def test_a_small_vocabulary_matrix(T, M, V, mesh, vocab_dim, dtype):
+    """All in one launch, at the edges of its tiles, its rows and its shards."""
+    for K, pad in ((None, True), (5, False), (128, True)):
+        if K is None or K < V:
+            Problem(T, M, V, dtype, K=K, mesh=mesh, vocab_dim=vocab_dim, pad=pad).stage().call().check()
+    for grad in ((False, False), (True, False), (False, True)):
+        Problem(T, M, V, dtype, mesh=mesh, vocab_dim=vocab_dim).stage(grad).call().check()
+
+
+@pytest.mark.parametrize("vocab_dim", [0, 1])
+@pytest.mark.parametrize("T,M,V", [(1, 8, 8), (2, 65, 7), (33, 64, 90), (65, 130, 257), (300, 72, 301)])
+@pytest.mark.parametrize("dtype,K,pad", [("bf16", None, True), ("bf16", 5, False), ("f32", None, False), ("f32", 100, True)])
+def test_small_sizes_by_products(T, M, V, vocab_dim, dtype, K, pad):
+    """The same without the one launch: a pinned product kernel stands for any."""
+    for mesh in ((1, 1), (2, 3)):
+        p = Problem(T, M, V, dtype, K=K, vocab_dim=vocab_dim, mesh=mesh, pad=pad).stage()
+        with pinned(MFMA):
+            p.call().check()
+
+
+@pytest.mark.parametrize("where", MESHES, ids=lambda m: "x".join(map(str, m["mesh"])) + ("" if m.get("share", True) else "_own"))
+def test_meshes_by_products(where):
+    for dtype, K, vocab_dim, pad in (("bf16", None, 0, True), ("bf16", 7, 1, False), ("f32", None, 1, True)):
+        p = Problem(41, 24, 203, dtype, K=K, vocab_dim=vocab_dim, pad=pad, **where).stage()
+        with pinned(MFMA):
+            p.call().check()
