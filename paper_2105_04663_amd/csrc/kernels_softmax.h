@@ -400,17 +400,24 @@ struct PackRows {
   int32_t per_cols, per, cols;   // column shards: columns apart in the result; shards of either kind: rows or columns of one; columns that exist in all
   int32_t copies;                // the rows again, `rows` further on
 };
-static_assert(sizeof(PackRows) <= 4096, "kernel arguments");
+// One or two of them in a launch, whose workgroups are the first's across x down, then the second's.
+struct PackTwo {
+  PackRows two[2];
+  int32_t across[2], down[2];
+};
+static_assert(sizeof(PackTwo) <= 4096, "kernel arguments");
 
 template <typename T>
-__global__ __launch_bounds__(256) void pack_rows_kernel(const PackRows args) {
-  const GSPMD_KERNARG PackRows& a = *first_kernel_argument<PackRows>();
+__global__ __launch_bounds__(256) void pack_rows_kernel(const PackTwo args) {
+  const GSPMD_KERNARG PackTwo& both = *first_kernel_argument<PackTwo>();
+  const int firsts = both.across[0] * both.down[0], which = static_cast<int>(blockIdx.x) >= firsts, block = blockIdx.x - which * firsts, across = both.across[which], down = both.down[which];
+  const GSPMD_KERNARG PackRows& a = both.two[which];
   constexpr int V = 16 / static_cast<int>(sizeof(T));
   typedef T vec __attribute__((ext_vector_type(V)));
   typedef T vec_any __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-  for (int row = blockIdx.y; row < a.rows; row += gridDim.y) {
-    const int chunk = blockIdx.x * 256 + threadIdx.x;
-    if (chunk >= a.chunks) continue;
+  const int chunk = block % across * 256 + threadIdx.x;
+  if (chunk >= a.chunks) return;
+  for (int row = block / across; row < a.rows; row += down) {
     const int col = chunk * V;
     GSPMD_GLOBAL const T* from;
     int n;                                      // columns that exist from `col` on

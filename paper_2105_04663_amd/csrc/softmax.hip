@@ -232,13 +232,32 @@ dim3 rows_grid(int64_t vectors, int64_t rows) {
   return dim3(static_cast<unsigned>((vectors + 255) / 256), static_cast<unsigned>(std::min<int64_t>(rows, 32768)));
 }
 
-int32_t launch_pack(const PackRows& a, int32_t dtype, hipStream_t stream) {
-  if (a.rows == 0 || a.chunks == 0) return GSPMD_OK;
-  const dim3 grid = rows_grid(a.chunks, a.rows);
-  if (dtype == GSPMD_BF16) hipLaunchKernelGGL((pack_rows_kernel<uint16_t>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((pack_rows_kernel<uint32_t>), grid, dim3(256), 0, stream, a);
-  return launched();
-}
+// Copies that nothing has needed yet, launched two at a time (x and w one after the other: 4 us more).
+struct Packs {
+  PackTwo args;
+  int n = 0;
+  int32_t dtype;
+  hipStream_t stream;
+  int32_t flush() {
+    if (n == 0) return GSPMD_OK;
+    int64_t blocks = 0;
+    for (int k = 0; k < 2; ++k) {
+      args.across[k] = k < n ? (args.two[k].chunks + 255) / 256 : 0;
+      args.down[k] = k < n ? std::min(args.two[k].rows, 32768) : 0;
+      blocks += static_cast<int64_t>(args.across[k]) * args.down[k];
+    }
+    const dim3 grid(static_cast<unsigned>(blocks));
+    if (dtype == GSPMD_BF16) hipLaunchKernelGGL((pack_rows_kernel<uint16_t>), grid, dim3(256), 0, stream, args);
+    else hipLaunchKernelGGL((pack_rows_kernel<uint32_t>), grid, dim3(256), 0, stream, args);
+    n = 0;
+    return launched();
+  }
+  int32_t add(const PackRows& a) {
+    if (a.rows <= 0 || a.chunks <= 0) return GSPMD_OK;       // (a table of shards beyond the last token)
+    args.two[n++] = a;
+    return n == 2 ? flush() : static_cast<int32_t>(GSPMD_OK);
+  }
+};
 
 int32_t launch_add_up(const AddUp& a, int32_t dtype, hipStream_t stream) {
   const dim3 grid = rows_grid((a.cols + 3) / 4, a.rows);
@@ -523,6 +542,9 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
   const int64_t e = l.esize(), ldz = l.ldz(), ldd = ldz * 4 / e, per_cols = l.per_cols(), nw = l.windows(), vec = 16 / e;
   const bool lost = l.with_lost(), small = may_be_small && pieces == 1;
 
+  Packs packs;
+  packs.dtype = l.dtype;
+  packs.stream = stream;
   // ---- the vocabulary matrix: shard by shard, or in one padded copy of all of them (zeros between)
   struct Window { const char* data; int64_t ld, col, entries; };
   std::vector<Window> windows;
@@ -554,7 +576,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
         a.by_columns = 1;
         a.cols = static_cast<int32_t>(l.V - from * l.vs);
       }
-      if ((st = launch_pack(a, l.dtype, stream)) != GSPMD_OK) return st;
+      if ((st = packs.add(a)) != GSPMD_OK) return st;
     }
     windows.push_back(Window{w_all, ld, 0, l.cols()});
   } else {
@@ -694,9 +716,9 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
         a.first_shard = static_cast<int32_t>(i0);
         a.cols = static_cast<int32_t>(l.M);
         a.copies = lost && l.dw ? 2 : 1;
-        return a.rows > 0 ? launch_pack(a, l.dtype, stream) : static_cast<int32_t>(GSPMD_OK);
+        return packs.add(a);
       });
-    if (st != GSPMD_OK) return st;
+    if (st != GSPMD_OK || (st = packs.flush()) != GSPMD_OK) return st;
     // ---- logits.  Where they need not be kept (without gradients) their tiles end in what the losses need of them.
     const int64_t groups = (l.cols() + 63) / 64, pair_bytes = round_up(groups * n * 8, kWsAlign), target_bytes = round_up(n * targets * 4, kWsAlign);
     bool stats = !l.dx && !l.dw && l.dtype == GSPMD_BF16 && l.M > 0 && n > 0 && per_cols % 64 == 0 && targets <= kStatsTargets && pair_bytes + 2 * target_bytes <= l.z_bytes(rows);
