@@ -71,7 +71,7 @@ struct Loss {
     if (!dx || rows == 0) return 1;
     const bool few = rows * parts() <= 128, small = dtype == GSPMD_F32 || few;
     const int64_t edge = small ? 64 : 256, tiles = ((rows * parts() + edge - 1) / edge) * ((M + edge - 1) / edge);
-    const int64_t want = dtype == GSPMD_F32 ? 1024 : few ? 512 : 256, least = small || rows * M <= kSmallSum ? 512 : 2048;         // workgroups; entries of a range
+    const int64_t want = dtype == GSPMD_F32 ? 1024 : few ? 512 : 256, least = dtype == GSPMD_F32 && rows <= 256 ? 256 : small || rows * M <= kSmallSum ? 512 : 2048;         // workgroups; entries of a range
     return std::max<int64_t>(1, std::min({want / std::max<int64_t>(tiles, 1), V / least, int64_t(16)}));
   }
   int64_t ranges_of_shard(int64_t rows) const { return std::max<int64_t>(1, std::min(ranges(rows), int64_t(32)) / windows()); }
