@@ -1,7 +1,8 @@
 // Losses over a split vocabulary (include/gspmd.h: gspmd_softmax_xent, gspmd_softmax_distill).
 //
 // Tokens are taken in pieces, in the order of all shards together.  A piece's logits go to the workspace as float32; softmax_rows_kernel makes of each row the token's loss
-// and, in place, D, the gradient with respect to the logits; two more products make of D the piece's rows of dx and its share of dw.
+// and, in place, D, the gradient with respect to the logits; two more products make of D the piece's rows of dx and its share of dw.  Losses alone do not keep the logits where their product goes to large
+// tiles (kernels_stats.h); a handful of tokens and a small vocabulary matrix have kernels of their own (kernels_few.h, kernels_small.h).
 // dx is a sum over the vocabulary.  Where the tokens give it too few output tiles to fill the chip, or the vocabulary's shards lie apart, its ranges are products of their own, float32 partials
 // that add_up_kernel adds in ascending order.  dw is a sum over the tokens: x from several shards is put together first (it is small beside w), and pieces add up in float32.
 #include <hip/hip_runtime.h>
@@ -23,24 +24,31 @@
 namespace gspmd {
 namespace {
 
-// Logits of a piece, at most (float32; at least one token's): what the workspace query provides for.
+// Logits of a piece, at most (float32; at least one token's): what the workspace query provides for.  Large, so that the products keep whole rounds of tiles and dw is summed once: pieces small enough
+// for the 256 MB cache saved no time (the logits' tiles are stored past it).
 constexpr int64_t kPieceBytes = int64_t(1) << 31;
 constexpr int64_t kColumnAlign = 64;
-// Up to so many tokens what D's rounding to bfloat16 loses takes part in the products, as rows of its own: these are bound by w and dw then.
+// Up to so many tokens what D's rounding to bfloat16 loses takes part in the products, as rows of its own: gradients are then off by their own rounding alone (0.0017 of their size, else 0.0024; with 16 tokens
+// one rounding of D does not average out).  These products are bound by w and dw: 2048 x 32000, 64 tokens 125 us, without 108; 128 tokens 149, 129.
 constexpr int64_t kFewTokens = 128;
-constexpr int64_t kFewRows = 256;            // less than a tile
-constexpr int64_t kSmallSum = int64_t(1) << 20;      // elements of a partial of dx that are hardly noticed
+// Shards of fewer tokens are put together, or each reads the vocabulary matrix for itself (losses of 200 tokens in 4 shards, 2048 x 16000: 30 us, else 40).
+constexpr int64_t kFewRows = 256;
+// Elements of a partial of dx that are hardly noticed: ranges of 512 entries, else of 2048 (200 tokens, 1001 x 16001: 73 us, by 2048 78; 1024 tokens, 2048 x 8000: 126, by 512 137).
+constexpr int64_t kSmallSum = int64_t(1) << 20;
+// Shards of the vocabulary of less than a tile, in products that are worth a copy of w and a launch for dw's places (losses of 4000 tokens, 2048 x 800 in 8 shards: 31 us, each for itself 34; gradients of
+// 16000 tokens, 8000 x 110 in 8 shards float32 1153, each for itself 3147; 1000 tokens, 1024 x 400, 0.4e9: 60.5, together 63).
 constexpr int64_t kNarrow = 128;
 constexpr double kNarrowWork = 2e9;
-constexpr int64_t kFewWeights = int64_t(32) << 20;
-// Logits that caches do not hold: not kept, even by the kernel that is slower at their product (losses alone, us kept / not kept: 4096 x 64 x 32000 232 / 103, 7884 x 404 x 55589 1032 / 634;
-// 9670 x 96 x 2251, 87 MB, 61 / 65).
-constexpr int64_t kLongLogits = int64_t(128) << 20;
+// Logits that caches do not hold: not kept, even by the kernel that is slower at their product (losses alone, us kept / not kept: 2048 x 128 x 16000, 131 MB, 54 / 37; 4096 x 64 x 32000 232 / 103;
+// 7884 x 404 x 55589 1032 / 634; 9670 x 96 x 2251, 87 MB, 61 / 65).
+constexpr int64_t kLongLogits = int64_t(96) << 20;
 // One launch for everything (kernels_small.h) against four to six, us a step with gradients, M x V: bfloat16 100 x 160, 4 tokens 18 / 31, 500 22 / 29, 4000 26 / 34; 256 x 256 (128 KB) 21 / 25, 27 / 28,
 // 31 / 34; 256 x 500 25 / 25, 33 / 31, 40 / 37; 512 x 512 33 / 26, 42 / 31, 57 / 39; float32 100 x 160 (64 KB) 19 / 26, 28 / 32, 34 / 39; 256 x 256 27 / 25, 40 / 35, 44 / 41.  Losses alone
 // (against two launches): 100 x 160 12 / 15.5; 256 x 256 bfloat16 12 / 15.5, float32 15 / 15, 500 tokens 18 / 15.
 constexpr int64_t kSmallMost = 4096, kSmallWeights = int64_t(128) << 10;
-constexpr int64_t kFewWorkgroups = 12 * 256;     // of the kernels for a handful of tokens
+// A handful of tokens (kernels_few.h): w that the caches hold, and workgroups of their kernels.
+constexpr int64_t kFewWeights = int64_t(32) << 20;
+constexpr int64_t kFewWorkgroups = 12 * 256;
 
 struct Loss {
   const gspmd_mesh* mesh = nullptr;
@@ -55,7 +63,7 @@ struct Loss {
   int64_t valid_v(int64_t j) const { return std::max<int64_t>(0, std::min(vs, V - j * vs)); }
   // a row of logits: the vocabulary shards that hold any entry, one after the other
   int64_t windows() const { return (V + vs - 1) / vs; }
-  // Shards start on whole lines, unless that would make rows much longer (16000 x 110 logits in 8 shards, 8000 wide: 3147 us float32), and on 64 columns where their products may end in statistics.
+  // Shards start on whole lines, unless that would make rows much longer (110 entries in 8 shards: 512 columns, not 112), and on 64 columns where their products may end in statistics.
   int64_t per_cols() const { return round_up(vs, windows() == 1 || vs >= 1024 || (vs >= kNarrow && !dx && !dw && dtype == GSPMD_BF16) ? kColumnAlign : 8); }
   int64_t cols() const { return (windows() - 1) * per_cols() + valid_v(windows() - 1); }
   int64_t ldz() const { return round_up(windows() * per_cols(), kColumnAlign); }
@@ -77,7 +85,8 @@ struct Loss {
   int64_t ranges_of_shard(int64_t rows) const { return std::max<int64_t>(1, std::min(ranges(rows), int64_t(32)) / windows()); }
   int64_t most_ranges(int64_t rows) const { return std::max(ranges(rows), windows() * ranges_of_shard(rows)); }
   bool adds_up(int64_t rows) const { return dx && (most_ranges(rows) > 1 || with_lost()); }
-  // Ranges of the tokens whose products make dw together, in one matrix of all shards ..
+  // Ranges of the tokens whose products make dw together, in one matrix of all shards, where its tiles are few (bfloat16, 4000 tokens, 512 x 2000 68 us, in one range 81; float32, 2000 tokens, 512 x 800
+  // 73 and 79; 12480 tokens, 135 x 707 153 and 285) ..
   int64_t dw_ranges() const {
     if (!dw || T == 0) return 1;
     const int64_t edge = dtype == GSPMD_F32 ? 64 : 256, tiles = ((cols() + edge - 1) / edge) * ((M + edge - 1) / edge);
@@ -85,7 +94,7 @@ struct Loss {
     return std::max<int64_t>(1, std::min({want / std::max<int64_t>(tiles, 1), T / least, int64_t(16)}));
   }
   bool narrow() const { return nb > 1 && vs < kNarrow && static_cast<double>(T) * static_cast<double>(M) * static_cast<double>(V) >= kNarrowWork; }         // shards of less than a tile, in products that are worth another launch
-  // .. of each shard of tokens by itself, where the partials are less than x put together: no copy of x then.
+  // .. of each shard of tokens by itself, where the partials are less than x put together: no copy of x then (12856 tokens in 3 shards, 2203 x 284: a copy is 27 of 165 us).
   bool ranges_by_shard() const { return dw && na > 1 && !with_lost() && ts >= kFewRows && na * V * 4 <= T * esize(); }
   int64_t dw_parts() const { return ranges_by_shard() ? na * std::max<int64_t>(1, dw_ranges() / na) : dw_ranges(); }
   bool joins_dw() const { return dw && M > 0 && (dw_parts() > 1 || narrow()); }
@@ -93,10 +102,15 @@ struct Loss {
   int64_t dw_part() const { return (vocab_dim == 0 ? ldz() : M) * ld_dw(); }
   int64_t joined_dw_bytes() const { return joins_dw() ? round_up(dw_parts() * dw_part() * 4, kWsAlign) : 0; }
   int64_t most_rows() const { return std::min(T, std::max<int64_t>(1, kPieceBytes / (ldz() * 4))); }
-  // A padded copy of operands whose rows are not padded to 16 bytes, which the products read several times slower than they are copied once: from this many rows of products on ..
-  bool packing_pays() const { return dtype == GSPMD_BF16 && T * (dx || dw ? 3 : 1) >= 1024; }
-  // .. and of a vocabulary in many shards, where dx's partials, one for each, would be more than that copy (4085 tokens, 2834 x 2393 on 3 x 8: 439 us without).
-  bool joining_pays() const { return windows() > 1 && ((dx && 2 * T * windows() >= V) || narrow()); }
+  // A padded copy of operands whose rows are not padded to 16 bytes, which the products read several times slower than they are copied once (1001 x 16001: 600 tokens 131 us, without 153; losses
+  // alone, 600 tokens 49 and 54, 2000 tokens 87 and 133; 200 tokens 78 and 73; losses of 512 tokens, 515 x 8001 26 and 21) ..
+  bool packing_pays() const {
+    const double work = static_cast<double>(T) * static_cast<double>(M) * static_cast<double>(V);
+    return dtype == GSPMD_BF16 && (T >= 1024 || (T >= (dx || dw ? 342 : 512) && work >= 4e9));
+  }
+  // .. and of a vocabulary in many shards, where dx's partials, one for each, would be more than that copy (bfloat16, 3000 tokens, 1024 x 16000 in 8 shards 329 us, apart 359; 4096 tokens, 2048 x 32000
+  // in 4: 1386, apart 1347), or whose shards are narrow.
+  bool joining_pays() const { return windows() > 1 && ((dx && 2 * T * windows() >= 3 * V) || narrow()); }
   int64_t packed_w_bytes() const { return round_up((vocab_dim == 0 ? ldz() * ldx() : std::max<int64_t>(M, 1) * ldz()) * esize(), kWsAlign); }
   // ---- the workspace, for pieces of `rows` tokens
   int64_t table_bytes() const { return round_up((na * nb + 32 + nb) * kTableBytesPerProblem, kWsAlign); }
