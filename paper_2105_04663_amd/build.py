@@ -15,6 +15,7 @@ CALL = os.path.join(HERE, "_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 # (source, object, extra flags); the MFMA kernels' sources are compiled once per operand layout
 UNITS = [(os.path.join(CSRC, f"{name}.hip"), f"{name}_l{n}.o", [f"-DGSPMD_TU_LAYOUT={n}"])
          for name in ("dot_mfma", "dot_split", "dot_mid", "dot_pair") for n in range(4)] + [
+    (os.path.join(CSRC, "dot_stats.hip"), f"dot_stats_l{n}.o", [f"-DGSPMD_TU_LAYOUT={n}"]) for n in (0, 2)] + [
     (os.path.join(CSRC, "gspmd.hip"), "gspmd.o", []),
     (os.path.join(CSRC, "softmax.hip"), "softmax.o", []),
     (os.path.join(CSRC, "plan.cpp"), "plan.o", []),

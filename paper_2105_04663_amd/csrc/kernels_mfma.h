@@ -32,7 +32,6 @@
 #include <type_traits>
 
 #include "kernels_basic.h"
-#include "kernels_stats.h"
 #include "launch.h"
 #include "mainloop_asm.h"
 #include "mfma_common.h"
@@ -763,23 +762,5 @@ bool launch_dot_mfma_layout(const MfmaLaunch& l, int32_t out_dtype, bool staged,
   if (!staged) return out_dtype == GSPMD_F32 ? launch_dot_mfma_as<float, LAYOUT, false>(l, stream) : launch_dot_mfma_as<bf16_bits, LAYOUT, false>(l, stream);
   return out_dtype == GSPMD_F32 ? launch_dot_mfma_as<float, LAYOUT, true>(l, stream) : launch_dot_mfma_as<bf16_bits, LAYOUT, true>(l, stream);
 }
-
-#if GSPMD_TU_LAYOUT == 0 || GSPMD_TU_LAYOUT == 2
-template <int LAYOUT>
-bool launch_dot_stats_layout(const MfmaLaunch& l, const SoftmaxFinish& finish, hipStream_t stream) {
-  static std::once_flag once[kMaxDevices];
-  static bool ok[kMaxDevices];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return false;
-  std::call_once(once[dev], [dev] {
-    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_mfma_kernel<float, LAYOUT, false, SoftmaxFinish>),
-                                  hipFuncAttributeMaxDynamicSharedMemorySize, kMfmaLds) == hipSuccess;
-  });
-  if (!ok[dev]) return false;
-  hipLaunchKernelGGL((dot_mfma_kernel<float, LAYOUT, false, SoftmaxFinish>), dim3(static_cast<unsigned>(l.tiles)), dim3(kMfmaThreads), kMfmaLds, stream, *l.inl, l.tab, l.n_prob,
-                     GSPMD_EPILOGUE_NONE, nullptr, nullptr, nullptr, 0, finish);
-  return hipGetLastError() == hipSuccess;
-}
-#endif
 
 }  // namespace gspmd
