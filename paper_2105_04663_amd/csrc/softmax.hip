@@ -122,14 +122,16 @@ struct Loss {
   // ---- a handful of tokens (kernels_few.h): as many as were measured faster there, all sizes of w from 0.6 to 262 MB together (us, a step with gradients, these kernels / the others;
   // M x V): float32, [V, M], 1 token 640 x 10368 32 / 51, 2048 x 32000 182 / 225; 8 tokens 37 / 52, 185 / 237; 16 tokens 55 / 53, 242 / 239; [M, V], 4 tokens 40 / 52, 183 / 225;
   // 8 tokens 50 / 53, 131 / 123 (2048 x 16000).  bfloat16, [V, M], 1 token 128 x 2304 27 / 34, 1024 x 16000 34 / 42, 2048 x 16000 55 / 57, 2048 x 32000 106 / 101; 3 tokens 24 / 32, 39 / 41,
-  // 63 / 58, 115 / 102; 8 tokens 640 x 10368 43 / 35; losses alone, 1 token 640 x 10368 15 / 16, 3 or more slower; [M, V], 3 tokens 640 x 10368 36 / 35, 2048 x 16000 84 / 59.
+  // 63 / 58, 115 / 102; 8 tokens 640 x 10368 43 / 35; losses alone, 1 token 640 x 10368 14 / 15.5, 1024 x 16000 15 / 17, 4 tokens
+  // 16 / 16.5; [M, V], 3 tokens 640 x 10368 36 / 35, 2048 x 16000 84 / 59.
   // bfloat16 beyond 32 MB of w: only where its rows are not whole lines, which the others read and write slowly (6390 x 116189 in 8 shards, rows of 6392: 1 token 1026 / 1357, 4 tokens 1058 / 1388;
-  // 904 x 50000, 4 tokens 84 / 97; whole lines: 3904 x 123392, 1 token 600 / 540, 4 tokens 612 / 548).
+  // 904 x 50000, 4 tokens 84 / 97; losses alone, 3001 x 20001, 1 token 35 / 58, 4 tokens 44 / 60; whole lines: 3904 x 123392, 1 token 600 / 540, 4 tokens 612 / 548; losses alone, 1 token 2048 x 32000 38.7 / 36.5,
+  // 4096 x 32000 67 / 64), and losses of one or two tokens over many short rows (1024 x 50000 31 / 35, 1536 x 80000 55 / 69, 2048 x 128000 110 / 144, 512 x 128000 41 / 41).
   bool few() const {
-    const int64_t most = dtype == GSPMD_F32 ? (vocab_dim == 0 || V * M * 4 <= kFewWeights ? 8 : 4) : vocab_dim == 0 && (dx || dw) ? 4 : 0;
+    const int64_t most = dtype == GSPMD_F32 ? (vocab_dim == 0 || V * M * 4 <= kFewWeights ? 8 : 4) : vocab_dim == 0 ? 4 : 0;
     return T > 0 && T <= most && M > 0 && nb <= kFewWindows && na <= kInlineTokenShards;
   }
-  bool few_takes(bool w_lines) const { return few() && (dtype == GSPMD_F32 || !w_lines || V * M * 2 <= kFewWeights); }
+  bool few_takes(bool w_lines) const { return few() && (dtype == GSPMD_F32 || !w_lines || V * M * 2 <= kFewWeights || (!dx && !dw && T <= 2 && V >= 48000 && M <= 2048)); }
   int64_t few_lanes() const {                // [V, M]: of a row
     int64_t lanes = 1;
     while (lanes < 64 && lanes * 16 / esize() < M) lanes *= 2;
