@@ -328,3 +328,30 @@ def test_meshes_by_products(where):
         p = Problem(41, 24, 203, dtype, K=K, vocab_dim=vocab_dim, pad=pad, **where).stage()
         with pinned(MFMA):
             p.call().check()
+
+
+@pytest.mark.parametrize("T,M,V,kw,grad", [(130, 64, 2000, dict(mesh=(2, 2)), True), (300, 72, 2003, dict(pad=False, vocab_dim=1), True), (3, 64, 2000, {}, True), (5, 300, 1000, dict(dtype="f32", vocab_dim=1, mesh=(1, 3)), True),
+                                           (2100, 300, 400, dict(mesh=(2, 3), K=4), True), (9, 40, 300, dict(K=9), True), (40, 40, 300, dict(dtype="f32"), True), (700, 512, 30001, dict(mesh=(2, 1)), False),
+                                           (1000, 1030, 5000, dict(pad=False, K=3), False)])
+def test_graphs_of_every_path(T, M, V, kw, grad):
+    """Recorded and replayed on other inputs, with eager calls between: the same bits as eager ones."""
+    p = Problem(T, M, V, **kw).stage((grad, grad))
+    outputs = [b[1] for b in (p.dxs or []) + (p.dws or [])] + [t[1][name] for t in p.ts for name in ("loss", "lse")]
+    p.call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.call(stream=torch.cuda.current_stream().cuda_stream)
+    for turn in range(3):
+        p.xs[0][1][:3].mul_(-1.0)
+        for o in outputs:
+            o.fill_(float(turn))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [o.clone() for o in outputs]
+        p.space.fill_(255)                              # what the workspace holds is of no consequence
+        for o in outputs:
+            o.fill_(float(turn))
+        p.call()
+        torch.cuda.synchronize()
+        for a, b in zip(replayed, outputs):
+            assert torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0))
