@@ -86,6 +86,15 @@ __device__ __forceinline__ TargetSums over_targets(int K, Q q_of, U u_of, Keep k
   const int lane = threadIdx.x & 63;
   auto most = [](float x, float y) { return x != x ? x : y != y ? y : fmaxf(x, y); };
   auto plus = [](float x, float y) { return x + y; };
+  // A label, most often: p = 1 (of a logit that is no number: none), without the exchanges (1 us of a row, for which its other waves wait: 1 token, 2048 x 32000 36.5 -> 35.5, 16 tokens, 1024 x 8000 with
+  // gradients 33.6 -> 32.7).
+  if (K == 1) {
+    auto first_lane = [](float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); };
+    const float q = first_lane(q_of(0)), zero = q - q;
+    if (q == -INFINITY) return TargetSums{false, 0.f};
+    if (lane == 0) keep(0, 1.f + zero);
+    return TargetSums{true, (1.f + zero) * (zero - first_lane(u_of(0)))};
+  }
   float q_most = -INFINITY;
   for (int k = lane; k < K; k += 64) q_most = most(q_most, q_of(k));
   q_most = over_wave(q_most, most);
