@@ -350,9 +350,9 @@ int32_t gspmd_resharded_dot(const gspmd_mesh* mesh, const gspmd_dot_dims* dims,
  *   dx = D w,  dw = D^T x                                                (summed over the vocabulary's and the tokens' mesh dimension, as an AllReduce)
  * The logits of all tokens are never held: tokens go through the workspace in pieces of at most 2 GiB of logits (less where the workspace is smaller).
  * Operands are bf16 or f32; logits, maxima, sums and losses are fp32; D is rounded once to the operands' type, as an operand of the
- * products that make the gradients, which accumulate in fp32 and are stored in that type (up to 128 tokens what that rounding loses is multiplied too).  A weight of 0 makes a token's D zero whatever its logits are; its x still
- * enters dw's sums, times 0, so x must be finite there (padding beyond the valid lengths may hold anything).  Logits that are NaN or
- * +infinity give NaN; -infinity throughout lse -infinity, and NaN for the loss and D. */
+ * products that make the gradients, which accumulate in fp32 and are stored in that type (up to 128 tokens what that rounding loses is multiplied too).
+ * A weight of 0 makes a token's D zero whatever its logits are; its x still enters dw's sums, times 0, so x must be finite there (padding beyond the valid
+ * lengths may hold anything).  Logits that are NaN or +infinity give NaN; -infinity throughout lse -infinity, and NaN for the loss and D. */
 #define GSPMD_MAX_TARGETS 1024
 
 /* One partition's arrays per token (device memory, dense, of the static token count of x's shard; padding may hold anything in the inputs and is written as 0 in

@@ -1,12 +1,13 @@
 // The losses over a split vocabulary where the whole vocabulary matrix is small (softmax.hip): a workgroup takes 16 tokens through everything -- their logits, which stay in LDS, the softmax,
 // D in the logits' place, their rows of dx, and, where 16 tokens are all there are, its share of dw.
 //
-// These calls are bound by launches and by what their kernels wait for, not by memory or arithmetic: the others take four to six launches of 5 to 8 us (8 tokens, 64 x 90 float32 in 4 shards: 14 us; 24 with the
-// kernels for a handful of tokens).  Every workgroup reads w once (16 tokens: for its logits
-// all of it) or twice, which is why w has to be small; it comes from L2 then.  A launch of few tokens has several workgroups for the same ones: each makes all their logits, and a part of dx's columns and of dw.
-// Code is kept short for the same reason: each instruction is fetched once and used a few times (with loops for
-// whole fragments and for others and two tokens a wave the kernel was 36 KB; 106 tokens, 90 x 217 in 4 shards, losses alone, 16 us, 9 so).  Fragments go from global memory straight to matrix instructions, at any element alignment.  An operand whose sum runs along its rows is loaded along them; of one whose sum runs across them a lane loads four
-// neighbouring columns of each of its rows, which are its fragments of four tiles (whose columns are then 4 n + tile).
+// These calls are bound by launches and by what their kernels wait for, not by memory or arithmetic: the others take four to six launches of 5 to 8 us (8 tokens, 64 x 90 float32 in 4 shards:
+// 14 us, with the kernels for a handful of tokens 24).  Every workgroup reads w once for its logits and once more for dx, from L2, which is why w has to be small.  A launch of few tokens has
+// several workgroups for the same ones: each makes all their logits, and a part of dx's columns and of dw.
+// Code is kept short for the same reason: each instruction is fetched once and used a few times (with loops of their own for whole fragments, and two tokens a wave, the kernel was 36 KB;
+// 106 tokens, 90 x 217 in 4 shards, losses alone, 16 us, so 9).
+// Fragments go from global memory straight to matrix instructions, at any element alignment.  An operand whose sum runs along its rows is loaded along them; of one whose sum runs across them a
+// lane loads four neighbouring columns of each of its rows, which are its fragments of four tiles (whose columns are then 4 n + tile).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

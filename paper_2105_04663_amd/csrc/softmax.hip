@@ -28,8 +28,8 @@ namespace {
 // for the 256 MB cache saved no time (the logits' tiles are stored past it).
 constexpr int64_t kPieceBytes = int64_t(1) << 31;
 constexpr int64_t kColumnAlign = 64;
-// Up to so many tokens what D's rounding to bfloat16 loses takes part in the products, as rows of its own: gradients are then off by their own rounding alone (0.0017 of their size, else 0.0024; with 16 tokens
-// one rounding of D does not average out).  These products are bound by w and dw: 2048 x 32000, 64 tokens 125 us, without 108; 128 tokens 149, 129.
+// Up to so many tokens what D's rounding to bfloat16 loses takes part in the products, as rows of its own: gradients are then off by their own rounding alone (0.0017 of their size, else 0.0024).
+// These products are bound by w and dw: 2048 x 32000, 64 tokens 125 us, without 108; 128 tokens 149, 129.
 constexpr int64_t kFewTokens = 128;
 // Shards of fewer tokens are put together, or each reads the vocabulary matrix for itself (losses of 200 tokens in 4 shards, 2048 x 16000: 30 us, else 40).
 constexpr int64_t kFewRows = 256;
@@ -79,7 +79,9 @@ struct Loss {
     if (!dx || rows == 0) return 1;
     const bool few = rows * parts() <= 128, small = dtype == GSPMD_F32 || few;
     const int64_t edge = small ? 64 : 256, tiles = ((rows * parts() + edge - 1) / edge) * ((M + edge - 1) / edge);
-    const int64_t want = dtype == GSPMD_F32 ? 1024 : few ? 512 : 256, least = dtype == GSPMD_F32 && rows <= 256 ? 256 : small || rows * M <= kSmallSum ? 512 : 2048;         // workgroups; entries of a range
+    const int64_t want = dtype == GSPMD_F32 ? 1024 : few ? 512 : 256;         // workgroups
+    // entries of a range (float32, 100 tokens, 300 x 3000 by 256 37.5 us, by 512 41; 512 tokens, 512 x 3000 73 and 69)
+    const int64_t least = dtype == GSPMD_F32 && rows <= 256 ? 256 : small || rows * M <= kSmallSum ? 512 : 2048;
     return std::max<int64_t>(1, std::min({want / std::max<int64_t>(tiles, 1), V / least, int64_t(16)}));
   }
   int64_t ranges_of_shard(int64_t rows) const { return std::max<int64_t>(1, std::min(ranges(rows), int64_t(32)) / windows()); }
@@ -93,7 +95,8 @@ struct Loss {
     const int64_t want = dtype == GSPMD_F32 ? 1024 : 256, least = dtype == GSPMD_F32 ? 512 : 1024;
     return std::max<int64_t>(1, std::min({want / std::max<int64_t>(tiles, 1), T / least, int64_t(16)}));
   }
-  bool narrow() const { return nb > 1 && vs < kNarrow && static_cast<double>(T) * static_cast<double>(M) * static_cast<double>(V) >= kNarrowWork; }         // shards of less than a tile, in products that are worth another launch
+  double work() const { return static_cast<double>(T) * static_cast<double>(M) * static_cast<double>(V); }
+  bool narrow() const { return nb > 1 && vs < kNarrow && work() >= kNarrowWork; }
   // .. of each shard of tokens by itself, where the partials are less than x put together: no copy of x then (12856 tokens in 3 shards, 2203 x 284: a copy is 27 of 165 us).
   bool ranges_by_shard() const { return dw && na > 1 && !with_lost() && ts >= kFewRows && na * V * 4 <= T * esize(); }
   int64_t dw_parts() const { return ranges_by_shard() ? na * std::max<int64_t>(1, dw_ranges() / na) : dw_ranges(); }
@@ -105,8 +108,7 @@ struct Loss {
   // A padded copy of operands whose rows are not padded to 16 bytes, which the products read several times slower than they are copied once (1001 x 16001: 600 tokens 131 us, without 153; losses
   // alone, 600 tokens 49 and 54, 2000 tokens 87 and 133; 200 tokens 78 and 73; losses of 512 tokens, 515 x 8001 26 and 21) ..
   bool packing_pays() const {
-    const double work = static_cast<double>(T) * static_cast<double>(M) * static_cast<double>(V);
-    return dtype == GSPMD_BF16 && (T >= 1024 || (T >= (dx || dw ? 342 : 512) && work >= 4e9));
+    return dtype == GSPMD_BF16 && (T >= 1024 || (T >= (dx || dw ? 342 : 512) && work() >= 4e9));
   }
   // .. and of a vocabulary in many shards, where dx's partials, one for each, would be more than that copy (bfloat16, 3000 tokens, 1024 x 16000 in 8 shards 329 us, apart 359; 4096 tokens, 2048 x 32000
   // in 4: 1386, apart 1347), or whose shards are narrow.
@@ -125,8 +127,8 @@ struct Loss {
   // 63 / 58, 115 / 102; 8 tokens 640 x 10368 43 / 35; losses alone, 1 token 640 x 10368 14 / 15.5, 1024 x 16000 15 / 17, 4 tokens
   // 16 / 16.5; [M, V], 3 tokens 640 x 10368 36 / 35, 2048 x 16000 84 / 59.
   // bfloat16 beyond 32 MB of w: only where its rows are not whole lines, which the others read and write slowly (6390 x 116189 in 8 shards, rows of 6392: 1 token 1026 / 1357, 4 tokens 1058 / 1388;
-  // 904 x 50000, 4 tokens 84 / 97; losses alone, 3001 x 20001, 1 token 35 / 58, 4 tokens 44 / 60; whole lines: 3904 x 123392, 1 token 600 / 540, 4 tokens 612 / 548; losses alone, 1 token 2048 x 32000 38.7 / 36.5,
-  // 4096 x 32000 67 / 64), and losses of one or two tokens over many short rows (1024 x 50000 31 / 35, 1536 x 80000 55 / 69, 2048 x 128000 110 / 144, 512 x 128000 41 / 41).
+  // 904 x 50000, 4 tokens 84 / 97; losses alone, 3001 x 20001, 1 token 35 / 58, 4 tokens 44 / 60; whole lines: 3904 x 123392, 1 token 600 / 540, 4 tokens 612 / 548; losses alone, 1 token
+  // 2048 x 32000 38.7 / 36.5, 4096 x 32000 67 / 64), and losses of one or two tokens over many short rows (1024 x 50000 31 / 35, 1536 x 80000 55 / 69, 2048 x 128000 110 / 144, 512 x 128000 41 / 41).
   bool few() const {
     const int64_t most = dtype == GSPMD_F32 ? (vocab_dim == 0 || V * M * 4 <= kFewWeights ? 8 : 4) : vocab_dim == 0 ? 4 : 0;
     return T > 0 && T <= most && M > 0 && nb <= kFewWindows && na <= kInlineTokenShards;
@@ -158,7 +160,8 @@ struct Loss {
   }
   // All in one workgroup for 16 tokens (kernels_small.h).
   bool small() const { return T > 0 && T <= kSmallMost && M >= 8 && (vocab_dim == 0 || vs >= 8) && V * M * esize() <= kSmallWeights && ldz() <= kSmallColumns && na <= kSmallShards && nb <= kSmallShards; }
-  // workgroups for the same tokens: as many as have a part of dx's columns or of dw's tiles to make
+  // Workgroups for the same tokens: as many as have a part of dx's columns or of dw's tiles to make (bfloat16, 16 tokens, 256 x 256 22 us, by one 25; 40 tokens, 600 x 100 24 and 27; 4 tokens, 100 x 160
+  // 17.7 and 17).
   int64_t small_slices() const {
     const int64_t across = (M + 63) / 64, blocks = (na * ts + kSmallTokens - 1) / kSmallTokens;
     int64_t want = 1;
