@@ -94,8 +94,8 @@ __device__ __forceinline__ T small_round(float v) {
   else return v;
 }
 
-// ORDER: vocab_dim (0: w [V, M], 1: [M, V]).
-template <typename T, int ORDER>
+// ORDER: vocab_dim (0: w [V, M], 1: [M, V]).  DW: dw is made here, of 16 tokens in all.
+template <typename T, int ORDER, bool DW>
 __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(const SmallLoss args) {
   constexpr int V = small_vec<T>(), kStep = 4 * V, kWaves = kSmallWaves;        // terms of a sum that an instruction (four, in float32) takes
   constexpr int kPartCols = 64 * kWaves;                                        // logits in parts: columns of all of them
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(const SmallLo
   __syncthreads();
 
   // ---- the softmax and D: a wave's token
-  const bool has_grad = a.dx[0] != nullptr || a.dw[0] != nullptr || r.z != nullptr;
+  const bool has_grad = a.dx[0] != nullptr || DW || r.z != nullptr;
   const float inv_tau = r.inv_tau, c = inv_tau * kLog2e;
   float* const z = logits + wave * ld;
   if (!has_token) {                             // padding of the last shards, or none of theirs
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(const SmallLo
 #pragma unroll 1
     for (int col = lane; col < groups * 64; col += 64) {
       float v = z[col];
-#pragma unroll 1
+#pragma unroll 4
       for (int p = 1; p < splits; ++p) v += z[p * kSmallTokens * ld + col];
       if (place(col).valid <= 0) v = -INFINITY;
       z[col] = v;
@@ -326,177 +326,179 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(const SmallLo
       }
     }
   }
-  if (a.dx[0] == nullptr && a.dw[0] == nullptr) return;
+  if (a.dx[0] == nullptr && !DW) return;
   __syncthreads();
 
   auto m_of = [&](int group) { return min(group * 64 + 4 * n16, M - 4); };       // the first of a lane's four of M
 
-  // ---- dx: sums over the columns, whose D is in LDS.  A round of the waves takes `at_once` groups of 64 of M, several waves sharing one's sum; their parts meet in LDS.
-  const int across = (M + 63) >> 6, mine_first = across * slice / slices, mine_end = across * (slice + 1) / slices;
-  if (a.dx[0] != nullptr && mine_end > mine_first) {
-    int shares = 1;
-    while (shares * 2 * (mine_end - mine_first) <= kWaves && shares * 2 * kStep <= groups * 64) shares *= 2;
-    const int at_once = kWaves / shares, each = (groups * 64 / shares + kStep - 1) / kStep * kStep;
-    for (int from = mine_first; from < mine_end; from += at_once) {
-      const int share = wave / at_once, group = from + wave - share * at_once, begin = share * each, end = min(begin + each, groups * 64);
-      float4_t acc[4] = {};
-      if (group < mine_end) {
-        constexpr int U = 2;
-        const int its = (end - begin + U * kStep - 1) / (U * kStep);
-#pragma unroll 1
-        for (int it = 0; it < its; ++it) {
-          const int k0 = turned(it, its, begin, U * kStep);
-          few_raw<T> fb[U][4];
-          small_four<T> raw[U][V];
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int k = k0 + u * kStep + quad * V;
-            const Place p = place(k);           // (V columns of one shard)
-            const int valid = k0 + u * kStep < end ? p.valid : 0;
-            GSPMD_GLOBAL const T* const w = (GSPMD_GLOBAL const T*)a.w[valid > 0 ? p.j : 0];
-            if constexpr (ORDER == 0) {
-#pragma unroll
-              for (int i = 0; i < V; ++i) raw[u][i] = *(GSPMD_GLOBAL const small_four<T>*)(w + (i < valid ? p.at + i : 0) * a.ldw + m_of(group));       // (times a D of 0)
-            } else {
-#pragma unroll
-              for (int n = 0; n < 4; ++n) fb[u][n] = small_keep<T>(small_along<T>(w + min(group * 64 + n * 16 + n16, M - 1) * a.ldw, valid > 0 ? p.at : 0, r.per), valid);
-            }
-          }
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            if (k0 + u * kStep >= end) break;
-            float d[V];
-#pragma unroll
-            for (int i = 0; i < V; i += 4) {
-              const float4_t four = *reinterpret_cast<const float4_t*>(logits + n16 * ld + k0 + u * kStep + quad * V + i);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) d[i + e] = four[e];
-            }
-            few_raw<T> hi, lo;
-            small_operand<T>(d, hi, lo);
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-              few_raw<T> b;
-              if constexpr (ORDER == 0) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) b[i] = raw[u][i][n];
-              } else {
-                b = fb[u][n];
-              }
-              small_multiply<T>(acc[n], hi, b);
-              if constexpr (sizeof(T) == 2) small_multiply<T>(acc[n], lo, b);
-            }
-          }
-        }
-        float* const out = part + (wave * kSmallTokens + quad * 4) * kPartLd + 4;       // (a lane's four may be moved back to before the group)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (ORDER == 0) {
-            *reinterpret_cast<any_float4*>(out + i * kPartLd + m_of(group) - group * 64) = float4_t{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
-          } else {
-#pragma unroll
-            for (int n = 0; n < 4; ++n) out[i * kPartLd + n * 16 + n16] = acc[n][i];
-          }
-        }
-      }
-      __syncthreads();
-      for (int n = t0; n < at_once * kSmallTokens * 64; n += kSmallThreads) {
-        const int which = n >> 10, tl = (n >> 6) & 15, m = (from + which) * 64 + (n & 63), g = first + tl;
-        if (from + which >= mine_end || m >= M || g >= a.token_shards * r.per_shard) continue;
-        float sum = 0.f;
-        for (int p = 0; p < shares; ++p) sum += part[((p * at_once + which) * kSmallTokens + tl) * kPartLd + 4 + (n & 63)];
-        const int i = g / r.per_shard;
-        ((GSPMD_GLOBAL T*)a.dx[i])[static_cast<int64_t>(g - i * r.per_shard) * a.lddx + m] = small_round<T>(g < r.tokens ? sum : 0.f);
-      }
-      __syncthreads();
-    }
-  }
+  const int across = (M + 63) >> 6, mine_first = across * slice / slices, mine_end = a.dx[0] != nullptr ? across * (slice + 1) / slices : mine_first;       // groups of 64 of M
 
-  // ---- dw, of 16 tokens in all: one instruction's sum (bfloat16: D in two parts, each times x)
-  if (a.dw[0] == nullptr) return;
+  // ---- dw, of 16 tokens in all: one instruction's sum (bfloat16: D in two parts, each times x).  Made by waves that have nothing of dx's sums, or before these are joined.
   constexpr int kTokensOf = sizeof(T) == 2 ? 1 : 3;       // a lane's V terms are tokens (quad & this) * V and following
   const int t_of = (quad & kTokensOf) * V;
   const bool second = sizeof(T) == 2 && quad >= 2;        // the part that D's rounding lost
   const int stored_cols = a.shards * r.per_cols;          // shards without an entry get zeros
   // rows of the result: entries ([V, M]) or M; columns in fours
   const int tiles = ORDER == 0 ? (stored_cols + 15) / 16 : (M + 15) / 16, fours = ORDER == 0 ? across : (stored_cols + 63) / 64;
-  const int units = slices * kWaves, unit = slice * kWaves + wave;
-  // a unit: one group of 64 columns and every `step`-th tile of rows
-  const int step = max(1, units / fours);
+  // A unit: one group of 64 columns and every `step`-th tile of rows, from the waves on that have none of dx's sums first.
+  auto make_dw = [&](int busy) {
+    const int units = slices * kWaves, unit = slice * kWaves + ((wave - busy) & (kWaves - 1));
+    const int step = max(1, units / fours);
 #pragma unroll 1
-  for (int n = unit; n < fours * step; n += units) {
-    const int four = n % fours, phase = n / fours;
-    const int col = four * 64 + 4 * n16, m0 = m_of(four);
-    const Place here = place(col);              // [M, V]: four columns of one shard, moved back as in four_of
-    const int back = max(here.at - (r.per - 4), 0), entries = here.valid + back, col0 = col - back;
-    few_raw<T> fb[4];
-    if constexpr (ORDER == 0) {
-      small_four<T> raw[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        raw[i] = *(GSPMD_GLOBAL const small_four<T>*)(x_row(t_of + i) + m0);
-        if (t_of + i >= r.tokens) raw[i] = 0;
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int i = 0; i < V; ++i) fb[e][i] = raw[i][e];
-    } else {
-      float d[4][V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float4_t v = {0.f, 0.f, 0.f, 0.f};
-        if (entries > 0) v = *reinterpret_cast<const any_float4*>(logits + (t_of + i) * ld + col0);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) d[e][i] = v[e];
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        few_raw<T> hi, lo;
-        small_operand<T>(d[e], hi, lo);
-        fb[e] = second ? lo : hi;
-      }
-    }
-#pragma unroll 1
-    for (int tile = phase; tile < tiles; tile += step) {
-      few_raw<T> fa;
+    for (int n = unit; n < fours * step; n += units) {
+      const int four = n % fours, phase = n / fours;
+      const int col = four * 64 + 4 * n16, m0 = m_of(four);
+      const Place here = place(col);              // [M, V]: four columns of one shard, moved back as in four_of
+      const int back = max(here.at - (r.per - 4), 0), entries = here.valid + back, col0 = col - back;
+      few_raw<T> fb[4];
       if constexpr (ORDER == 0) {
-        const int entry = min(tile * 16 + n16, groups * 64 - 1);
-        float d[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) d[i] = logits[(t_of + i) * ld + entry];
-        few_raw<T> hi, lo;
-        small_operand<T>(d, hi, lo);
-        fa = second ? lo : hi;
-      } else {
-        const int m = min(tile * 16 + n16, M - 1);
+        small_four<T> raw[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          fa[i] = x_row(t_of + i)[m];
-          if (t_of + i >= r.tokens) fa[i] = 0;
+          raw[i] = *(GSPMD_GLOBAL const small_four<T>*)(x_row(t_of + i) + m0);
+          if (t_of + i >= r.tokens) raw[i] = 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int i = 0; i < V; ++i) fb[e][i] = raw[i][e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float d[V];
+#pragma unroll
+          for (int i = 0; i < V; ++i) d[i] = entries > 0 ? logits[(t_of + i) * ld + col0 + e] : 0.f;
+          few_raw<T> hi, lo;
+          small_operand<T>(d, hi, lo);
+          fb[e] = second ? lo : hi;
         }
       }
-      float4_t acc[4] = {};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) small_multiply<T>(acc[e], fa, fb[e]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = tile * 16 + quad * 4 + i;
-        small_four<T> out;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) out[e] = small_round<T>(acc[e][i]);
+#pragma unroll 1
+      for (int tile = phase; tile < tiles; tile += step) {
+        few_raw<T> fa;
         if constexpr (ORDER == 0) {
-          const Place p = place(row);
-          if (p.valid <= 0) out = 0;
-          if (row < stored_cols && p.stored > 0) *(GSPMD_GLOBAL small_four<T>*)((GSPMD_GLOBAL T*)a.dw[p.j] + p.at * a.lddw + m0) = out;
-        } else {
+          const int entry = min(tile * 16 + n16, groups * 64 - 1);
+          float d[V];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (e >= entries) out[e] = 0;
-          if (row < M && col < stored_cols) *(GSPMD_GLOBAL small_four<T>*)((GSPMD_GLOBAL T*)a.dw[here.j] + row * a.lddw + here.at - back) = out;
+          for (int i = 0; i < V; ++i) d[i] = logits[(t_of + i) * ld + entry];
+          few_raw<T> hi, lo;
+          small_operand<T>(d, hi, lo);
+          fa = second ? lo : hi;
+        } else {
+          const int m = min(tile * 16 + n16, M - 1);
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            fa[i] = x_row(t_of + i)[m];
+            if (t_of + i >= r.tokens) fa[i] = 0;
+          }
+        }
+        float4_t acc[4] = {};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) small_multiply<T>(acc[e], fa, fb[e]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = tile * 16 + quad * 4 + i;
+          small_four<T> out;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) out[e] = small_round<T>(acc[e][i]);
+          if constexpr (ORDER == 0) {
+            const Place p = place(row);
+            if (p.valid <= 0) out = 0;
+            if (row < stored_cols && p.stored > 0) *(GSPMD_GLOBAL small_four<T>*)((GSPMD_GLOBAL T*)a.dw[p.j] + p.at * a.lddw + m0) = out;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (e >= entries) out[e] = 0;
+            if (row < M && col < stored_cols) *(GSPMD_GLOBAL small_four<T>*)((GSPMD_GLOBAL T*)a.dw[here.j] + row * a.lddw + here.at - back) = out;
+          }
         }
       }
     }
+  };
+
+  // ---- dx: sums over the columns, whose D is in LDS.  A round of the waves takes `at_once` groups of 64 of M, several waves sharing one's sum; their parts meet in LDS.
+  int shares = 1;
+  while (shares * 2 * max(mine_end - mine_first, 1) <= kWaves && shares * 2 * kStep <= groups * 64) shares *= 2;
+  const int at_once = kWaves / shares, each = (groups * 64 / shares + kStep - 1) / kStep * kStep;
+  bool dw_left = DW;
+  for (int from = mine_first; from < mine_end || dw_left; from += at_once) {
+    const int share = wave / at_once, group = from + wave - share * at_once, begin = share * each, end = min(begin + each, groups * 64);
+    float4_t acc[4] = {};
+    if (group < mine_end) {
+      constexpr int U = DW && sizeof(T) == 2 && ORDER == 1 ? 1 : 2;       // (with 2 there, three registers spill)
+      const int its = (end - begin + U * kStep - 1) / (U * kStep);
+#pragma unroll 1
+      for (int it = 0; it < its; ++it) {
+        const int k0 = turned(it, its, begin, U * kStep);
+        few_raw<T> fb[U][4];
+        small_four<T> raw[U][V];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int k = k0 + u * kStep + quad * V;
+          const Place p = place(k);           // (V columns of one shard)
+          const int valid = k0 + u * kStep < end ? p.valid : 0;
+          GSPMD_GLOBAL const T* const w = (GSPMD_GLOBAL const T*)a.w[valid > 0 ? p.j : 0];
+          if constexpr (ORDER == 0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) raw[u][i] = *(GSPMD_GLOBAL const small_four<T>*)(w + (i < valid ? p.at + i : 0) * a.ldw + m_of(group));       // (times a D of 0)
+          } else {
+#pragma unroll
+            for (int n = 0; n < 4; ++n) fb[u][n] = small_keep<T>(small_along<T>(w + min(group * 64 + n * 16 + n16, M - 1) * a.ldw, valid > 0 ? p.at : 0, r.per), valid);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (k0 + u * kStep >= end) break;
+          float d[V];
+#pragma unroll
+          for (int i = 0; i < V; i += 4) {
+            const float4_t four = *reinterpret_cast<const float4_t*>(logits + n16 * ld + k0 + u * kStep + quad * V + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[i + e] = four[e];
+          }
+          few_raw<T> hi, lo;
+          small_operand<T>(d, hi, lo);
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            few_raw<T> b;
+            if constexpr (ORDER == 0) {
+#pragma unroll
+              for (int i = 0; i < V; ++i) b[i] = raw[u][i][n];
+            } else {
+              b = fb[u][n];
+            }
+            small_multiply<T>(acc[n], hi, b);
+            if constexpr (sizeof(T) == 2) small_multiply<T>(acc[n], lo, b);
+          }
+        }
+      }
+      float* const out = part + (wave * kSmallTokens + quad * 4) * kPartLd + 4;       // (a lane's four may be moved back to before the group)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (ORDER == 0) {
+          *reinterpret_cast<any_float4*>(out + i * kPartLd + m_of(group) - group * 64) = float4_t{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
+        } else {
+#pragma unroll
+          for (int n = 0; n < 4; ++n) out[i * kPartLd + n * 16 + n16] = acc[n][i];
+        }
+      }
+    }
+    if constexpr (DW) {
+      if (dw_left) make_dw(min(mine_end - from, at_once) * shares & (kWaves - 1));
+      dw_left = false;
+      if (from >= mine_end) break;              // (dw alone)
+    }
+    __syncthreads();
+    for (int n = t0; n < at_once * kSmallTokens * 64; n += kSmallThreads) {
+      const int which = n >> 10, tl = (n >> 6) & 15, m = (from + which) * 64 + (n & 63), g = first + tl;
+      if (from + which >= mine_end || m >= M || g >= a.token_shards * r.per_shard) continue;
+      float sum = 0.f;
+#pragma unroll 4
+      for (int p = 0; p < shares; ++p) sum += part[((p * at_once + which) * kSmallTokens + tl) * kPartLd + 4 + (n & 63)];
+      const int i = g / r.per_shard;
+      ((GSPMD_GLOBAL T*)a.dx[i])[static_cast<int64_t>(g - i * r.per_shard) * a.lddx + m] = small_round<T>(g < r.tokens ? sum : 0.f);
+    }
+    __syncthreads();
   }
 }
 

@@ -381,8 +381,12 @@ int32_t run_few(const Loss& l, FewTokens& a, const SoftmaxRows& rows, AddUp& sum
 template <typename T>
 int32_t launch_small(const SmallLoss& a, const Loss& l, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>((l.na * l.ts + kSmallTokens - 1) / kSmallTokens), static_cast<unsigned>(l.small_slices()));
-  if (l.vocab_dim == 0) hipLaunchKernelGGL((small_loss_kernel<T, 0>), grid, dim3(kSmallThreads), 0, stream, a);
-  else hipLaunchKernelGGL((small_loss_kernel<T, 1>), grid, dim3(kSmallThreads), 0, stream, a);
+  auto go = [&](auto dw) {
+    constexpr bool kDw = decltype(dw)::value;
+    if (l.vocab_dim == 0) hipLaunchKernelGGL((small_loss_kernel<T, 0, kDw>), grid, dim3(kSmallThreads), 0, stream, a);
+    else hipLaunchKernelGGL((small_loss_kernel<T, 1, kDw>), grid, dim3(kSmallThreads), 0, stream, a);
+  };
+  if (a.dw[0] != nullptr) go(std::true_type{}); else go(std::false_type{});
   return launched();
 }
 
