@@ -413,6 +413,14 @@ int32_t mark_moved_back(std::vector<Problem>& ps) {
 // 127, the worst of eleven; below it is 6 to 18 %).
 constexpr int64_t kPastBytes = 96000000, kPastTiles = 512, kPastInBytes = 64000000;
 
+// dot_pair_kernel's bf16 outputs go past all caches, but for rows that are not whole lines of 128 bytes apart, whose parts the caches put together, where K is short enough for the operands to leave
+// them room (gradients of a vocabulary matrix, us past / plain, the product alone up to 110 / 51: K 26, 5217 x 20956 266 / 207; 56, 872 x 90598 213 / 176; 82, 3460 x 80128 671 / 609; 114, 2965 x 47505
+// 377 / 342; 148, 1189 x 39927 171 / 158; 250, 7106 x 59172 776 / 804; rows of whole lines: 32, 4096 x 32000 167 / 196; 82, 3456 x 80128 462 / 533).
+bool pair_stores_past(const std::vector<Problem>& ps) {
+  constexpr int32_t kPairPlainK = 192;
+  return std::any_of(ps.begin(), ps.end(), [](const Problem& p) { return p.Kv > kPairPlainK || (p.ldc % 64 == 0 && reinterpret_cast<uintptr_t>(p.C) % 128 == 0); });
+}
+
 int32_t launch_problems(std::vector<Problem>& all, int32_t layout, int32_t in_dtype, int32_t out_dtype, int32_t epilogue,
                         bool ordered, void* workspace, int64_t workspace_bytes, hipStream_t stream, const JoinSpace* join = nullptr) {
   // problems with an empty static output block write nothing
@@ -511,7 +519,8 @@ int32_t launch_problems(std::vector<Problem>& all, int32_t layout, int32_t in_dt
       l.past = out_bytes > kPastBytes || tiles > kPastTiles || launch_size(ps, layout).in_bytes > kPastInBytes;
       if (!launch_dot_mid(l, layout, out_dtype, join != nullptr, choice.staged, stream)) return GSPMD_ERR_DEVICE;
     } else if (pair) {
-      const MfmaLaunch l{&inl, tab, n, static_cast<int>(tiles), epilogue, nullptr, nullptr, nullptr, 0};
+      MfmaLaunch l{&inl, tab, n, static_cast<int>(tiles), epilogue, nullptr, nullptr, nullptr, 0};
+      l.past = pair_stores_past(ps);
       if (!launch_dot_pair(l, layout, out_dtype, stream)) return GSPMD_ERR_DEVICE;
     } else if (mfma) {
       if (join && join->tiles > 0) {

@@ -37,7 +37,8 @@ constexpr int kPairThreads = 256, kPairStages = 3;
 constexpr int kPairPartA = kPairRows * kMfmaBK * 2, kPairPartB = kPairCols * kMfmaBK * 2, kPairStage = kPairPartA + kPairPartB;
 constexpr int kPairLds = kPairStages * kPairStage;
 
-template <typename TOut, int LAYOUT>
+// PAST: bf16 outputs past all caches (pair_stores_past in gspmd.hip)
+template <typename TOut, int LAYOUT, bool PAST>
 __global__ __launch_bounds__(kPairThreads, 2) void dot_pair_kernel(const InlineProblems inl, const Problem* __restrict__ tab, int n_prob, int epilogue) {
   constexpr bool AKM = (LAYOUT & GSPMD_LAYOUT_LHS_K_MAJOR) != 0, BKC = (LAYOUT & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) != 0;
   constexpr int R = kPairStages, kLoads = 6;     // a wave's load instructions of a tile: four of the lhs's part, two of the rhs's
@@ -196,7 +197,7 @@ __global__ __launch_bounds__(kPairThreads, 2) void dot_pair_kernel(const InlineP
   constexpr int kAtOnce = sizeof(TOut) == 2 ? 8 : 4;
   static_assert(4 * line_slice<TOut>(kAtOnce) <= kPairLds, "");
   __syncthreads();                              // every wave's fragment reads are over
-  store_lines<TOut, 8, kAtOnce, sizeof(TOut) == 2 ? kLinesPast : kLinesPlain>(smem + wave * line_slice<TOut>(kAtOnce), C, P, m0 + wm, n0 + wn, m0 + kPairRows <= P.Mv && n0 + kPairCols <= P.Nv, epilogue, lane,
+  store_lines<TOut, 8, kAtOnce, PAST ? kLinesPast : kLinesPlain>(smem + wave * line_slice<TOut>(kAtOnce), C, P, m0 + wm, n0 + wn, m0 + kPairRows <= P.Mv && n0 + kPairCols <= P.Nv, epilogue, lane,
                                 [&](int i, int j) { return acc[i][j]; });
   // zeros of the static block below the last row tile, over this tile's columns (what lies further down, and whole tile
   // columns of padding, the fill kernel clears), and right of a tile that was moved back
@@ -208,23 +209,24 @@ __global__ __launch_bounds__(kPairThreads, 2) void dot_pair_kernel(const InlineP
   }
 }
 
-template <int LAYOUT, typename TOut>
+template <int LAYOUT, typename TOut, bool PAST>
 inline bool launch_dot_pair_as(const MfmaLaunch& l, hipStream_t stream) {
   static std::once_flag once[kMaxDevices];
   static bool ok[kMaxDevices];
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return false;
   std::call_once(once[dev], [dev] {
-    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_pair_kernel<TOut, LAYOUT>), hipFuncAttributeMaxDynamicSharedMemorySize, kPairLds) == hipSuccess;
+    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_pair_kernel<TOut, LAYOUT, PAST>), hipFuncAttributeMaxDynamicSharedMemorySize, kPairLds) == hipSuccess;
   });
   if (!ok[dev]) return false;
-  hipLaunchKernelGGL((dot_pair_kernel<TOut, LAYOUT>), dim3(static_cast<unsigned>(l.tiles)), dim3(kPairThreads), kPairLds, stream, *l.inl, l.tab, l.n_prob, l.epilogue);
+  hipLaunchKernelGGL((dot_pair_kernel<TOut, LAYOUT, PAST>), dim3(static_cast<unsigned>(l.tiles)), dim3(kPairThreads), kPairLds, stream, *l.inl, l.tab, l.n_prob, l.epilogue);
   return hipGetLastError() == hipSuccess;
 }
 
 template <int LAYOUT>
 bool launch_dot_pair_layout(const MfmaLaunch& l, int32_t out_dtype, hipStream_t stream) {
-  return out_dtype == GSPMD_F32 ? launch_dot_pair_as<LAYOUT, float>(l, stream) : launch_dot_pair_as<LAYOUT, bf16_bits>(l, stream);
+  if (out_dtype == GSPMD_F32) return launch_dot_pair_as<LAYOUT, float, false>(l, stream);
+  return l.past ? launch_dot_pair_as<LAYOUT, bf16_bits, true>(l, stream) : launch_dot_pair_as<LAYOUT, bf16_bits, false>(l, stream);
 }
 
 }  // namespace gspmd
