@@ -126,9 +126,9 @@ struct Loss {
   // 8 tokens 50 / 53, 131 / 123 (2048 x 16000).  bfloat16, [V, M], 1 token 128 x 2304 27 / 34, 1024 x 16000 34 / 42, 2048 x 16000 55 / 57, 2048 x 32000 106 / 101; 3 tokens 24 / 32, 39 / 41,
   // 63 / 58, 115 / 102; 8 tokens 640 x 10368 43 / 35; losses alone, 1 token 640 x 10368 14 / 15.5, 1024 x 16000 15 / 17, 4 tokens
   // 16 / 16.5; [M, V], 3 tokens 640 x 10368 36 / 35, 2048 x 16000 84 / 59.
-  // bfloat16 beyond 32 MB of w: only where its rows are not whole lines, which the others read and write slowly (6390 x 116189 in 8 shards, rows of 6392: 1 token 1026 / 1357, 4 tokens 1058 / 1388;
-  // 904 x 50000, 4 tokens 84 / 97; losses alone, 3001 x 20001, 1 token 35 / 58, 4 tokens 44 / 60; whole lines: 3904 x 123392, 1 token 600 / 540, 4 tokens 612 / 548; losses alone, 1 token
-  // 2048 x 32000 38.7 / 36.5, 4096 x 32000 67 / 64), and losses of one or two tokens over many short rows (1024 x 50000 31 / 35, 1536 x 80000 55 / 69, 2048 x 128000 110 / 144, 512 x 128000 41 / 41).
+  // bfloat16 beyond 32 MB of w: only where its rows are not whole lines, which the others read slowly (3001 x 20001 in 4 shards, 1 token 98 / 137, 4 tokens 111 / 140; 904 x 50000, 2 tokens 85 / 99,
+  // 4 tokens 90 / 100; 1900 x 20000 76 / 90; 6390 x 116189 in 8 shards, rows of 6392, 1026 / 1018; losses alone, 3001 x 20001, 1 token 35 / 58, 4 tokens 44 / 60;
+  // whole lines: 3904 x 123392, 1 token 600 / 540, 4 tokens 612 / 548; losses alone, 1 token 2048 x 32000 38.7 / 36.5, 4096 x 32000 67 / 64), and losses of one or two tokens over many short rows (1024 x 50000 31 / 35, 1536 x 80000 55 / 69, 2048 x 128000 110 / 144, 512 x 128000 41 / 41).
   bool few() const {
     const int64_t most = dtype == GSPMD_F32 ? (vocab_dim == 0 || V * M * 4 <= kFewWeights ? 8 : 4) : vocab_dim == 0 ? 4 : 0;
     return T > 0 && T <= most && M > 0 && nb <= kFewWindows && na <= kInlineTokenShards;
