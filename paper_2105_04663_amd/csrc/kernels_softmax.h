@@ -411,7 +411,7 @@ struct PackRows {
   int32_t first_shard;           // the table's first
   int32_t by_columns;            // column shards (one row shard) instead
   int32_t per_cols, per, cols;   // column shards: columns apart in the result; shards of either kind: rows or columns of one; columns that exist in all
-  int32_t copies;                // the rows again, `rows` further on
+  int32_t copies, apart;         // the rows again, `apart` rows further on (of all of a piece's rows: a launch may have a table's only)
 };
 // One or two of them in a launch, whose workgroups are the first's across x down, then the second's.
 struct PackTwo {
@@ -454,7 +454,7 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const PackTwo args) {
         if (e < n) v[e] = from[e];
     }
     GSPMD_GLOBAL T* const to = (GSPMD_GLOBAL T*)a.to + static_cast<int64_t>(row) * a.ld + col;
-    for (int k = 0; k < a.copies; ++k) *(GSPMD_GLOBAL vec*)(to + static_cast<int64_t>(k) * a.rows * a.ld) = v;
+    for (int k = 0; k < a.copies; ++k) *(GSPMD_GLOBAL vec*)(to + static_cast<int64_t>(k) * a.apart * a.ld) = v;
   }
 }
 

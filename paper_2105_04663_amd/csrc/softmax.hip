@@ -739,6 +739,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
         a.first_shard = static_cast<int32_t>(i0);
         a.cols = static_cast<int32_t>(l.M);
         a.copies = lost && l.dw ? 2 : 1;
+        a.apart = static_cast<int32_t>(n);
         return packs.add(a);
       });
     if (st != GSPMD_OK || (st = packs.flush()) != GSPMD_OK) return st;
