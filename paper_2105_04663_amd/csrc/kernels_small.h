@@ -94,7 +94,7 @@ __device__ __forceinline__ T small_round(float v) {
   else return v;
 }
 
-// ORDER: vocab_dim (0: w [V, M], 1: [M, V]).  DW: dw is made here, of 16 tokens in all.
+// ORDER: vocab_dim (0: w [V, M], 1: [M, V]).  DW: dw is made here, of 16 tokens in all, by the workgroups of the first 16 rows.
 template <typename T, int ORDER, bool DW>
 __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(const SmallLoss args) {
   constexpr int V = small_vec<T>(), kStep = 4 * V, kWaves = kSmallWaves;        // terms of a sum that an instruction (four, in float32) takes
@@ -420,7 +420,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(const SmallLo
   int shares = 1;
   while (shares * 2 * max(mine_end - mine_first, 1) <= kWaves && shares * 2 * kStep <= groups * 64) shares *= 2;
   const int at_once = kWaves / shares, each = (groups * 64 / shares + kStep - 1) / kStep * kStep;
-  bool dw_left = DW;
+  bool dw_left = DW && blockIdx.x == 0;         // (others have padding rows of the shards only: 16 tokens in 3 shards are 18 rows)
   for (int from = mine_first; from < mine_end || dw_left; from += at_once) {
     const int share = wave / at_once, group = from + wave - share * at_once, begin = share * each, end = min(begin + each, groups * 64);
     float4_t acc[4] = {};
