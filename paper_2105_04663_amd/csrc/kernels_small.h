@@ -18,6 +18,7 @@
 #include "kernels_few.h"
 #include "kernels_softmax.h"
 #include "mfma_common.h"
+#include "tile_index.h"
 
 namespace gspmd {
 
@@ -127,12 +128,13 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(const SmallLo
     return begin + (from >= its ? from - its : from) * step;
   };
   // Four neighbouring columns of one shard from `col` on, moved back to end with the shard's static part (what lies there beyond its entries may be anything).
-  struct Four { int j, at, col; bool there; };
+  struct Four { int j, at, col, others; bool there; };
   auto four_of = [&](int col) {
     const Place p = place(col);
     const bool there = p.j < a.shards && p.valid > 0;
-    const int at = min(p.at, r.per - 4), j = there ? p.j : 0;
-    return Four{j, there ? at : 0, j * r.per_cols + at, there};
+    const FourColumns four = four_columns(p.at, r.per);
+    const int j = there ? p.j : 0;
+    return Four{j, there ? four.at : 0, j * r.per_cols + four.at, four.others, there};
   };
   typedef float any_float4 __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -226,7 +228,15 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(const SmallLo
 #pragma unroll
           for (int c = 0; c < 4; ++c) out[i * ld + c * 16 + n16] = acc[c][i];
         } else {
-          if (four.there) *reinterpret_cast<any_float4*>(logits + (split * kSmallTokens + quad * 4 + i) * ld + four.col) = float4_t{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
+          // (without those of another lane, whose wave may have begun the sum elsewhere and round otherwise: with two writers the bits would be those of the later one)
+          float* const to = logits + (split * kSmallTokens + quad * 4 + i) * ld + four.col;
+          if (four.there && four.others == 0) {
+            *reinterpret_cast<any_float4*>(to) = float4_t{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
+          } else if (four.there) {
+#pragma unroll
+            for (int e = 1; e < 4; ++e)
+              if (e >= four.others) to[e] = acc[e][i];
+          }
         }
       }
     }

@@ -211,4 +211,14 @@ GSPMD_INDEX_FN int f32_km_column(int x, int cols_valid) { return x >= (cols_vali
 // row 4 group of a column; row 4 group + i at + i * 256, the second 16 k at + 4096
 GSPMD_INDEX_FN uint32_t f32_km_place(int col, int group) { return static_cast<uint32_t>(group * 4 * 256 + (((col >> 2) ^ (group << 2)) << 4) + (col & 3) * 4); }
 
+// ---- small_loss_kernel: a lane's four neighbouring columns of a shard of `per` (at least 4), from its own place `at` (a multiple of 4 below `per`) on, moved back to end with the shard.  The
+// first `others` of them are then also the lane's before it, in another wave where that one's group of 64 columns ends: made by both, to be kept from that lane alone.
+struct FourColumns {
+  int at, others;
+};
+GSPMD_INDEX_FN FourColumns four_columns(int at, int per) {
+  const int moved = at < per - 4 ? at : per - 4;
+  return FourColumns{moved, at - moved};
+}
+
 }  // namespace gspmd
