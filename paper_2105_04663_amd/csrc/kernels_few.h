@@ -209,6 +209,10 @@ __global__ __launch_bounds__(256) void few_gradients_kernel(const FewTokens args
           out[e] = fmaf(d, few_float<T>(xv[t], e), out[e]);
         }
       }
+      if constexpr (!kFull)
+        if (v >= valid)                           // padding: zeros, whatever x is
+#pragma unroll
+          for (int e = 0; e < V; ++e) out[e] = 0.f;
       if (has_dw) few_store<T, kWhole>(dw + static_cast<int64_t>(v) * a.lddw, out, room);
     }
   };
@@ -391,6 +395,10 @@ __global__ __launch_bounds__(256) void few_gradients_across_kernel(const FewToke
         }
         sum[r * NT + t] = s;
       }
+      if constexpr (!kWhole)
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (e >= room) out[e] = 0.f;            // padding: zeros, whatever x is
       if (has_dw && (kFull || r0 + r < rows) && (kWhole || store_room > 0)) few_store<T, kWhole>(dw + static_cast<int64_t>(chunk + r0 + r) * a.lddw, out, store_room);
     }
     if (!has_dx) return;
