@@ -355,7 +355,7 @@ int32_t gspmd_resharded_dot(const gspmd_mesh* mesh, const gspmd_dot_dims* dims,
  * lengths may hold anything).  Logits that are NaN or +infinity give NaN; -infinity throughout lse -infinity, and NaN for the loss and D. */
 #define GSPMD_MAX_TARGETS 1024
 
-/* One partition's arrays per token (device memory, dense, of the static token count of x's shard; padding may hold anything in the inputs and is written as 0 in
+/* One partition's arrays per token (device memory, dense, at their elements' alignment or GSPMD_ERR_BAD_BUFFER, of the static token count of x's shard; padding may hold anything in the inputs and is written as 0 in
  * loss and lse).  Partitions of the same tokens may pass the same pointers (loss and lse are then written once). */
 typedef struct {
   const int32_t* ids;     /* [tokens, targets]: vocabulary entries (0 .. V - 1); any other value: no target there */

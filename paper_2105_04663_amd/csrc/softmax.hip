@@ -301,6 +301,12 @@ int32_t check_shard(const gspmd_shard_buf& b, int32_t dtype, int64_t rows, int64
   return GSPMD_OK;
 }
 
+// Every array of a token at its elements' alignment: weights and losses are reached by scalar instructions too, which take an address's last two bits for zeros.
+bool aligned(const gspmd_token_buf& tb, bool teacher) {
+  const uintptr_t words = reinterpret_cast<uintptr_t>(tb.ids) | reinterpret_cast<uintptr_t>(tb.weights) | reinterpret_cast<uintptr_t>(tb.loss) | reinterpret_cast<uintptr_t>(tb.lse);
+  return !(words & 3) && !(teacher && (reinterpret_cast<uintptr_t>(tb.logits) & (tb.logits_dtype == GSPMD_BF16 ? 1 : 3)));
+}
+
 Problem product(const void* a, int64_t lda, const void* b, int64_t ldb, void* c, int64_t ldc, int64_t m, int64_t n, int64_t k, int64_t m_static, int64_t n_static) {
   Problem p;
   std::memset(&p, 0, sizeof(p));
@@ -427,6 +433,7 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
     if (l.ts > 0 && (!tb.ids || !tb.loss || (teacher && !tb.logits))) return GSPMD_ERR_NULL;
     if (teacher && tb.logits_dtype != GSPMD_F32 && tb.logits_dtype != GSPMD_BF16) return GSPMD_ERR_UNSUPPORTED;
     if (teacher && tb.logits_dtype != tokens[0].logits_dtype) return GSPMD_ERR_UNSUPPORTED;
+    if (l.ts > 0 && !aligned(tb, teacher)) return GSPMD_ERR_BAD_BUFFER;
     const bool ts = seen_t[static_cast<size_t>(i)], vs = seen_v[static_cast<size_t>(j)];
     if (!ts) x[static_cast<size_t>(i)].first = x_shards[p];
     if (!vs) w[static_cast<size_t>(j)].first = w_shards[p];
