@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void few_logits_kernel(const FewTokens args) {
   float sum[ROWS * NT];
 #pragma unroll
   for (int i = 0; i < ROWS * NT; ++i) sum[i] = 0.f;
-  // Whole vectors only, where a row has one: the last lane's is moved back to end with the row, and x there is 0 for what its neighbour has.
+  // Whole vectors only, where a row has one: the last lane's is moved back to end with the row, and x and w there are 0 for what its neighbour has (both: either may be infinite, which 0 times it is not).
   struct Held { few_raw<T> w[ROWS]; };
   const bool narrow = a.M < V;
   auto load = [&](int m) {
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256) void few_logits_kernel(const FewTokens args) {
     for (int r = 0; r < ROWS; ++r) held.w[r] = narrow ? few_load<T, false>(row[r], a.M) : few_load<T, true>(row[r] + min(m, a.M - V), V);
     return held;
   };
-  auto take = [&](const Held& held, int m) {
+  auto take = [&](Held held, int m) {
     few_raw<T> xv[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -131,10 +131,13 @@ __global__ __launch_bounds__(256) void few_logits_kernel(const FewTokens args) {
     }
     if (!narrow && m + V > a.M)
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int e = 0; e < V; ++e)
+        if (a.M - V + e < m) {
 #pragma unroll
-        for (int e = 0; e < V; ++e)
-          if (a.M - V + e < m) xv[t][e] = 0;
+          for (int t = 0; t < NT; ++t) xv[t][e] = 0;
+#pragma unroll
+          for (int r = 0; r < ROWS; ++r) held.w[r][e] = 0;
+        }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
