@@ -414,11 +414,15 @@ int32_t mark_moved_back(std::vector<Problem>& ps) {
 constexpr int64_t kPastBytes = 96000000, kPastTiles = 512, kPastInBytes = 64000000;
 
 // dot_pair_kernel's bf16 outputs go past all caches, but for rows that are not whole lines of 128 bytes apart, whose parts the caches put together, where K is short enough for the operands to leave
-// them room (gradients of a vocabulary matrix, us past / plain, the product alone up to 110 / 51: K 26, 5217 x 20956 266 / 207; 56, 872 x 90598 213 / 176; 82, 3460 x 80128 671 / 609; 114, 2965 x 47505
-// 377 / 342; 148, 1189 x 39927 171 / 158; 250, 7106 x 59172 776 / 804; rows of whole lines: 32, 4096 x 32000 167 / 196; 82, 3456 x 80128 462 / 533).
+// them room (us past / plain, the product alone: gradients of a vocabulary matrix, K 26, 5217 x 20956 110 / 51; products of one or two problems, 5208 x 65 x 46431 285 / 159, 4096 x 160 x 32840 130 / 98,
+// two of 4928 x 95 x 25577 287 / 172, 4096 x 160 x 4104 20 / 18, two of them 33 / 34.5 to 36; rows of whole lines: K 32, 4096 x 32000 167 / 196; 82, 3456 x 80128 462 / 533).  Of more problems with operands
+// of their own, for shorter K only: eight of 4096 x K x 4104, K 64 104 / 83, 96 99 / 98, 128 102 / 111, 160 93 to 103 / 122 to 127; four of 4096 x 160 x 8200 93 to 101 / 119 to 122; sixteen of
+// 4416 x 44 x 4499 335 / 202, of 5034 x 154 x 1576 99 / 135 (the worst below the limit, eight of 1989 x 94 x 4248, 55 / 59, with a kernel that reads them 102 / 98).  Not of those that share one, a vocabulary's shards (the losses' call: 4 shards, K 120, 2056 x 40008 255 / 205, 192, 4104 x 32000 263 / 275; 8 shards, K 104,
+// 3000 x 50000 310 / 287, 180, 2056 x 64040 322 / 304).
 bool pair_stores_past(const std::vector<Problem>& ps) {
-  constexpr int32_t kPairPlainK = 192;
-  return std::any_of(ps.begin(), ps.end(), [](const Problem& p) { return p.Kv > kPairPlainK || (p.ldc % 64 == 0 && reinterpret_cast<uintptr_t>(p.C) % 128 == 0); });
+  const bool shared = std::all_of(ps.begin(), ps.end(), [&](const Problem& p) { return p.A == ps[0].A; }) || std::all_of(ps.begin(), ps.end(), [&](const Problem& p) { return p.B == ps[0].B; });
+  const int32_t plain_k = ps.size() <= 2 || shared ? 192 : 96;
+  return std::any_of(ps.begin(), ps.end(), [&](const Problem& p) { return p.Kv > plain_k || (p.ldc % 64 == 0 && reinterpret_cast<uintptr_t>(p.C) % 128 == 0); });
 }
 
 int32_t launch_problems(std::vector<Problem>& all, int32_t layout, int32_t in_dtype, int32_t out_dtype, int32_t epilogue,
