@@ -427,8 +427,8 @@ int32_t run_loss(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const 
     if ((st = check_shard(x_shards[p], l.dtype, l.ts, l.M)) != GSPMD_OK || (st = check_shard(w_shards[p], l.dtype, w_rows, w_cols)) != GSPMD_OK) return st;
     if (l.dx && (st = check_shard(dx_shards[p], l.dtype, l.ts, l.M)) != GSPMD_OK) return st;
     if (l.dw && (st = check_shard(dw_shards[p], l.dtype, w_rows, w_cols)) != GSPMD_OK) return st;
-    if (x_shards[p].row_stride != x_shards[0].row_stride || w_shards[p].row_stride != w_shards[0].row_stride || (l.dx && dx_shards[p].row_stride != dx_shards[0].row_stride) ||
-        (l.dw && dw_shards[p].row_stride != dw_shards[0].row_stride)) return GSPMD_ERR_BAD_BUFFER;
+    auto other_stride = [&](const gspmd_shard_buf* shards, int64_t cols) { return shards && stride_of(shards[p], cols) != stride_of(shards[0], cols); };      // (0 is that of a dense shard)
+    if (other_stride(x_shards, l.M) || other_stride(w_shards, w_cols) || other_stride(dx_shards, l.M) || other_stride(dw_shards, w_cols)) return GSPMD_ERR_BAD_BUFFER;
     const gspmd_token_buf& tb = tokens[p];
     if (l.ts > 0 && (!tb.ids || !tb.loss || (teacher && !tb.logits))) return GSPMD_ERR_NULL;
     if (teacher && tb.logits_dtype != GSPMD_F32 && tb.logits_dtype != GSPMD_BF16) return GSPMD_ERR_UNSUPPORTED;
