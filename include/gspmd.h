@@ -386,7 +386,7 @@ int32_t gspmd_softmax_xent(const gspmd_mesh* mesh,
                            void* workspace, int64_t workspace_bytes, void* hip_stream);
 
 /* Distillation from a teacher's top logits: `targets` (1 .. GSPMD_MAX_TARGETS) entries per token, ids and logits [tokens, targets]; an entry whose id is outside
- * 0 .. V - 1 is absent.  With tau = temperature (positive, finite) and p = softmax over a token's entries of logits / tau,
+ * 0 .. V - 1 is absent.  With tau = temperature (positive, finite, its reciprocal too) and p = softmax over a token's entries of logits / tau,
  *   loss[t] = sum_k p_k (log p_k - (z[t, id_k] / tau - lse[t])),   0 log 0 = 0:
  * the divergence of the student's distribution from the teacher's over its entries.  An id given twice counts twice.  A token without entries (or with logits of -infinity only) has loss 0
  * and takes no part in the gradients.  (A loss scaled by tau^2 is one with weights scaled by it.)  Other arguments as gspmd_softmax_xent. */

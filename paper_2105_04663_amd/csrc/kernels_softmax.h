@@ -1,12 +1,12 @@
 // The losses over a split vocabulary (softmax.hip): what happens beside the products.
 //
-// A row of logits z holds the vocabulary's shards one after the other, each `per_cols` columns wide (a multiple of 64), of which the first `per` (of the
-// last shard: what is left of the vocabulary) stand for entries.  With u = z / tau, the entries' maximum m and total = sum exp(u - m), and the token's
+// A row of logits z holds the vocabulary's shards one after the other, each `per_cols` columns wide, of which the first `per` (of the last shard: what is left of the vocabulary) stand for entries.
+// per_cols is a multiple of 8, so that no vector of four logits and no 16 bytes of an operand lie in two shards, and of 64 where the products may end in statistics.  With u = z / tau, the entries' maximum m and total = sum exp(u - m), and the token's
 // targets p (one label: p = 1; a teacher's entries: the softmax of their logits / tau):
 //   lse = m + log(total)     loss = sum_k p_k (log p_k - (u_k - lse))     D = weight / tau (exp(u - lse) - p)
 // D replaces the logits in place, in the operands' type: a bfloat16 row then takes the first half of its float32 row's bytes.  Everything up to D is float32, and D is
-// rounded to the operands' type once: it is an operand of the products that make the gradients.  With few tokens what that rounding loses is kept as a second
-// row (LOST) and takes part in the products too, which are bound by the vocabulary matrix then.  exp is v_exp_f32 of the exponent times log2(e), of differences to the maximum.
+// rounded to the operands' type once: it is an operand of the products that make the gradients, whose matrix instructions take that type.  With few tokens what that rounding loses is kept as a second
+// row (LOST) and takes part in the products too, which are bound by the vocabulary matrix then; with many it would be twice the flops of two products of three.  exp is v_exp_f32 of the exponent times log2(e), of differences to the maximum.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -21,7 +21,7 @@ struct SoftmaxFinish {
   float c;                       // log2(e) / tau
 
   // Targets that a thread has in registers: the next ones are on their way while what is found among these is stored (1024 tokens of 100 targets, 1024 x 128000: a load and a barrier after the
-  // other, eight at a time, 393 us; 32 held 328; 56, all of a tile's 25600 at once, 314).
+  // other, eight at a time, 393 us; 32 held 328; 56, all of a tile's 25600 at once, 314; more than 112 targets a token take a second round).
   static constexpr int kHeld = 56, kAtOnce = kHeld * 512;
 
   __device__ __forceinline__ void operator()(float16_t (&acc)[8], const Problem& P, TileRows own, int n0, unsigned char* smem) const {

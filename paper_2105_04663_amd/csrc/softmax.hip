@@ -27,11 +27,11 @@ namespace {
 // Logits of a piece, at most (float32; at least one token's): what the workspace query provides for.  Large, so that the products keep whole rounds of tiles and dw is summed once: pieces small enough
 // for the 256 MB cache saved no time (the logits' tiles are stored past it).
 constexpr int64_t kPieceBytes = int64_t(1) << 31;
-constexpr int64_t kColumnAlign = 64;
+constexpr int64_t kColumnAlign = 64;           // and 8 in narrow shards (Loss::per_cols): the kernels take four logits, or 16 bytes of an operand, of one shard at a time
 // Up to so many tokens what D's rounding to bfloat16 loses takes part in the products, as rows of its own: gradients are then off by their own rounding alone (0.0017 of their size, else 0.0024).
 // These products are bound by w and dw: 2048 x 32000, 64 tokens 125 us, without 108; 128 tokens 149, 129.
 constexpr int64_t kFewTokens = 128;
-// Shards of fewer tokens are put together, or each reads the vocabulary matrix for itself (losses of 200 tokens in 4 shards, 2048 x 16000: 30 us, else 40).
+// Shards of fewer tokens (than a row of tiles) are put together, or each reads the vocabulary matrix for itself (losses of 200 tokens in 4 shards, 2048 x 16000: 30 us, else 40).
 constexpr int64_t kFewRows = 256;
 // Elements of a partial of dx that are hardly noticed: ranges of 512 entries, else of 2048 (200 tokens, 1001 x 16001: 73 us, by 2048 78; 1024 tokens, 2048 x 8000: 126, by 512 137).
 constexpr int64_t kSmallSum = int64_t(1) << 20;
@@ -79,7 +79,7 @@ struct Loss {
     if (!dx || rows == 0) return 1;
     const bool few = rows * parts() <= 128, small = dtype == GSPMD_F32 || few;
     const int64_t edge = small ? 64 : 256, tiles = ((rows * parts() + edge - 1) / edge) * ((M + edge - 1) / edge);
-    const int64_t want = dtype == GSPMD_F32 ? 1024 : few ? 512 : 256;         // workgroups
+    const int64_t want = dtype == GSPMD_F32 ? 1024 : few ? 512 : 256;         // workgroups: a round of those kernels' on 256 compute units (not searched: nor is the cap of 16)
     // entries of a range (float32, 100 tokens, 300 x 3000 by 256 37.5 us, by 512 41; 512 tokens, 512 x 3000 73 and 69)
     const int64_t least = dtype == GSPMD_F32 && rows <= 256 ? 256 : small || rows * M <= kSmallSum ? 512 : 2048;
     return std::max<int64_t>(1, std::min({want / std::max<int64_t>(tiles, 1), V / least, int64_t(16)}));
@@ -110,8 +110,8 @@ struct Loss {
   bool packing_pays() const {
     return dtype == GSPMD_BF16 && (T >= 1024 || (T >= (dx || dw ? 342 : 512) && work() >= 4e9));
   }
-  // .. and of a vocabulary in many shards, where dx's partials, one for each, would be more than that copy (bfloat16, 3000 tokens, 1024 x 16000 in 8 shards 329 us, apart 359; 4096 tokens, 2048 x 32000
-  // in 4: 1386, apart 1347), or whose shards are narrow.
+  // .. and of a vocabulary in many shards, where dx's partials, one for each, would be more than that copy (bfloat16, 3000 tokens, 1024 x 16000 in 8 shards, 2 T windows / V = 3, 329 us, apart 359; 4096 tokens,
+  // 2048 x 32000 in 4, 1.0, 1386, apart 1347; nothing was measured between the two, the limit is the upper one), or whose shards are narrow.
   bool joining_pays() const { return windows() > 1 && ((dx && 2 * T * windows() >= 3 * V) || narrow()); }
   int64_t packed_w_bytes() const { return round_up((vocab_dim == 0 ? ldz() * ldx() : std::max<int64_t>(M, 1) * ldz()) * esize(), kWsAlign); }
   // ---- the workspace, for pieces of `rows` tokens
