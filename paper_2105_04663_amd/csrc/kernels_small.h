@@ -152,7 +152,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(const SmallLo
     if (has_token && k < K) {
       const int64_t at = static_cast<int64_t>(token) * K + k;
       const int here = ((GSPMD_GLOBAL const int32_t*)s.ids)[at];
-      q[n] = teachers_logit(s, r.logits_bf16, at) * r.inv_tau;
+      q[n] = teachers_logit(s, r.logits_bf16, at);
       if (here >= 0 && here < r.vocab) id[n] = here;
       else q[n] = -INFINITY;
     }
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(const SmallLo
       column[n] = id[n] >= 0 ? j * r.per_cols + (id[n] - j * r.per) : -1;
       u[n] = column[n] >= 0 ? z[column[n]] * inv_tau : 0.f;
     }
-    const TargetSums of = over_targets(K, [&](int k) { return k < 64 ? q[0] : q[1]; }, [&](int k) { return k < 64 ? u[0] : u[1]; }, [&](int k, float share) { (k < 64 ? p[0] : p[1]) = share; });
+    const TargetSums of = over_targets(K, inv_tau, [&](int k) { return k < 64 ? q[0] : q[1]; }, [&](int k) { return k < 64 ? u[0] : u[1]; }, [&](int k, float share) { (k < 64 ? p[0] : p[1]) = share; });
     if (lane == 0 && slice == 0) {
       s.loss[token] = of.any ? of.sum + u_most + log_total : 0.f;
       if (s.lse) s.lse[token] = u_most + log_total;

@@ -75,14 +75,15 @@ __device__ __forceinline__ float teachers_logit(const GSPMD_KERNARG TokenShard& 
   return is_bf16 ? bf16_to_float(static_cast<const bf16_bits*>(s.logits)[at]) : static_cast<const float*>(s.logits)[at];
 }
 
-// A token's targets, by one wave: shares p_k = softmax of q_k (-infinity: no target), given to `keep`, and sum_k p_k (log p_k - u_k).
+// A token's targets, by one wave: shares p_k = softmax of q_k / tau (-infinity: no target), given to `keep`, and sum_k p_k (log p_k - u_k).  Differences to the largest q are divided by tau, not the q: at
+// a tau below 1 the lowest and largest values of their type would become infinite.
 // A NaN among the teacher's logits stays: the shares, the loss and the gradient of its token are NaN.
 struct TargetSums {
   bool any;
   float sum;
 };
 template <typename Q, typename U, typename Keep>
-__device__ __forceinline__ TargetSums over_targets(int K, Q q_of, U u_of, Keep keep) {
+__device__ __forceinline__ TargetSums over_targets(int K, float inv_tau, Q q_of, U u_of, Keep keep) {
   const int lane = threadIdx.x & 63;
   auto most = [](float x, float y) { return x != x ? x : y != y ? y : fmaxf(x, y); };
   auto plus = [](float x, float y) { return x + y; };
@@ -100,11 +101,11 @@ __device__ __forceinline__ TargetSums over_targets(int K, Q q_of, U u_of, Keep k
   q_most = over_wave(q_most, most);
   if (q_most == -INFINITY) return TargetSums{false, 0.f};
   float total = 0.f, sum = 0.f;
-  for (int k = lane; k < K; k += 64) total += __builtin_amdgcn_exp2f((q_of(k) - q_most) * kLog2e);
+  for (int k = lane; k < K; k += 64) total += __builtin_amdgcn_exp2f((q_of(k) - q_most) * inv_tau * kLog2e);
   total = over_wave(total, plus);
   const float log_total = logf(total);
   for (int k = lane; k < K; k += 64) {
-    const float q = q_of(k) - q_most, p = __builtin_amdgcn_exp2f(q * kLog2e) / total;
+    const float q = (q_of(k) - q_most) * inv_tau, p = __builtin_amdgcn_exp2f(q * kLog2e) / total;
     if (p != 0.f) sum += p * ((q - log_total) - u_of(k));
     keep(k, p);
   }
@@ -118,7 +119,7 @@ __device__ __forceinline__ TargetSums over_targets(int K, Q q_of, U u_of, Keep k
 // T: the operands' type.  A thread holds VECS vectors of 4 logits; LONG: rows of more than THREADS * VECS * 4, taken in several rounds.
 template <typename T, int THREADS, int VECS, bool LONG, bool GRAD, bool LOST>
 __global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 4) void softmax_rows_kernel(const SoftmaxRows args) {
-  extern __shared__ __attribute__((aligned(16))) float targets_lds[];       // u, p (first: the teacher's logit / tau) and id of every target, in fours
+  extern __shared__ __attribute__((aligned(16))) float targets_lds[];       // u, p (first: the teacher's logit) and id of every target, in fours
   __shared__ float shared[16];
   __shared__ bool any_target;
   const GSPMD_KERNARG SoftmaxRows& a = *first_kernel_argument<SoftmaxRows>();
@@ -181,11 +182,11 @@ __global__ __launch_bounds__(THREADS, LONG ? 6 : VECS <= 8 ? 8 : 4) void softmax
       int id = s.ids[at];
       if (id < 0 || id >= a.vocab) id = -1;
       u_of[k] = id >= 0 ? z[column(id)] * inv_tau : 0.f;
-      p_of[k] = id >= 0 ? teachers_logit(s, a.logits_bf16, at) * inv_tau : -INFINITY;
+      p_of[k] = id >= 0 ? teachers_logit(s, a.logits_bf16, at) : -INFINITY;
       id_of[k] = id;
     }
     if (t < K4 - K) id_of[K + t] = -1;
-    const TargetSums of = over_targets(K, [&](int k) { return p_of[k]; }, [&](int k) { return u_of[k]; }, [&](int k, float p) { p_of[k] = p; });
+    const TargetSums of = over_targets(K, inv_tau, [&](int k) { return p_of[k]; }, [&](int k) { return u_of[k]; }, [&](int k, float p) { p_of[k] = p; });
     of_targets = of.sum;
     if (t == 0) any_target = of.any;
   }
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(kMergeThreads) void softmax_merge_kernel(const Soft
     u[n] = 0.f;
     const int column = has_token && k < K ? ((GSPMD_GLOBAL const int32_t*)first_kernel_argument<SoftmaxMerge>()->columns)[at + k] : -1;
     if (column >= 0 && column < first_kernel_argument<SoftmaxMerge>()->end) {
-      q[n] = teachers_logit(s, a.logits_bf16, static_cast<int64_t>(token) * K + k) * inv_tau;
+      q[n] = teachers_logit(s, a.logits_bf16, static_cast<int64_t>(token) * K + k);
       u[n] = ((GSPMD_GLOBAL const float*)first_kernel_argument<SoftmaxMerge>()->logits)[at + k] * inv_tau;
     }
   }
@@ -392,7 +393,7 @@ __global__ __launch_bounds__(kMergeThreads) void softmax_merge_kernel(const Soft
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) mine = join(mine, float2_t{__shfl_xor(mine.x, d), __shfl_xor(mine.y, d)});
   const float u_most = mine.x * inv_tau, log_total = logf(mine.y);
-  const TargetSums of = over_targets(K, [&](int k) { return q[k >> 6]; }, [&](int k) { return u[k >> 6]; }, [](int, float) {});
+  const TargetSums of = over_targets(K, inv_tau, [&](int k) { return q[k >> 6]; }, [&](int k) { return u[k >> 6]; }, [](int, float) {});
   if (lane == 0) {
     s.loss[token] = of.any ? of.sum + u_most + log_total : 0.f;
     if (s.lse) s.lse[token] = u_most + log_total;
