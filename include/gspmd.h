@@ -273,6 +273,24 @@ int32_t gspmd_grouped_dot_noalloc(const gspmd_mesh* mesh, const gspmd_dot_dims* 
                                   const gspmd_shard_buf* out_shards, const gspmd_sharding* out_sh,
                                   const int64_t* lhs_fill, int32_t epilogue, void* hip_stream);
 
+/* gspmd_grouped_dot of experts whose rows only the device counts, packed: matrix products grouped by expert of ragged sizes (the mixture-of-experts einsums of Section 5.4
+ * without a capacity).  In the Dot's terms the rows are a tensor [E, S, M] of E experts with up to S rows each; what a shard buffer holds of it is ONE array
+ * [S, M], expert e's sizes[e] rows ("slots") behind those of expert e - 1.  The matrices are tensors [E, M, H] as everywhere.  Two forms, dims with batch (0) and (0):
+ *   rows     out[e, s, ..] = rows[e, s, :] w[e]: contracting (2) with (1) or, w as [E, H, M], with (2); out is packed like lhs.  The gradient of the rows is this with the other one of the two.
+ *   matrices out[e] = sum over e's slots of lhs[s, :]^T rhs[s, :]: contracting (1) with (1), both operands packed, out [E, M, H] (the gradient of w).
+ * Anything else is GSPMD_ERR_UNSUPPORTED.  sizes: [E] int32, DEVICE memory, read when the kernels run; negative ones count as 0, and slots end at S (at most 2^24), so no values
+ * lead out of the buffers.  Of a packed out the rows behind the last slot are left as they were; an expert without slots has a matrix of zeros.
+ * Only dimension 0 may be split, alike in all three (else GSPMD_ERR_NEEDS_RESHARD): a partition reads and writes its own experts' slots, in their places in the whole array, and no others; of partitions
+ * that share one out buffer that is the whole array.  lhs_shards, rhs_shards, out_shards: P entries by partition id; partitions of the same experts may share
+ * buffers, distinct out buffers are each written.  Matrices of padded experts are written as zeros.  Types, row strides, epilogue and accumulation as gspmd_grouped_dot; out must not overlap the operands.
+ * No workspace; kernels only, so the call may be recorded into a HIP graph, whose replays read the sizes anew.  Equal sizes, values and alignments give equal bits; one row's
+ * may differ with how many the others are (within fp32 accumulation). */
+int32_t gspmd_ragged_dot(const gspmd_mesh* mesh, const gspmd_dot_dims* dims,
+                         const gspmd_shard_buf* lhs_shards, const gspmd_sharding* lhs_sh,
+                         const gspmd_shard_buf* rhs_shards, const gspmd_sharding* rhs_sh,
+                         const gspmd_shard_buf* out_shards, const gspmd_sharding* out_sh,
+                         const int32_t* sizes, int32_t epilogue, void* hip_stream);
+
 /* out[i] = partials[0][i] + partials[1][i] + ... + partials[n_partials-1][i] in fp32, in that
  * order (the arithmetic of the AllReduce/ReduceScatter of Section 4.2 along a contracting
  * mesh dimension).  partials: host array of n_partials (1..16) device pointers to dense fp32

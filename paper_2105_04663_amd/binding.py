@@ -23,6 +23,7 @@ EXPORTED_SYMBOLS = (
     "gspmd_compatible_operand_shardings", "gspmd_resharded_dot_workspace_bytes", "gspmd_resharded_dot",
     "gspmd_grouped_dot_noalloc", "gspmd_set_tile_timeline",
     "gspmd_softmax_workspace_bytes", "gspmd_softmax_xent", "gspmd_softmax_distill",
+    "gspmd_ragged_dot",
 )
 TILE_TIMELINE_WORDS = 8
 MAX_TARGETS = 1024
@@ -116,6 +117,7 @@ def load_library():
     lib.gspmd_softmax_workspace_bytes.argtypes = [pm, ps, ps, C.c_int32, C.c_int32, C.c_int32, pi64, pi64]
     lib.gspmd_softmax_xent.argtypes = [pm, pbs, ps, pbs, ps, C.c_int32, pbs, pbs, pbs, C.c_void_p, C.c_int64, C.c_void_p]
     lib.gspmd_softmax_distill.argtypes = [pm, pbs, ps, pbs, ps, C.c_int32, pbs, C.c_int32, C.c_float, pbs, pbs, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.gspmd_ragged_dot.argtypes = [pm, pd, pbs, ps, pbs, ps, pbs, ps, C.c_void_p, C.c_int32, C.c_void_p]
     lib.gspmd_set_tile_timeline.argtypes = [C.c_void_p, C.c_int64]
     for name in EXPORTED_SYMBOLS[1:]:
         getattr(lib, name).restype = C.c_int32
@@ -516,3 +518,17 @@ def softmax_distill(mesh: Mesh, x_shards: Sequence[ShardBuf], x_sh: Sharding, w_
     xs, ws, dxs, dws = _loss_shards(mesh, x_shards, w_shards, tokens, dx_shards, dw_shards)
     _check(load_library().gspmd_softmax_distill(C.byref(m), xs, C.byref(a), ws, C.byref(b), int(vocab_dim), _token_bufs(tokens), int(targets), float(temperature),
                                                 dxs, dws, C.c_void_p(workspace), int(workspace_bytes), C.c_void_p(stream)), "gspmd_softmax_distill")
+
+
+def _per_partition(mesh: Mesh, *shards):
+    if any(len(s) != mesh.n_partitions for s in shards):
+        raise ValueError("one shard buffer per partition is required")
+
+
+def ragged_dot(mesh: Mesh, dims: DotDims, lhs_shards: Sequence[ShardBuf], lhs_sh: Sharding, rhs_shards: Sequence[ShardBuf], rhs_sh: Sharding,
+               out_shards: Sequence[ShardBuf], out_sh: Sharding, sizes: int, stream: int = 0, epilogue: int = EPILOGUE_NONE) -> None:
+    """Products grouped by expert over packed rows; sizes: address of the experts' int32 row counts in device memory (gspmd_ragged_dot)."""
+    _per_partition(mesh, lhs_shards, rhs_shards, out_shards)
+    m, d, a, b, o = mesh._c(), dims._c(), lhs_sh._c(), rhs_sh._c(), out_sh._c()
+    _check(load_library().gspmd_ragged_dot(C.byref(m), C.byref(d), _bufs(lhs_shards), C.byref(a), _bufs(rhs_shards), C.byref(b), _bufs(out_shards), C.byref(o),
+                                           C.c_void_p(sizes), int(epilogue), C.c_void_p(stream)), "gspmd_ragged_dot")

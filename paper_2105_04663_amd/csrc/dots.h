@@ -14,6 +14,18 @@ constexpr int64_t kWsAlign = 256;          // of every workspace and of the piec
 // All of `ps` (one layout, one pair of types) in one launch; `tables`: device memory of `table_bytes`, kTableBytesPerProblem per problem.
 int32_t run_dots(std::vector<Problem>& ps, int32_t layout, int32_t in_dtype, int32_t out_dtype, void* tables, int64_t table_bytes, hipStream_t stream);
 
+// Which kernel a launch of such problems takes (by the rule on their sizes and alignments, or a test's pin), for launches that are made elsewhere.
+struct DotChoice {
+  int32_t kernel = 0;                      // GSPMD_TESTING_* (testing.h)
+  int row_blocks = 0, col_blocks = 0;      // dot_split_kernel
+  bool staged = false;                     // dot_mid_kernel: operands through registers
+  bool moves_back = false;                 // rhs rows may need kProblemMovesBack
+  bool past = false;                       // dot_mid_kernel, dot_pair_kernel: bf16 outputs past all caches
+  bool f32_wide = false, f32_lean = false; // dot_f32_kernel's variants
+  int bm = 0, bn = 0;                      // its tiles
+};
+DotChoice choose_dot(const std::vector<Problem>& ps, int32_t layout, int32_t in_dtype);      // (never dot_mfma_kernel through registers)
+
 struct SoftmaxFinish;
 // Products of bfloat16 operands that end in `finish` (kernels_stats.h) instead of outputs, for launches that takes_stats() names: those that go to 256 x 256 tiles with direct
 // loads anyhow, and with long_outputs those whose outputs rather than products make them go to another kernel.

@@ -744,6 +744,42 @@ int32_t run_dots(std::vector<Problem>& ps, int32_t layout, int32_t in_dtype, int
   return launch_problems(ps, layout, in_dtype, out_dtype, GSPMD_EPILOGUE_NONE, false, tables, table_bytes, stream);
 }
 
+DotChoice choose_dot(const std::vector<Problem>& ps, int32_t layout, int32_t in_dtype) {
+  DotChoice c;
+  const KernelPath path = kernel_path(ps, in_dtype, layout);
+  MfmaChoice m = pick_kernel(ps, path, layout, false);
+  const LaunchSize size = launch_size(ps, layout);
+  if (m.kernel == kMfmaBig && big_staged(size, path, layout))
+    m = path != kPathMfmaStaged || mid_stages_whole(size, layout) ? MfmaChoice{kMfmaMid, 0} : MfmaChoice{kMfmaSplit, 4, 4};
+  c.kernel = m.kernel;
+  c.row_blocks = m.row_blocks;
+  c.col_blocks = m.kernel == kMfmaSplit ? m.col_blocks : 0;
+  c.staged = m.kernel == kMfmaMid && path == kPathMfmaStaged;
+  c.moves_back = m.kernel != kMfmaNone && m.kernel != kMfmaSplit && !c.staged && path == kPathMfmaWords && !(layout & GSPMD_LAYOUT_RHS_K_CONTIGUOUS);
+  switch (m.kernel) {
+    case kMfmaSplit: c.bm = 16 * c.row_blocks; c.bn = 16 * c.col_blocks; break;
+    case kMfmaMid: c.bm = c.bn = kMidTile; break;
+    case kMfmaPair: c.bm = kPairRows; c.bn = kPairCols; break;
+    case kMfmaBig: c.bm = kMfmaBM; c.bn = kMfmaBN; break;
+    default: c.bm = c.bn = kGenTile;
+  }
+  int64_t out_bytes = 0, tiles = 0;
+  for (const auto& p : ps) {
+    out_bytes += static_cast<int64_t>(p.Mv) * p.Nv * 2;
+    tiles += tiles_of(p, c.bm, c.bn);
+  }
+  c.past = m.kernel == kMfmaMid ? out_bytes > kPastBytes || tiles > kPastTiles || size.in_bytes > kPastInBytes : m.kernel == kMfmaPair && pair_stores_past(ps);
+  c.f32_wide = f32_wide(ps);
+  c.f32_lean = !c.f32_wide && f32_four(tiles, size.k);
+  t_last.kernel = c.kernel;
+  t_last.row_blocks = c.row_blocks;
+  t_last.col_blocks = c.col_blocks;
+  t_last.one_launch = 0;
+  t_last.table_bytes = 0;
+  t_last.moved_back = 0;
+  return c;
+}
+
 bool takes_stats(const std::vector<Problem>& ps, int32_t layout, bool long_outputs) {
   if (ps.empty() || (layout & GSPMD_LAYOUT_LHS_K_MAJOR)) return false;
   const KernelPath path = kernel_path(ps, GSPMD_BF16, layout);

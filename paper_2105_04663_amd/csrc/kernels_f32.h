@@ -25,6 +25,7 @@
 #include "kernels_basic.h"
 #include "mfma_common.h"
 #include "plan.h"
+#include "ragged.h"
 #include "tile_index.h"
 
 namespace gspmd {
@@ -38,7 +39,7 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // LEAN: LDS for four workgroups on a compute unit (f32_four).  WIDE: rows beyond 32-bit offsets (512 MiB and more), a lane's offsets in 64 bits and one
 // addition per load.
-template <int LAYOUT, bool LEAN, bool WIDE = false>
+template <int LAYOUT, bool LEAN, bool WIDE = false, bool RAGGED = false>
 __global__ __launch_bounds__(kF32Threads, LEAN ? 4 : 3) void dot_f32_kernel(const InlineProblems inl, const Problem* __restrict__ tab, int n_prob, int epilogue) {
   constexpr bool AKM = (LAYOUT & GSPMD_LAYOUT_LHS_K_MAJOR) != 0, BKC = (LAYOUT & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) != 0;
   constexpr int R = f32_stages<LEAN>();
@@ -50,8 +51,12 @@ __global__ __launch_bounds__(kF32Threads, LEAN ? 4 : 3) void dot_f32_kernel(cons
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
-  const int tile = logical_tile(blockIdx.x, gridDim.x);
-  const Problem P = lookup_problem(tab, n_prob, tile);
+  RaggedTile ragged;
+  if constexpr (RAGGED) {
+    if (!ragged.find<kF32Tile, kF32Tile>(n_prob, sizeof(float), sizeof(float), blockIdx.x, gridDim.x)) return;
+  }
+  const int tile = RAGGED ? ragged.tile : logical_tile(blockIdx.x, gridDim.x);
+  const Problem P = RAGGED ? ragged.problem : lookup_problem(tab, n_prob, tile);
   const int local = tile - P.tile_begin;
   // bands of 8 tile rows, the row index running fastest: tiles that are in flight together share operand panels in L2
   const int tiles_m = (P.Mv + kF32Tile - 1) / kF32Tile;

@@ -36,6 +36,7 @@
 #include "mainloop_asm.h"
 #include "mfma_common.h"
 #include "plan.h"
+#include "ragged.h"
 #include "tile_index.h"
 
 namespace gspmd {
@@ -87,7 +88,7 @@ __device__ __forceinline__ void zero_rows_below(TOut* __restrict__ C, int ldc, i
 constexpr int kMfmaCodeAlign = 16384;
 // `finish`: what becomes of a tile's accumulators instead of the epilogue, in a launch without joined problems.
 struct NoFinish {};
-template <typename TOut, int LAYOUT, bool STAGED, typename Finish>
+template <typename TOut, int LAYOUT, bool STAGED, typename Finish, bool RAGGED = false>
 __global__ __attribute__((aligned(kMfmaCodeAlign))) __launch_bounds__(kMfmaThreads) void dot_mfma_kernel(const InlineProblems inl, const Problem* __restrict__ tab, int n_prob, int epilogue,
                                                                 float* __restrict__ join_partials, uint32_t* __restrict__ join_counters,
                                                                 unsigned long long* __restrict__ timeline, int timeline_records, const Finish finish) {
@@ -99,8 +100,12 @@ __global__ __attribute__((aligned(kMfmaCodeAlign))) __launch_bounds__(kMfmaThrea
 
   unsigned long long* const rec = timeline_record(timeline, timeline_records);
   if (rec != nullptr) timeline_stamp(rec, 0, t, timeline_where());
-  const int tile = logical_tile(blockIdx.x, gridDim.x);
-  const Problem P = lookup_problem(tab, n_prob, tile);
+  RaggedTile ragged;
+  if constexpr (RAGGED) {
+    if (!ragged.find<kMfmaBM, kMfmaBN>(n_prob, sizeof(bf16_bits), sizeof(TOut), blockIdx.x, gridDim.x)) return;
+  }
+  const int tile = RAGGED ? ragged.tile : logical_tile(blockIdx.x, gridDim.x);
+  const Problem P = RAGGED ? ragged.problem : lookup_problem(tab, n_prob, tile);
   const int local = tile - P.tile_begin;            // which of its problem's output tiles this workgroup computes
   int tile_row, n0;
   tile_origin(local, P.Mv, P.tiles_n, &tile_row, &n0);
@@ -486,7 +491,7 @@ __global__ __attribute__((aligned(kMfmaCodeAlign))) __launch_bounds__(kMfmaThrea
   // scope counter update by a wait for the stores and the workgroup barriers.  A release fence would do the same for
   // plain stores, but it writes back the XCD's whole L2 and was measured to cost tens of microseconds per tile; an
   // acquire fence would drop every operand panel the XCD has cached.
-  if (P.join_count > 1) {
+  if (!RAGGED && P.join_count > 1) {
     constexpr int kDeviceScope = 16 | 2;                   // sc1, and nt: a slot is written once and read once (measured +1 to 2 %)
     const int S = P.join_count;
     const int64_t jt = static_cast<int64_t>(P.join_first) + local;
@@ -740,19 +745,19 @@ __global__ __attribute__((aligned(kMfmaCodeAlign))) __launch_bounds__(kMfmaThrea
 
 // The kernel needs all 160 KiB of LDS as dynamic shared memory: raised once per instantiation and device.  Callable
 // from several host threads.
-template <typename TOut, int LAYOUT, bool STAGED>
+template <typename TOut, int LAYOUT, bool STAGED, bool RAGGED = false>
 inline bool launch_dot_mfma_as(const MfmaLaunch& l, hipStream_t stream) {
   static std::once_flag once[kMaxDevices];
   static bool ok[kMaxDevices];
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return false;
   std::call_once(once[dev], [dev] {
-    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_mfma_kernel<TOut, LAYOUT, STAGED, NoFinish>),
+    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_mfma_kernel<TOut, LAYOUT, STAGED, NoFinish, RAGGED>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, kMfmaLds) == hipSuccess;
   });
   if (!ok[dev]) return false;
   const dim3 grid(static_cast<unsigned>(l.tiles)), block(kMfmaThreads);
-  hipLaunchKernelGGL((dot_mfma_kernel<TOut, LAYOUT, STAGED, NoFinish>), grid, block, kMfmaLds, stream, *l.inl, l.tab, l.n_prob, l.epilogue, l.join_partials,
+  hipLaunchKernelGGL((dot_mfma_kernel<TOut, LAYOUT, STAGED, NoFinish, RAGGED>), grid, block, kMfmaLds, stream, *l.inl, l.tab, l.n_prob, l.epilogue, l.join_partials,
                      l.join_counters, l.timeline, l.timeline_records, NoFinish{});
   return hipGetLastError() == hipSuccess;
 }

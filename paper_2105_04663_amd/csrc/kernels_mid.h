@@ -26,6 +26,7 @@
 #include "launch.h"
 #include "mfma_common.h"
 #include "plan.h"
+#include "ragged.h"
 #include "tile_index.h"
 
 namespace gspmd {
@@ -43,7 +44,8 @@ constexpr int kMidUnroll = 5;                         // K steps after which the
 // every chunk is whole.  Bound by the address unit, 64 cycles for a KiB at an odd address (both operands: 430 ns per 32-wide
 // tile, one 270).  Measured (us, before in 256 x 256 staged tiles or dot_split_kernel / now): 601 x 1203 x 697, six of them 49.5 / 17.5,
 // 4999 x 576 x 1193 28.1 / 15.2, 152 x 209 x 1094, 32 of them 23.7 / 16.6.
-template <typename TOut, int LAYOUT, bool CHAIN, int PER_CU, bool STAGED>
+// RAGGED: where the table holds parts of experts whose rows only the device counts (ragged.h).
+template <typename TOut, int LAYOUT, bool CHAIN, int PER_CU, bool STAGED, bool RAGGED>
 __global__ __launch_bounds__(kMidThreads, CHAIN && PER_CU == 1 ? 1 : 2)   // (one: the sums' accumulators take the other half of the registers)
  void dot_mid_kernel(const InlineProblems inl, const Problem* __restrict__ tab, int n_prob, int epilogue) {
   constexpr bool AKM = (LAYOUT & GSPMD_LAYOUT_LHS_K_MAJOR) != 0, BKC = (LAYOUT & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) != 0;
@@ -59,9 +61,14 @@ __global__ __launch_bounds__(kMidThreads, CHAIN && PER_CU == 1 ? 1 : 2)   // (on
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
-  const int tile = logical_tile(blockIdx.x, gridDim.x);
-  const int which = lookup_problem_index(tab, n_prob, tile);
-  Problem P = problem_at(tab, which);
+  RaggedTile ragged;
+  if constexpr (RAGGED) {
+    static_assert(!CHAIN, "");
+    if (!ragged.find<kMidTile, kMidTile>(n_prob, sizeof(bf16_bits), sizeof(TOut), blockIdx.x, gridDim.x)) return;
+  }
+  const int tile = RAGGED ? ragged.tile : logical_tile(blockIdx.x, gridDim.x);
+  const int which = RAGGED ? 0 : lookup_problem_index(tab, n_prob, tile);
+  Problem P = RAGGED ? ragged.problem : problem_at(tab, which);
   const int local = tile - P.tile_begin;
   // bands of kBandRows tile rows, the row index running fastest: tiles in flight together share operand panels in L2
   const int tiles_m = (P.Mv + kMidTile - 1) / kMidTile;
@@ -458,7 +465,7 @@ __global__ __launch_bounds__(kMidThreads, CHAIN && PER_CU == 1 ? 1 : 2)   // (on
   }
 }
 
-template <typename TOut, int LAYOUT, bool CHAIN, int PER_CU, bool STAGED = false>
+template <typename TOut, int LAYOUT, bool CHAIN, int PER_CU, bool STAGED = false, bool RAGGED = false>
 inline bool launch_dot_mid_as(const MfmaLaunch& l, hipStream_t stream) {
   constexpr int lds = mid_stages<PER_CU>() * kMidStage;
   static std::once_flag once[kMaxDevices];
@@ -466,11 +473,11 @@ inline bool launch_dot_mid_as(const MfmaLaunch& l, hipStream_t stream) {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return false;
   std::call_once(once[dev], [dev] {
-    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_mid_kernel<TOut, LAYOUT, CHAIN, PER_CU, STAGED>),
+    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_mid_kernel<TOut, LAYOUT, CHAIN, PER_CU, STAGED, RAGGED>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
   });
   if (!ok[dev]) return false;
-  hipLaunchKernelGGL((dot_mid_kernel<TOut, LAYOUT, CHAIN, PER_CU, STAGED>), dim3(static_cast<unsigned>(l.tiles)), dim3(kMidThreads), lds, stream, *l.inl, l.tab,
+  hipLaunchKernelGGL((dot_mid_kernel<TOut, LAYOUT, CHAIN, PER_CU, STAGED, RAGGED>), dim3(static_cast<unsigned>(l.tiles)), dim3(kMidThreads), lds, stream, *l.inl, l.tab,
                      l.n_prob, !STAGED && sizeof(TOut) == 2 && l.past ? l.epilogue | kStorePast : l.epilogue);
   return hipGetLastError() == hipSuccess;
 }

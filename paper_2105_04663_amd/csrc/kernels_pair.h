@@ -29,6 +29,7 @@
 #include "launch.h"
 #include "mfma_common.h"
 #include "plan.h"
+#include "ragged.h"
 #include "tile_index.h"
 
 namespace gspmd {
@@ -38,7 +39,7 @@ constexpr int kPairPartA = kPairRows * kMfmaBK * 2, kPairPartB = kPairCols * kMf
 constexpr int kPairLds = kPairStages * kPairStage;
 
 // PAST: bf16 outputs past all caches (pair_stores_past in gspmd.hip)
-template <typename TOut, int LAYOUT, bool PAST>
+template <typename TOut, int LAYOUT, bool PAST, bool RAGGED>
 __global__ __launch_bounds__(kPairThreads, 2) void dot_pair_kernel(const InlineProblems inl, const Problem* __restrict__ tab, int n_prob, int epilogue) {
   constexpr bool AKM = (LAYOUT & GSPMD_LAYOUT_LHS_K_MAJOR) != 0, BKC = (LAYOUT & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) != 0;
   constexpr int R = kPairStages, kLoads = 6;     // a wave's load instructions of a tile: four of the lhs's part, two of the rhs's
@@ -47,8 +48,12 @@ __global__ __launch_bounds__(kPairThreads, 2) void dot_pair_kernel(const InlineP
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = (wave >> 1) * 128, wn = (wave & 1) * 64;
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
-  const int tile = logical_tile(blockIdx.x, gridDim.x);
-  const Problem P = lookup_problem(tab, n_prob, tile);
+  RaggedTile ragged;
+  if constexpr (RAGGED) {
+    if (!ragged.find<kPairRows, kPairCols>(n_prob, sizeof(bf16_bits), sizeof(TOut), blockIdx.x, gridDim.x)) return;
+  }
+  const int tile = RAGGED ? ragged.tile : logical_tile(blockIdx.x, gridDim.x);
+  const Problem P = RAGGED ? ragged.problem : lookup_problem(tab, n_prob, tile);
   const int local = tile - P.tile_begin;
   // bands of 1024 rows, the row index running fastest: tiles in flight together share operand panels in L2
   constexpr int kBand = kBandRows / 2;
@@ -209,17 +214,17 @@ __global__ __launch_bounds__(kPairThreads, 2) void dot_pair_kernel(const InlineP
   }
 }
 
-template <int LAYOUT, typename TOut, bool PAST>
+template <int LAYOUT, typename TOut, bool PAST, bool RAGGED = false>
 inline bool launch_dot_pair_as(const MfmaLaunch& l, hipStream_t stream) {
   static std::once_flag once[kMaxDevices];
   static bool ok[kMaxDevices];
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return false;
   std::call_once(once[dev], [dev] {
-    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_pair_kernel<TOut, LAYOUT, PAST>), hipFuncAttributeMaxDynamicSharedMemorySize, kPairLds) == hipSuccess;
+    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_pair_kernel<TOut, LAYOUT, PAST, RAGGED>), hipFuncAttributeMaxDynamicSharedMemorySize, kPairLds) == hipSuccess;
   });
   if (!ok[dev]) return false;
-  hipLaunchKernelGGL((dot_pair_kernel<TOut, LAYOUT, PAST>), dim3(static_cast<unsigned>(l.tiles)), dim3(kPairThreads), kPairLds, stream, *l.inl, l.tab, l.n_prob, l.epilogue);
+  hipLaunchKernelGGL((dot_pair_kernel<TOut, LAYOUT, PAST, RAGGED>), dim3(static_cast<unsigned>(l.tiles)), dim3(kPairThreads), kPairLds, stream, *l.inl, l.tab, l.n_prob, l.epilogue);
   return hipGetLastError() == hipSuccess;
 }
 

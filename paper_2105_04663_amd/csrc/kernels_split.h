@@ -36,6 +36,7 @@
 #include "kernels_basic.h"
 #include "launch.h"
 #include "plan.h"
+#include "ragged.h"
 #include "tile_index.h"
 
 namespace gspmd {
@@ -68,7 +69,7 @@ template <int W> __device__ __forceinline__ int split_pair(int block, int krow) 
   else return block;
 }
 
-template <typename TOut, int LAYOUT, int RB, int CB>
+template <typename TOut, int LAYOUT, int RB, int CB, bool RAGGED>
 __global__ __launch_bounds__(kSplitThreads) void dot_split_kernel(const InlineProblems inl, const Problem* __restrict__ tab, int n_prob, int epilogue, int spread,
                                                                   unsigned long long* __restrict__ timeline, int timeline_records) {
   constexpr bool AKM = (LAYOUT & GSPMD_LAYOUT_LHS_K_MAJOR) != 0, BKC = (LAYOUT & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) != 0;
@@ -79,8 +80,12 @@ __global__ __launch_bounds__(kSplitThreads) void dot_split_kernel(const InlinePr
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   unsigned long long* const rec = timeline_record(timeline, timeline_records);
   if (rec != nullptr) timeline_stamp(rec, 0, t, timeline_where());
-  const int tile = spread ? spread_tile(blockIdx.x, gridDim.x) : logical_tile(blockIdx.x, gridDim.x);
-  const Problem P = lookup_problem(tab, n_prob, tile);
+  RaggedTile ragged;
+  if constexpr (RAGGED) {
+    if (!ragged.find<BM, BN>(n_prob, sizeof(bf16_bits), sizeof(TOut), blockIdx.x, gridDim.x)) return;
+  }
+  const int tile = RAGGED ? ragged.tile : spread ? spread_tile(blockIdx.x, gridDim.x) : logical_tile(blockIdx.x, gridDim.x);
+  const Problem P = RAGGED ? ragged.problem : lookup_problem(tab, n_prob, tile);
   const int local = tile - P.tile_begin;
   // the row index runs fastest: the row tiles that share a weight panel are on one XCD at the same time
   const int tiles_m = (P.Mv + BM - 1) / BM;
@@ -337,7 +342,7 @@ __global__ __launch_bounds__(kSplitThreads) void dot_split_kernel(const InlinePr
   }
 }
 
-template <typename TOut, int LAYOUT, int RB, int CB>
+template <typename TOut, int LAYOUT, int RB, int CB, bool RAGGED = false>
 inline bool launch_dot_split_as(const MfmaLaunch& l, hipStream_t stream) {
   constexpr int lds = split_lds<RB, CB>();
   static std::once_flag once[kMaxDevices];
@@ -345,22 +350,22 @@ inline bool launch_dot_split_as(const MfmaLaunch& l, hipStream_t stream) {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return false;
   std::call_once(once[dev], [dev] {
-    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_split_kernel<TOut, LAYOUT, RB, CB>),
+    ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_split_kernel<TOut, LAYOUT, RB, CB, RAGGED>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
   });
   if (!ok[dev]) return false;
-  hipLaunchKernelGGL((dot_split_kernel<TOut, LAYOUT, RB, CB>), dim3(static_cast<unsigned>(l.tiles)), dim3(kSplitThreads), lds, stream, *l.inl, l.tab,
+  hipLaunchKernelGGL((dot_split_kernel<TOut, LAYOUT, RB, CB, RAGGED>), dim3(static_cast<unsigned>(l.tiles)), dim3(kSplitThreads), lds, stream, *l.inl, l.tab,
                      l.n_prob, l.epilogue, l.spread ? 1 : 0, l.timeline, l.timeline_records);
   return hipGetLastError() == hipSuccess;
 }
 
-template <int LAYOUT, typename TOut>
+template <int LAYOUT, typename TOut, bool RAGGED = false>
 bool launch_dot_split_out(const MfmaLaunch& l, int row_blocks, int col_blocks, hipStream_t stream) {
-  if (col_blocks == 2) return row_blocks == 1 ? launch_dot_split_as<TOut, LAYOUT, 1, 2>(l, stream) : launch_dot_split_as<TOut, LAYOUT, 2, 2>(l, stream);
+  if (col_blocks == 2) return row_blocks == 1 ? launch_dot_split_as<TOut, LAYOUT, 1, 2, RAGGED>(l, stream) : launch_dot_split_as<TOut, LAYOUT, 2, 2, RAGGED>(l, stream);
   switch (row_blocks) {
-    case 1: return launch_dot_split_as<TOut, LAYOUT, 1, 4>(l, stream);
-    case 2: return launch_dot_split_as<TOut, LAYOUT, 2, 4>(l, stream);
-    default: return launch_dot_split_as<TOut, LAYOUT, 4, 4>(l, stream);
+    case 1: return launch_dot_split_as<TOut, LAYOUT, 1, 4, RAGGED>(l, stream);
+    case 2: return launch_dot_split_as<TOut, LAYOUT, 2, 4, RAGGED>(l, stream);
+    default: return launch_dot_split_as<TOut, LAYOUT, 4, 4, RAGGED>(l, stream);
   }
 }
 template <int LAYOUT>

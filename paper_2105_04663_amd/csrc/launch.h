@@ -95,4 +95,14 @@ inline bool launch_dot_pair(const MfmaLaunch& l, int32_t layout, int32_t out_dty
 }
 #endif
 
+// The kernels above for parts of experts (ragged.h): layouts 0, 1, 2.
+template <int LAYOUT>
+bool launch_ragged_mfma_layout(const MfmaLaunch& l, int32_t out_dtype, hipStream_t stream);
+template <int LAYOUT>
+bool launch_ragged_split_layout(const MfmaLaunch& l, int32_t out_dtype, int row_blocks, int col_blocks, hipStream_t stream);
+template <int LAYOUT>
+bool launch_ragged_mid_layout(const MfmaLaunch& l, int32_t out_dtype, bool staged, hipStream_t stream);
+template <int LAYOUT>
+bool launch_ragged_pair_layout(const MfmaLaunch& l, int32_t out_dtype, hipStream_t stream);
+
 }  // namespace gspmd
