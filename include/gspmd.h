@@ -415,6 +415,65 @@ int32_t gspmd_softmax_distill(const gspmd_mesh* mesh,
                               const gspmd_shard_buf* dx_shards, const gspmd_shard_buf* dw_shards,
                               void* workspace, int64_t workspace_bytes, void* hip_stream);
 
+/* Rows of a vocabulary matrix that is split on the mesh: what a partitioned language model begins with.  w and its shardings are those of the losses above (a matrix may serve both), the rows
+ * y [T, M] of T tokens are sharded like their x.  ids: host array of P entries by partition id, each the entries (int32, device memory, dense, of the static token count of y's shard) of the partition's
+ * tokens; partitions of the same tokens share them.  An id outside 0 .. V - 1 is a token without an entry.
+ *   gspmd_embed       y[t, :] = scale * w[id t, :]           (the AllReduce over the vocabulary's mesh dimension); zeros for a token without an entry
+ *   gspmd_embed_grad  dw[v, :] = scale * sum over the tokens t with id v of dy[t, :]     (over all of the tokens' mesh dimension); a token without an entry takes no part
+ * All buffers of a call have one type, bf16 or f32; products and sums are fp32, in one fixed order, rounded once (a scale of 1 copies bits).  Equal calls give equal bits.
+ * accumulate: dw holds a gradient already, to which this one is added (the losses', of a matrix that serves both): entries without tokens keep their bits.  0: dw is written whole, zeros where there
+ * are no tokens.  Padding of the static shapes is written as 0 either way.  All shards of one tensor have one row stride; distinct buffers of the same data are each written.
+ * At most 64 shards of tokens and of the vocabulary, 2^24 tokens.  Kernels only: both may be recorded into a HIP graph. */
+int32_t gspmd_embed(const gspmd_mesh* mesh, const int32_t* const* ids,
+                    const gspmd_shard_buf* w_shards, const gspmd_sharding* w_sh, int32_t vocab_dim, float scale,
+                    const gspmd_shard_buf* y_shards, const gspmd_sharding* y_sh, void* hip_stream);
+/* Bytes of device workspace gspmd_embed_grad needs (the tokens sorted by entry).  dtype: of the gradients.  Pure host work. */
+int32_t gspmd_embed_grad_workspace_bytes(const gspmd_mesh* mesh, const gspmd_sharding* dy_sh, const gspmd_sharding* dw_sh, int32_t vocab_dim, int32_t dtype, int64_t* bytes);
+int32_t gspmd_embed_grad(const gspmd_mesh* mesh, const int32_t* const* ids,
+                         const gspmd_shard_buf* dy_shards, const gspmd_sharding* dy_sh,
+                         const gspmd_shard_buf* dw_shards, const gspmd_sharding* dw_sh, int32_t vocab_dim, float scale, int32_t accumulate,
+                         void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* Experts of tokens (the gating of Section 5.4), without a capacity: every choice of a token is a row ("slot") of the packed arrays that gspmd_ragged_dot works on. */
+#define GSPMD_MAX_EXPERTS 512
+#define GSPMD_MAX_CHOICES 16
+
+/* A routing of T tokens with k choices each among E experts: device memory, dense, of ALL tokens and the same for all partitions. */
+typedef struct {
+  int32_t* experts;   /* [T, k]: a token's experts, the one with the largest logit first; -1: none */
+  float* weights;     /* [T, k]: their weights; 0 where there is none */
+  int32_t* slots;     /* [T, k]: their places in the packed arrays; -1 where there is none */
+  int32_t* order;     /* [T k]: of every slot the choice (token * k + its number) it belongs to; -1 behind the last */
+  int32_t* sizes;     /* [E]: slots of every expert, as gspmd_ragged_dot takes them */
+} gspmd_route_buf;
+
+/* Choose experts: logits [T, E] (bf16 or f32; dimension 0 split over a mesh dimension or whole, E whole).  A token takes the `choices` (1 .. GSPMD_MAX_CHOICES, at most E, E at most
+ * GSPMD_MAX_EXPERTS) experts of its largest logits, the lowest of equal ones; never one with a logit of -infinity (an expert that is masked; all of them: a padded token) or NaN, so it may have fewer.
+ * weights: exp of their logits over the sum of exp of all of the token's logits, or (normalise) of the chosen ones; NaN where that has a NaN or +infinity in it.  Slots are ordered by expert,
+ * then by token, then by choice.  All arrays of `route` are written whole.  workspace: 256-byte aligned, gspmd_route_workspace_bytes (which may be 0, then it may be NULL).
+ * Kernels only, equal calls give equal bits.  At most 64 shards of tokens, 2^24 choices. */
+int32_t gspmd_route_workspace_bytes(const gspmd_mesh* mesh, const gspmd_sharding* logits_sh, int32_t choices, int64_t* bytes);
+int32_t gspmd_route(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_shards, const gspmd_sharding* logits_sh, int32_t choices, int32_t normalise,
+                    const gspmd_route_buf* route, void* workspace, int64_t workspace_bytes, void* hip_stream);
+/* The gradient with respect to the logits of sum of dweights * weights, dweights [T, k] f32 (ignored where there is no expert): p (g - sum of p g) over the softmax's experts, g an expert's
+ * dweight or 0.  Reads route's experts and weights.  dlogits: shards like logits, written whole (zeros for a token without experts and in the padding). */
+int32_t gspmd_route_grad(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_shards, const gspmd_sharding* logits_sh, int32_t choices, int32_t normalise,
+                         const gspmd_route_buf* route, const float* dweights, const gspmd_shard_buf* dlogits_shards, void* hip_stream);
+
+/* Between tokens' rows [T, M] (dimension 0 split or whole) and experts' packed rows, a tensor [E, S, M] held as gspmd_ragged_dot holds it (dimension 0 split or whole, S at least T k): the AllToAlls around
+ * the experts.  Arrays of `route` that a call names have to be there, others may be NULL; values that are no expert, slot or choice count as none.  One type, bf16 or f32; sums in fp32.
+ *   gspmd_dispatch      rows[s, :] = x[token of s, :]                        reads order, experts; its gradient is gspmd_combine of the rows' gradient, not weighted
+ *   gspmd_combine       y[t, :] = sum over t's choices of weight * rows[slot, :], in their order; not `weighted`: weights of 1.  Reads slots, experts, weights
+ *   gspmd_combine_grad  drows[slot, :] = weight * dy[t, :], dweights[t, i] = sum over M of dy[t, :] rows[slot, :] (0 where there is no slot)     reads slots, experts, weights
+ * A partition's rows are those of its own experts, in their places: others, and those behind the last slot, are left as they were and never read.  The rows of y's padding are zeros.
+ * Distinct buffers of the same data are each written; outputs must not overlap inputs.  Kernels only. */
+int32_t gspmd_dispatch(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const gspmd_sharding* x_sh, int32_t choices, const gspmd_route_buf* route,
+                       const gspmd_shard_buf* rows_shards, const gspmd_sharding* rows_sh, void* hip_stream);
+int32_t gspmd_combine(const gspmd_mesh* mesh, const gspmd_shard_buf* rows_shards, const gspmd_sharding* rows_sh, int32_t choices, const gspmd_route_buf* route, int32_t weighted,
+                      const gspmd_shard_buf* y_shards, const gspmd_sharding* y_sh, void* hip_stream);
+int32_t gspmd_combine_grad(const gspmd_mesh* mesh, const gspmd_shard_buf* dy_shards, const gspmd_sharding* dy_sh, const gspmd_shard_buf* rows_shards, const gspmd_sharding* rows_sh, int32_t choices,
+                           const gspmd_route_buf* route, const gspmd_shard_buf* drows_shards, float* dweights, void* hip_stream);
+
 /* Utility (no counterpart in the paper; a profiling aid for the MFMA contraction kernel).  While a record buffer is
  * set, every later Dot launch of this process (any entry point, any stream) makes workgroup b < n_records of its
  * MFMA kernel write record b: eight 64-bit words of the GPU's 100 MHz constant-rate counter at kernel entry (bits

@@ -12,5 +12,6 @@ from .binding import (  # noqa: F401
     infer_out_sharding, local_dot, plan_dot, reduce_partials, reshard, reshard_workspace_bytes, shard_assemble, shard_bounds, shard_extract,
     status_string, EXPORTED_SYMBOLS, set_tile_timeline, TILE_TIMELINE_WORDS,
     MAX_TARGETS, TokenBuf, softmax_distill, softmax_workspace_bytes, softmax_xent,
-    ragged_dot,
+    ragged_dot, embed, embed_grad, embed_grad_workspace_bytes,
+    MAX_CHOICES, MAX_EXPERTS, RouteBuf, combine, combine_grad, dispatch, route, route_grad, route_workspace_bytes,
 )

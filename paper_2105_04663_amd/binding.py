@@ -23,10 +23,12 @@ EXPORTED_SYMBOLS = (
     "gspmd_compatible_operand_shardings", "gspmd_resharded_dot_workspace_bytes", "gspmd_resharded_dot",
     "gspmd_grouped_dot_noalloc", "gspmd_set_tile_timeline",
     "gspmd_softmax_workspace_bytes", "gspmd_softmax_xent", "gspmd_softmax_distill",
-    "gspmd_ragged_dot",
+    "gspmd_ragged_dot", "gspmd_embed", "gspmd_embed_grad_workspace_bytes", "gspmd_embed_grad", "gspmd_route_workspace_bytes", "gspmd_route", "gspmd_route_grad",
+    "gspmd_dispatch", "gspmd_combine", "gspmd_combine_grad",
 )
 TILE_TIMELINE_WORDS = 8
 MAX_TARGETS = 1024
+MAX_EXPERTS, MAX_CHOICES = 512, 16
 NOALLOC_MAX_WORKSPACE_BYTES = 32 * 1024 * 1024
 
 
@@ -65,6 +67,10 @@ class _CTokenBuf(C.Structure):
 
 if (C.sizeof(_CTokenBuf), _CTokenBuf.logits_dtype.offset, _CTokenBuf.weights.offset, _CTokenBuf.lse.offset) != (48, 16, 24, 40):
     raise ImportError("unexpected layout of gspmd_token_buf")
+
+
+class _CRouteBuf(C.Structure):
+    _fields_ = [("experts", C.c_void_p), ("weights", C.c_void_p), ("slots", C.c_void_p), ("order", C.c_void_p), ("sizes", C.c_void_p)]
 
 
 class _CGemmDesc(C.Structure):
@@ -118,6 +124,16 @@ def load_library():
     lib.gspmd_softmax_xent.argtypes = [pm, pbs, ps, pbs, ps, C.c_int32, pbs, pbs, pbs, C.c_void_p, C.c_int64, C.c_void_p]
     lib.gspmd_softmax_distill.argtypes = [pm, pbs, ps, pbs, ps, C.c_int32, pbs, C.c_int32, C.c_float, pbs, pbs, C.c_void_p, C.c_int64, C.c_void_p]
     lib.gspmd_ragged_dot.argtypes = [pm, pd, pbs, ps, pbs, ps, pbs, ps, C.c_void_p, C.c_int32, C.c_void_p]
+    pr = C.POINTER(_CRouteBuf)
+    lib.gspmd_embed.argtypes = [pm, C.c_void_p, pbs, ps, C.c_int32, C.c_float, pbs, ps, C.c_void_p]
+    lib.gspmd_embed_grad_workspace_bytes.argtypes = [pm, ps, ps, C.c_int32, C.c_int32, pi64]
+    lib.gspmd_embed_grad.argtypes = [pm, C.c_void_p, pbs, ps, pbs, ps, C.c_int32, C.c_float, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.gspmd_route_workspace_bytes.argtypes = [pm, ps, C.c_int32, pi64]
+    lib.gspmd_route.argtypes = [pm, pbs, ps, C.c_int32, C.c_int32, pr, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.gspmd_route_grad.argtypes = [pm, pbs, ps, C.c_int32, C.c_int32, pr, C.c_void_p, pbs, C.c_void_p]
+    lib.gspmd_dispatch.argtypes = [pm, pbs, ps, C.c_int32, pr, pbs, ps, C.c_void_p]
+    lib.gspmd_combine.argtypes = [pm, pbs, ps, C.c_int32, pr, C.c_int32, pbs, ps, C.c_void_p]
+    lib.gspmd_combine_grad.argtypes = [pm, pbs, ps, pbs, ps, C.c_int32, pr, pbs, C.c_void_p, C.c_void_p]
     lib.gspmd_set_tile_timeline.argtypes = [C.c_void_p, C.c_int64]
     for name in EXPORTED_SYMBOLS[1:]:
         getattr(lib, name).restype = C.c_int32
@@ -532,3 +548,92 @@ def ragged_dot(mesh: Mesh, dims: DotDims, lhs_shards: Sequence[ShardBuf], lhs_sh
     m, d, a, b, o = mesh._c(), dims._c(), lhs_sh._c(), rhs_sh._c(), out_sh._c()
     _check(load_library().gspmd_ragged_dot(C.byref(m), C.byref(d), _bufs(lhs_shards), C.byref(a), _bufs(rhs_shards), C.byref(b), _bufs(out_shards), C.byref(o),
                                            C.c_void_p(sizes), int(epilogue), C.c_void_p(stream)), "gspmd_ragged_dot")
+
+
+def _id_arrays(ids: Sequence[int]):
+    return (C.c_void_p * max(1, len(ids)))(*[C.c_void_p(a) for a in ids])
+
+
+def embed(mesh: Mesh, ids: Sequence[int], w_shards: Sequence[ShardBuf], w_sh: Sharding, y_shards: Sequence[ShardBuf], y_sh: Sharding,
+          vocab_dim: int = 0, scale: float = 1.0, stream: int = 0) -> None:
+    """Rows of the split vocabulary matrix by tokens' entries; ids: one address per partition (gspmd_embed)."""
+    _per_partition(mesh, ids, w_shards, y_shards)
+    m, a, b = mesh._c(), w_sh._c(), y_sh._c()
+    _check(load_library().gspmd_embed(C.byref(m), _id_arrays(ids), _bufs(w_shards), C.byref(a), int(vocab_dim), float(scale), _bufs(y_shards), C.byref(b), C.c_void_p(stream)), "gspmd_embed")
+
+
+def embed_grad_workspace_bytes(mesh: Mesh, dy_sh: Sharding, dw_sh: Sharding, vocab_dim: int, dtype: int) -> int:
+    m, a, b, n = mesh._c(), dy_sh._c(), dw_sh._c(), C.c_int64(0)
+    _check(load_library().gspmd_embed_grad_workspace_bytes(C.byref(m), C.byref(a), C.byref(b), int(vocab_dim), int(dtype), C.byref(n)), "gspmd_embed_grad_workspace_bytes")
+    return n.value
+
+
+def embed_grad(mesh: Mesh, ids: Sequence[int], dy_shards: Sequence[ShardBuf], dy_sh: Sharding, dw_shards: Sequence[ShardBuf], dw_sh: Sharding, vocab_dim: int = 0,
+               scale: float = 1.0, accumulate: bool = False, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Gradient of embed with respect to the vocabulary matrix, written or (accumulate) added to dw (gspmd_embed_grad)."""
+    _per_partition(mesh, ids, dy_shards, dw_shards)
+    m, a, b = mesh._c(), dy_sh._c(), dw_sh._c()
+    _check(load_library().gspmd_embed_grad(C.byref(m), _id_arrays(ids), _bufs(dy_shards), C.byref(a), _bufs(dw_shards), C.byref(b), int(vocab_dim), float(scale), int(bool(accumulate)),
+                                           C.c_void_p(workspace), int(workspace_bytes), C.c_void_p(stream)), "gspmd_embed_grad")
+
+
+@dataclass
+class RouteBuf:
+    """A routing's arrays: addresses in device memory (0 = none), dense, of all tokens."""
+    experts: int           # int32 [T, k]
+    weights: int           # float32 [T, k]
+    slots: int             # int32 [T, k]
+    order: int             # int32 [T * k]
+    sizes: int             # int32 [E]
+
+    def _c(self):
+        return _CRouteBuf(*[C.c_void_p(a) for a in (self.experts, self.weights, self.slots, self.order, self.sizes)])
+
+
+def route_workspace_bytes(mesh: Mesh, logits_sh: Sharding, choices: int) -> int:
+    m, a, n = mesh._c(), logits_sh._c(), C.c_int64(0)
+    _check(load_library().gspmd_route_workspace_bytes(C.byref(m), C.byref(a), int(choices), C.byref(n)), "gspmd_route_workspace_bytes")
+    return n.value
+
+
+def route(mesh: Mesh, logits_shards: Sequence[ShardBuf], logits_sh: Sharding, choices: int, route: RouteBuf, normalise: bool = False,
+          workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Choose every token's experts, their weights and slots (gspmd_route)."""
+    _per_partition(mesh, logits_shards)
+    m, a, r = mesh._c(), logits_sh._c(), route._c()
+    _check(load_library().gspmd_route(C.byref(m), _bufs(logits_shards), C.byref(a), int(choices), int(bool(normalise)), C.byref(r), C.c_void_p(workspace), int(workspace_bytes),
+                                      C.c_void_p(stream)), "gspmd_route")
+
+
+def route_grad(mesh: Mesh, logits_shards: Sequence[ShardBuf], logits_sh: Sharding, choices: int, route: RouteBuf, dweights: int, dlogits_shards: Sequence[ShardBuf],
+               normalise: bool = False, stream: int = 0) -> None:
+    """Gradient of route's weights with respect to the logits (gspmd_route_grad)."""
+    _per_partition(mesh, logits_shards, dlogits_shards)
+    m, a, r = mesh._c(), logits_sh._c(), route._c()
+    _check(load_library().gspmd_route_grad(C.byref(m), _bufs(logits_shards), C.byref(a), int(choices), int(bool(normalise)), C.byref(r), C.c_void_p(dweights), _bufs(dlogits_shards),
+                                           C.c_void_p(stream)), "gspmd_route_grad")
+
+
+def dispatch(mesh: Mesh, x_shards: Sequence[ShardBuf], x_sh: Sharding, choices: int, route: RouteBuf, rows_shards: Sequence[ShardBuf], rows_sh: Sharding, stream: int = 0) -> None:
+    """Tokens' rows to their experts' slots (gspmd_dispatch)."""
+    _per_partition(mesh, x_shards, rows_shards)
+    m, a, b, r = mesh._c(), x_sh._c(), rows_sh._c(), route._c()
+    _check(load_library().gspmd_dispatch(C.byref(m), _bufs(x_shards), C.byref(a), int(choices), C.byref(r), _bufs(rows_shards), C.byref(b), C.c_void_p(stream)), "gspmd_dispatch")
+
+
+def combine(mesh: Mesh, rows_shards: Sequence[ShardBuf], rows_sh: Sharding, choices: int, route: RouteBuf, y_shards: Sequence[ShardBuf], y_sh: Sharding,
+            weighted: bool = True, stream: int = 0) -> None:
+    """Experts' rows added up for their tokens (gspmd_combine)."""
+    _per_partition(mesh, rows_shards, y_shards)
+    m, a, b, r = mesh._c(), rows_sh._c(), y_sh._c(), route._c()
+    _check(load_library().gspmd_combine(C.byref(m), _bufs(rows_shards), C.byref(a), int(choices), C.byref(r), int(bool(weighted)), _bufs(y_shards), C.byref(b), C.c_void_p(stream)),
+           "gspmd_combine")
+
+
+def combine_grad(mesh: Mesh, dy_shards: Sequence[ShardBuf], dy_sh: Sharding, rows_shards: Sequence[ShardBuf], rows_sh: Sharding, choices: int, route: RouteBuf,
+                 drows_shards: Sequence[ShardBuf], dweights: int, stream: int = 0) -> None:
+    """Gradients of combine with respect to the rows and the weights (gspmd_combine_grad)."""
+    _per_partition(mesh, dy_shards, rows_shards, drows_shards)
+    m, a, b, r = mesh._c(), dy_sh._c(), rows_sh._c(), route._c()
+    _check(load_library().gspmd_combine_grad(C.byref(m), _bufs(dy_shards), C.byref(a), _bufs(rows_shards), C.byref(b), int(choices), C.byref(r), _bufs(drows_shards), C.c_void_p(dweights),
+                                             C.c_void_p(stream)), "gspmd_combine_grad")

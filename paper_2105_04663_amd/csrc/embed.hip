@@ -1,0 +1,216 @@
+// gspmd_embed, gspmd_embed_grad (include/gspmd.h): the host's part.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <vector>
+
+#include "../../include/gspmd.h"
+#include "dots.h"
+#include "kernels_embed.h"
+#include "kernels_sort.h"
+#include "plan.h"
+#include "sort.h"
+#include "tokens.h"
+
+namespace gspmd {
+namespace {
+
+struct Embed {
+  int64_t P = 0, T = 0, M = 0, V = 0;
+  int64_t na = 1, nb = 1, ts = 0, vs = 0;       // shards of tokens and of the vocabulary, their static extents
+  int axis_t = -1, axis_v = -1, vocab_dim = 0;
+  int64_t chunks() const { return T / kChunk; }
+  // the workspace: sorted keys, their tokens, what sorting needs, sums of whole chunks
+  int64_t list_bytes() const { return round_up(T * 4, kWsAlign); }
+  int64_t bytes() const { return T == 0 ? 0 : 2 * list_bytes() + round_up(sort_bytes(T, V), kWsAlign) + round_up(chunks() * M * 4, kWsAlign); }
+};
+
+int32_t analyse(const gspmd_mesh* mesh, const gspmd_sharding* rows_sh, const gspmd_sharding* w_sh, int32_t vocab_dim, Embed* e) {
+  int32_t st = validate_mesh(mesh, &e->P);
+  if (st != GSPMD_OK) return st;
+  if ((st = validate_sharding(mesh, rows_sh)) != GSPMD_OK || (st = validate_sharding(mesh, w_sh)) != GSPMD_OK) return st;
+  if (rows_sh->rank != 2 || w_sh->rank != 2 || (vocab_dim != 0 && vocab_dim != 1)) return GSPMD_ERR_BAD_DOT_DIMS;
+  e->T = rows_sh->global_shape[0];
+  e->M = rows_sh->global_shape[1];
+  e->V = w_sh->global_shape[vocab_dim];
+  e->vocab_dim = vocab_dim;
+  if (w_sh->global_shape[1 - vocab_dim] != e->M || e->V < 1) return GSPMD_ERR_BAD_DOT_DIMS;
+  if (split_axis(mesh, rows_sh, 1) >= 0 || split_axis(mesh, w_sh, 1 - vocab_dim) >= 0) return GSPMD_ERR_NEEDS_RESHARD;
+  e->axis_t = split_axis(mesh, rows_sh, 0);
+  e->axis_v = split_axis(mesh, w_sh, vocab_dim);
+  if (e->axis_t >= 0 && e->axis_t == e->axis_v) return GSPMD_ERR_NEEDS_RESHARD;
+  e->na = e->axis_t >= 0 ? mesh->shape[e->axis_t] : 1;
+  e->nb = e->axis_v >= 0 ? mesh->shape[e->axis_v] : 1;
+  e->ts = (e->T + e->na - 1) / e->na;
+  e->vs = (e->V + e->nb - 1) / e->nb;
+  constexpr int64_t kMost = INT32_MAX >> 2;
+  if (e->na > kTokenShards || e->nb > kVocabShards || e->T > (1 << 24) || e->M > kMost || e->V > kMost || e->ts * e->na > kMost || e->vs * e->nb > kMost) return GSPMD_ERR_UNSUPPORTED;
+  return GSPMD_OK;
+}
+
+struct Shards {                                 // a call's arguments by shard
+  std::vector<const int32_t*> ids;
+  Replicas rows, vocab;
+  int64_t ld_rows = -1, ld_vocab = -1;
+};
+
+int32_t collect(const gspmd_mesh* mesh, const Embed& e, const int32_t* const* ids, const gspmd_shard_buf* rows, const gspmd_shard_buf* vocab, Shards* s) {
+  const int32_t dtype = rows[0].dtype;
+  if (dtype != GSPMD_F32 && dtype != GSPMD_BF16) return GSPMD_ERR_UNSUPPORTED;
+  s->ids.assign(static_cast<size_t>(e.na), nullptr);
+  for (int64_t p = 0; p < e.P; ++p) {
+    int64_t coords[kMaxRank];
+    int32_t st = mesh_coords(mesh, p, coords);
+    if (st != GSPMD_OK) return st;
+    const int64_t i = e.axis_t >= 0 ? coords[e.axis_t] : 0, j = e.axis_v >= 0 ? coords[e.axis_v] : 0;
+    if ((st = check_rows(rows[p], dtype, e.M, e.ts * e.M > 0, &s->ld_rows)) != GSPMD_OK) return st;
+    if ((st = check_rows(vocab[p], dtype, e.vocab_dim == 0 ? e.M : e.vs, e.M > 0, &s->ld_vocab)) != GSPMD_OK) return st;
+    if (e.ts > 0 && !ids[p]) return GSPMD_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(ids[p]) & 3) return GSPMD_ERR_BAD_BUFFER;
+    if (!s->ids[static_cast<size_t>(i)]) s->ids[static_cast<size_t>(i)] = ids[p];
+    s->rows.add(i, rows[p].data);
+    s->vocab.add(j, vocab[p].data);
+  }
+  return GSPMD_OK;
+}
+
+EmbedArgs arguments(const Embed& e, const Shards& s, float scale) {
+  EmbedArgs a{};
+  for (int64_t i = 0; i < e.na; ++i) a.tokens[i] = TokenShard{s.ids[static_cast<size_t>(i)], s.rows.which[0][static_cast<size_t>(i)]};
+  for (int64_t j = 0; j < e.nb; ++j) a.vocab[j] = s.vocab.which[0][static_cast<size_t>(j)];
+  a.T = static_cast<int32_t>(e.T);
+  a.ts = static_cast<int32_t>(e.ts);
+  a.token_shards = static_cast<int32_t>(e.na);
+  a.V = static_cast<int32_t>(e.V);
+  a.vs = static_cast<int32_t>(e.vs);
+  a.vocab_shards = static_cast<int32_t>(e.nb);
+  a.M = static_cast<int32_t>(e.M);
+  a.ld_rows = static_cast<int32_t>(s.ld_rows);
+  a.ld_vocab = s.ld_vocab;
+  a.scale = scale;
+  return a;
+}
+
+template <typename T>
+int32_t launch_embed(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
+  const int64_t rows = static_cast<int64_t>(a.ts) * a.token_shards;
+  constexpr int n = Sixteen<T>::n;
+  if (vocab_dim == 0) {
+    const int log = row_lanes_log(a.M, n);
+    const int64_t piece = static_cast<int64_t>(kEmbedUnroll) * n << log, per_group = int64_t(4) << (6 - log);
+    const dim3 grid(static_cast<unsigned>((rows + per_group - 1) / per_group), static_cast<unsigned>((a.M + piece - 1) / piece));
+    if (grid.y > 65535) return GSPMD_ERR_UNSUPPORTED;
+    if (a.scale == 1.f) hipLaunchKernelGGL((embed_rows_kernel<T, false>), grid, dim3(256), 0, stream, a, log);
+    else hipLaunchKernelGGL((embed_rows_kernel<T, true>), grid, dim3(256), 0, stream, a, log);
+  } else {
+    const int64_t token_blocks = (rows + kColumnTokens - 1) / kColumnTokens, col_blocks = (a.M + kColumnCols - 1) / kColumnCols;
+    const int64_t groups = 8 * token_blocks * ((col_blocks + 7) / 8);
+    if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((embed_columns_kernel<T>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, stream, a, static_cast<int>(token_blocks), static_cast<int>(col_blocks));
+  }
+  return launched();
+}
+
+template <typename T>
+int32_t launch_chunks(const EmbedArgs& a, hipStream_t stream) {
+  constexpr int n = Sixteen<T>::n;
+  const dim3 grid(static_cast<unsigned>(a.T / kChunk), static_cast<unsigned>((a.M + 64 * n - 1) / (64 * n)));
+  if (grid.y > 65535) return GSPMD_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL((embed_chunks_kernel<T>), grid, dim3(256), 0, stream, a);
+  return launched();
+}
+
+template <typename T>
+int32_t launch_gradient(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
+  constexpr int n = Sixteen<T>::n;
+  if (vocab_dim == 0) {
+    const int log = row_lanes_log(a.M, n);
+    int across = 0;
+    while (across < 2 && (static_cast<int64_t>(n) << (log + across)) < a.M) ++across;
+    const int64_t piece = static_cast<int64_t>(n) << (log + across), rows = static_cast<int64_t>(a.vs) * a.vocab_shards;
+    const dim3 grid(static_cast<unsigned>((rows + kRowsSide - 1) / kRowsSide), static_cast<unsigned>((a.M + piece - 1) / piece));
+    if (grid.y > 65535) return GSPMD_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((embed_grad_rows_kernel<T>), grid, dim3(256), 0, stream, a, log, across);
+  } else {
+    const dim3 grid(static_cast<unsigned>((a.vs + kTurnEntries - 1) / kTurnEntries * a.vocab_shards), static_cast<unsigned>((a.M + kTurnRows - 1) / kTurnRows));
+    if (grid.y > 65535) return GSPMD_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((embed_grad_columns_kernel<T>), grid, dim3(256), 0, stream, a);
+  }
+  return launched();
+}
+
+}  // namespace
+}  // namespace gspmd
+
+using namespace gspmd;
+
+extern "C" {
+
+int32_t gspmd_embed(const gspmd_mesh* mesh, const int32_t* const* ids, const gspmd_shard_buf* w_shards, const gspmd_sharding* w_sh, int32_t vocab_dim, float scale,
+                    const gspmd_shard_buf* y_shards, const gspmd_sharding* y_sh, void* hip_stream) try {
+  if (!ids || !w_shards || !y_shards) return GSPMD_ERR_NULL;
+  Embed e;
+  int32_t st = analyse(mesh, y_sh, w_sh, vocab_dim, &e);
+  if (st != GSPMD_OK) return st;
+  Shards s{{}, Replicas(e.na), Replicas(e.nb)};
+  if ((st = collect(mesh, e, ids, y_shards, w_shards, &s)) != GSPMD_OK) return st;
+  if (e.T == 0 || e.M == 0 || launches_are_dry()) return GSPMD_OK;
+  EmbedArgs a = arguments(e, s, scale);
+  for (const auto& level : s.rows.which) {
+    for (int64_t i = 0; i < e.na; ++i) a.tokens[i].rows = level[static_cast<size_t>(i)];
+    st = y_shards[0].dtype == GSPMD_BF16 ? launch_embed<bf16_bits>(a, vocab_dim, static_cast<hipStream_t>(hip_stream)) : launch_embed<float>(a, vocab_dim, static_cast<hipStream_t>(hip_stream));
+    if (st != GSPMD_OK) return st;
+  }
+  return GSPMD_OK;
+} catch (...) { return GSPMD_ERR_HOST_MEMORY; }
+
+int32_t gspmd_embed_grad_workspace_bytes(const gspmd_mesh* mesh, const gspmd_sharding* dy_sh, const gspmd_sharding* dw_sh, int32_t vocab_dim, int32_t dtype, int64_t* bytes) try {
+  if (!bytes) return GSPMD_ERR_NULL;
+  Embed e;
+  const int32_t st = analyse(mesh, dy_sh, dw_sh, vocab_dim, &e);
+  if (st != GSPMD_OK) return st;
+  if (dtype != GSPMD_F32 && dtype != GSPMD_BF16) return GSPMD_ERR_UNSUPPORTED;
+  *bytes = e.bytes();
+  return GSPMD_OK;
+} catch (...) { return GSPMD_ERR_HOST_MEMORY; }
+
+int32_t gspmd_embed_grad(const gspmd_mesh* mesh, const int32_t* const* ids, const gspmd_shard_buf* dy_shards, const gspmd_sharding* dy_sh, const gspmd_shard_buf* dw_shards,
+                         const gspmd_sharding* dw_sh, int32_t vocab_dim, float scale, int32_t accumulate, void* workspace, int64_t workspace_bytes, void* hip_stream) try {
+  if (!ids || !dy_shards || !dw_shards) return GSPMD_ERR_NULL;
+  Embed e;
+  int32_t st = analyse(mesh, dy_sh, dw_sh, vocab_dim, &e);
+  if (st != GSPMD_OK) return st;
+  Shards s{{}, Replicas(e.na), Replicas(e.nb)};
+  if ((st = collect(mesh, e, ids, dy_shards, dw_shards, &s)) != GSPMD_OK) return st;
+  if (e.bytes() > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & (kWsAlign - 1)) || workspace_bytes < e.bytes())) return GSPMD_ERR_WORKSPACE;
+  if (e.M == 0 || launches_are_dry()) return GSPMD_OK;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const bool bf16 = dy_shards[0].dtype == GSPMD_BF16;
+  EmbedArgs a = arguments(e, s, scale);
+  a.accumulate = accumulate != 0;
+  if (e.T > 0) {
+    char* at = static_cast<char*>(workspace);
+    int32_t* const keys = reinterpret_cast<int32_t*>(at);
+    int32_t* const order = reinterpret_cast<int32_t*>(at + e.list_bytes());
+    at += 2 * e.list_bytes();
+    SortKeys in{};
+    for (int64_t i = 0; i < e.na; ++i) in.shard[i] = s.ids[static_cast<size_t>(i)];
+    in.per = a.ts;
+    in.shards = a.token_shards;
+    in.count = a.T;
+    in.keys = a.V;
+    if ((st = run_sort(in, SortOut{keys, order, nullptr, nullptr}, at, stream)) != GSPMD_OK) return st;
+    a.keys = keys;
+    a.order = order;
+    a.chunks = reinterpret_cast<float*>(at + round_up(sort_bytes(e.T, e.V), kWsAlign));
+    if (e.chunks() > 0 && (st = bf16 ? launch_chunks<bf16_bits>(a, stream) : launch_chunks<float>(a, stream)) != GSPMD_OK) return st;
+  }
+  for (const auto& level : s.vocab.which) {
+    for (int64_t j = 0; j < e.nb; ++j) a.vocab[j] = level[static_cast<size_t>(j)];
+    if ((st = bf16 ? launch_gradient<bf16_bits>(a, vocab_dim, stream) : launch_gradient<float>(a, vocab_dim, stream)) != GSPMD_OK) return st;
+  }
+  return GSPMD_OK;
+} catch (...) { return GSPMD_ERR_HOST_MEMORY; }
+
+}  // extern "C"

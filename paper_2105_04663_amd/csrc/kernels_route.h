@@ -1,0 +1,298 @@
+// The choice of experts and the exchange of rows with them (gspmd_route, gspmd_dispatch, gspmd_combine and their gradients).
+//
+// Routing: sixteen lanes have a token, each R neighbouring experts in registers.  The largest logit is found k times over: every lane's own, a maximum over the sixteen by rotations
+// within their row of the wave, and of those that have it the lowest lane, whose experts are the lowest.  It is bound by that chain, 8 + 3 R instructions a choice, not by the logits.
+// Exchange: bound by memory, rows copied or added up 16 bytes a lane.  Every row has one writer; a token's rows are added in the order of its choices.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kernels_basic.h"
+#include "kernels_embed.h"
+#include "mfma_common.h"
+
+namespace gspmd {
+
+constexpr int kRouteLanes = 16, kMostExperts = GSPMD_MAX_EXPERTS, kMostChoices = GSPMD_MAX_CHOICES;
+static_assert(kMostChoices <= kRouteLanes, "a lane for every choice");
+
+struct RouteArgs {
+  struct Shard {
+    const void* logits;
+    void* dlogits;                 // null: none to be written
+  } shard[kTokenShards];           // (first in the kernel's arguments: read there)
+  int32_t T, ts, shards, E, k, ld, ld_d;
+  int32_t normalise;
+  int32_t* experts;                // [T][k]
+  float* weights;                  // [T][k]
+  const float* dweights;           // the gradient's
+};
+
+// v combined over the sixteen lanes of a row, in all of them.  (Rotations: every lane adds in another order, but of max and of the two-by-two sums the bits are the same.)
+template <typename Op>
+__device__ __forceinline__ float over_row(float v, Op op) {
+  auto turned = [](float x, auto ctrl) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true)); };
+  v = op(v, turned(v, std::integral_constant<int, 0x128>{}));      // row_ror:8
+  v = op(v, turned(v, std::integral_constant<int, 0x124>{}));
+  v = op(v, turned(v, std::integral_constant<int, 0x122>{}));
+  return op(v, turned(v, std::integral_constant<int, 0x121>{}));
+}
+__device__ __forceinline__ float row_max(float v) { return over_row(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float row_sum(float v) { return over_row(v, [](float a, float b) { return a + b; }); }
+// of those lanes of this one's row of sixteen that say yes, a mask
+__device__ __forceinline__ uint32_t row_ballot(bool yes, int lane) { return static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(yes) >> (lane & 48)) & 0xffffu; }
+
+// This lane's experts' logits, -infinity where there are none; NaN as -infinity, and whether there was one among the token's.
+template <typename T, int R>
+__device__ __forceinline__ bool route_load(const T* z, int E, int of_row, int lane, float (&v)[R]) {
+  bool strange = false;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int e = of_row * R + r;
+    v[r] = -INFINITY;
+    if (z != nullptr && e < E) v[r] = load_as_float<T>((const T*)z + e);
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (v[r] != v[r]) {
+      strange = true;
+      v[r] = -INFINITY;
+    }
+  return row_ballot(strange, lane) != 0;
+}
+
+// The sum of exp(logit - most) over a token's experts; NaN where a logit is.
+template <int R>
+__device__ __forceinline__ float route_total(const float (&v)[R], float most, bool strange) {
+  float sum = 0.f;
+#pragma unroll
+  for (int r = 0; r < R; ++r) sum += expf(v[r] - most);
+  sum = row_sum(sum);
+  return strange ? NAN : sum;
+}
+
+template <typename T, int R>
+__global__ __launch_bounds__(256) void route_kernel(const RouteArgs a) {
+  const int lane = threadIdx.x & 63, of_row = lane & 15, token = (blockIdx.x * 256 + threadIdx.x) / kRouteLanes;
+  const T* z = nullptr;
+  if (token < a.T) {
+    const int shard = embed_shard(token, a.ts, a.shards);
+    z = static_cast<const T*>(first_kernel_argument<RouteArgs>()->shard[shard].logits) + static_cast<int64_t>(token - shard * a.ts) * a.ld;
+  }
+  float v[R];
+  const bool strange = route_load<T, R>(z, a.E, of_row, lane, v);
+  float best = v[0];
+#pragma unroll
+  for (int r = 1; r < R; ++r) best = fmaxf(best, v[r]);
+  const float most = row_max(best);
+  float total = a.normalise ? 0.f : route_total<R>(v, most, strange);
+  int expert = -1;
+  float logit = -INFINITY;
+  for (int i = 0; i < a.k; ++i) {
+    int at = 0;
+    best = v[0];
+#pragma unroll
+    for (int r = 1; r < R; ++r)
+      if (v[r] > best) {
+        best = v[r];
+        at = r;
+      }
+    const float here = row_max(best);
+    const uint32_t those = row_ballot(best == here && here > -INFINITY, lane);
+    if (those != 0) {                            // (alike for the sixteen lanes)
+      const int winner = __builtin_ctz(those), chosen = __shfl(of_row * R + at, (lane & 48) + winner);
+      if (of_row == i) {
+        expert = chosen;
+        logit = here;
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (of_row * R + r == chosen) v[r] = -INFINITY;
+    }
+  }
+  float share = expert >= 0 ? expf(logit - most) : 0.f;
+  if (a.normalise) total = row_sum(share);
+  if (token < a.T && of_row < a.k) {
+    a.experts[static_cast<int64_t>(token) * a.k + of_row] = expert;
+    a.weights[static_cast<int64_t>(token) * a.k + of_row] = expert >= 0 ? share / total : 0.f;
+  }
+}
+
+// dlogits: of weights from all experts p (g - sum p g), g zero where not chosen; from the chosen ones the same among them, zeros elsewhere.
+template <typename T, int R>
+__global__ __launch_bounds__(256) void route_grad_kernel(const RouteArgs a) {
+  const int lane = threadIdx.x & 63, of_row = lane & 15, token = (blockIdx.x * 256 + threadIdx.x) / kRouteLanes;
+  const bool in = token < a.ts * a.shards, live = token < a.T;
+  const int shard = in ? embed_shard(token, a.ts, a.shards) : 0, within = token - shard * a.ts;
+  const T* z = live && !a.normalise ? static_cast<const T*>(first_kernel_argument<RouteArgs>()->shard[shard].logits) + static_cast<int64_t>(within) * a.ld : nullptr;
+  T* const d = in ? static_cast<T*>(first_kernel_argument<RouteArgs>()->shard[shard].dlogits) : nullptr;
+  float v[R];
+  if (a.normalise) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = 0.f;
+  } else {
+    const bool strange = route_load<T, R>(z, a.E, of_row, lane, v);
+    float best = v[0];
+#pragma unroll
+    for (int r = 1; r < R; ++r) best = fmaxf(best, v[r]);
+    const float most = row_max(best), total = route_total<R>(v, most, strange);
+    const bool none = most == -INFINITY && !strange;        // no expert at all
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = none ? 0.f : expf(v[r] - most) / total;
+  }
+  const int64_t at = static_cast<int64_t>(token) * a.k + of_row;
+  const bool mine = live && of_row < a.k;
+  const int expert = mine ? a.experts[at] : -1;
+  const bool chosen = expert >= 0 && expert < a.E;
+  const float w = chosen ? a.weights[at] : 0.f, g = chosen ? a.dweights[at] : 0.f;
+  const float mean = row_sum(w * g);
+#pragma unroll
+  for (int r = 0; r < R; ++r) v[r] *= -mean;
+  const float own = a.normalise ? w * (g - mean) : w * g;
+  for (int i = 0; i < a.k; ++i) {
+    const int e = __shfl(chosen ? expert : -1, (lane & 48) + i);
+    const float add = __shfl(own, (lane & 48) + i);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (of_row * R + r == e) v[r] += add;
+  }
+  if (d == nullptr) return;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (of_row * R + r < a.E) store_from_float<T>(d + static_cast<int64_t>(within) * a.ld_d + of_row * R + r, live ? v[r] : 0.f);
+}
+
+// ---- the exchange
+constexpr int kExpertShards = 64;
+struct ExchangeArgs {
+  void* tokens[kTokenShards];      // rows by token: x, y or dy; null: none to be written.  (These three first in the kernel's arguments: read there.)
+  void* rows[kExpertShards];       // by slot, of the experts' shards
+  void* drows[kExpertShards];
+  int32_t T, ts, token_shards, k, E, es, expert_shards, M;
+  int64_t ld_tokens, ld_rows, ld_drows;
+  const int32_t *experts, *slots, *order;
+  const float* weights;            // null: all 1
+  float* dweights;
+};
+__device__ __forceinline__ const GSPMD_KERNARG ExchangeArgs* exchange_arguments() { return first_kernel_argument<ExchangeArgs>(); }
+
+// The shard of choice `o`'s expert, or -1 if it has none.
+__device__ __forceinline__ int expert_shard(const ExchangeArgs& a, int o) {
+  if (a.expert_shards == 1) return 0;
+  const uint32_t e = static_cast<uint32_t>(((GSPMD_GLOBAL const int32_t*)a.experts)[o]);
+  return e < static_cast<uint32_t>(a.E) ? static_cast<int>(e / static_cast<uint32_t>(a.es)) : -1;
+}
+
+// rows[slot] = x[token of the slot]: a wave has a piece of a row, or a few short rows; blockIdx.y the piece.
+constexpr int kExchangeUnroll = 4;
+template <typename T>
+__global__ __launch_bounds__(256) void dispatch_kernel(const ExchangeArgs a, int log_lanes) {
+  constexpr int n = Sixteen<T>::n;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lanes = 1 << log_lanes;
+  const int slot = ((blockIdx.x * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);
+  if (slot >= a.T * a.k) return;
+  const int o = ((GSPMD_GLOBAL const int32_t*)a.order)[slot];
+  if (static_cast<uint32_t>(o) >= static_cast<uint32_t>(a.T * a.k)) return;
+  const int part = expert_shard(a, o);
+  if (part < 0) return;
+  T* const to = static_cast<T*>(exchange_arguments()->rows[part]);
+  if (to == nullptr) return;
+  const int token = static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(a.k)), shard = embed_shard(token, a.ts, a.token_shards);
+  const T* const x = static_cast<const T*>(exchange_arguments()->tokens[shard]) + (token - shard * a.ts) * a.ld_tokens;
+  const int col0 = ((blockIdx.y * kExchangeUnroll) << log_lanes) * n + (lane & (lanes - 1)) * n, step = n << log_lanes;
+  u32x4_t v[kExchangeUnroll];
+#pragma unroll
+  for (int u = 0; u < kExchangeUnroll; ++u)
+    if (col0 + u * step < a.M) v[u] = load_up_to(x + col0 + u * step, a.M - col0 - u * step);
+#pragma unroll
+  for (int u = 0; u < kExchangeUnroll; ++u)
+    if (col0 + u * step < a.M) store_up_to(to + slot * a.ld_rows + col0 + u * step, v[u], a.M - col0 - u * step);
+}
+
+// y[t] = sum over t's choices of weight * rows[slot], in float32, in their order; what has no slot adds nothing.
+constexpr int kCombineAhead = 4;
+template <typename T>
+__global__ __launch_bounds__(256) void combine_kernel(const ExchangeArgs a, int log_lanes) {
+  constexpr int n = Sixteen<T>::n;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lanes = 1 << log_lanes;
+  const int token = ((blockIdx.x * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);
+  if (token >= a.ts * a.token_shards) return;
+  const int shard = embed_shard(token, a.ts, a.token_shards), col = ((blockIdx.y << log_lanes) + (lane & (lanes - 1))) * n;
+  T* const y = static_cast<T*>(exchange_arguments()->tokens[shard]);
+  if (y == nullptr || col >= a.M) return;
+  float sum[n];
+#pragma unroll
+  for (int e = 0; e < n; ++e) sum[e] = 0.f;
+  if (token < a.T) {
+    for (int i = 0; i < a.k; i += kCombineAhead) {
+      u32x4_t v[kCombineAhead];
+      float w[kCombineAhead];
+#pragma unroll
+      for (int u = 0; u < kCombineAhead; ++u) {
+        v[u] = u32x4_t{0u, 0u, 0u, 0u};
+        w[u] = 0.f;
+        if (i + u >= a.k) continue;
+        const int o = token * a.k + i + u, slot = ((GSPMD_GLOBAL const int32_t*)a.slots)[o], part = expert_shard(a, o);
+        if (static_cast<uint32_t>(slot) >= static_cast<uint32_t>(a.T * a.k) || part < 0) continue;
+        w[u] = a.weights ? ((GSPMD_GLOBAL const float*)a.weights)[o] : 1.f;
+        v[u] = load_up_to(static_cast<const T*>(exchange_arguments()->rows[part]) + slot * a.ld_rows + col, a.M - col);
+      }
+#pragma unroll
+      for (int u = 0; u < kCombineAhead; ++u) {
+        float f[n];
+        Sixteen<T>::open(v[u], f);
+#pragma unroll
+        for (int e = 0; e < n; ++e) sum[e] = fmaf(w[u], f[e], sum[e]);
+      }
+    }
+  }
+  store_up_to(y + (token - shard * a.ts) * a.ld_tokens + col, Sixteen<T>::close(sum), a.M - col);
+}
+
+// drows[slot] = weight * dy[t] and dweight = the product of dy[t] and rows[slot], a wave for a choice (or a few with short rows).
+template <typename T>
+__global__ __launch_bounds__(256) void combine_grad_kernel(const ExchangeArgs a, int log_lanes) {
+  constexpr int n = Sixteen<T>::n, kAhead = 2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lanes = 1 << log_lanes;
+  const int o = ((blockIdx.x * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);
+  const bool in = o < a.T * a.k;
+  const int slot = in ? ((GSPMD_GLOBAL const int32_t*)a.slots)[o] : -1, part = in ? expert_shard(a, o) : -1;
+  const bool there = static_cast<uint32_t>(slot) < static_cast<uint32_t>(a.T * a.k) && part >= 0;
+  float dot = 0.f;
+  if (there) {
+    const int token = static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(a.k)), shard = embed_shard(token, a.ts, a.token_shards);
+    const T* const dy = static_cast<const T*>(exchange_arguments()->tokens[shard]) + (token - shard * a.ts) * a.ld_tokens;
+    const T* const row = static_cast<const T*>(exchange_arguments()->rows[part]) + slot * a.ld_rows;
+    T* drow = static_cast<T*>(exchange_arguments()->drows[part]);
+    if (drow != nullptr) drow += slot * a.ld_drows;
+    const float w = ((GSPMD_GLOBAL const float*)a.weights)[o];
+    const int step = n << log_lanes;
+    for (int col0 = (lane & (lanes - 1)) * n; col0 < a.M; col0 += kAhead * step) {
+      u32x4_t g[kAhead], v[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int col = col0 + u * step;
+        g[u] = v[u] = u32x4_t{0u, 0u, 0u, 0u};
+        if (col >= a.M) continue;
+        g[u] = load_up_to(dy + col, a.M - col);
+        v[u] = load_up_to(row + col, a.M - col);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int col = col0 + u * step;
+        float p[n], q[n];
+        Sixteen<T>::open(g[u], p);
+        Sixteen<T>::open(v[u], q);
+#pragma unroll
+        for (int e = 0; e < n; ++e) dot = fmaf(p[e], q[e], dot);
+#pragma unroll
+        for (int e = 0; e < n; ++e) p[e] *= w;
+        if (drow != nullptr && col < a.M) store_up_to(drow + col, Sixteen<T>::close(p), a.M - col);
+      }
+    }
+  }
+  for (int by = 1; by < lanes; by *= 2) dot += __shfl_xor(dot, by);
+  if (in && (lane & (lanes - 1)) == 0) a.dweights[o] = there ? dot : 0.f;
+}
+
+}  // namespace gspmd
