@@ -143,6 +143,9 @@ def load_library():
         _call = None
     if _call is not None:
         _call.bind(C.cast(lib.gspmd_grouped_dot, C.c_void_p).value, C.cast(lib.gspmd_local_dot, C.c_void_p).value, Mesh, DotDims, Sharding, ShardBuf)
+        # (numbers of the entry points for the native entry: their order here)
+        _call.bind_tokens(tuple(C.cast(getattr(lib, "gspmd_" + name), C.c_void_p).value for name in
+                                ("ragged_dot", "embed", "embed_grad", "route", "route_grad", "dispatch", "combine", "combine_grad")), RouteBuf)
         _CALL = _call
     _LIB = lib
     return lib
@@ -536,6 +539,9 @@ def softmax_distill(mesh: Mesh, x_shards: Sequence[ShardBuf], x_sh: Sharding, w_
                                                 dxs, dws, C.c_void_p(workspace), int(workspace_bytes), C.c_void_p(stream)), "gspmd_softmax_distill")
 
 
+_RAGGED, _EMBED, _EMBED_GRAD, _ROUTE, _ROUTE_GRAD, _DISPATCH, _COMBINE, _COMBINE_GRAD = range(8)
+
+
 def _per_partition(mesh: Mesh, *shards):
     if any(len(s) != mesh.n_partitions for s in shards):
         raise ValueError("one shard buffer per partition is required")
@@ -544,6 +550,10 @@ def _per_partition(mesh: Mesh, *shards):
 def ragged_dot(mesh: Mesh, dims: DotDims, lhs_shards: Sequence[ShardBuf], lhs_sh: Sharding, rhs_shards: Sequence[ShardBuf], rhs_sh: Sharding,
                out_shards: Sequence[ShardBuf], out_sh: Sharding, sizes: int, stream: int = 0, epilogue: int = EPILOGUE_NONE) -> None:
     """Products grouped by expert over packed rows; sizes: address of the experts' int32 row counts in device memory (gspmd_ragged_dot)."""
+    if _CALL is not None:
+        status = _CALL.token_call(_RAGGED, mesh, dims, lhs_shards, lhs_sh, rhs_shards, rhs_sh, out_shards, out_sh, sizes, epilogue, stream)
+        if status is not None:
+            return _check(status, "gspmd_ragged_dot")
     _per_partition(mesh, lhs_shards, rhs_shards, out_shards)
     m, d, a, b, o = mesh._c(), dims._c(), lhs_sh._c(), rhs_sh._c(), out_sh._c()
     _check(load_library().gspmd_ragged_dot(C.byref(m), C.byref(d), _bufs(lhs_shards), C.byref(a), _bufs(rhs_shards), C.byref(b), _bufs(out_shards), C.byref(o),
@@ -557,6 +567,10 @@ def _id_arrays(ids: Sequence[int]):
 def embed(mesh: Mesh, ids: Sequence[int], w_shards: Sequence[ShardBuf], w_sh: Sharding, y_shards: Sequence[ShardBuf], y_sh: Sharding,
           vocab_dim: int = 0, scale: float = 1.0, stream: int = 0) -> None:
     """Rows of the split vocabulary matrix by tokens' entries; ids: one address per partition (gspmd_embed)."""
+    if _CALL is not None:
+        status = _CALL.token_call(_EMBED, mesh, ids, w_shards, w_sh, vocab_dim, scale, y_shards, y_sh, stream)
+        if status is not None:
+            return _check(status, "gspmd_embed")
     _per_partition(mesh, ids, w_shards, y_shards)
     m, a, b = mesh._c(), w_sh._c(), y_sh._c()
     _check(load_library().gspmd_embed(C.byref(m), _id_arrays(ids), _bufs(w_shards), C.byref(a), int(vocab_dim), float(scale), _bufs(y_shards), C.byref(b), C.c_void_p(stream)), "gspmd_embed")
@@ -571,6 +585,10 @@ def embed_grad_workspace_bytes(mesh: Mesh, dy_sh: Sharding, dw_sh: Sharding, voc
 def embed_grad(mesh: Mesh, ids: Sequence[int], dy_shards: Sequence[ShardBuf], dy_sh: Sharding, dw_shards: Sequence[ShardBuf], dw_sh: Sharding, vocab_dim: int = 0,
                scale: float = 1.0, accumulate: bool = False, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
     """Gradient of embed with respect to the vocabulary matrix, written or (accumulate) added to dw (gspmd_embed_grad)."""
+    if _CALL is not None:
+        status = _CALL.token_call(_EMBED_GRAD, mesh, ids, dy_shards, dy_sh, dw_shards, dw_sh, vocab_dim, scale, accumulate, workspace, workspace_bytes, stream)
+        if status is not None:
+            return _check(status, "gspmd_embed_grad")
     _per_partition(mesh, ids, dy_shards, dw_shards)
     m, a, b = mesh._c(), dy_sh._c(), dw_sh._c()
     _check(load_library().gspmd_embed_grad(C.byref(m), _id_arrays(ids), _bufs(dy_shards), C.byref(a), _bufs(dw_shards), C.byref(b), int(vocab_dim), float(scale), int(bool(accumulate)),
@@ -599,6 +617,10 @@ def route_workspace_bytes(mesh: Mesh, logits_sh: Sharding, choices: int) -> int:
 def route(mesh: Mesh, logits_shards: Sequence[ShardBuf], logits_sh: Sharding, choices: int, route: RouteBuf, normalise: bool = False,
           workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
     """Choose every token's experts, their weights and slots (gspmd_route)."""
+    if _CALL is not None:
+        status = _CALL.token_call(_ROUTE, mesh, logits_shards, logits_sh, choices, normalise, route, workspace, workspace_bytes, stream)
+        if status is not None:
+            return _check(status, "gspmd_route")
     _per_partition(mesh, logits_shards)
     m, a, r = mesh._c(), logits_sh._c(), route._c()
     _check(load_library().gspmd_route(C.byref(m), _bufs(logits_shards), C.byref(a), int(choices), int(bool(normalise)), C.byref(r), C.c_void_p(workspace), int(workspace_bytes),
@@ -608,6 +630,10 @@ def route(mesh: Mesh, logits_shards: Sequence[ShardBuf], logits_sh: Sharding, ch
 def route_grad(mesh: Mesh, logits_shards: Sequence[ShardBuf], logits_sh: Sharding, choices: int, route: RouteBuf, dweights: int, dlogits_shards: Sequence[ShardBuf],
                normalise: bool = False, stream: int = 0) -> None:
     """Gradient of route's weights with respect to the logits (gspmd_route_grad)."""
+    if _CALL is not None:
+        status = _CALL.token_call(_ROUTE_GRAD, mesh, logits_shards, logits_sh, choices, normalise, route, dweights, dlogits_shards, stream)
+        if status is not None:
+            return _check(status, "gspmd_route_grad")
     _per_partition(mesh, logits_shards, dlogits_shards)
     m, a, r = mesh._c(), logits_sh._c(), route._c()
     _check(load_library().gspmd_route_grad(C.byref(m), _bufs(logits_shards), C.byref(a), int(choices), int(bool(normalise)), C.byref(r), C.c_void_p(dweights), _bufs(dlogits_shards),
@@ -616,6 +642,10 @@ def route_grad(mesh: Mesh, logits_shards: Sequence[ShardBuf], logits_sh: Shardin
 
 def dispatch(mesh: Mesh, x_shards: Sequence[ShardBuf], x_sh: Sharding, choices: int, route: RouteBuf, rows_shards: Sequence[ShardBuf], rows_sh: Sharding, stream: int = 0) -> None:
     """Tokens' rows to their experts' slots (gspmd_dispatch)."""
+    if _CALL is not None:
+        status = _CALL.token_call(_DISPATCH, mesh, x_shards, x_sh, choices, route, rows_shards, rows_sh, stream)
+        if status is not None:
+            return _check(status, "gspmd_dispatch")
     _per_partition(mesh, x_shards, rows_shards)
     m, a, b, r = mesh._c(), x_sh._c(), rows_sh._c(), route._c()
     _check(load_library().gspmd_dispatch(C.byref(m), _bufs(x_shards), C.byref(a), int(choices), C.byref(r), _bufs(rows_shards), C.byref(b), C.c_void_p(stream)), "gspmd_dispatch")
@@ -624,6 +654,10 @@ def dispatch(mesh: Mesh, x_shards: Sequence[ShardBuf], x_sh: Sharding, choices: 
 def combine(mesh: Mesh, rows_shards: Sequence[ShardBuf], rows_sh: Sharding, choices: int, route: RouteBuf, y_shards: Sequence[ShardBuf], y_sh: Sharding,
             weighted: bool = True, stream: int = 0) -> None:
     """Experts' rows added up for their tokens (gspmd_combine)."""
+    if _CALL is not None:
+        status = _CALL.token_call(_COMBINE, mesh, rows_shards, rows_sh, choices, route, weighted, y_shards, y_sh, stream)
+        if status is not None:
+            return _check(status, "gspmd_combine")
     _per_partition(mesh, rows_shards, y_shards)
     m, a, b, r = mesh._c(), rows_sh._c(), y_sh._c(), route._c()
     _check(load_library().gspmd_combine(C.byref(m), _bufs(rows_shards), C.byref(a), int(choices), C.byref(r), int(bool(weighted)), _bufs(y_shards), C.byref(b), C.c_void_p(stream)),
@@ -633,6 +667,10 @@ def combine(mesh: Mesh, rows_shards: Sequence[ShardBuf], rows_sh: Sharding, choi
 def combine_grad(mesh: Mesh, dy_shards: Sequence[ShardBuf], dy_sh: Sharding, rows_shards: Sequence[ShardBuf], rows_sh: Sharding, choices: int, route: RouteBuf,
                  drows_shards: Sequence[ShardBuf], dweights: int, stream: int = 0) -> None:
     """Gradients of combine with respect to the rows and the weights (gspmd_combine_grad)."""
+    if _CALL is not None:
+        status = _CALL.token_call(_COMBINE_GRAD, mesh, dy_shards, dy_sh, rows_shards, rows_sh, choices, route, drows_shards, dweights, stream)
+        if status is not None:
+            return _check(status, "gspmd_combine_grad")
     _per_partition(mesh, dy_shards, rows_shards, drows_shards)
     m, a, b, r = mesh._c(), dy_sh._c(), rows_sh._c(), route._c()
     _check(load_library().gspmd_combine_grad(C.byref(m), _bufs(dy_shards), C.byref(a), _bufs(rows_shards), C.byref(b), int(choices), C.byref(r), _bufs(drows_shards), C.c_void_p(dweights),

@@ -21,7 +21,7 @@ UNITS = [(os.path.join(CSRC, f"{name}.hip"), f"{name}_l{n}.o", [f"-DGSPMD_TU_LAY
     (os.path.join(CSRC, "gspmd.hip"), "gspmd.o", []),
     (os.path.join(CSRC, "ragged.hip"), "ragged.o", []),
     (os.path.join(CSRC, "softmax.hip"), "softmax.o", []),
-    (os.path.join(CSRC, "sort.hip"), "sort.o", []),
+    (os.path.join(CSRC, "order.hip"), "order.o", []),
     (os.path.join(CSRC, "embed.hip"), "embed.o", []),
     (os.path.join(CSRC, "route.hip"), "route.o", []),
     (os.path.join(CSRC, "plan.cpp"), "plan.o", []),

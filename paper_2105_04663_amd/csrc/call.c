@@ -1,9 +1,9 @@
-/* The two Dot entry points called from Python without ctypes, for arguments in their plain form: descriptor objects whose C form the binding
+/* The two Dot entry points, and those that choose by a token's index, called from Python without ctypes, for arguments in their plain form: descriptor objects whose C form the binding
  * holds (made from the very field objects they still have), lists or tuples of ShardBuf with int fields and of int fill counts.  Anything else is
  * handed back (None), and the binding converts it as ever, with the errors that belong to it.
  *
  * What a small call costs on the host is this conversion: of a Dot over 4 partitions 7.7 of 10.5 us, over 32 21 of 30 (ctypes, attribute by
- * attribute in Python); with it 0.9 and 4.
+ * attribute in Python); with it 0.9 and 4.  Of an embedding on one partition 7.6 us, with it 1.0.
  */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -184,6 +184,179 @@ static PyObject* local_dot(PyObject* self, PyObject* const* a, Py_ssize_t n_args
   return PyLong_FromLong(status);
 }
 
+/* ---- the entry points that choose by a token's index.  What each takes after its number: m mesh, d dot dimensions, s sharding, b shard buffers and a addresses (one for every
+ * partition), i a 32-bit and l a 64-bit integer, p an address, f a float, t whether something is true, r a routing's arrays. */
+enum { kRagged, kEmbed, kEmbedGrad, kRoute, kRouteGrad, kDispatch, kCombine, kCombineGrad, kTokenCalls };
+static const char* const takes[kTokenCalls] = {"mdbsbsbspip", "mabsifbsp", "mabsbsiftplp", "mbsitrplp", "mbsitrpbp", "mbsirbsp", "mbsirtbsp", "mbsbsirbpp"};
+enum { kMostArguments = 12, kMostLists = 3 };
+static void (*token_calls[kTokenCalls])(void);
+static PyObject* route_type;
+static PyObject* route_fields[5];
+
+typedef union {
+  const void* p;
+  int64_t l;
+  float f;
+} argument;
+
+static int routing(PyObject* obj, gspmd_route_buf* out) {
+  int64_t at[5];
+  if ((PyObject*)Py_TYPE(obj) != route_type) return 0;
+  PyObject* dict = PyObject_GenericGetDict(obj, NULL);
+  if (!dict) {
+    PyErr_Clear();
+    return 0;
+  }
+  int plain = 1;
+  for (int i = 0; plain && i < 5; ++i) plain = plain_int(PyDict_GetItem(dict, route_fields[i]), at + i) && at[i] >= 0;
+  Py_DECREF(dict);
+  if (!plain) return 0;
+  out->experts = (int32_t*)(uintptr_t)at[0];
+  out->weights = (float*)(uintptr_t)at[1];
+  out->slots = (int32_t*)(uintptr_t)at[2];
+  out->order = (int32_t*)(uintptr_t)at[3];
+  out->sizes = (int32_t*)(uintptr_t)at[4];
+  return 1;
+}
+
+static int addresses(PyObject* seq, int64_t n, const void** out) {
+  if (!PyList_CheckExact(seq) && !PyTuple_CheckExact(seq)) return 0;
+  if (PySequence_Fast_GET_SIZE(seq) != n) return 0;
+  for (int64_t i = 0; i < n; ++i) {
+    int64_t at;
+    if (!plain_int(PySequence_Fast_GET_ITEM(seq, i), &at) || at < 0) return 0;
+    out[i] = (const void*)(uintptr_t)at;
+  }
+  return 1;
+}
+
+#define M (v[0].p)
+#define P(i) (v[i].p)
+#define I(i) ((int32_t)v[i].l)
+#define W(i) ((void*)(uintptr_t)v[i].l)
+static int32_t token_status(int which, const argument* v) {
+  switch (which) {
+    case kRagged:
+      return ((int32_t (*)(const gspmd_mesh*, const gspmd_dot_dims*, const gspmd_shard_buf*, const gspmd_sharding*, const gspmd_shard_buf*, const gspmd_sharding*, const gspmd_shard_buf*,
+                           const gspmd_sharding*, const int32_t*, int32_t, void*))token_calls[which])(M, P(1), P(2), P(3), P(4), P(5), P(6), P(7), W(8), I(9), W(10));
+    case kEmbed:
+      return ((int32_t (*)(const gspmd_mesh*, const int32_t* const*, const gspmd_shard_buf*, const gspmd_sharding*, int32_t, float, const gspmd_shard_buf*, const gspmd_sharding*,
+                           void*))token_calls[which])(M, P(1), P(2), P(3), I(4), v[5].f, P(6), P(7), W(8));
+    case kEmbedGrad:
+      return ((int32_t (*)(const gspmd_mesh*, const int32_t* const*, const gspmd_shard_buf*, const gspmd_sharding*, const gspmd_shard_buf*, const gspmd_sharding*, int32_t, float, int32_t, void*,
+                           int64_t, void*))token_calls[which])(M, P(1), P(2), P(3), P(4), P(5), I(6), v[7].f, I(8), W(9), v[10].l, W(11));
+    case kRoute:
+      return ((int32_t (*)(const gspmd_mesh*, const gspmd_shard_buf*, const gspmd_sharding*, int32_t, int32_t, const gspmd_route_buf*, void*, int64_t, void*))token_calls[which])(
+          M, P(1), P(2), I(3), I(4), P(5), W(6), v[7].l, W(8));
+    case kRouteGrad:
+      return ((int32_t (*)(const gspmd_mesh*, const gspmd_shard_buf*, const gspmd_sharding*, int32_t, int32_t, const gspmd_route_buf*, const float*, const gspmd_shard_buf*,
+                           void*))token_calls[which])(M, P(1), P(2), I(3), I(4), P(5), W(6), P(7), W(8));
+    case kDispatch:
+      return ((int32_t (*)(const gspmd_mesh*, const gspmd_shard_buf*, const gspmd_sharding*, int32_t, const gspmd_route_buf*, const gspmd_shard_buf*, const gspmd_sharding*,
+                           void*))token_calls[which])(M, P(1), P(2), I(3), P(4), P(5), P(6), W(7));
+    case kCombine:
+      return ((int32_t (*)(const gspmd_mesh*, const gspmd_shard_buf*, const gspmd_sharding*, int32_t, const gspmd_route_buf*, int32_t, const gspmd_shard_buf*, const gspmd_sharding*,
+                           void*))token_calls[which])(M, P(1), P(2), I(3), P(4), I(5), P(6), P(7), W(8));
+    default:
+      return ((int32_t (*)(const gspmd_mesh*, const gspmd_shard_buf*, const gspmd_sharding*, const gspmd_shard_buf*, const gspmd_sharding*, int32_t, const gspmd_route_buf*, const gspmd_shard_buf*,
+                           float*, void*))token_calls[which])(M, P(1), P(2), P(3), P(4), I(5), P(6), P(7), W(8), W(9));
+  }
+}
+#undef M
+#undef P
+#undef I
+#undef W
+
+/* token_call(number, ..): status, or None */
+static PyObject* token_call(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
+  (void)self;
+  int64_t which, n = 1;
+  if (n_args < 2 || !plain_int(a[0], &which) || which < 0 || which >= kTokenCalls || !token_calls[which]) Py_RETURN_NONE;
+  const char* const sorts = takes[which];
+  const int count = (int)strlen(sorts);
+  if (n_args != count + 1) Py_RETURN_NONE;
+  PyObject* held[kMostArguments] = {NULL};
+  argument v[kMostArguments];
+  gspmd_route_buf route;
+  gspmd_shard_buf few[kMostLists * kOnStack], *bufs = few;
+  const void *few_at[kOnStack], **at = few_at;
+  int plain = (held[0] = held_form(a[1], mesh_type, mesh_fields, 2)) != NULL;
+  if (plain) {
+    const gspmd_mesh* const mesh = v[0].p = PyLong_AsVoidPtr(PyTuple_GET_ITEM(held[0], 3));
+    for (int32_t i = 0; i < mesh->rank && n > 0; ++i) n = mesh->shape[i] < 1 || mesh->shape[i] > kMost || n > kMost ? 0 : n * mesh->shape[i];
+    plain = n > 0;
+    if (plain && n > kOnStack) {
+      bufs = PyMem_Malloc((size_t)(kMostLists * n) * sizeof(*bufs));
+      at = PyMem_Malloc((size_t)n * sizeof(*at));
+      plain = bufs && at;
+    }
+  }
+  int lists = 0;
+  for (int i = 1; plain && i < count; ++i) {
+    PyObject* const x = a[i + 1];
+    argument* const to = v + i;
+    switch (sorts[i]) {
+      case 'd':
+      case 's':
+        plain = (held[i] = sorts[i] == 'd' ? held_form(x, dims_type, dims_fields, 4) : held_form(x, sharding_type, sharding_fields, 2)) != NULL;
+        if (plain) to->p = PyLong_AsVoidPtr(PyTuple_GET_ITEM(held[i], 3));
+        break;
+      case 'b':
+        to->p = bufs + lists * n;
+        plain = shards(x, n, bufs + lists++ * n);
+        break;
+      case 'a':
+        to->p = at;
+        plain = addresses(x, n, at);
+        break;
+      case 'r':
+        to->p = &route;
+        plain = routing(x, &route);
+        break;
+      case 'f':
+        plain = PyFloat_CheckExact(x);
+        if (plain) to->f = (float)PyFloat_AS_DOUBLE(x);
+        break;
+      case 't':
+        plain = PyBool_Check(x);
+        to->l = x == Py_True;
+        break;
+      default:
+        plain = plain_int(x, &to->l) && (sorts[i] != 'i' || to->l == (int32_t)to->l) && (sorts[i] != 'p' || to->l >= 0);
+    }
+  }
+  int32_t status = 0;
+  if (plain) {
+    Py_BEGIN_ALLOW_THREADS
+    status = token_status((int)which, v);
+    Py_END_ALLOW_THREADS
+  }
+  if (bufs != few) PyMem_Free(bufs);
+  if (at != few_at) PyMem_Free((void*)at);
+  for (int i = 0; i < count; ++i) Py_XDECREF(held[i]);
+  if (!plain) Py_RETURN_NONE;
+  return PyLong_FromLong(status);
+}
+
+/* bind_tokens(addresses of those entry points in the order above, RouteBuf) */
+static PyObject* bind_tokens(PyObject* self, PyObject* args) {
+  (void)self;
+  PyObject *calls, *route;
+  if (!PyArg_ParseTuple(args, "O!O", &PyTuple_Type, &calls, &route)) return NULL;
+  if (PyTuple_GET_SIZE(calls) != kTokenCalls) {
+    PyErr_SetString(PyExc_ValueError, "an address for every entry point is required");
+    return NULL;
+  }
+  for (int i = 0; i < kTokenCalls; ++i) {
+    void* p = PyLong_AsVoidPtr(PyTuple_GET_ITEM(calls, i));
+    if (PyErr_Occurred()) return NULL;
+    memcpy(&token_calls[i], &p, sizeof(p));
+  }
+  Py_INCREF(route);
+  route_type = route;
+  Py_RETURN_NONE;
+}
+
 /* bind(address of gspmd_grouped_dot, of gspmd_local_dot, Mesh, DotDims, Sharding, ShardBuf) */
 static PyObject* bind(PyObject* self, PyObject* args) {
   (void)self;
@@ -202,6 +375,8 @@ static PyMethodDef methods[] = {
   {"grouped_dot", (PyCFunction)(void (*)(void))grouped_dot, METH_FASTCALL, NULL},
   {"local_dot", (PyCFunction)(void (*)(void))local_dot, METH_FASTCALL, NULL},
   {"bind", bind, METH_VARARGS, NULL},
+  {"token_call", (PyCFunction)(void (*)(void))token_call, METH_FASTCALL, NULL},
+  {"bind_tokens", bind_tokens, METH_VARARGS, NULL},
   {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
@@ -219,5 +394,7 @@ PyMODINIT_FUNC PyInit__call(void) {
   dims_fields[1] = PyUnicode_InternFromString("rhs_batch");
   dims_fields[2] = PyUnicode_InternFromString("lhs_contract");
   dims_fields[3] = PyUnicode_InternFromString("rhs_contract");
+  const char* const names[5] = {"experts", "weights", "slots", "order", "sizes"};
+  for (int i = 0; i < 5; ++i) route_fields[i] = PyUnicode_InternFromString(names[i]);
   return PyModule_Create(&module);
 }

@@ -8,9 +8,8 @@
 #include "../../include/gspmd.h"
 #include "dots.h"
 #include "kernels_embed.h"
-#include "kernels_sort.h"
+#include "order.h"
 #include "plan.h"
-#include "sort.h"
 #include "tokens.h"
 
 namespace gspmd {
@@ -21,9 +20,10 @@ struct Embed {
   int64_t na = 1, nb = 1, ts = 0, vs = 0;       // shards of tokens and of the vocabulary, their static extents
   int axis_t = -1, axis_v = -1, vocab_dim = 0;
   int64_t chunks() const { return T / kChunk; }
-  // the workspace: sorted keys, their tokens, what sorting needs, sums of whole chunks
-  int64_t list_bytes() const { return round_up(T * 4, kWsAlign); }
-  int64_t bytes() const { return T == 0 ? 0 : 2 * list_bytes() + round_up(sort_bytes(T, V), kWsAlign) + round_up(chunks() * M * 4, kWsAlign); }
+  // the workspace: the tokens' order, where an entry's begin, sums of whole chunks
+  int64_t order_bytes() const { return round_up(T * 4, kWsAlign); }
+  int64_t begins_bytes() const { return round_up((V + 1) * 4, kWsAlign); }
+  int64_t bytes() const { return T == 0 ? 0 : order_bytes() + begins_bytes() + round_up(chunks() * M * 4, kWsAlign); }
 };
 
 int32_t analyse(const gspmd_mesh* mesh, const gspmd_sharding* rows_sh, const gspmd_sharding* w_sh, int32_t vocab_dim, Embed* e) {
@@ -99,10 +99,11 @@ int32_t launch_embed(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
   if (vocab_dim == 0) {
     const int log = row_lanes_log(a.M, n);
     const int64_t piece = static_cast<int64_t>(kEmbedUnroll) * n << log, per_group = int64_t(4) << (6 - log);
-    const dim3 grid(static_cast<unsigned>((rows + per_group - 1) / per_group), static_cast<unsigned>((a.M + piece - 1) / piece));
-    if (grid.y > 65535) return GSPMD_ERR_UNSUPPORTED;
-    if (a.scale == 1.f) hipLaunchKernelGGL((embed_rows_kernel<T, false>), grid, dim3(256), 0, stream, a, log);
-    else hipLaunchKernelGGL((embed_rows_kernel<T, true>), grid, dim3(256), 0, stream, a, log);
+    const int64_t pieces = (a.M + piece - 1) / piece, groups = (rows + per_group - 1) / per_group * pieces;
+    if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
+    const dim3 grid(static_cast<unsigned>(groups));
+    if (a.scale == 1.f) hipLaunchKernelGGL((embed_rows_kernel<T, false>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
+    else hipLaunchKernelGGL((embed_rows_kernel<T, true>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
   } else {
     const int64_t token_blocks = (rows + kColumnTokens - 1) / kColumnTokens, col_blocks = (a.M + kColumnCols - 1) / kColumnCols;
     const int64_t groups = 8 * token_blocks * ((col_blocks + 7) / 8);
@@ -191,19 +192,18 @@ int32_t gspmd_embed_grad(const gspmd_mesh* mesh, const int32_t* const* ids, cons
   a.accumulate = accumulate != 0;
   if (e.T > 0) {
     char* at = static_cast<char*>(workspace);
-    int32_t* const keys = reinterpret_cast<int32_t*>(at);
-    int32_t* const order = reinterpret_cast<int32_t*>(at + e.list_bytes());
-    at += 2 * e.list_bytes();
-    SortKeys in{};
+    int32_t* const order = reinterpret_cast<int32_t*>(at);
+    int32_t* const begins = reinterpret_cast<int32_t*>(at + e.order_bytes());
+    OrderKeys in{};
     for (int64_t i = 0; i < e.na; ++i) in.shard[i] = s.ids[static_cast<size_t>(i)];
     in.per = a.ts;
     in.shards = a.token_shards;
     in.count = a.T;
     in.keys = a.V;
-    if ((st = run_sort(in, SortOut{keys, order, nullptr, nullptr}, at, stream)) != GSPMD_OK) return st;
-    a.keys = keys;
+    if ((st = run_order(in, OrderOut{order, begins}, stream)) != GSPMD_OK) return st;
     a.order = order;
-    a.chunks = reinterpret_cast<float*>(at + round_up(sort_bytes(e.T, e.V), kWsAlign));
+    a.begins = begins;
+    a.chunks = reinterpret_cast<float*>(at + e.order_bytes() + e.begins_bytes());
     if (e.chunks() > 0 && (st = bf16 ? launch_chunks<bf16_bits>(a, stream) : launch_chunks<float>(a, stream)) != GSPMD_OK) return st;
   }
   for (const auto& level : s.vocab.which) {

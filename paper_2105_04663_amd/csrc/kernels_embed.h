@@ -2,8 +2,8 @@
 //
 // Both are bound by memory: the rows that are read and the rows that are written, once each.  A vocabulary matrix [V, M] has an entry's row in one piece, read and written 16 bytes a lane at
 // element alignment, neighbouring lanes side by side; in one [M, V] an entry is a column, and tiles turn in LDS.
-// The gradient has one writer for each of its elements: tokens are sorted by entry (kernels_sort.h), a row of dw is the sum over its run of them, in float32, in ascending order of the tokens -- but
-// for whole chunks of the sorted order that lie inside one run, which are added up by themselves first, so that an entry that half of a text consists of is no chain of
+// The gradient has one writer for each of its elements: tokens are ordered by entry (kernels_order.h), a row of dw is the sum over its run of them, in float32, in ascending order of the tokens -- but
+// for whole chunks of that order that lie inside one run, which are added up by themselves first, so that an entry that half of a text consists of is no chain of
 // thousands of loads.  So equal inputs give equal bits, and a row without tokens is zeros.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -30,11 +30,11 @@ struct EmbedArgs {
   int64_t ld_vocab;
   float scale;
   int32_t accumulate;
-  // the gradient's: the sorted order, and sums of whole chunks of it, [chunk][M]
-  const int32_t *keys, *order;
+  // the gradient's: tokens in the order of their entries, where an entry's begin [V + 1], and sums of whole chunks of the order, [chunk][M]
+  const int32_t *order, *begins;
   float* chunks;
 };
-constexpr int kChunk = 64;     // tokens
+constexpr int kChunk = 32;     // tokens
 
 typedef __attribute__((address_space(4))) const EmbedArgs embed_args;
 __device__ __forceinline__ embed_args* embed_arguments() { return first_kernel_argument<EmbedArgs>(); }
@@ -109,13 +109,14 @@ __host__ __device__ __forceinline__ int row_lanes_log(int elements, int per_lane
   return log;
 }
 
-// y [V, M]: a wave has a piece of a row (or a few short rows), kEmbedUnroll x 16 bytes a lane; blockIdx.y the piece.
+// y [V, M]: a wave has a piece of a row (or a few short rows), kEmbedUnroll x 16 bytes a lane.
 constexpr int kEmbedUnroll = 4;
 template <typename T, bool SCALED>
-__global__ __launch_bounds__(256) void embed_rows_kernel(const EmbedArgs a, int log_lanes) {
+__global__ __launch_bounds__(256) void embed_rows_kernel(const EmbedArgs a, int log_lanes, int pieces) {
   constexpr int n = Sixteen<T>::n;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lanes = 1 << log_lanes;
-  const int row = ((blockIdx.x * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);       // static rows of all shards, one after the other
+  const int group = blockIdx.x / pieces, piece = blockIdx.x - group * pieces;              // (neighbouring pieces of rows together)
+  const int row = ((group * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);            // static rows of all shards, one after the other
   if (row >= a.ts * a.token_shards) return;
   const int shard = embed_shard(row, a.ts, a.token_shards), within = row - shard * a.ts;
   const TokenShard to = {embed_arguments()->tokens[shard].ids, embed_arguments()->tokens[shard].rows};
@@ -125,7 +126,7 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(const EmbedArgs a, int 
   T* const y = static_cast<T*>(to.rows) + static_cast<int64_t>(within) * a.ld_rows;
   const int of = there ? embed_shard(id, a.vs, a.vocab_shards) : 0;
   const T* const w = static_cast<const T*>(embed_arguments()->vocab[of]) + (there ? static_cast<int64_t>(id - of * a.vs) * a.ld_vocab : 0);
-  const int col0 = ((blockIdx.y * kEmbedUnroll) << log_lanes) * n + (lane & (lanes - 1)) * n, step = n << log_lanes;
+  const int col0 = ((piece * kEmbedUnroll) << log_lanes) * n + (lane & (lanes - 1)) * n, step = n << log_lanes;
   u32x4_t v[kEmbedUnroll];
 #pragma unroll
   for (int u = 0; u < kEmbedUnroll; ++u) {
@@ -203,10 +204,10 @@ __device__ __forceinline__ const T* token_row(const EmbedArgs& a, int token) {
   return static_cast<const T*>(embed_arguments()->tokens[shard].rows) + static_cast<int64_t>(token - shard * a.ts) * a.ld_rows;
 }
 
-// sum += the `count` tokens' 16 bytes at `col` from place `at` of the sorted order on, ascending
+// sum += the `count` tokens' 16 bytes at `col` from place `at` of the order on, ascending
 template <typename T>
 __device__ __forceinline__ void add_tokens(const EmbedArgs& a, int at, int count, int col, float (&sum)[Sixteen<T>::n]) {
-  constexpr int n = Sixteen<T>::n, kAhead = 4;
+  constexpr int n = Sixteen<T>::n, kAhead = 8;
   GSPMD_GLOBAL const int32_t* const order = (GSPMD_GLOBAL const int32_t*)a.order + at;
   int i = 0;
   for (; i + kAhead <= count; i += kAhead) {
@@ -234,9 +235,11 @@ template <typename T>
 __global__ __launch_bounds__(256) void embed_chunks_kernel(const EmbedArgs a) {
   constexpr int n = Sixteen<T>::n;
   const int at = blockIdx.x * kChunk, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  GSPMD_GLOBAL const int32_t* const keys = (GSPMD_GLOBAL const int32_t*)a.keys;
-  const int key = keys[at];
-  if (key >= a.V || keys[at + kChunk - 1] != key) return;
+  GSPMD_GLOBAL const int32_t* const begins = (GSPMD_GLOBAL const int32_t*)a.begins;
+  if (at + kChunk > begins[a.V]) return;        // some of it no token's place
+  const int first = ((GSPMD_GLOBAL const int32_t*)a.order)[at], shard = embed_shard(first, a.ts, a.token_shards);
+  const int key = ((GSPMD_GLOBAL const int32_t*)embed_arguments()->tokens[shard].ids)[first - shard * a.ts];
+  if (static_cast<uint32_t>(key) >= static_cast<uint32_t>(a.V) || begins[key + 1] < at + kChunk) return;
   __shared__ float sums[4][64 * n];
   const int col = (blockIdx.y * 64 + lane) * n;
   float sum[n];
@@ -250,7 +253,7 @@ __global__ __launch_bounds__(256) void embed_chunks_kernel(const EmbedArgs a) {
   for (int i = threadIdx.x; i < 64 * n && blockIdx.y * 64 * n + i < a.M; i += 256) out[i] = ((sums[0][i] + sums[1][i]) + sums[2][i]) + sums[3][i];
 }
 
-// The sum over places [begin, end) of the sorted order, one entry's run, for the columns from `col` on.
+// The sum over places [begin, end) of the order, one entry's run, for the columns from `col` on.
 template <typename T>
 __device__ __forceinline__ void add_run(const EmbedArgs& a, int begin, int end, int col, float (&sum)[Sixteen<T>::n]) {
   constexpr int n = Sixteen<T>::n;
@@ -278,42 +281,14 @@ __device__ __forceinline__ void add_run(const EmbedArgs& a, int begin, int end, 
   add_tokens<T>(a, last * kChunk, end - last * kChunk, col, sum);
 }
 
-// The first place of the sorted order whose key is not below `key`: a wave narrows it down sixty-four ways at a time.
-__device__ __forceinline__ int first_not_below(GSPMD_GLOBAL const int32_t* keys, int count, int key, int lane) {
-  int lo = 0, left = count;                     // the answer is in lo .. lo + left
-  while (left > 0) {
-    const int step = (left + 63) / 64, at = lo + lane * step + step - 1;       // the last of this lane's part
-    const bool below = at < lo + left && keys[at] < key;
-    const int parts = __builtin_popcountll(__builtin_amdgcn_ballot_w64(below));
-    const int next = lo + parts * step, rest = lo + left - next;
-    left = min(step - 1, rest);                 // (the part's last is not below)
-    lo = next;
-  }
-  return lo;
-}
-// Where the runs of entries first .. first + COUNT begin, into `begins` [COUNT + 1]; by a whole wave.
-template <int COUNT>
-__device__ __forceinline__ void find_runs(const EmbedArgs& a, int first, int lane, int* begins) {
-  GSPMD_GLOBAL const int32_t* const keys = (GSPMD_GLOBAL const int32_t*)a.keys;
-  const int begin = first_not_below(keys, a.T, first, lane);
-  const int key = begin + lane < a.T ? keys[begin + lane] : INT32_MAX;
-  for (int i = 0; i <= COUNT; ++i) {
-    int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(key < first + i));
-    at = at < 64 ? begin + at : first_not_below(keys, a.T, first + i, lane);
-    if (lane == 0) begins[i] = at;
-  }
-}
-
 // dw [V, M]: a workgroup has kRowsSide entries and 4 waves' columns of them (blockIdx.y), or fewer columns and the rows shared out.
 constexpr int kRowsSide = 16;
 template <typename T>
 __global__ __launch_bounds__(256) void embed_grad_rows_kernel(const EmbedArgs a, int log_lanes, int log_across) {
   constexpr int n = Sixteen<T>::n;
-  __shared__ int begins[kRowsSide + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row0 = blockIdx.x * kRowsSide, rows = a.vs * a.vocab_shards;
-  if (wave == 0) find_runs<kRowsSide>(a, row0, lane, begins);
-  __syncthreads();
+  GSPMD_GLOBAL const int32_t* const begins = (GSPMD_GLOBAL const int32_t*)a.begins;
   const int across = 1 << log_across, side = 64 >> log_lanes;        // waves along a row; rows of a wave at a time
   const int col = ((blockIdx.y * across + (wave & (across - 1))) << log_lanes) * n + (lane & ((1 << log_lanes) - 1)) * n;
   if (col >= a.M) return;
@@ -324,7 +299,7 @@ __global__ __launch_bounds__(256) void embed_grad_rows_kernel(const EmbedArgs a,
     T* dw = static_cast<T*>(embed_arguments()->vocab[shard]);
     if (dw == nullptr) continue;
     dw += static_cast<int64_t>(row - shard * a.vs) * a.ld_vocab + col;
-    const int begin = begins[r], end = row < a.V ? begins[r + 1] : begin;
+    const int begin = a.T > 0 && row < a.V ? begins[row] : 0, end = a.T > 0 && row < a.V ? begins[row + 1] : 0;
     if (a.accumulate && begin == end && row < a.V) continue;
     float sum[n];
 #pragma unroll
@@ -358,7 +333,7 @@ __global__ __launch_bounds__(256) void embed_grad_columns_kernel(const EmbedArgs
   const int row0 = shard * a.vs + c0, m0 = blockIdx.y * kTurnRows, entries = min(kTurnEntries, a.vs - c0);
   T* const dw = static_cast<T*>(embed_arguments()->vocab[shard]);
   if (dw == nullptr) return;
-  if (wave == 0) find_runs<kTurnEntries>(a, row0, lane, begins);
+  if (t <= kTurnEntries) begins[t] = a.T > 0 ? ((GSPMD_GLOBAL const int32_t*)a.begins)[min(row0 + t, a.V)] : 0;
   __syncthreads();
   const int col = m0 + (lane & (lanes - 1)) * n;
   for (int r = wave * side + lane / lanes; r < kTurnEntries; r += 4 * side) {

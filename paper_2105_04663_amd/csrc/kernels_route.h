@@ -10,6 +10,8 @@
 #include "kernels_basic.h"
 #include "kernels_embed.h"
 #include "mfma_common.h"
+#include "order.h"
+#include "ragged.h"
 
 namespace gspmd {
 
@@ -71,9 +73,10 @@ __device__ __forceinline__ float route_total(const float (&v)[R], float most, bo
   return strange ? NAN : sum;
 }
 
+// The sixteen lanes' choices: lane i of them has the i-th, its expert (-1: none) and weight.
 template <typename T, int R>
-__global__ __launch_bounds__(256) void route_kernel(const RouteArgs a) {
-  const int lane = threadIdx.x & 63, of_row = lane & 15, token = (blockIdx.x * 256 + threadIdx.x) / kRouteLanes;
+__device__ __forceinline__ void route_choose(const RouteArgs& a, int token, int lane, int* chosen_expert, float* weight) {
+  const int of_row = lane & 15;
   const T* z = nullptr;
   if (token < a.T) {
     const int shard = embed_shard(token, a.ts, a.shards);
@@ -110,12 +113,183 @@ __global__ __launch_bounds__(256) void route_kernel(const RouteArgs a) {
         if (of_row * R + r == chosen) v[r] = -INFINITY;
     }
   }
-  float share = expert >= 0 ? expf(logit - most) : 0.f;
+  const float share = expert >= 0 ? expf(logit - most) : 0.f;
   if (a.normalise) total = row_sum(share);
+  *chosen_expert = expert;
+  *weight = expert >= 0 ? share / total : 0.f;
+}
+
+// The choices of sixty-four tokens, and how many of them each expert has: counts [tile][E].
+constexpr int kFewRouted = kOrderThreads / kRouteLanes, kTileTokens = kFewRouted;
+template <typename T, int R>
+__global__ __launch_bounds__(kOrderThreads) void route_kernel(const RouteArgs a, int32_t* counts) {
+  __shared__ int32_t here[kMostExperts];
+  const int t = threadIdx.x, lane = t & 63, of_row = lane & 15, token = blockIdx.x * kTileTokens + t / kRouteLanes;
+  if (t < a.E) here[t] = 0;
+  int expert;
+  float weight;
+  route_choose<T, R>(a, token, lane, &expert, &weight);
+  __syncthreads();
   if (token < a.T && of_row < a.k) {
     a.experts[static_cast<int64_t>(token) * a.k + of_row] = expert;
-    a.weights[static_cast<int64_t>(token) * a.k + of_row] = expert >= 0 ? share / total : 0.f;
+    a.weights[static_cast<int64_t>(token) * a.k + of_row] = weight;
+    if (expert >= 0) atomicAdd(&here[expert], 1);
   }
+  __syncthreads();
+  if (t < a.E) counts[static_cast<int64_t>(blockIdx.x) * a.E + t] = here[t];
+}
+static_assert(kMostExperts <= kOrderThreads, "a thread for every expert");
+
+// Where a tile's choices begin, of every expert: the choices of lower experts, and those of its own in earlier tiles.  With few tiles a workgroup adds them up itself (route_places_kernel); with many, one
+// for every expert turns the tiles' counts into sums of the earlier ones, and its total.
+constexpr int kTilesSummed = 512;
+__global__ __launch_bounds__(kOrderThreads) static void route_sums_kernel(int32_t* counts, int tiles, int E, int32_t* totals) {
+  __shared__ uint32_t sums[kOrderWaves];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, e = blockIdx.x;
+  int before = 0;
+  for (int base = 0; base < tiles; base += kOrderThreads) {
+    int32_t* const at = counts + static_cast<int64_t>(base + t) * E + e;
+    const int n = base + t < tiles ? *at : 0, to_here = wave_sum_to_here(n);
+    if (lane == 63) sums[wave] = static_cast<uint32_t>(to_here);
+    __syncthreads();
+    int sum = before + to_here - n;
+    for (int w = 0; w < kOrderWaves; ++w) {
+      if (w < wave) sum += static_cast<int>(sums[w]);
+      before += static_cast<int>(sums[w]);
+    }
+    if (base + t < tiles) *at = sum;
+    __syncthreads();
+  }
+  if (t == 0) totals[e] = before;
+}
+
+// The places of up to a workgroup's 1024 keys, each below 1 << bits, among them, those of equal keys in the order of the threads: lanes with equal keys are found by a ballot for each bit, and
+// sums over [keys][waves] are places.  `counts`: LDS, [1 << bits][waves]; returns with where each key's run begins in counts[key][0].
+__device__ __forceinline__ int place_of_mine(uint32_t key, int bits, uint16_t* counts, uint32_t* sums) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, entries = kOrderWaves << bits;
+  for (int i = t; i < entries / 2; i += kOrderThreads) reinterpret_cast<uint32_t*>(counts)[i] = 0;
+  __syncthreads();
+  uint64_t same = ~uint64_t(0);
+  for (int b = 0; b < bits; ++b) {
+    const bool on = (key >> b) & 1;
+    const uint64_t with = __builtin_amdgcn_ballot_w64(on);
+    same &= on ? with : ~with;
+  }
+  const int rank = __builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
+  uint16_t* const mine = counts + key * kOrderWaves + wave;
+  if (rank == 0) *mine = static_cast<uint16_t>(__builtin_popcountll(same));
+  __syncthreads();
+  const int each = (entries + kOrderThreads - 1) / kOrderThreads, first = t * each;
+  int sum = 0;
+  for (int i = 0; i < each; ++i) sum += first + i < entries ? counts[first + i] : 0;
+  const int to_here = wave_sum_to_here(sum);
+  if (lane == 63) sums[wave] = static_cast<uint32_t>(to_here);
+  __syncthreads();
+  int at = to_here - sum;
+  for (int w = 0; w < wave; ++w) at += static_cast<int>(sums[w]);
+  for (int i = 0; i < each; ++i)
+    if (first + i < entries) {
+      const int n = counts[first + i];
+      counts[first + i] = static_cast<uint16_t>(at);
+      at += n;
+    }
+  __syncthreads();
+  return rank + *mine;
+}
+
+// Slots of a tile's choices, a choice a thread.  `totals`: null where counts are the tiles' own (kTilesSummed).
+__global__ __launch_bounds__(kOrderThreads) static void route_places_kernel(const int32_t* experts, const int32_t* counts, const int32_t* totals, int n, int each, int E, int tiles, int bits, int32_t* slots,
+                                                                         int32_t* order, int32_t* sizes) {
+  __shared__ uint16_t of_tile[kOrderWaves << kMostRange];
+  __shared__ uint32_t sums[kOrderWaves];
+  __shared__ int32_t begins[kMostExperts], parts[2][kOrderThreads];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, tile = blockIdx.x, at = tile * each + t;
+  const bool mine = t < each && at < n;
+  const int expert = mine ? experts[at] : -1;
+  const uint32_t key = mine ? static_cast<uint32_t>(min(static_cast<uint32_t>(expert), static_cast<uint32_t>(E))) : (1u << bits) - 1;
+  // of expert t % E: choices of all tiles and of the earlier ones, a share of the tiles a thread
+  int total = 0, earlier = 0;
+  const int shares = min(kOrderThreads / E, 32);
+  if (totals == nullptr) {
+    const int share = t / E, e = t - share * E;
+    if (share < shares) {
+      const int per = (tiles + shares - 1) / shares, first = share * per, end = min(first + per, tiles);
+      GSPMD_GLOBAL const int32_t* from = (GSPMD_GLOBAL const int32_t*)counts + static_cast<int64_t>(first) * E + e;
+      int i = first;
+      for (; i + 8 <= end; i += 8, from += 8 * static_cast<int64_t>(E)) {
+        int32_t v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = from[u * static_cast<int64_t>(E)];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          total += v[u];
+          earlier += i + u < tile ? v[u] : 0;
+        }
+      }
+      for (; i < end; ++i, from += E) {
+        total += *from;
+        earlier += i < tile ? *from : 0;
+      }
+    }
+    parts[0][t] = total;
+    parts[1][t] = earlier;
+    __syncthreads();
+    total = earlier = 0;
+    if (t < E)
+      for (int s = 0; s < shares; ++s) {
+        total += parts[0][s * E + t];
+        earlier += parts[1][s * E + t];
+      }
+  } else if (t < E) {
+    total = totals[t];
+    earlier = counts[static_cast<int64_t>(tile) * E + t];
+  }
+  const int to_here = wave_sum_to_here(total);
+  if (lane == 63) sums[wave] = static_cast<uint32_t>(to_here);
+  __syncthreads();
+  int lower = to_here - total, all = 0;
+  for (int w = 0; w < kOrderWaves; ++w) {
+    if (w < wave) lower += static_cast<int>(sums[w]);
+    all += static_cast<int>(sums[w]);
+  }
+  if (t < E) {
+    begins[t] = lower + earlier;
+    if (tile == 0) sizes[t] = total;
+  }
+  __syncthreads();                              // (sums are used again)
+  const int place = place_of_mine(key, bits, of_tile, sums);
+  if (mine) {
+    const bool there = key < static_cast<uint32_t>(E);
+    const int slot = there ? begins[key] + place - of_tile[key * kOrderWaves] : -1;
+    slots[at] = slot;
+    if (there) order[slot] = at;
+    if (at >= all) order[at] = -1;              // behind the last slot
+  }
+}
+
+// A routing of a few tokens, with its order, by one workgroup.
+template <typename T, int R>
+__global__ __launch_bounds__(kOrderThreads) void route_few_kernel(const RouteArgs a, int bits, int32_t* slots, int32_t* order, int32_t* sizes) {
+  __shared__ uint16_t counts[kOrderWaves << kMostRange];
+  __shared__ uint32_t keys[kOrderThreads], sums[kOrderWaves];
+  const int t = threadIdx.x, lane = t & 63, of_row = lane & 15, token = t / kRouteLanes, n = a.T * a.k;
+  int expert;
+  float weight;
+  route_choose<T, R>(a, token, lane, &expert, &weight);
+  if (token < a.T && of_row < a.k) {
+    a.experts[token * a.k + of_row] = expert;
+    a.weights[token * a.k + of_row] = weight;
+    keys[token * a.k + of_row] = static_cast<uint32_t>(expert >= 0 ? expert : a.E);
+  }
+  __syncthreads();
+  const uint32_t key = t < n ? keys[t] : (1u << bits) - 1;   // behind all others, or among those without an expert and behind them
+  const int place = place_of_mine(key, bits, counts, sums);
+  const bool there = key < static_cast<uint32_t>(a.E);
+  if (t < n) {
+    slots[t] = there ? place : -1;
+    order[place] = there ? t : -1;
+  }
+  for (int e = t; e < a.E; e += kOrderThreads) sizes[e] = counts[(e + 1) * kOrderWaves] - counts[e * kOrderWaves];
 }
 
 // dlogits: of weights from all experts p (g - sum p g), g zero where not chosen; from the chosen ones the same among them, zeros elsewhere.
@@ -183,13 +357,14 @@ __device__ __forceinline__ int expert_shard(const ExchangeArgs& a, int o) {
   return e < static_cast<uint32_t>(a.E) ? static_cast<int>(e / static_cast<uint32_t>(a.es)) : -1;
 }
 
-// rows[slot] = x[token of the slot]: a wave has a piece of a row, or a few short rows; blockIdx.y the piece.
+// rows[slot] = x[token of the slot]: a wave has a piece of a row, or a few short rows.
 constexpr int kExchangeUnroll = 4;
 template <typename T>
-__global__ __launch_bounds__(256) void dispatch_kernel(const ExchangeArgs a, int log_lanes) {
+__global__ __launch_bounds__(256) void dispatch_kernel(const ExchangeArgs a, int log_lanes, int pieces) {
   constexpr int n = Sixteen<T>::n;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lanes = 1 << log_lanes;
-  const int slot = ((blockIdx.x * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);
+  const int group = blockIdx.x / pieces, piece = blockIdx.x - group * pieces;       // (neighbouring pieces of rows together)
+  const int slot = ((group * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);
   if (slot >= a.T * a.k) return;
   const int o = ((GSPMD_GLOBAL const int32_t*)a.order)[slot];
   if (static_cast<uint32_t>(o) >= static_cast<uint32_t>(a.T * a.k)) return;
@@ -199,7 +374,7 @@ __global__ __launch_bounds__(256) void dispatch_kernel(const ExchangeArgs a, int
   if (to == nullptr) return;
   const int token = static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(a.k)), shard = embed_shard(token, a.ts, a.token_shards);
   const T* const x = static_cast<const T*>(exchange_arguments()->tokens[shard]) + (token - shard * a.ts) * a.ld_tokens;
-  const int col0 = ((blockIdx.y * kExchangeUnroll) << log_lanes) * n + (lane & (lanes - 1)) * n, step = n << log_lanes;
+  const int col0 = ((piece * kExchangeUnroll) << log_lanes) * n + (lane & (lanes - 1)) * n, step = n << log_lanes;
   u32x4_t v[kExchangeUnroll];
 #pragma unroll
   for (int u = 0; u < kExchangeUnroll; ++u)
@@ -212,12 +387,13 @@ __global__ __launch_bounds__(256) void dispatch_kernel(const ExchangeArgs a, int
 // y[t] = sum over t's choices of weight * rows[slot], in float32, in their order; what has no slot adds nothing.
 constexpr int kCombineAhead = 4;
 template <typename T>
-__global__ __launch_bounds__(256) void combine_kernel(const ExchangeArgs a, int log_lanes) {
+__global__ __launch_bounds__(256) void combine_kernel(const ExchangeArgs a, int log_lanes, int pieces) {
   constexpr int n = Sixteen<T>::n;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lanes = 1 << log_lanes;
-  const int token = ((blockIdx.x * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);
+  const int group = blockIdx.x / pieces, piece = blockIdx.x - group * pieces;
+  const int token = ((group * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);
   if (token >= a.ts * a.token_shards) return;
-  const int shard = embed_shard(token, a.ts, a.token_shards), col = ((blockIdx.y << log_lanes) + (lane & (lanes - 1))) * n;
+  const int shard = embed_shard(token, a.ts, a.token_shards), col = ((piece << log_lanes) + (lane & (lanes - 1))) * n;
   T* const y = static_cast<T*>(exchange_arguments()->tokens[shard]);
   if (y == nullptr || col >= a.M) return;
   float sum[n];

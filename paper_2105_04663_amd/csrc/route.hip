@@ -8,9 +8,7 @@
 #include "../../include/gspmd.h"
 #include "dots.h"
 #include "kernels_route.h"
-#include "kernels_sort.h"
 #include "plan.h"
-#include "sort.h"
 #include "tokens.h"
 
 namespace gspmd {
@@ -21,6 +19,11 @@ constexpr int64_t kMostTokens = 1 << 24;        // choices of all tokens, too
 struct Route {
   int64_t P = 0, T = 0, E = 0, k = 0, na = 1, ts = 0;
   int axis = -1;
+  bool few() const { return T <= kFewRouted && T * k <= kOrderThreads; }
+  int64_t tiles() const { return (T + kTileTokens - 1) / kTileTokens; }
+  // the workspace: the tiles' counts, and with many tiles the experts' totals
+  int64_t counts_bytes() const { return round_up(tiles() * E * 4, kWsAlign); }
+  int64_t workspace() const { return few() ? 0 : counts_bytes() + (tiles() > kTilesSummed ? round_up(E * 4, kWsAlign) : 0); }
 };
 
 int32_t analyse(const gspmd_mesh* mesh, const gspmd_sharding* sh, int32_t choices, Route* r) {
@@ -173,10 +176,11 @@ int32_t launch_exchange(Exchanged what, const ExchangeArgs& a, hipStream_t strea
   const int log = row_lanes_log(a.M, n);
   const int64_t side = int64_t(4) << (6 - log), rows = what == kCombine ? static_cast<int64_t>(a.ts) * a.token_shards : static_cast<int64_t>(a.T) * a.k;
   const int64_t piece = (static_cast<int64_t>(n) << log) * (what == kDispatch ? kExchangeUnroll : 1);
-  const dim3 grid(static_cast<unsigned>((rows + side - 1) / side), what == kCombineGrad ? 1u : static_cast<unsigned>((a.M + piece - 1) / piece));
-  if (grid.y > 65535) return GSPMD_ERR_UNSUPPORTED;
-  if (what == kDispatch) hipLaunchKernelGGL((dispatch_kernel<T>), grid, dim3(256), 0, stream, a, log);
-  else if (what == kCombine) hipLaunchKernelGGL((combine_kernel<T>), grid, dim3(256), 0, stream, a, log);
+  const int64_t pieces = what == kCombineGrad ? 1 : (a.M + piece - 1) / piece, groups = (rows + side - 1) / side * pieces;
+  if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
+  const dim3 grid(static_cast<unsigned>(groups));
+  if (what == kDispatch) hipLaunchKernelGGL((dispatch_kernel<T>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
+  else if (what == kCombine) hipLaunchKernelGGL((combine_kernel<T>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
   else hipLaunchKernelGGL((combine_grad_kernel<T>), grid, dim3(256), 0, stream, a, log);
   return launched();
 }
@@ -197,7 +201,7 @@ int32_t gspmd_route_workspace_bytes(const gspmd_mesh* mesh, const gspmd_sharding
   Route r;
   const int32_t st = analyse(mesh, logits_sh, choices, &r);
   if (st != GSPMD_OK) return st;
-  *bytes = round_up(sort_bytes(r.T * r.k, r.E), kWsAlign);
+  *bytes = r.workspace();
   return GSPMD_OK;
 } catch (...) { return GSPMD_ERR_HOST_MEMORY; }
 
@@ -213,26 +217,38 @@ int32_t gspmd_route(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_shards
   Replicas logits(r.na);
   int64_t ld = -1;
   if ((st = collect(mesh, r, logits_shards, dtype, &ld, &logits)) != GSPMD_OK) return st;
-  const int64_t bytes = sort_bytes(r.T * r.k, r.E);
-  if (bytes > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & (kWsAlign - 1)) || workspace_bytes < round_up(bytes, kWsAlign))) return GSPMD_ERR_WORKSPACE;
+  const int64_t bytes = r.workspace();
+  if (bytes > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & (kWsAlign - 1)) || workspace_bytes < bytes)) return GSPMD_ERR_WORKSPACE;
   if (launches_are_dry()) return GSPMD_OK;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  if (r.T > 0) {
-    const RouteArgs a = arguments(r, logits, ld, *route, normalise);
+  const RouteArgs a = arguments(r, logits, ld, *route, normalise);
+  int bits = 1;
+  while ((int64_t(1) << bits) <= r.E) ++bits;               // of the numbers 0 .. E
+  if (r.few()) {
     by_experts(r.E, [&](auto each) {
       constexpr int R = decltype(each)::value;
-      if (dtype == GSPMD_BF16) hipLaunchKernelGGL((route_kernel<bf16_bits, R>), token_grid(r.T), dim3(256), 0, stream, a);
-      else hipLaunchKernelGGL((route_kernel<float, R>), token_grid(r.T), dim3(256), 0, stream, a);
+      if (dtype == GSPMD_BF16) hipLaunchKernelGGL((route_few_kernel<bf16_bits, R>), dim3(1), dim3(kOrderThreads), 0, stream, a, bits, route->slots, route->order, route->sizes);
+      else hipLaunchKernelGGL((route_few_kernel<float, R>), dim3(1), dim3(kOrderThreads), 0, stream, a, bits, route->slots, route->order, route->sizes);
     });
+    return launched();
+  }
+  int32_t* const counts = static_cast<int32_t*>(workspace);
+  const unsigned tiles = static_cast<unsigned>(r.tiles());
+  by_experts(r.E, [&](auto each) {
+    constexpr int R = decltype(each)::value;
+    if (dtype == GSPMD_BF16) hipLaunchKernelGGL((route_kernel<bf16_bits, R>), dim3(tiles), dim3(kOrderThreads), 0, stream, a, counts);
+    else hipLaunchKernelGGL((route_kernel<float, R>), dim3(tiles), dim3(kOrderThreads), 0, stream, a, counts);
+  });
+  if ((st = launched()) != GSPMD_OK) return st;
+  int32_t* totals = nullptr;
+  if (tiles > kTilesSummed) {
+    totals = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + r.counts_bytes());
+    hipLaunchKernelGGL(route_sums_kernel, dim3(static_cast<unsigned>(r.E)), dim3(kOrderThreads), 0, stream, counts, static_cast<int>(tiles), a.E, totals);
     if ((st = launched()) != GSPMD_OK) return st;
   }
-  SortKeys in{};
-  in.shard[0] = route->experts;
-  in.count = static_cast<int32_t>(r.T * r.k);
-  in.per = std::max(in.count, 1);
-  in.shards = 1;
-  in.keys = static_cast<int32_t>(r.E);
-  return run_sort(in, SortOut{nullptr, route->order, route->slots, route->sizes}, workspace, stream);
+  hipLaunchKernelGGL(route_places_kernel, dim3(tiles), dim3(kOrderThreads), 0, stream, route->experts, counts, totals, a.T * a.k, kTileTokens * a.k, a.E, static_cast<int>(tiles), bits, route->slots,
+                     route->order, route->sizes);
+  return launched();
 } catch (...) { return GSPMD_ERR_HOST_MEMORY; }
 
 int32_t gspmd_route_grad(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_shards, const gspmd_sharding* logits_sh, int32_t choices, int32_t normalise, const gspmd_route_buf* route,

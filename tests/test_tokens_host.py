@@ -108,11 +108,10 @@ def test_route_refusals(grad):
         assert status(call, ok, dweights=0) == NULL and status(call, ok, dweights=(1 << 22) + 1) == BUFFER
         assert status(call, ok, dlogits_shards=bufs(4, g.BF16)) == UNSUPPORTED
     else:
-        big = make(T=20000)
+        assert g.route_workspace_bytes(ok["mesh"], ok["logits_sh"], 2) == 0 and status(call, ok, workspace=0, workspace_bytes=0) == 0      # few tokens
+        big = make(T=2000)
         need = g.route_workspace_bytes(big["mesh"], big["logits_sh"], 2)
-        assert need > 0 and g.route_workspace_bytes(ok["mesh"], ok["logits_sh"], 2) == 0
-        assert status(call, ok, workspace=0, workspace_bytes=0) == 0
-        assert status(call, big, workspace_bytes=need) == 0
+        assert need > 0 and status(call, big, workspace_bytes=need) == 0
         for more in (dict(workspace_bytes=need - 1), dict(workspace=0), dict(workspace=(1 << 24) + 8)):
             assert status(call, big, **more) == WORKSPACE
 
