@@ -134,9 +134,11 @@ int32_t launch_gradient(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
     if (grid.y > 65535) return GSPMD_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((embed_grad_rows_kernel<T>), grid, dim3(256), 0, stream, a, log, across);
   } else {
-    const dim3 grid(static_cast<unsigned>((a.vs + kTurnEntries - 1) / kTurnEntries * a.vocab_shards), static_cast<unsigned>((a.M + kTurnRows - 1) / kTurnRows));
+    constexpr int kRows = kTurnLanes * n;
+    const dim3 grid(static_cast<unsigned>((a.vs + kTurnEntries - 1) / kTurnEntries * a.vocab_shards), static_cast<unsigned>((a.M + kRows - 1) / kRows));
     if (grid.y > 65535) return GSPMD_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((embed_grad_columns_kernel<T>), grid, dim3(256), 0, stream, a);
+    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, float>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, T>), grid, dim3(256), 0, stream, a);
   }
   return launched();
 }

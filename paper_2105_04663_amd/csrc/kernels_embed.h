@@ -110,7 +110,7 @@ __host__ __device__ __forceinline__ int row_lanes_log(int elements, int per_lane
 }
 
 // y [V, M]: a wave has a piece of a row (or a few short rows), kEmbedUnroll x 16 bytes a lane.
-constexpr int kEmbedUnroll = 4;
+constexpr int kEmbedUnroll = 8;
 template <typename T, bool SCALED>
 __global__ __launch_bounds__(256) void embed_rows_kernel(const EmbedArgs a, int log_lanes, int pieces) {
   constexpr int n = Sixteen<T>::n;
@@ -281,31 +281,57 @@ __device__ __forceinline__ void add_run(const EmbedArgs& a, int begin, int end, 
   add_tokens<T>(a, last * kChunk, end - last * kChunk, col, sum);
 }
 
-// dw [V, M]: a workgroup has kRowsSide entries and 4 waves' columns of them (blockIdx.y), or fewer columns and the rows shared out.
-constexpr int kRowsSide = 16;
+// dw [V, M]: a workgroup has kRowsSide entries and 4 waves' columns of them (blockIdx.y), or fewer columns and the rows shared out.  Most entries have no token, and most that have any have one: where the
+// runs begin is read at once, and the first tokens of four rows are on their way together.
+constexpr int kRowsSide = 16, kRowsAhead = 4;
 template <typename T>
 __global__ __launch_bounds__(256) void embed_grad_rows_kernel(const EmbedArgs a, int log_lanes, int log_across) {
   constexpr int n = Sixteen<T>::n;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row0 = blockIdx.x * kRowsSide, rows = a.vs * a.vocab_shards;
-  GSPMD_GLOBAL const int32_t* const begins = (GSPMD_GLOBAL const int32_t*)a.begins;
+  const int begins = a.T > 0 ? ((GSPMD_GLOBAL const int32_t*)a.begins)[min(row0 + min(lane, kRowsSide), a.V)] : 0;      // (of a row behind the last entry: the end of all, as its successor's)
   const int across = 1 << log_across, side = 64 >> log_lanes;        // waves along a row; rows of a wave at a time
   const int col = ((blockIdx.y * across + (wave & (across - 1))) << log_lanes) * n + (lane & ((1 << log_lanes) - 1)) * n;
-  if (col >= a.M) return;
-  for (int r = (wave >> log_across) * side + (lane >> log_lanes); r < kRowsSide; r += (4 >> log_across) * side) {
-    const int row = row0 + r;
-    if (row >= rows) break;
-    const int shard = embed_shard(row, a.vs, a.vocab_shards);
-    T* dw = static_cast<T*>(embed_arguments()->vocab[shard]);
-    if (dw == nullptr) continue;
-    dw += static_cast<int64_t>(row - shard * a.vs) * a.ld_vocab + col;
-    const int begin = a.T > 0 && row < a.V ? begins[row] : 0, end = a.T > 0 && row < a.V ? begins[row + 1] : 0;
-    if (a.accumulate && begin == end && row < a.V) continue;
-    float sum[n];
+  const int turn = (4 >> log_across) * side;                          // from a lane's row to its next
+  const bool in = col < a.M;
+  for (int r0 = (wave >> log_across) * side + (lane >> log_lanes); r0 - (lane >> log_lanes) < kRowsSide; r0 += kRowsAhead * turn) {
+    int begin[kRowsAhead], end[kRowsAhead], token[kRowsAhead];
+    u32x4_t v[kRowsAhead];
 #pragma unroll
-    for (int e = 0; e < n; ++e) sum[e] = 0.f;
-    if (begin < end) {
-      add_run<T>(a, begin, end, col, sum);
+    for (int u = 0; u < kRowsAhead; ++u) {
+      const int r = r0 + u * turn;
+      begin[u] = __shfl(begins, min(r, kRowsSide));
+      end[u] = __shfl(begins, min(r + 1, kRowsSide));
+      token[u] = 0;
+      v[u] = u32x4_t{0u, 0u, 0u, 0u};
+    }
+    bool any = false;
+#pragma unroll
+    for (int u = 0; u < kRowsAhead; ++u) any = any || begin[u] < end[u];
+    if (any && in) {
+#pragma unroll
+      for (int u = 0; u < kRowsAhead; ++u) token[u] = ((GSPMD_GLOBAL const int32_t*)a.order)[begin[u] < end[u] ? begin[u] : 0];
+      const bool whole = col + n <= a.M;
+#pragma unroll
+      for (int u = 0; u < kRowsAhead; ++u)
+        if (whole) v[u] = load16(token_row<T>(a, begin[u] < end[u] ? token[u] : 0) + col);
+        else if (begin[u] < end[u]) v[u] = load_some(token_row<T>(a, token[u]) + col, a.M - col);
+    }
+#pragma unroll
+    for (int u = 0; u < kRowsAhead; ++u) {
+      const int r = r0 + u * turn, row = row0 + r;
+      if (r >= kRowsSide || row >= rows || !in) continue;
+      const int shard = embed_shard(row, a.vs, a.vocab_shards);
+      T* dw = static_cast<T*>(embed_arguments()->vocab[shard]);
+      if (dw == nullptr) continue;
+      dw += static_cast<int64_t>(row - shard * a.vs) * a.ld_vocab + col;
+      if (begin[u] == end[u]) {
+        if (!a.accumulate || row >= a.V) store_up_to(dw, u32x4_t{0u, 0u, 0u, 0u}, a.M - col);
+        continue;
+      }
+      float sum[n];
+      Sixteen<T>::open(v[u], sum);
+      if (begin[u] + 1 < end[u]) add_run<T>(a, begin[u] + 1, end[u], col, sum);
 #pragma unroll
       for (int e = 0; e < n; ++e) sum[e] *= a.scale;
       if (a.accumulate) {
@@ -314,56 +340,81 @@ __global__ __launch_bounds__(256) void embed_grad_rows_kernel(const EmbedArgs a,
 #pragma unroll
         for (int e = 0; e < n; ++e) sum[e] += f[e];
       }
+      store_up_to(dw, Sixteen<T>::close(sum), a.M - col);
     }
-    store_up_to(dw, Sixteen<T>::close(sum), a.M - col);
   }
 }
 
-// dw [M, V]: 64 entries x 64 rows of dw a workgroup.  A wave has every fourth entry, a lane sixteen bytes of its tokens' rows (8 lanes, or 16 of float32, a token: the lanes beside them other
-// entries); the tile turns in LDS.
-constexpr int kTurnEntries = 64, kTurnRows = 64;
-template <typename T>
+// dw [M, V]: 64 entries x 16 lanes' 16 bytes of dw's rows a workgroup.  Sixteen lanes have an entry, four of them one after the other, whose first tokens are on their way together; what they add up turns in
+// LDS, rounded but for what is still to be added to (TTile float).  Bound by what is on its way: 8 workgroups on a compute unit, each 5 KB of rows and 16 of dw.
+constexpr int kTurnEntries = 64, kTurnLanes = 16;
+template <typename T, typename TTile>
 __global__ __launch_bounds__(256) void embed_grad_columns_kernel(const EmbedArgs a) {
-  constexpr int n = Sixteen<T>::n, lanes = kTurnRows / n, side = 64 / lanes;
-  __shared__ float tile[kTurnRows][kTurnEntries + 1];
+  constexpr int n = Sixteen<T>::n, kRows = kTurnLanes * n, side = 64 / kTurnLanes, kEach = kTurnEntries / (4 * side), kPitch = kTurnEntries + (sizeof(TTile) == 2 ? 2 : 1);
+  __shared__ __attribute__((aligned(4))) TTile tile[kRows][kPitch];
   __shared__ int begins[kTurnEntries + 1];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   // entries of one shard: blockIdx.x counts blocks of every shard
   const int per_shard = (a.vs + kTurnEntries - 1) / kTurnEntries, shard = blockIdx.x / per_shard, c0 = (blockIdx.x - shard * per_shard) * kTurnEntries;
-  const int row0 = shard * a.vs + c0, m0 = blockIdx.y * kTurnRows, entries = min(kTurnEntries, a.vs - c0);
+  const int row0 = shard * a.vs + c0, m0 = blockIdx.y * kRows, entries = min(kTurnEntries, a.vs - c0);
   T* const dw = static_cast<T*>(embed_arguments()->vocab[shard]);
   if (dw == nullptr) return;
   if (t <= kTurnEntries) begins[t] = a.T > 0 ? ((GSPMD_GLOBAL const int32_t*)a.begins)[min(row0 + t, a.V)] : 0;
   __syncthreads();
-  const int col = m0 + (lane & (lanes - 1)) * n;
-  for (int r = wave * side + lane / lanes; r < kTurnEntries; r += 4 * side) {
-    const int begin = begins[r], end = r < entries && row0 + r < a.V ? begins[r + 1] : begin;
+  const int col = m0 + (lane & (kTurnLanes - 1)) * n, r0 = wave * side + lane / kTurnLanes;
+  int begin[kEach], end[kEach], token[kEach];
+  u32x4_t v[kEach];
+  bool any = false;
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const int r = r0 + u * 4 * side;
+    begin[u] = begins[r];
+    end[u] = r < entries ? begins[r + 1] : begin[u];
+    any = any || begin[u] < end[u];
+    v[u] = u32x4_t{0u, 0u, 0u, 0u};
+    token[u] = 0;
+  }
+  if (any && col < a.M) {
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) token[u] = ((GSPMD_GLOBAL const int32_t*)a.order)[begin[u] < end[u] ? begin[u] : 0];
+    const bool whole = col + n <= a.M;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u)
+      if (whole) v[u] = load16(token_row<T>(a, begin[u] < end[u] ? token[u] : 0) + col);
+      else if (begin[u] < end[u]) v[u] = load_some(token_row<T>(a, token[u]) + col, a.M - col);
+  }
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
     float sum[n];
+    Sixteen<T>::open(v[u], sum);
+    if (begin[u] + 1 < end[u] && col < a.M) add_run<T>(a, begin[u] + 1, end[u], col, sum);
+    const int r = r0 + u * 4 * side;
 #pragma unroll
-    for (int e = 0; e < n; ++e) sum[e] = 0.f;
-    if (begin < end && col < a.M) add_run<T>(a, begin, end, col, sum);
-#pragma unroll
-    for (int e = 0; e < n; ++e) tile[(lane & (lanes - 1)) * n + e][r] = sum[e] * a.scale;
+    for (int e = 0; e < n; ++e) store_from_float<TTile>(&tile[(lane & (kTurnLanes - 1)) * n + e][r], begin[u] < end[u] ? sum[e] * a.scale : 0.f);
   }
   __syncthreads();
-  for (int i = t; i < kTurnRows * (kTurnEntries / n); i += 256) {
+  for (int i = t; i < kRows * (kTurnEntries / n); i += 256) {
     const int m = i / (kTurnEntries / n), c = (i - m * (kTurnEntries / n)) * n, count = entries - c;
     if (m0 + m >= a.M || count <= 0) continue;
     T* const at = dw + (m0 + m) * a.ld_vocab + c0 + c;
-    float f[n];
+    if constexpr (sizeof(TTile) == 2) {
+      u32x4_t o;
 #pragma unroll
-    for (int e = 0; e < n; ++e) f[e] = tile[m][c + e];
-    if (a.accumulate) {
-      // untouched entries keep their bits: a wave may have none in its columns, others are added to
-      float before[n];
-      Sixteen<T>::open(load_up_to(at, count), before);
+      for (int e = 0; e < 4; ++e) o[e] = *reinterpret_cast<const uint32_t*>(&tile[m][c + 2 * e]);
+      store_up_to(at, o, count);
+    } else {
+      float f[n];
 #pragma unroll
-      for (int e = 0; e < n; ++e) {
-        const int entry = row0 + c + e;
-        if (e < count && entry < a.V) f[e] = begins[c + e] == begins[c + e + 1] ? before[e] : before[e] + f[e];
+      for (int e = 0; e < n; ++e) f[e] = tile[m][c + e];
+      if (a.accumulate) {                       // entries without tokens keep what they have
+        float before[n];
+        Sixteen<T>::open(load_up_to(at, count), before);
+#pragma unroll
+        for (int e = 0; e < n; ++e)
+          if (e < count && row0 + c + e < a.V) f[e] = begins[c + e] == begins[c + e + 1] ? before[e] : before[e] + f[e];
       }
+      store_up_to(at, Sixteen<T>::close(f), count);
     }
-    store_up_to(at, Sixteen<T>::close(f), count);
   }
 }
 

@@ -29,7 +29,10 @@ __global__ __launch_bounds__(kOrderThreads) void order_kernel(const OrderKeys in
   for (int base = first; base < end; base += 64 * kAhead) {
     int key[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) key[u] = base + u * 64 + lane < end ? in.at(base + u * 64 + lane) : INT32_MAX;
+    for (int u = 0; u < kAhead; ++u) key[u] = in.at(min(base + u * 64 + lane, end - 1));      // (no branch: a load under one is waited for there)
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (base + u * 64 + lane >= end) key[u] = INT32_MAX;
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       less += key[u] < lo;
@@ -65,7 +68,10 @@ __global__ __launch_bounds__(kOrderThreads) void order_kernel(const OrderKeys in
   for (int base = first; base < end; base += 64 * kAhead) {
     int key[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) key[u] = base + u * 64 + lane < end ? in.at(base + u * 64 + lane) : INT32_MAX;
+    for (int u = 0; u < kAhead; ++u) key[u] = in.at(min(base + u * 64 + lane, end - 1));      // (no branch: a load under one is waited for there)
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (base + u * 64 + lane >= end) key[u] = INT32_MAX;
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int index = key[u] - lo;

@@ -48,11 +48,32 @@ __device__ __forceinline__ uint32_t row_ballot(bool yes, int lane) { return stat
 template <typename T, int R>
 __device__ __forceinline__ bool route_load(const T* z, int E, int of_row, int lane, float (&v)[R]) {
   bool strange = false;
+  constexpr int n = Sixteen<T>::n;
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int e = of_row * R + r;
-    v[r] = -INFINITY;
-    if (z != nullptr && e < E) v[r] = load_as_float<T>((const T*)z + e);
+  for (int r = 0; r < R; ++r) v[r] = -INFINITY;
+  if (z != nullptr && (of_row + 1) * R <= E) {
+    const T* const from = z + of_row * R;
+    if constexpr (R % n == 0) {
+      u32x4_t w[R / n];
+#pragma unroll
+      for (int i = 0; i < R / n; ++i) w[i] = load16(from + i * n);
+#pragma unroll
+      for (int i = 0; i < R / n; ++i) {
+        float f[n];
+        Sixteen<T>::open(w[i], f);
+#pragma unroll
+        for (int e = 0; e < n; ++e) v[i * n + e] = f[e];
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < R; ++r) v[r] = load_as_float<T>(from + r);
+    }
+  } else if (z != nullptr && of_row * R < E) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = load_as_float<T>(z + min(of_row * R + r, E - 1));      // (no branch: a load under one is waited for there)
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (of_row * R + r >= E) v[r] = -INFINITY;
   }
 #pragma unroll
   for (int r = 0; r < R; ++r)
@@ -331,6 +352,20 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteArgs a) {
       if (of_row * R + r == e) v[r] += add;
   }
   if (d == nullptr) return;
+  constexpr int n = Sixteen<T>::n;
+  if constexpr (R % n == 0) {
+    if ((of_row + 1) * R <= a.E) {
+      T* const to = d + static_cast<int64_t>(within) * a.ld_d + of_row * R;
+#pragma unroll
+      for (int i = 0; i < R / n; ++i) {
+        float f[n];
+#pragma unroll
+        for (int e = 0; e < n; ++e) f[e] = live ? v[i * n + e] : 0.f;
+        store16(to + i * n, Sixteen<T>::close(f));
+      }
+      return;
+    }
+  }
 #pragma unroll
   for (int r = 0; r < R; ++r)
     if (of_row * R + r < a.E) store_from_float<T>(d + static_cast<int64_t>(within) * a.ld_d + of_row * R + r, live ? v[r] : 0.f);
@@ -385,7 +420,7 @@ __global__ __launch_bounds__(256) void dispatch_kernel(const ExchangeArgs a, int
 }
 
 // y[t] = sum over t's choices of weight * rows[slot], in float32, in their order; what has no slot adds nothing.
-constexpr int kCombineAhead = 4;
+constexpr int kCombineAhead = 4, kCombineUnroll = 2;
 template <typename T>
 __global__ __launch_bounds__(256) void combine_kernel(const ExchangeArgs a, int log_lanes, int pieces) {
   constexpr int n = Sixteen<T>::n;
@@ -393,36 +428,64 @@ __global__ __launch_bounds__(256) void combine_kernel(const ExchangeArgs a, int 
   const int group = blockIdx.x / pieces, piece = blockIdx.x - group * pieces;
   const int token = ((group * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);
   if (token >= a.ts * a.token_shards) return;
-  const int shard = embed_shard(token, a.ts, a.token_shards), col = ((piece << log_lanes) + (lane & (lanes - 1))) * n;
+  const int shard = embed_shard(token, a.ts, a.token_shards), col0 = (((piece * kCombineUnroll) << log_lanes) + (lane & (lanes - 1))) * n, step = n << log_lanes;
   T* const y = static_cast<T*>(exchange_arguments()->tokens[shard]);
-  if (y == nullptr || col >= a.M) return;
-  float sum[n];
+  if (y == nullptr || col0 >= a.M) return;
+  float sum[kCombineUnroll][n];
 #pragma unroll
-  for (int e = 0; e < n; ++e) sum[e] = 0.f;
+  for (int p = 0; p < kCombineUnroll; ++p)
+#pragma unroll
+    for (int e = 0; e < n; ++e) sum[p][e] = 0.f;
   if (token < a.T) {
     for (int i = 0; i < a.k; i += kCombineAhead) {
-      u32x4_t v[kCombineAhead];
+      u32x4_t v[kCombineAhead][kCombineUnroll];
       float w[kCombineAhead];
+      const T* from[kCombineAhead];
+      // choices beyond the last are the last again, those without a slot the first row, with a weight of 0 and zeros for a row: no branch, a load under one is waited for there
+      int slot[kCombineAhead], part[kCombineAhead];
 #pragma unroll
       for (int u = 0; u < kCombineAhead; ++u) {
-        v[u] = u32x4_t{0u, 0u, 0u, 0u};
-        w[u] = 0.f;
-        if (i + u >= a.k) continue;
-        const int o = token * a.k + i + u, slot = ((GSPMD_GLOBAL const int32_t*)a.slots)[o], part = expert_shard(a, o);
-        if (static_cast<uint32_t>(slot) >= static_cast<uint32_t>(a.T * a.k) || part < 0) continue;
+        const int o = token * a.k + min(i + u, a.k - 1);
+        slot[u] = ((GSPMD_GLOBAL const int32_t*)a.slots)[o];
+        part[u] = a.expert_shards == 1 ? 0 : ((GSPMD_GLOBAL const int32_t*)a.experts)[o];
         w[u] = a.weights ? ((GSPMD_GLOBAL const float*)a.weights)[o] : 1.f;
-        v[u] = load_up_to(static_cast<const T*>(exchange_arguments()->rows[part]) + slot * a.ld_rows + col, a.M - col);
       }
+      bool there[kCombineAhead];
 #pragma unroll
       for (int u = 0; u < kCombineAhead; ++u) {
-        float f[n];
-        Sixteen<T>::open(v[u], f);
-#pragma unroll
-        for (int e = 0; e < n; ++e) sum[e] = fmaf(w[u], f[e], sum[e]);
+        there[u] = i + u < a.k && static_cast<uint32_t>(slot[u]) < static_cast<uint32_t>(a.T * a.k) && (a.expert_shards == 1 || static_cast<uint32_t>(part[u]) < static_cast<uint32_t>(a.E));
+        const int of = there[u] && a.expert_shards != 1 ? static_cast<int>(static_cast<uint32_t>(part[u]) / static_cast<uint32_t>(a.es)) : 0;
+        from[u] = static_cast<const T*>(exchange_arguments()->rows[of]) + (there[u] ? slot[u] : 0) * a.ld_rows;
       }
+      if (col0 + (kCombineUnroll - 1) * step + n <= a.M) {
+#pragma unroll
+        for (int u = 0; u < kCombineAhead; ++u)
+#pragma unroll
+          for (int p = 0; p < kCombineUnroll; ++p) v[u][p] = load16(from[u] + col0 + p * step);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kCombineAhead; ++u)
+#pragma unroll
+          for (int p = 0; p < kCombineUnroll; ++p) {
+            v[u][p] = u32x4_t{0u, 0u, 0u, 0u};
+            if (col0 + p * step < a.M) v[u][p] = load_up_to(from[u] + col0 + p * step, a.M - col0 - p * step);
+          }
+      }
+#pragma unroll
+      for (int u = 0; u < kCombineAhead; ++u)
+#pragma unroll
+        for (int p = 0; p < kCombineUnroll; ++p) {
+          float f[n];
+          Sixteen<T>::open(v[u][p], f);
+          const float wu = there[u] ? w[u] : 0.f;
+#pragma unroll
+          for (int e = 0; e < n; ++e) sum[p][e] = fmaf(wu, there[u] ? f[e] : 0.f, sum[p][e]);
+        }
     }
   }
-  store_up_to(y + (token - shard * a.ts) * a.ld_tokens + col, Sixteen<T>::close(sum), a.M - col);
+#pragma unroll
+  for (int p = 0; p < kCombineUnroll; ++p)
+    if (col0 + p * step < a.M) store_up_to(y + (token - shard * a.ts) * a.ld_tokens + col0 + p * step, Sixteen<T>::close(sum[p]), a.M - col0 - p * step);
 }
 
 // drows[slot] = weight * dy[t] and dweight = the product of dy[t] and rows[slot], a wave for a choice (or a few with short rows).

@@ -175,7 +175,7 @@ int32_t launch_exchange(Exchanged what, const ExchangeArgs& a, hipStream_t strea
   constexpr int n = Sixteen<T>::n;
   const int log = row_lanes_log(a.M, n);
   const int64_t side = int64_t(4) << (6 - log), rows = what == kCombine ? static_cast<int64_t>(a.ts) * a.token_shards : static_cast<int64_t>(a.T) * a.k;
-  const int64_t piece = (static_cast<int64_t>(n) << log) * (what == kDispatch ? kExchangeUnroll : 1);
+  const int64_t piece = (static_cast<int64_t>(n) << log) * (what == kDispatch ? kExchangeUnroll : kCombineUnroll);
   const int64_t pieces = what == kCombineGrad ? 1 : (a.M + piece - 1) / piece, groups = (rows + side - 1) / side * pieces;
   if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(groups));
