@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 #include <vector>
 
 #include "../../include/gspmd.h"
@@ -19,11 +20,13 @@ struct Embed {
   int64_t P = 0, T = 0, M = 0, V = 0;
   int64_t na = 1, nb = 1, ts = 0, vs = 0;       // shards of tokens and of the vocabulary, their static extents
   int axis_t = -1, axis_v = -1, vocab_dim = 0;
-  int64_t chunks() const { return T / kChunk; }
-  // the workspace: the tokens' order, where an entry's begin, sums of whole chunks
-  int64_t order_bytes() const { return round_up(T * 4, kWsAlign); }
+  int64_t chunks() const { return (T + kChunk - 1) / kChunk; }
+  // the workspace: the tokens' order and their entries in it, up to a chunk's end; where an entry's begin; chunks' sums, two of each; with dw [M, V] the sums of runs of two tokens and more
+  int64_t order_bytes() const { return round_up(chunks() * kChunk * 4, kWsAlign); }
   int64_t begins_bytes() const { return round_up((V + 1) * 4, kWsAlign); }
-  int64_t bytes() const { return T == 0 ? 0 : order_bytes() + begins_bytes() + round_up(chunks() * M * 4, kWsAlign); }
+  int64_t chunks_bytes() const { return round_up(chunks() * M * 4, kWsAlign); }
+  int64_t sums_bytes() const { return vocab_dim == 1 ? round_up(T / 2 * M * 4, kWsAlign) : 0; }
+  int64_t bytes() const { return T == 0 ? 0 : 2 * order_bytes() + begins_bytes() + 2 * chunks_bytes() + sums_bytes(); }
 };
 
 int32_t analyse(const gspmd_mesh* mesh, const gspmd_sharding* rows_sh, const gspmd_sharding* w_sh, int32_t vocab_dim, Embed* e) {
@@ -44,8 +47,8 @@ int32_t analyse(const gspmd_mesh* mesh, const gspmd_sharding* rows_sh, const gsp
   e->nb = e->axis_v >= 0 ? mesh->shape[e->axis_v] : 1;
   e->ts = (e->T + e->na - 1) / e->na;
   e->vs = (e->V + e->nb - 1) / e->nb;
-  constexpr int64_t kMost = INT32_MAX >> 2;
-  if (e->na > kTokenShards || e->nb > kVocabShards || e->T > (1 << 24) || e->M > kMost || e->V > kMost || e->ts * e->na > kMost || e->vs * e->nb > kMost) return GSPMD_ERR_UNSUPPORTED;
+  constexpr int64_t kMost = INT32_MAX >> 2, kMostColumns = 1 << 21;
+  if (e->na > kTokenShards || e->nb > kVocabShards || e->T > (1 << 24) || e->M > kMostColumns || e->V > kMost || e->ts * e->na > kMost || e->vs * e->nb > kMost) return GSPMD_ERR_UNSUPPORTED;
   return GSPMD_OK;
 }
 
@@ -92,6 +95,16 @@ EmbedArgs arguments(const Embed& e, const Shards& s, float scale) {
   return a;
 }
 
+template <typename Go>
+int32_t by_lines(Lines lines, Go go) {
+  switch (lines) {
+    case kExact: go(std::integral_constant<int, kExact>{}); break;
+    case kNarrow: go(std::integral_constant<int, kNarrow>{}); break;
+    default: go(std::integral_constant<int, kWide>{});
+  }
+  return launched();
+}
+
 template <typename T>
 int32_t launch_embed(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
   const int64_t rows = static_cast<int64_t>(a.ts) * a.token_shards;
@@ -102,45 +115,93 @@ int32_t launch_embed(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
     const int64_t pieces = (a.M + piece - 1) / piece, groups = (rows + per_group - 1) / per_group * pieces;
     if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
     const dim3 grid(static_cast<unsigned>(groups));
-    if (a.scale == 1.f) hipLaunchKernelGGL((embed_rows_kernel<T, false>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
-    else hipLaunchKernelGGL((embed_rows_kernel<T, true>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
-  } else {
-    const int64_t token_blocks = (rows + kColumnTokens - 1) / kColumnTokens, col_blocks = (a.M + kColumnCols - 1) / kColumnCols;
-    const int64_t groups = 8 * token_blocks * ((col_blocks + 7) / 8);
-    if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((embed_columns_kernel<T>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, stream, a, static_cast<int>(token_blocks), static_cast<int>(col_blocks));
+    return by_lines(lines_of<T>(a.M), [&](auto lines) {
+      constexpr int L = decltype(lines)::value;
+      if (a.scale == 1.f) hipLaunchKernelGGL((embed_rows_kernel<T, L, false>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
+      else hipLaunchKernelGGL((embed_rows_kernel<T, L, true>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
+    });
   }
+  const int64_t token_blocks = (rows + kColumnTokens - 1) / kColumnTokens, col_blocks = (a.M + kColumnCols - 1) / kColumnCols;
+  const int64_t groups = 8 * token_blocks * ((col_blocks + 7) / 8);
+  if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL((embed_columns_kernel<T>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, stream, a, static_cast<int>(token_blocks), static_cast<int>(col_blocks));
+  return launched();
+}
+
+// Sums over the runs of the order: rows of dw [V, M], or what embed_grad_columns_kernel reads.
+template <typename T, bool COLUMNS>
+int32_t launch_runs(const EmbedArgs& a, hipStream_t stream) {
+  constexpr int n = Sixteen<T>::n;
+  const int64_t chunks = (static_cast<int64_t>(a.T) + kChunk - 1) / kChunk;
+  const Lines lines = a.accumulate && !COLUMNS ? kExact : lines_of<T>(a.M);
+  const int log = row_lanes_log(a.M, n);
+  int across = 0;
+  while (across < 2 && (static_cast<int64_t>(n) << (log + across)) < a.M) ++across;
+  const int64_t piece = static_cast<int64_t>(n) << (log + across), units = int64_t(4) >> across << (6 - log);
+  const dim3 grid(static_cast<unsigned>((chunks + units - 1) / units), static_cast<unsigned>((a.M + piece - 1) / piece));
+  const int32_t st = by_lines(lines, [&](auto l) { hipLaunchKernelGGL((embed_runs_kernel<T, decltype(l)::value, COLUMNS>), grid, dim3(256), 0, stream, a, log, across); });
+  if (st != GSPMD_OK || chunks < 2) return st;
+  const dim3 joins(static_cast<unsigned>(chunks - 1), static_cast<unsigned>((a.M + 64 * n - 1) / (64 * n)));
+  if (lines == kExact) hipLaunchKernelGGL((embed_joins_kernel<T, kExact, COLUMNS>), joins, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((embed_joins_kernel<T, kWide, COLUMNS>), joins, dim3(256), 0, stream, a);
   return launched();
 }
 
 template <typename T>
-int32_t launch_chunks(const EmbedArgs& a, hipStream_t stream) {
-  constexpr int n = Sixteen<T>::n;
-  const dim3 grid(static_cast<unsigned>(a.T / kChunk), static_cast<unsigned>((a.M + 64 * n - 1) / (64 * n)));
-  if (grid.y > 65535) return GSPMD_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL((embed_chunks_kernel<T>), grid, dim3(256), 0, stream, a);
+int32_t launch_turn(const EmbedArgs& a, hipStream_t stream) {
+  constexpr int n = Sixteen<T>::n, kRows = kTurnLanes * n;
+  const dim3 grid(static_cast<unsigned>((a.vs + kTurnEntries - 1) / kTurnEntries * a.vocab_shards), static_cast<unsigned>((a.M + kRows - 1) / kRows)), block(256);
+  if (a.M < n) {
+    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, kExact, float>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, kExact, T>), grid, block, 0, stream, a);
+  } else {
+    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, kNarrow, float>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, kNarrow, T>), grid, block, 0, stream, a);
+  }
   return launched();
 }
 
+// The gradient: the tokens' order and zeros, the runs' sums, dw's columns.
 template <typename T>
-int32_t launch_gradient(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
-  constexpr int n = Sixteen<T>::n;
-  if (vocab_dim == 0) {
-    const int log = row_lanes_log(a.M, n);
-    int across = 0;
-    while (across < 2 && (static_cast<int64_t>(n) << (log + across)) < a.M) ++across;
-    const int64_t piece = static_cast<int64_t>(n) << (log + across), rows = static_cast<int64_t>(a.vs) * a.vocab_shards;
-    const dim3 grid(static_cast<unsigned>((rows + kRowsSide - 1) / kRowsSide), static_cast<unsigned>((a.M + piece - 1) / piece));
-    if (grid.y > 65535) return GSPMD_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((embed_grad_rows_kernel<T>), grid, dim3(256), 0, stream, a, log, across);
-  } else {
-    constexpr int kRows = kTurnLanes * n;
-    const dim3 grid(static_cast<unsigned>((a.vs + kTurnEntries - 1) / kTurnEntries * a.vocab_shards), static_cast<unsigned>((a.M + kRows - 1) / kRows));
-    if (grid.y > 65535) return GSPMD_ERR_UNSUPPORTED;
-    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, float>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, T>), grid, dim3(256), 0, stream, a);
+int32_t gradient(const Embed& e, const Shards& s, EmbedArgs a, char* workspace, hipStream_t stream) {
+  int32_t st = GSPMD_OK;
+  OrderKeys in{};
+  OrderOut out{};
+  if (e.T > 0) {
+    char* at = workspace;
+    auto take = [&at](int64_t bytes) { char* const here = at; at += bytes; return here; };
+    out.order = reinterpret_cast<int32_t*>(take(e.order_bytes()));
+    out.entries = reinterpret_cast<int32_t*>(take(e.order_bytes()));
+    out.begins = reinterpret_cast<int32_t*>(take(e.begins_bytes()));
+    a.heads = reinterpret_cast<float*>(take(e.chunks_bytes()));
+    a.tails = reinterpret_cast<float*>(take(e.chunks_bytes()));
+    a.sums = reinterpret_cast<float*>(take(e.sums_bytes()));
+    a.order = out.order;
+    a.entries = out.entries;
+    a.begins = out.begins;
+    for (int64_t i = 0; i < e.na; ++i) in.shard[i] = s.ids[static_cast<size_t>(i)];
+    in.per = a.ts;
+    in.shards = a.token_shards;
+    in.count = a.T;
+    in.keys = a.V;
   }
-  return launched();
+  for (const auto& level : s.vocab.which) {
+    for (int64_t j = 0; j < e.nb; ++j) a.vocab[j] = level[static_cast<size_t>(j)];
+    ZeroRows zero{};
+    if (e.vocab_dim == 0) {                     // rows without tokens, and the padding
+      for (int64_t j = 0; j < e.nb; ++j) zero.shard[j] = level[static_cast<size_t>(j)];
+      zero.per = a.vs;
+      zero.shards = a.vocab_shards;
+      zero.from = a.accumulate ? a.V : 0;
+      zero.halves = a.M * static_cast<int32_t>(sizeof(T) / 2);
+      zero.stride = a.ld_vocab * static_cast<int64_t>(sizeof(T) / 2);
+    }
+    if ((st = run_order(in, out, zero, stream)) != GSPMD_OK) return st;
+    if (e.T > 0 && (e.vocab_dim == 0 || in.count > 0) && (st = e.vocab_dim == 0 ? launch_runs<T, false>(a, stream) : launch_runs<T, true>(a, stream)) != GSPMD_OK) return st;
+    in.count = 0;                               // (ordered, for the next replicas; columns' sums are there, too)
+    if (e.vocab_dim == 1 && (st = launch_turn<T>(a, stream)) != GSPMD_OK) return st;
+  }
+  return st;
 }
 
 }  // namespace
@@ -192,27 +253,7 @@ int32_t gspmd_embed_grad(const gspmd_mesh* mesh, const int32_t* const* ids, cons
   const bool bf16 = dy_shards[0].dtype == GSPMD_BF16;
   EmbedArgs a = arguments(e, s, scale);
   a.accumulate = accumulate != 0;
-  if (e.T > 0) {
-    char* at = static_cast<char*>(workspace);
-    int32_t* const order = reinterpret_cast<int32_t*>(at);
-    int32_t* const begins = reinterpret_cast<int32_t*>(at + e.order_bytes());
-    OrderKeys in{};
-    for (int64_t i = 0; i < e.na; ++i) in.shard[i] = s.ids[static_cast<size_t>(i)];
-    in.per = a.ts;
-    in.shards = a.token_shards;
-    in.count = a.T;
-    in.keys = a.V;
-    if ((st = run_order(in, OrderOut{order, begins}, stream)) != GSPMD_OK) return st;
-    a.order = order;
-    a.begins = begins;
-    a.chunks = reinterpret_cast<float*>(at + e.order_bytes() + e.begins_bytes());
-    if (e.chunks() > 0 && (st = bf16 ? launch_chunks<bf16_bits>(a, stream) : launch_chunks<float>(a, stream)) != GSPMD_OK) return st;
-  }
-  for (const auto& level : s.vocab.which) {
-    for (int64_t j = 0; j < e.nb; ++j) a.vocab[j] = level[static_cast<size_t>(j)];
-    if ((st = bf16 ? launch_gradient<bf16_bits>(a, vocab_dim, stream) : launch_gradient<float>(a, vocab_dim, stream)) != GSPMD_OK) return st;
-  }
-  return GSPMD_OK;
+  return bf16 ? gradient<bf16_bits>(e, s, a, static_cast<char*>(workspace), stream) : gradient<float>(e, s, a, static_cast<char*>(workspace), stream);
 } catch (...) { return GSPMD_ERR_HOST_MEMORY; }
 
 }  // extern "C"

@@ -2,14 +2,16 @@
 //
 // Both are bound by memory: the rows that are read and the rows that are written, once each.  A vocabulary matrix [V, M] has an entry's row in one piece, read and written 16 bytes a lane at
 // element alignment, neighbouring lanes side by side; in one [M, V] an entry is a column, and tiles turn in LDS.
-// The gradient has one writer for each of its elements: tokens are ordered by entry (kernels_order.h), a row of dw is the sum over its run of them, in float32, in ascending order of the tokens -- but
-// for whole chunks of that order that lie inside one run, which are added up by themselves first, so that an entry that half of a text consists of is no chain of
-// thousands of loads.  So equal inputs give equal bits, and a row without tokens is zeros.
+// The gradient has one writer for each of its elements.  Tokens are ordered by entry (kernels_order.h); an entry's are a run of that order, and its row of dw is the sum over the run, in float32.  The
+// order is cut into chunks of 32 tokens, which are added up side by side whatever the runs are, so that an entry that half of a text consists of is no chain of thousands of loads: a run inside a chunk
+// is finished there, what a chunk has of runs that begin before it or end behind it are partial sums, added up by the chunk that a run begins in, in a second launch.  All sums have one
+// fixed order, so equal inputs give equal bits.  Rows of dw [V, M] without tokens are zeroed in the launch that orders; a dw [M, V] is written whole from the sums.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include "kernels_basic.h"
+#include "kernels_rows.h"
 #include "mfma_common.h"
 
 namespace gspmd {
@@ -30,9 +32,10 @@ struct EmbedArgs {
   int64_t ld_vocab;
   float scale;
   int32_t accumulate;
-  // the gradient's: tokens in the order of their entries, where an entry's begin [V + 1], and sums of whole chunks of the order, [chunk][M]
-  const int32_t *order, *begins;
-  float* chunks;
+  // the gradient's: the token and its entry at every place of the order, where an entry's begin [V + 1], chunks' sums [chunk][M] of a run that began before and of one that begins there and ends
+  // behind it, and (dw [M, V]) runs' sums, at half the place where they begin, [T / 2][M]
+  const int32_t *order, *entries, *begins;
+  float *heads, *tails, *sums;
 };
 constexpr int kChunk = 32;     // tokens
 
@@ -41,98 +44,31 @@ __device__ __forceinline__ embed_args* embed_arguments() { return first_kernel_a
 // (one shard: no division)
 __device__ __forceinline__ int embed_shard(int i, int per, int shards) { return shards == 1 ? 0 : static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(per)); }
 
-template <typename T> struct Sixteen;          // 16 bytes as float32, and back with one rounding
-template <> struct Sixteen<bf16_bits> {
-  static constexpr int n = 8;
-  static __device__ __forceinline__ void open(u32x4_t v, float (&f)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
-  }
-  static __device__ __forceinline__ u32x4_t close(const float (&f)[8]) {
-    typedef __attribute__((ext_vector_type(8))) float float8_t;
-    float8_t v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = f[i];
-    return __builtin_bit_cast(u32x4_t, __builtin_convertvector(v, bf16x8_t));
-  }
-};
-template <> struct Sixteen<float> {
-  static constexpr int n = 4;
-  static __device__ __forceinline__ void open(u32x4_t v, float (&f)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
-  }
-  static __device__ __forceinline__ u32x4_t close(const float (&f)[4]) {
-    u32x4_t v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(f[i]);
-    return v;
-  }
-};
-template <typename T> struct AnyAligned;
-template <> struct AnyAligned<bf16_bits> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2))); };
-template <> struct AnyAligned<float> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4))); };
-template <typename T> __device__ __forceinline__ u32x4_t load16(const T* p) { return *(GSPMD_GLOBAL const typename AnyAligned<T>::type*)p; }
-template <typename T> __device__ __forceinline__ void store16(T* p, u32x4_t v) { *(GSPMD_GLOBAL typename AnyAligned<T>::type*)p = v; }
-// the first `count` elements of 16 bytes
-template <typename T> __device__ __forceinline__ u32x4_t load_some(const T* p, int count) {
-  u32x4_t v = {0u, 0u, 0u, 0u};
-  constexpr int n = Sixteen<T>::n;
-#pragma unroll
-  for (int i = 0; i < n; ++i)
-    if (i < count) {
-      const uint32_t bits = sizeof(T) == 2 ? static_cast<uint32_t>(((GSPMD_GLOBAL const uint16_t*)p)[i]) : ((GSPMD_GLOBAL const uint32_t*)p)[i];
-      if constexpr (sizeof(T) == 2) v[i >> 1] |= bits << ((i & 1) * 16);
-      else v[i] = bits;
-    }
-  return v;
-}
-template <typename T> __device__ __forceinline__ void store_some(T* p, u32x4_t v, int count) {
-  constexpr int n = Sixteen<T>::n;
-#pragma unroll
-  for (int i = 0; i < n; ++i)
-    if (i < count) {
-      if constexpr (sizeof(T) == 2) ((GSPMD_GLOBAL uint16_t*)p)[i] = static_cast<uint16_t>(v[i >> 1] >> ((i & 1) * 16));
-      else ((GSPMD_GLOBAL uint32_t*)p)[i] = v[i];
-    }
-}
-template <typename T> __device__ __forceinline__ u32x4_t load_up_to(const T* p, int count) { return count >= Sixteen<T>::n ? load16(p) : load_some(p, count); }
-template <typename T> __device__ __forceinline__ void store_up_to(T* p, u32x4_t v, int count) {
-  if (count >= Sixteen<T>::n) store16(p, v);
-  else store_some(p, v, count);
-}
-
-// How many lanes a row of `elements` takes: a power of two, up to a wave.
-__host__ __device__ __forceinline__ int row_lanes_log(int elements, int per_lane) {
-  int log = 0;
-  while (log < 6 && (per_lane << log) < elements) ++log;
-  return log;
-}
-
 // y [V, M]: a wave has a piece of a row (or a few short rows), kEmbedUnroll x 16 bytes a lane.
-constexpr int kEmbedUnroll = 8;
-template <typename T, bool SCALED>
+constexpr int kEmbedUnroll = 4;
+template <typename T, int LINES, bool SCALED>
 __global__ __launch_bounds__(256) void embed_rows_kernel(const EmbedArgs a, int log_lanes, int pieces) {
   constexpr int n = Sixteen<T>::n;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lanes = 1 << log_lanes;
+  const int log = LINES == kWide ? 6 : log_lanes, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = blockIdx.x / pieces, piece = blockIdx.x - group * pieces;              // (neighbouring pieces of rows together)
-  const int row = ((group * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);            // static rows of all shards, one after the other
+  const int row = of_row<LINES>(((group * 4 + wave) << (6 - log)) + (lane >> log));        // static rows of all shards, one after the other
   if (row >= a.ts * a.token_shards) return;
-  const int shard = embed_shard(row, a.ts, a.token_shards), within = row - shard * a.ts;
+  const int shard = of_row<LINES>(embed_shard(row, a.ts, a.token_shards)), within = row - shard * a.ts;
   const TokenShard to = {embed_arguments()->tokens[shard].ids, embed_arguments()->tokens[shard].rows};
   if (to.rows == nullptr) return;
-  const int id = row < a.T ? ((GSPMD_GLOBAL const int32_t*)to.ids)[within] : -1;
+  const int id = row < a.T ? of_row<LINES>(((GSPMD_GLOBAL const int32_t*)to.ids)[within]) : -1;
   const bool there = static_cast<uint32_t>(id) < static_cast<uint32_t>(a.V);
   T* const y = static_cast<T*>(to.rows) + static_cast<int64_t>(within) * a.ld_rows;
-  const int of = there ? embed_shard(id, a.vs, a.vocab_shards) : 0;
+  const int of = there ? of_row<LINES>(embed_shard(id, a.vs, a.vocab_shards)) : 0;
   const T* const w = static_cast<const T*>(embed_arguments()->vocab[of]) + (there ? static_cast<int64_t>(id - of * a.vs) * a.ld_vocab : 0);
-  const int col0 = ((piece * kEmbedUnroll) << log_lanes) * n + (lane & (lanes - 1)) * n, step = n << log_lanes;
+  const int col0 = (((piece * kEmbedUnroll) << log) + (lane & ((1 << log) - 1))) * n, step = n << log;
   u32x4_t v[kEmbedUnroll];
+  if (there) {
 #pragma unroll
-  for (int u = 0; u < kEmbedUnroll; ++u) {
-    v[u] = u32x4_t{0u, 0u, 0u, 0u};
-    const int col = col0 + u * step;
-    if (there && col < a.M) v[u] = load_up_to(w + col, a.M - col);
+    for (int u = 0; u < kEmbedUnroll; ++u) v[u] = load_line<LINES, T>(w, line_at<LINES, T>(col0 + u * step, a.M), a.M);
+  } else {
+#pragma unroll
+    for (int u = 0; u < kEmbedUnroll; ++u) v[u] = u32x4_t{0u, 0u, 0u, 0u};
   }
 #pragma unroll
   for (int u = 0; u < kEmbedUnroll; ++u) {
@@ -144,7 +80,7 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(const EmbedArgs a, int 
       for (int i = 0; i < n; ++i) f[i] *= a.scale;
       v[u] = Sixteen<T>::close(f);
     }
-    if (col < a.M) store_up_to(y + col, v[u], a.M - col);
+    if (col < a.M) store_line<LINES, T>(y, line_at<LINES, T>(col, a.M), a.M, v[u]);
   }
 }
 
@@ -204,154 +140,130 @@ __device__ __forceinline__ const T* token_row(const EmbedArgs& a, int token) {
   return static_cast<const T*>(embed_arguments()->tokens[shard].rows) + static_cast<int64_t>(token - shard * a.ts) * a.ld_rows;
 }
 
-// sum += the `count` tokens' 16 bytes at `col` from place `at` of the order on, ascending
-template <typename T>
-__device__ __forceinline__ void add_tokens(const EmbedArgs& a, int at, int count, int col, float (&sum)[Sixteen<T>::n]) {
-  constexpr int n = Sixteen<T>::n, kAhead = 8;
-  GSPMD_GLOBAL const int32_t* const order = (GSPMD_GLOBAL const int32_t*)a.order + at;
-  int i = 0;
-  for (; i + kAhead <= count; i += kAhead) {
-    u32x4_t v[kAhead];
+// dw's row of an entry [V, M] from its sum.  (Added to what is there: LINES exact.)
+template <typename T, int LINES>
+__device__ __forceinline__ void finish_row(const EmbedArgs& a, int entry, int at, float (&sum)[Sixteen<T>::n]) {
+  constexpr int n = Sixteen<T>::n;
+  const int shard = of_row<LINES>(embed_shard(entry, a.vs, a.vocab_shards));
+  T* dw = static_cast<T*>(embed_arguments()->vocab[shard]);
+  if (dw == nullptr) return;
+  dw += static_cast<int64_t>(entry - shard * a.vs) * a.ld_vocab;
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) v[u] = load_up_to(token_row<T>(a, order[i + u]) + col, a.M - col);
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
+  for (int e = 0; e < n; ++e) sum[e] *= a.scale;
+  if constexpr (LINES == kExact) {
+    if (a.accumulate) {
       float f[n];
-      Sixteen<T>::open(v[u], f);
+      Sixteen<T>::open(load_line<LINES, T>(dw, at, a.M), f);
 #pragma unroll
       for (int e = 0; e < n; ++e) sum[e] += f[e];
     }
   }
-  for (; i < count; ++i) {
-    float f[n];
-    Sixteen<T>::open(load_up_to(token_row<T>(a, order[i]) + col, a.M - col), f);
-#pragma unroll
-    for (int e = 0; e < n; ++e) sum[e] += f[e];
-  }
+  store_line<LINES, T>(dw, at, a.M, Sixteen<T>::close(sum));
 }
 
-// Sums of the chunks that lie inside one entry's run: blockIdx.x the chunk, blockIdx.y 64 x 16 bytes of the row; a wave a quarter of the tokens.
-template <typename T>
-__global__ __launch_bounds__(256) void embed_chunks_kernel(const EmbedArgs a) {
-  constexpr int n = Sixteen<T>::n;
-  const int at = blockIdx.x * kChunk, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  GSPMD_GLOBAL const int32_t* const begins = (GSPMD_GLOBAL const int32_t*)a.begins;
-  if (at + kChunk > begins[a.V]) return;        // some of it no token's place
-  const int first = ((GSPMD_GLOBAL const int32_t*)a.order)[at], shard = embed_shard(first, a.ts, a.token_shards);
-  const int key = ((GSPMD_GLOBAL const int32_t*)embed_arguments()->tokens[shard].ids)[first - shard * a.ts];
-  if (static_cast<uint32_t>(key) >= static_cast<uint32_t>(a.V) || begins[key + 1] < at + kChunk) return;
-  __shared__ float sums[4][64 * n];
-  const int col = (blockIdx.y * 64 + lane) * n;
+// Chunks of the order: a wave (or a few lanes of one, with short rows) has a chunk and 16 bytes a lane of its tokens' rows, eight tokens' on their way at a time.
+// COLUMNS: dw is [M, V]; runs of several tokens are put by for embed_grad_columns_kernel, those of one it reads itself.
+template <typename T, int LINES, bool COLUMNS>
+__global__ __launch_bounds__(256) void embed_runs_kernel(const EmbedArgs a, int log_lanes, int log_across) {
+  constexpr int n = Sixteen<T>::n, kAhead = 8;
+  const int log = LINES == kWide ? 6 : log_lanes, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int across = 1 << log_across, units = (4 >> log_across) << (6 - log);              // waves along a row; chunks of a workgroup
+  const int chunk = of_row<LINES>(blockIdx.x * units + ((wave >> log_across) << (6 - log)) + (lane >> log));
+  const int col = (((blockIdx.y * across + (wave & (across - 1))) << log) + (lane & ((1 << log) - 1))) * n;
+  const int total = ((GSPMD_GLOBAL const int32_t*)a.begins)[a.V], begin = chunk * kChunk, end = min(begin + kChunk, total);
+  if (begin >= total || col >= a.M) return;
+  GSPMD_GLOBAL const int32_t* const order = (GSPMD_GLOBAL const int32_t*)a.order;
+  GSPMD_GLOBAL const int32_t* const entries = (GSPMD_GLOBAL const int32_t*)a.entries;
+  const int at = line_at<LINES, T>(col, a.M);
+  bool open = begin > 0 && entries[max(begin - 1, 0)] == entries[begin];       // the run began before the chunk
+  int first = begin;                                                           // the run's first place here
   float sum[n];
 #pragma unroll
   for (int e = 0; e < n; ++e) sum[e] = 0.f;
-  if (col < a.M) add_tokens<T>(a, at + wave * (kChunk / 4), kChunk / 4, col, sum);
+#pragma unroll 1
+  for (int base = begin; base < end; base += kAhead) {
+    int entry[kAhead + 1];
+    u32x4_t v[kAhead];
 #pragma unroll
-  for (int e = 0; e < n; ++e) sums[wave][lane * n + e] = sum[e];
-  __syncthreads();
-  float* const out = a.chunks + static_cast<int64_t>(blockIdx.x) * a.M + blockIdx.y * 64 * n;
-  for (int i = threadIdx.x; i < 64 * n && blockIdx.y * 64 * n + i < a.M; i += 256) out[i] = ((sums[0][i] + sums[1][i]) + sums[2][i]) + sums[3][i];
-}
-
-// The sum over places [begin, end) of the order, one entry's run, for the columns from `col` on.
-template <typename T>
-__device__ __forceinline__ void add_run(const EmbedArgs& a, int begin, int end, int col, float (&sum)[Sixteen<T>::n]) {
-  constexpr int n = Sixteen<T>::n;
-  const int first = (begin + kChunk - 1) / kChunk, last = end / kChunk;        // whole chunks
-  if (first >= last) {
-    add_tokens<T>(a, begin, end - begin, col, sum);
-    return;
-  }
-  add_tokens<T>(a, begin, first * kChunk - begin, col, sum);
-  GSPMD_GLOBAL const float* at = (GSPMD_GLOBAL const float*)a.chunks + static_cast<int64_t>(first) * a.M + col;
-  constexpr int kAhead = 4;
-  int c = first;
-  for (; c < last; c += kAhead) {
-    float v[kAhead][n];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-      for (int e = 0; e < n; ++e) v[u][e] = c + u < last && col + e < a.M ? at[u * static_cast<int64_t>(a.M) + e] : 0.f;
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-      for (int e = 0; e < n; ++e) sum[e] += v[u][e];
-    at += kAhead * static_cast<int64_t>(a.M);
-  }
-  add_tokens<T>(a, last * kChunk, end - last * kChunk, col, sum);
-}
-
-// dw [V, M]: a workgroup has kRowsSide entries and 4 waves' columns of them (blockIdx.y), or fewer columns and the rows shared out.  Most entries have no token, and most that have any have one: where the
-// runs begin is read at once, and the first tokens of four rows are on their way together.
-constexpr int kRowsSide = 16, kRowsAhead = 4;
-template <typename T>
-__global__ __launch_bounds__(256) void embed_grad_rows_kernel(const EmbedArgs a, int log_lanes, int log_across) {
-  constexpr int n = Sixteen<T>::n;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row0 = blockIdx.x * kRowsSide, rows = a.vs * a.vocab_shards;
-  const int begins = a.T > 0 ? ((GSPMD_GLOBAL const int32_t*)a.begins)[min(row0 + min(lane, kRowsSide), a.V)] : 0;      // (of a row behind the last entry: the end of all, as its successor's)
-  const int across = 1 << log_across, side = 64 >> log_lanes;        // waves along a row; rows of a wave at a time
-  const int col = ((blockIdx.y * across + (wave & (across - 1))) << log_lanes) * n + (lane & ((1 << log_lanes) - 1)) * n;
-  const int turn = (4 >> log_across) * side;                          // from a lane's row to its next
-  const bool in = col < a.M;
-  for (int r0 = (wave >> log_across) * side + (lane >> log_lanes); r0 - (lane >> log_lanes) < kRowsSide; r0 += kRowsAhead * turn) {
-    int begin[kRowsAhead], end[kRowsAhead], token[kRowsAhead];
-    u32x4_t v[kRowsAhead];
-#pragma unroll
-    for (int u = 0; u < kRowsAhead; ++u) {
-      const int r = r0 + u * turn;
-      begin[u] = __shfl(begins, min(r, kRowsSide));
-      end[u] = __shfl(begins, min(r + 1, kRowsSide));
-      token[u] = 0;
-      v[u] = u32x4_t{0u, 0u, 0u, 0u};
+    for (int u = 0; u < kAhead; ++u) {          // (places up to the chunk's end exist; those behind the last token hold anything)
+      const int token = of_row<LINES>(order[base + u]);
+      entry[u] = of_row<LINES>(entries[base + u]);
+      v[u] = load_line<LINES, T>(token_row<T>(a, base + u < end ? token : 0), at, a.M);
     }
-    bool any = false;
+    entry[kAhead] = base + kAhead < total ? of_row<LINES>(entries[base + kAhead]) : a.V;
 #pragma unroll
-    for (int u = 0; u < kRowsAhead; ++u) any = any || begin[u] < end[u];
-    if (any && in) {
-#pragma unroll
-      for (int u = 0; u < kRowsAhead; ++u) token[u] = ((GSPMD_GLOBAL const int32_t*)a.order)[begin[u] < end[u] ? begin[u] : 0];
-      const bool whole = col + n <= a.M;
-#pragma unroll
-      for (int u = 0; u < kRowsAhead; ++u)
-        if (whole) v[u] = load16(token_row<T>(a, begin[u] < end[u] ? token[u] : 0) + col);
-        else if (begin[u] < end[u]) v[u] = load_some(token_row<T>(a, token[u]) + col, a.M - col);
-    }
-#pragma unroll
-    for (int u = 0; u < kRowsAhead; ++u) {
-      const int r = r0 + u * turn, row = row0 + r;
-      if (r >= kRowsSide || row >= rows || !in) continue;
-      const int shard = embed_shard(row, a.vs, a.vocab_shards);
-      T* dw = static_cast<T*>(embed_arguments()->vocab[shard]);
-      if (dw == nullptr) continue;
-      dw += static_cast<int64_t>(row - shard * a.vs) * a.ld_vocab + col;
-      if (begin[u] == end[u]) {
-        if (!a.accumulate || row >= a.V) store_up_to(dw, u32x4_t{0u, 0u, 0u, 0u}, a.M - col);
-        continue;
-      }
-      float sum[n];
-      Sixteen<T>::open(v[u], sum);
-      if (begin[u] + 1 < end[u]) add_run<T>(a, begin[u] + 1, end[u], col, sum);
-#pragma unroll
-      for (int e = 0; e < n; ++e) sum[e] *= a.scale;
-      if (a.accumulate) {
+    for (int u = 0; u < kAhead; ++u) {
+      const int place = base + u;
+      if (place < end) {
         float f[n];
-        Sixteen<T>::open(load_up_to(dw, a.M - col), f);
+        Sixteen<T>::open(v[u], f);
 #pragma unroll
         for (int e = 0; e < n; ++e) sum[e] += f[e];
+        const bool ends = place + 1 == total || entry[u + 1] != entry[u];
+        if (ends || place + 1 == end) {
+          const bool part = open || !ends;
+          if (part || COLUMNS) {
+            float* const to = open ? a.heads + static_cast<int64_t>(chunk) * a.M : part ? a.tails + static_cast<int64_t>(chunk) * a.M : a.sums + static_cast<int64_t>(first >> 1) * a.M;
+            if (part || first != place) store_sums<LINES, n>(to, at, a.M, sum);
+          } else {
+            finish_row<T, LINES>(a, entry[u], at, sum);
+          }
+          open = false;
+          first = place + 1;
+#pragma unroll
+          for (int e = 0; e < n; ++e) sum[e] = 0.f;
+        }
       }
-      store_up_to(dw, Sixteen<T>::close(sum), a.M - col);
     }
   }
 }
 
-// dw [M, V]: 64 entries x 16 lanes' 16 bytes of dw's rows a workgroup.  Sixteen lanes have an entry, four of them one after the other, whose first tokens are on their way together; what they add up turns in
-// LDS, rounded but for what is still to be added to (TTile float).  Bound by what is on its way: 8 workgroups on a compute unit, each 5 KB of rows and 16 of dw.
+// Runs of several chunks: a workgroup for the chunk that one begins in (blockIdx.x) and 64 x 16 bytes of the row (blockIdx.y), a wave every fourth of the chunks behind it.
+template <typename T, int LINES, bool COLUMNS>
+__global__ __launch_bounds__(256) void embed_joins_kernel(const EmbedArgs a) {
+  constexpr int n = Sixteen<T>::n, kAhead = 4;
+  const int chunk = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  GSPMD_GLOBAL const int32_t* const entries = (GSPMD_GLOBAL const int32_t*)a.entries;
+  GSPMD_GLOBAL const int32_t* const begins = (GSPMD_GLOBAL const int32_t*)a.begins;
+  const int begin = chunk * kChunk, end = begin + kChunk;
+  if (end >= begins[a.V]) return;               // nothing behind it
+  const int entry = entries[end - 1];
+  if (entries[end] != entry || begins[entry] < begin) return;
+  const int last = (begins[entry + 1] - 1) / kChunk, col = (blockIdx.y * 64 + lane) * n, at = line_at<LINES, T>(col, a.M);
+  float sum[n];
+#pragma unroll
+  for (int e = 0; e < n; ++e) sum[e] = 0.f;
+#pragma unroll 1
+  for (int c = chunk + 1 + wave; c <= last; c += 4 * kAhead) {
+    float v[kAhead][n];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) load_sums<LINES, n>(a.heads + static_cast<int64_t>(min(c + 4 * u, last)) * a.M, at, a.M, v[u]);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int e = 0; e < n; ++e) sum[e] += c + 4 * u <= last ? v[u][e] : 0.f;
+  }
+  __shared__ float sums[4][n][64];
+#pragma unroll
+  for (int e = 0; e < n; ++e) sums[wave][e][lane] = sum[e];
+  __syncthreads();
+  if (wave > 0 || col >= a.M) return;
+  load_sums<LINES, n>(a.tails + static_cast<int64_t>(chunk) * a.M, at, a.M, sum);
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+#pragma unroll
+    for (int e = 0; e < n; ++e) sum[e] += sums[w][e][lane];
+  if constexpr (COLUMNS) store_sums<LINES, n>(a.sums + static_cast<int64_t>(begins[entry] >> 1) * a.M, at, a.M, sum);
+  else finish_row<T, LINES>(a, entry, at, sum);
+}
+
+// dw [M, V]: 64 entries x 16 lanes' 16 bytes of dw's rows a workgroup.  Sixteen lanes have an entry, four of them one after the other, on their way together: the row of its token, or the sum of its
+// tokens'.  They turn in LDS, rounded but for what is still to be added to (TTile float).
 constexpr int kTurnEntries = 64, kTurnLanes = 16;
-template <typename T, typename TTile>
+template <typename T, int LINES, typename TTile>
 __global__ __launch_bounds__(256) void embed_grad_columns_kernel(const EmbedArgs a) {
   constexpr int n = Sixteen<T>::n, kRows = kTurnLanes * n, side = 64 / kTurnLanes, kEach = kTurnEntries / (4 * side), kPitch = kTurnEntries + (sizeof(TTile) == 2 ? 2 : 1);
-  __shared__ __attribute__((aligned(4))) TTile tile[kRows][kPitch];
+  __shared__ __attribute__((aligned(4))) TTile tile[n + kRows][kPitch];        // (n rows before the tile's: what the lane at the row's end has of its neighbours' may begin there)
   __shared__ int begins[kTurnEntries + 1];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   // entries of one shard: blockIdx.x counts blocks of every shard
@@ -361,59 +273,56 @@ __global__ __launch_bounds__(256) void embed_grad_columns_kernel(const EmbedArgs
   if (dw == nullptr) return;
   if (t <= kTurnEntries) begins[t] = a.T > 0 ? ((GSPMD_GLOBAL const int32_t*)a.begins)[min(row0 + t, a.V)] : 0;
   __syncthreads();
-  const int col = m0 + (lane & (kTurnLanes - 1)) * n, r0 = wave * side + lane / kTurnLanes;
-  int begin[kEach], end[kEach], token[kEach];
+  const int col = m0 + (lane & (kTurnLanes - 1)) * n, at = line_at<LINES, T>(col, a.M), r0 = wave * side + lane / kTurnLanes;
+  int begin[kEach], count[kEach], token[kEach];
   u32x4_t v[kEach];
   bool any = false;
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
     const int r = r0 + u * 4 * side;
     begin[u] = begins[r];
-    end[u] = r < entries ? begins[r + 1] : begin[u];
-    any = any || begin[u] < end[u];
+    count[u] = r < entries ? begins[r + 1] - begin[u] : 0;
+    any = any || count[u] > 0;
     v[u] = u32x4_t{0u, 0u, 0u, 0u};
     token[u] = 0;
   }
   if (any && col < a.M) {
 #pragma unroll
-    for (int u = 0; u < kEach; ++u) token[u] = ((GSPMD_GLOBAL const int32_t*)a.order)[begin[u] < end[u] ? begin[u] : 0];
-    const bool whole = col + n <= a.M;
+    for (int u = 0; u < kEach; ++u) token[u] = ((GSPMD_GLOBAL const int32_t*)a.order)[count[u] > 0 ? begin[u] : 0];
 #pragma unroll
-    for (int u = 0; u < kEach; ++u)
-      if (whole) v[u] = load16(token_row<T>(a, begin[u] < end[u] ? token[u] : 0) + col);
-      else if (begin[u] < end[u]) v[u] = load_some(token_row<T>(a, token[u]) + col, a.M - col);
+    for (int u = 0; u < kEach; ++u) v[u] = load_line<LINES, T>(token_row<T>(a, count[u] > 0 ? token[u] : 0), at, a.M);
   }
 #pragma unroll
   for (int u = 0; u < kEach; ++u) {
     float sum[n];
     Sixteen<T>::open(v[u], sum);
-    if (begin[u] + 1 < end[u] && col < a.M) add_run<T>(a, begin[u] + 1, end[u], col, sum);
-    const int r = r0 + u * 4 * side;
+    if (count[u] > 1 && col < a.M) load_sums<LINES, n>(a.sums + static_cast<int64_t>(begin[u] >> 1) * a.M, at, a.M, sum);
 #pragma unroll
-    for (int e = 0; e < n; ++e) store_from_float<TTile>(&tile[(lane & (kTurnLanes - 1)) * n + e][r], begin[u] < end[u] ? sum[e] * a.scale : 0.f);
+    for (int e = 0; e < n; ++e)
+      if (col < a.M) store_from_float<TTile>(&tile[n + at - m0 + e][r0 + u * 4 * side], count[u] > 0 ? sum[e] * a.scale : 0.f);
   }
   __syncthreads();
   for (int i = t; i < kRows * (kTurnEntries / n); i += 256) {
-    const int m = i / (kTurnEntries / n), c = (i - m * (kTurnEntries / n)) * n, count = entries - c;
-    if (m0 + m >= a.M || count <= 0) continue;
-    T* const at = dw + (m0 + m) * a.ld_vocab + c0 + c;
+    const int m = i / (kTurnEntries / n), c = (i - m * (kTurnEntries / n)) * n, keep = entries - c;
+    if (m0 + m >= a.M || keep <= 0) continue;
+    T* const to = dw + (m0 + m) * a.ld_vocab + c0 + c;
     if constexpr (sizeof(TTile) == 2) {
       u32x4_t o;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = *reinterpret_cast<const uint32_t*>(&tile[m][c + 2 * e]);
-      store_up_to(at, o, count);
+      for (int e = 0; e < 4; ++e) o[e] = *reinterpret_cast<const uint32_t*>(&tile[n + m][c + 2 * e]);
+      store_up_to(to, o, keep);
     } else {
       float f[n];
 #pragma unroll
-      for (int e = 0; e < n; ++e) f[e] = tile[m][c + e];
+      for (int e = 0; e < n; ++e) f[e] = tile[n + m][c + e];
       if (a.accumulate) {                       // entries without tokens keep what they have
         float before[n];
-        Sixteen<T>::open(load_up_to(at, count), before);
+        Sixteen<T>::open(load_up_to(to, keep), before);
 #pragma unroll
         for (int e = 0; e < n; ++e)
-          if (e < count && row0 + c + e < a.V) f[e] = begins[c + e] == begins[c + e + 1] ? before[e] : before[e] + f[e];
+          if (e < keep && row0 + c + e < a.V) f[e] = begins[c + e] == begins[c + e + 1] ? before[e] : before[e] + f[e];
       }
-      store_up_to(at, Sixteen<T>::close(f), count);
+      store_up_to(to, Sixteen<T>::close(f), keep);
     }
   }
 }

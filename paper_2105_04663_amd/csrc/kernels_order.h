@@ -10,29 +10,86 @@
 #include <stdint.h>
 
 #include "kernels_basic.h"
+#include "kernels_rows.h"
 #include "mfma_common.h"
 #include "order.h"
 #include "ragged.h"
 
 namespace gspmd {
 
-__global__ __launch_bounds__(kOrderThreads) void order_kernel(const OrderKeys in, const OrderOut out, int log_range) {
+struct OrderWork {
+  OrderKeys in;
+  OrderOut out;
+  ZeroRows zero;
+  int32_t log_range, groups;                    // of workgroups that order; those behind them zero rows
+  int32_t zero_log, zero_pieces;                // lanes of a row, as a power of two; pieces of kZeroUnroll x 16 bytes a lane
+};
+
+// Rows zeroed: a workgroup has a piece of every so-many-th row, a wave one row (or a few short ones) at a time.
+constexpr int kZeroUnroll = 4;
+__device__ __forceinline__ void zero_rows(const OrderWork& w) {
+  typedef bf16_bits half;
+  constexpr int n = Sixteen<half>::n;
+  const ZeroRows& z = w.zero;
+  const int block = blockIdx.x - w.groups, of = gridDim.x - w.groups, piece = block % w.zero_pieces, log = w.zero_log, side = 6 - log;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), count = z.per * z.shards - z.from;
+  const int col0 = (((piece * kZeroUnroll) << log) + (lane & ((1 << log) - 1))) * n, turn = (of / w.zero_pieces * kOrderWaves) << side;
+  for (int64_t base = static_cast<int64_t>(block / w.zero_pieces * kOrderWaves + wave) << side; base < count; base += turn) {
+    const int row = static_cast<int>(base) + (lane >> log) + z.from;
+    if (row - z.from >= count) break;
+    int shard = z.shards == 1 ? 0 : static_cast<int>(static_cast<uint32_t>(row) / static_cast<uint32_t>(z.per));
+    if (log == 6) shard = __builtin_amdgcn_readfirstlane(shard);
+    half* const to = static_cast<half*>(z.shards == 1 ? z.shard[0] : first_kernel_argument<OrderWork>()->zero.shard[shard]);
+    if (to == nullptr) continue;
+    half* const at = to + static_cast<int64_t>(row - shard * z.per) * z.stride;
+    const u32x4_t zeros = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int u = 0; u < kZeroUnroll; ++u) {
+      const int col = col0 + ((u << log) * n);
+      if (col < z.halves) {
+        if (z.halves >= n) store_line<kNarrow, half>(at, line_at<kNarrow, half>(col, z.halves), z.halves, zeros);
+        else store_some(at, zeros, z.halves);
+      }
+    }
+  }
+}
+
+__global__ __launch_bounds__(kOrderThreads) void order_kernel(const OrderWork w) {
   extern __shared__ __attribute__((aligned(16))) int32_t counts[];      // [range][waves]
   __shared__ int32_t sums[kOrderWaves], below[kOrderWaves];
-  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), entries = kOrderWaves << log_range;
+  __shared__ const int32_t* from[kKeyShards];
+  if (static_cast<int>(blockIdx.x) >= w.groups) {
+    zero_rows(w);
+    return;
+  }
+  const OrderKeys& in = w.in;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), log_range = w.log_range, entries = kOrderWaves << log_range;
   const int lo = blockIdx.x << log_range, range = min(1 << log_range, in.keys - lo);
   const int part = ((in.count + kOrderWaves - 1) / kOrderWaves + 63) & ~63, first = min(wave * part, in.count), end = min(first + part, in.count);
+  if (in.shards > 1 && t < in.shards) from[t] = first_kernel_argument<OrderWork>()->in.shard[t];
   for (int i = t; i < entries; i += kOrderThreads) counts[i] = 0;
   __syncthreads();
-  constexpr int kAhead = 16;
-  int less = 0;
-  for (int base = first; base < end; base += 64 * kAhead) {
-    int key[kAhead];
+  constexpr int kAhead = 8;
+  int key[kAhead];
+  // this lane's of 64 x kAhead keys from `base` on, INT32_MAX behind the wave's last; what is no key is `keys`.  (No branch: a load in one is waited for there.)
+  auto load = [&](int base) {
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) key[u] = in.at(min(base + u * 64 + lane, end - 1));      // (no branch: a load under one is waited for there)
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = min(base + u * 64 + lane, end - 1);
+      if (in.shards == 1) {
+        key[u] = ((GSPMD_GLOBAL const int32_t*)in.shard[0])[i];
+      } else {
+        const int s = static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(in.per));
+        key[u] = ((GSPMD_GLOBAL const int32_t*)from[s])[i - s * in.per];
+      }
+    }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
-      if (base + u * 64 + lane >= end) key[u] = INT32_MAX;
+      key[u] = base + u * 64 + lane >= end ? INT32_MAX : static_cast<int>(min(static_cast<uint32_t>(key[u]), static_cast<uint32_t>(in.keys)));
+  };
+  int less = 0;
+  for (int base = first; base < end; base += 64 * kAhead) {
+    load(base);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       less += key[u] < lo;
@@ -49,11 +106,9 @@ __global__ __launch_bounds__(kOrderThreads) void order_kernel(const OrderKeys in
   const int to_here = wave_sum_to_here(sum);
   if (lane == 63) sums[wave] = to_here;
   __syncthreads();
-  int at = to_here - sum, total = 0;
-  for (int w = 0; w < kOrderWaves; ++w) {
-    at += below[w] + (w < wave ? sums[w] : 0);
-    total += below[w] + sums[w];
-  }
+  const int of_waves = wave_sum_to_here(lane < kOrderWaves ? sums[lane] : 0), all_below = wave_sum_to_here(lane < kOrderWaves ? below[lane] : 0);
+  const int lower = __builtin_amdgcn_readlane(all_below, kOrderWaves - 1);
+  int at = lower + to_here - sum + (wave > 0 ? __builtin_amdgcn_readlane(of_waves, max(wave - 1, 0)) : 0);
   for (int i = 0; i < each; ++i)
     if (mine + i < entries) {
       const int n = counts[mine + i];
@@ -61,23 +116,19 @@ __global__ __launch_bounds__(kOrderThreads) void order_kernel(const OrderKeys in
       at += n;
     }
   __syncthreads();
-  for (int i = t; i < range; i += kOrderThreads) out.begins[lo + i] = counts[i * kOrderWaves];
-  if (lo + range == in.keys && t == 0) out.begins[in.keys] = total;
+  for (int i = t; i < range; i += kOrderThreads) w.out.begins[lo + i] = counts[i * kOrderWaves];
+  if (lo + range == in.keys && t == 0) w.out.begins[in.keys] = lower + __builtin_amdgcn_readlane(of_waves, kOrderWaves - 1);
   __syncthreads();                              // (what was read there changes below)
   const uint64_t before = (uint64_t(1) << lane) - 1;
   for (int base = first; base < end; base += 64 * kAhead) {
-    int key[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) key[u] = in.at(min(base + u * 64 + lane, end - 1));      // (no branch: a load under one is waited for there)
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-      if (base + u * 64 + lane >= end) key[u] = INT32_MAX;
+    if (end - first > 64 * kAhead) load(base);  // (else they are there)
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int index = key[u] - lo;
       const bool here = key[u] >= lo && index < range;
       uint64_t same = __builtin_amdgcn_ballot_w64(here);
       if (same == 0) continue;
+#pragma unroll 1
       for (int b = 0; b < log_range; ++b) {
         const bool on = (index >> b) & 1;
         const uint64_t with = __builtin_amdgcn_ballot_w64(here && on);
@@ -88,7 +139,8 @@ __global__ __launch_bounds__(kOrderThreads) void order_kernel(const OrderKeys in
         const int place = *next + __builtin_popcountll(same & before);
         staged_in_order();                      // all have read before the first of each counts them
         if ((same & before) == 0) *next += __builtin_popcountll(same);
-        out.order[place] = base + u * 64 + lane;
+        w.out.order[place] = base + u * 64 + lane;
+        w.out.entries[place] = key[u];
       }
       staged_in_order();
     }

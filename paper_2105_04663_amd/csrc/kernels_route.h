@@ -9,6 +9,7 @@
 
 #include "kernels_basic.h"
 #include "kernels_embed.h"
+#include "kernels_rows.h"
 #include "mfma_common.h"
 #include "order.h"
 #include "ragged.h"

@@ -16,20 +16,22 @@ constexpr int kMostRange = 10;                  // indexes of a workgroup's rang
 struct OrderKeys {
   const int32_t* shard[kKeyShards];
   int32_t per, shards, count, keys;
-  __device__ __forceinline__ int at(int i) const {
-    const int s = shards == 1 ? 0 : static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(per));
-    const int32_t* const from = shards == 1 ? shard[0] : first_kernel_argument<OrderKeys>()->shard[s];
-    const uint32_t key = static_cast<uint32_t>(((GSPMD_GLOBAL const int32_t*)from)[i - s * per]);
-    return static_cast<int>(min(key, static_cast<uint32_t>(keys)));
-  }
 };
 
-// order: of every place the key's number, up to the last that is one; begins [keys + 1]: where each index's run begins.
+// order, entries: of every place the key's number and the key, up to the last that is one; begins [keys + 1]: where each index's run begins.
 struct OrderOut {
-  int32_t *order, *begins;
+  int32_t *order, *entries, *begins;
 };
 
-// One launch; nothing else is needed.
-int32_t run_order(const OrderKeys& in, const OrderOut& out, hipStream_t stream);
+// Rows to be zeroed by the same launch, in workgroups of their own: `per` rows in each shard (null: none), row numbers from `from` on through all of them.
+struct ZeroRows {
+  void* shard[kKeyShards];
+  int32_t per, shards, from;
+  int32_t halves;              // 2-byte units of a row
+  int64_t stride;              // of them
+};
+
+// One launch; nothing else is needed.  No keys: rows are zeroed only; no rows, no shards: keys are ordered only.
+int32_t run_order(const OrderKeys& in, const OrderOut& out, const ZeroRows& zero, hipStream_t stream);
 
 }  // namespace gspmd

@@ -1,6 +1,8 @@
 // Tokens ordered by an index (kernels_order.h): the launch.
 #include "order.h"
 
+#include <algorithm>
+
 #include "kernels_order.h"
 #include "tokens.h"
 
@@ -9,11 +11,31 @@ namespace gspmd {
 // Ranges for about a workgroup on every compute unit: with more, the keys are read more often, with fewer, longer.
 constexpr int kOrderGroups = 256;
 
-int32_t run_order(const OrderKeys& in, const OrderOut& out, hipStream_t stream) {
-  int log = 0;
-  while (log < kMostRange && (static_cast<int64_t>(kOrderGroups) << log) < in.keys) ++log;
-  const unsigned groups = static_cast<unsigned>((static_cast<int64_t>(in.keys) + (int64_t(1) << log) - 1) >> log);
-  hipLaunchKernelGGL(order_kernel, dim3(groups), dim3(kOrderThreads), static_cast<size_t>(kOrderWaves << log) * 4, stream, in, out, log);
+// Workgroups that zero rows, at most: two on every compute unit are there at a time.
+constexpr int kZeroGroups = 1024;
+
+int32_t run_order(const OrderKeys& in, const OrderOut& out, const ZeroRows& zero, hipStream_t stream) {
+  OrderWork w{};
+  w.in = in;
+  w.out = out;
+  w.zero = zero;
+  if (in.count > 0) {
+    while (w.log_range < kMostRange && (static_cast<int64_t>(kOrderGroups) << w.log_range) < in.keys) ++w.log_range;
+    w.groups = static_cast<int32_t>((static_cast<int64_t>(in.keys) + (int64_t(1) << w.log_range) - 1) >> w.log_range);
+  }
+  int64_t groups = 0;
+  const int64_t rows = static_cast<int64_t>(zero.per) * zero.shards - zero.from;
+  if (rows > 0 && zero.halves > 0) {
+    constexpr int n = Sixteen<bf16_bits>::n;
+    w.zero_log = row_lanes_log(zero.halves, n);
+    const int64_t piece = static_cast<int64_t>(kZeroUnroll) * n << w.zero_log, at_once = static_cast<int64_t>(kOrderWaves) << (6 - w.zero_log);
+    w.zero_pieces = static_cast<int32_t>((zero.halves + piece - 1) / piece);
+    groups = std::min<int64_t>((rows + at_once - 1) / at_once, std::max<int64_t>(1, kZeroGroups / w.zero_pieces)) * w.zero_pieces;
+  }
+  groups += w.groups;
+  if (groups == 0) return GSPMD_OK;
+  if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL(order_kernel, dim3(static_cast<unsigned>(groups)), dim3(kOrderThreads), static_cast<size_t>(kOrderWaves << w.log_range) * 4, stream, w);
   return launched();
 }
 
