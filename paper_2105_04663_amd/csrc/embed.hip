@@ -3,7 +3,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 #include <vector>
 
 #include "../../include/gspmd.h"
@@ -20,9 +19,10 @@ struct Embed {
   int64_t P = 0, T = 0, M = 0, V = 0;
   int64_t na = 1, nb = 1, ts = 0, vs = 0;       // shards of tokens and of the vocabulary, their static extents
   int axis_t = -1, axis_v = -1, vocab_dim = 0;
-  int64_t chunks() const { return (T + kChunk - 1) / kChunk; }
+  int64_t chunk() const { return T <= kFewTokens ? kSmallChunk : kLargeChunk; }
+  int64_t chunks() const { return (T + chunk() - 1) / chunk(); }
   // the workspace: the tokens' order and their entries in it, up to a chunk's end; where an entry's begin; chunks' sums, two of each; with dw [M, V] the sums of runs of two tokens and more
-  int64_t order_bytes() const { return round_up(chunks() * kChunk * 4, kWsAlign); }
+  int64_t order_bytes() const { return round_up(chunks() * chunk() * 4, kWsAlign); }
   int64_t begins_bytes() const { return round_up((V + 1) * 4, kWsAlign); }
   int64_t chunks_bytes() const { return round_up(chunks() * M * 4, kWsAlign); }
   int64_t sums_bytes() const { return vocab_dim == 1 ? round_up(T / 2 * M * 4, kWsAlign) : 0; }
@@ -95,16 +95,6 @@ EmbedArgs arguments(const Embed& e, const Shards& s, float scale) {
   return a;
 }
 
-template <typename Go>
-int32_t by_lines(Lines lines, Go go) {
-  switch (lines) {
-    case kExact: go(std::integral_constant<int, kExact>{}); break;
-    case kNarrow: go(std::integral_constant<int, kNarrow>{}); break;
-    default: go(std::integral_constant<int, kWide>{});
-  }
-  return launched();
-}
-
 template <typename T>
 int32_t launch_embed(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
   const int64_t rows = static_cast<int64_t>(a.ts) * a.token_shards;
@@ -129,34 +119,42 @@ int32_t launch_embed(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
 }
 
 // Sums over the runs of the order: rows of dw [V, M], or what embed_grad_columns_kernel reads.
-template <typename T, bool COLUMNS>
-int32_t launch_runs(const EmbedArgs& a, hipStream_t stream) {
+template <typename T, bool COLUMNS, int CHUNK>
+int32_t launch_chunks(const EmbedArgs& a, hipStream_t stream) {
   constexpr int n = Sixteen<T>::n;
-  const int64_t chunks = (static_cast<int64_t>(a.T) + kChunk - 1) / kChunk;
+  const int64_t chunks = (static_cast<int64_t>(a.T) + CHUNK - 1) / CHUNK;
   const Lines lines = a.accumulate && !COLUMNS ? kExact : lines_of<T>(a.M);
   const int log = row_lanes_log(a.M, n);
   int across = 0;
   while (across < 2 && (static_cast<int64_t>(n) << (log + across)) < a.M) ++across;
   const int64_t piece = static_cast<int64_t>(n) << (log + across), units = int64_t(4) >> across << (6 - log);
   const dim3 grid(static_cast<unsigned>((chunks + units - 1) / units), static_cast<unsigned>((a.M + piece - 1) / piece));
-  const int32_t st = by_lines(lines, [&](auto l) { hipLaunchKernelGGL((embed_runs_kernel<T, decltype(l)::value, COLUMNS>), grid, dim3(256), 0, stream, a, log, across); });
+  const int32_t st = by_lines(lines, [&](auto l) { hipLaunchKernelGGL((embed_runs_kernel<T, decltype(l)::value, COLUMNS, CHUNK>), grid, dim3(256), 0, stream, a, log, across); });
   if (st != GSPMD_OK || chunks < 2) return st;
   const dim3 joins(static_cast<unsigned>(chunks - 1), static_cast<unsigned>((a.M + 64 * n - 1) / (64 * n)));
-  if (lines == kExact) hipLaunchKernelGGL((embed_joins_kernel<T, kExact, COLUMNS>), joins, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((embed_joins_kernel<T, kWide, COLUMNS>), joins, dim3(256), 0, stream, a);
+  if (lines == kExact) hipLaunchKernelGGL((embed_joins_kernel<T, kExact, COLUMNS, CHUNK>), joins, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((embed_joins_kernel<T, kWide, COLUMNS, CHUNK>), joins, dim3(256), 0, stream, a);
   return launched();
+}
+template <typename T>
+int32_t launch_runs(const Embed& e, const EmbedArgs& a, hipStream_t stream) {
+  if (e.vocab_dim == 0) return e.chunk() == kSmallChunk ? launch_chunks<T, false, kSmallChunk>(a, stream) : launch_chunks<T, false, kLargeChunk>(a, stream);
+  return e.chunk() == kSmallChunk ? launch_chunks<T, true, kSmallChunk>(a, stream) : launch_chunks<T, true, kLargeChunk>(a, stream);
 }
 
 template <typename T>
 int32_t launch_turn(const EmbedArgs& a, hipStream_t stream) {
   constexpr int n = Sixteen<T>::n, kRows = kTurnLanes * n;
-  const dim3 grid(static_cast<unsigned>((a.vs + kTurnEntries - 1) / kTurnEntries * a.vocab_shards), static_cast<unsigned>((a.M + kRows - 1) / kRows)), block(256);
+  const int64_t across = (a.vs + kTurnEntries - 1) / kTurnEntries * static_cast<int64_t>(a.vocab_shards), tiles = across * ((a.M + kRows - 1) / kRows);
+  if (tiles > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
+  const dim3 grid(static_cast<unsigned>(tiles)), block(256);
+  const int x = static_cast<int>(across);
   if (a.M < n) {
-    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, kExact, float>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, kExact, T>), grid, block, 0, stream, a);
+    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, kExact, float>), grid, block, 0, stream, a, x);
+    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, kExact, T>), grid, block, 0, stream, a, x);
   } else {
-    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, kNarrow, float>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, kNarrow, T>), grid, block, 0, stream, a);
+    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, kNarrow, float>), grid, block, 0, stream, a, x);
+    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, kNarrow, T>), grid, block, 0, stream, a, x);
   }
   return launched();
 }
@@ -197,7 +195,7 @@ int32_t gradient(const Embed& e, const Shards& s, EmbedArgs a, char* workspace, 
       zero.stride = a.ld_vocab * static_cast<int64_t>(sizeof(T) / 2);
     }
     if ((st = run_order(in, out, zero, stream)) != GSPMD_OK) return st;
-    if (e.T > 0 && (e.vocab_dim == 0 || in.count > 0) && (st = e.vocab_dim == 0 ? launch_runs<T, false>(a, stream) : launch_runs<T, true>(a, stream)) != GSPMD_OK) return st;
+    if (e.T > 0 && (e.vocab_dim == 0 || in.count > 0) && (st = launch_runs<T>(e, a, stream)) != GSPMD_OK) return st;
     in.count = 0;                               // (ordered, for the next replicas; columns' sums are there, too)
     if (e.vocab_dim == 1 && (st = launch_turn<T>(a, stream)) != GSPMD_OK) return st;
   }

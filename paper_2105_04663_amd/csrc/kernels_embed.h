@@ -3,7 +3,7 @@
 // Both are bound by memory: the rows that are read and the rows that are written, once each.  A vocabulary matrix [V, M] has an entry's row in one piece, read and written 16 bytes a lane at
 // element alignment, neighbouring lanes side by side; in one [M, V] an entry is a column, and tiles turn in LDS.
 // The gradient has one writer for each of its elements.  Tokens are ordered by entry (kernels_order.h); an entry's are a run of that order, and its row of dw is the sum over the run, in float32.  The
-// order is cut into chunks of 32 tokens, which are added up side by side whatever the runs are, so that an entry that half of a text consists of is no chain of thousands of loads: a run inside a chunk
+// order is cut into chunks of a few tokens, which are added up side by side whatever the runs are, so that an entry that half of a text consists of is no chain of thousands of loads: a run inside a chunk
 // is finished there, what a chunk has of runs that begin before it or end behind it are partial sums, added up by the chunk that a run begins in, in a second launch.  All sums have one
 // fixed order, so equal inputs give equal bits.  Rows of dw [V, M] without tokens are zeroed in the launch that orders; a dw [M, V] is written whole from the sums.
 #pragma once
@@ -13,6 +13,7 @@
 #include "kernels_basic.h"
 #include "kernels_rows.h"
 #include "mfma_common.h"
+#include "tile_index.h"
 
 namespace gspmd {
 
@@ -37,7 +38,9 @@ struct EmbedArgs {
   const int32_t *order, *entries, *begins;
   float *heads, *tails, *sums;
 };
-constexpr int kChunk = 32;     // tokens
+// Tokens of a chunk: few where there are few chunks, as a chunk's tokens wait for each other; more where there are many, as their sums are read again (us, 8 / 16: 2048 tokens of 2048 29.3 / 30.9,
+// 8192 of 1024 25.1 / 25.5, 32768 of 4096 172 / 159).
+constexpr int kSmallChunk = 8, kLargeChunk = 16, kFewTokens = 8192;
 
 typedef __attribute__((address_space(4))) const EmbedArgs embed_args;
 __device__ __forceinline__ embed_args* embed_arguments() { return first_kernel_argument<EmbedArgs>(); }
@@ -161,75 +164,72 @@ __device__ __forceinline__ void finish_row(const EmbedArgs& a, int entry, int at
   store_line<LINES, T>(dw, at, a.M, Sixteen<T>::close(sum));
 }
 
-// Chunks of the order: a wave (or a few lanes of one, with short rows) has a chunk and 16 bytes a lane of its tokens' rows, eight tokens' on their way at a time.
+// Chunks of the order: a wave (or a few lanes of one, with short rows) has a chunk and 16 bytes a lane of its tokens' rows, all on their way together.
 // COLUMNS: dw is [M, V]; runs of several tokens are put by for embed_grad_columns_kernel, those of one it reads itself.
-template <typename T, int LINES, bool COLUMNS>
+template <typename T, int LINES, bool COLUMNS, int CHUNK>
 __global__ __launch_bounds__(256) void embed_runs_kernel(const EmbedArgs a, int log_lanes, int log_across) {
-  constexpr int n = Sixteen<T>::n, kAhead = 8;
+  constexpr int n = Sixteen<T>::n;
   const int log = LINES == kWide ? 6 : log_lanes, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int across = 1 << log_across, units = (4 >> log_across) << (6 - log);              // waves along a row; chunks of a workgroup
   const int chunk = of_row<LINES>(blockIdx.x * units + ((wave >> log_across) << (6 - log)) + (lane >> log));
   const int col = (((blockIdx.y * across + (wave & (across - 1))) << log) + (lane & ((1 << log) - 1))) * n;
-  const int total = ((GSPMD_GLOBAL const int32_t*)a.begins)[a.V], begin = chunk * kChunk, end = min(begin + kChunk, total);
+  const int total = ((GSPMD_GLOBAL const int32_t*)a.begins)[a.V], begin = chunk * CHUNK, end = min(begin + CHUNK, total);
   if (begin >= total || col >= a.M) return;
   GSPMD_GLOBAL const int32_t* const order = (GSPMD_GLOBAL const int32_t*)a.order;
   GSPMD_GLOBAL const int32_t* const entries = (GSPMD_GLOBAL const int32_t*)a.entries;
   const int at = line_at<LINES, T>(col, a.M);
-  bool open = begin > 0 && entries[max(begin - 1, 0)] == entries[begin];       // the run began before the chunk
-  int first = begin;                                                           // the run's first place here
+  int entry[CHUNK + 1];
+  u32x4_t v[CHUNK];
+#pragma unroll
+  for (int u = 0; u < CHUNK; ++u) {             // (places up to the chunk's end exist; those behind the last token hold anything)
+    const int token = of_row<LINES>(order[begin + u]);
+    entry[u] = of_row<LINES>(entries[begin + u]);
+    v[u] = load_line<LINES, T>(token_row<T>(a, begin + u < end ? token : 0), at, a.M);
+  }
+  entry[CHUNK] = begin + CHUNK < total ? of_row<LINES>(entries[begin + CHUNK]) : a.V;
+  bool open = begin > 0 && of_row<LINES>(entries[max(begin - 1, 0)]) == entry[0];          // the run began before the chunk
+  int first = begin;                                                                       // the run's first place here
   float sum[n];
 #pragma unroll
   for (int e = 0; e < n; ++e) sum[e] = 0.f;
-#pragma unroll 1
-  for (int base = begin; base < end; base += kAhead) {
-    int entry[kAhead + 1];
-    u32x4_t v[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {          // (places up to the chunk's end exist; those behind the last token hold anything)
-      const int token = of_row<LINES>(order[base + u]);
-      entry[u] = of_row<LINES>(entries[base + u]);
-      v[u] = load_line<LINES, T>(token_row<T>(a, base + u < end ? token : 0), at, a.M);
-    }
-    entry[kAhead] = base + kAhead < total ? of_row<LINES>(entries[base + kAhead]) : a.V;
+  for (int u = 0; u < CHUNK; ++u) {
+    const int place = begin + u;
+    if (place < end) {
+      float f[n];
+      Sixteen<T>::open(v[u], f);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int place = base + u;
-      if (place < end) {
-        float f[n];
-        Sixteen<T>::open(v[u], f);
-#pragma unroll
-        for (int e = 0; e < n; ++e) sum[e] += f[e];
-        const bool ends = place + 1 == total || entry[u + 1] != entry[u];
-        if (ends || place + 1 == end) {
-          const bool part = open || !ends;
-          if (part || COLUMNS) {
-            float* const to = open ? a.heads + static_cast<int64_t>(chunk) * a.M : part ? a.tails + static_cast<int64_t>(chunk) * a.M : a.sums + static_cast<int64_t>(first >> 1) * a.M;
-            if (part || first != place) store_sums<LINES, n>(to, at, a.M, sum);
-          } else {
-            finish_row<T, LINES>(a, entry[u], at, sum);
-          }
-          open = false;
-          first = place + 1;
-#pragma unroll
-          for (int e = 0; e < n; ++e) sum[e] = 0.f;
+      for (int e = 0; e < n; ++e) sum[e] += f[e];
+      const bool ends = place + 1 == total || entry[u + 1] != entry[u];
+      if (ends || place + 1 == end) {
+        const bool part = open || !ends;
+        if (part || COLUMNS) {
+          float* const to = open ? a.heads + static_cast<int64_t>(chunk) * a.M : part ? a.tails + static_cast<int64_t>(chunk) * a.M : a.sums + static_cast<int64_t>(first >> 1) * a.M;
+          if (part || first != place) store_sums<LINES, n>(to, at, a.M, sum);
+        } else {
+          finish_row<T, LINES>(a, entry[u], at, sum);
         }
+        open = false;
+        first = place + 1;
+#pragma unroll
+        for (int e = 0; e < n; ++e) sum[e] = 0.f;
       }
     }
   }
 }
 
 // Runs of several chunks: a workgroup for the chunk that one begins in (blockIdx.x) and 64 x 16 bytes of the row (blockIdx.y), a wave every fourth of the chunks behind it.
-template <typename T, int LINES, bool COLUMNS>
+template <typename T, int LINES, bool COLUMNS, int CHUNK>
 __global__ __launch_bounds__(256) void embed_joins_kernel(const EmbedArgs a) {
   constexpr int n = Sixteen<T>::n, kAhead = 4;
   const int chunk = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   GSPMD_GLOBAL const int32_t* const entries = (GSPMD_GLOBAL const int32_t*)a.entries;
   GSPMD_GLOBAL const int32_t* const begins = (GSPMD_GLOBAL const int32_t*)a.begins;
-  const int begin = chunk * kChunk, end = begin + kChunk;
+  const int begin = chunk * CHUNK, end = begin + CHUNK;
   if (end >= begins[a.V]) return;               // nothing behind it
   const int entry = entries[end - 1];
   if (entries[end] != entry || begins[entry] < begin) return;
-  const int last = (begins[entry + 1] - 1) / kChunk, col = (blockIdx.y * 64 + lane) * n, at = line_at<LINES, T>(col, a.M);
+  const int last = (begins[entry + 1] - 1) / CHUNK, col = (blockIdx.y * 64 + lane) * n, at = line_at<LINES, T>(col, a.M);
   float sum[n];
 #pragma unroll
   for (int e = 0; e < n; ++e) sum[e] = 0.f;
@@ -261,14 +261,16 @@ __global__ __launch_bounds__(256) void embed_joins_kernel(const EmbedArgs a) {
 // tokens'.  They turn in LDS, rounded but for what is still to be added to (TTile float).
 constexpr int kTurnEntries = 64, kTurnLanes = 16;
 template <typename T, int LINES, typename TTile>
-__global__ __launch_bounds__(256) void embed_grad_columns_kernel(const EmbedArgs a) {
+__global__ __launch_bounds__(256) void embed_grad_columns_kernel(const EmbedArgs a, int blocks_x) {
   constexpr int n = Sixteen<T>::n, kRows = kTurnLanes * n, side = 64 / kTurnLanes, kEach = kTurnEntries / (4 * side), kPitch = kTurnEntries + (sizeof(TTile) == 2 ? 2 : 1);
   __shared__ __attribute__((aligned(4))) TTile tile[n + kRows][kPitch];        // (n rows before the tile's: what the lane at the row's end has of its neighbours' may begin there)
   __shared__ int begins[kTurnEntries + 1];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  // entries of one shard: blockIdx.x counts blocks of every shard
-  const int per_shard = (a.vs + kTurnEntries - 1) / kTurnEntries, shard = blockIdx.x / per_shard, c0 = (blockIdx.x - shard * per_shard) * kTurnEntries;
-  const int row0 = shard * a.vs + c0, m0 = blockIdx.y * kRows, entries = min(kTurnEntries, a.vs - c0);
+  // neighbouring entries' tiles, whose lines of dw are shared where rows are not aligned, on one XCD
+  const int logical = logical_tile(blockIdx.x, gridDim.x), block_m = logical / blocks_x, block_x = logical - block_m * blocks_x;
+  // entries of one shard: block_x counts blocks of every shard
+  const int per_shard = (a.vs + kTurnEntries - 1) / kTurnEntries, shard = block_x / per_shard, c0 = (block_x - shard * per_shard) * kTurnEntries;
+  const int row0 = shard * a.vs + c0, m0 = block_m * kRows, entries = min(kTurnEntries, a.vs - c0);
   T* const dw = static_cast<T*>(embed_arguments()->vocab[shard]);
   if (dw == nullptr) return;
   if (t <= kTurnEntries) begins[t] = a.T > 0 ? ((GSPMD_GLOBAL const int32_t*)a.begins)[min(row0 + t, a.V)] : 0;

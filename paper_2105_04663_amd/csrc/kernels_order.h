@@ -4,7 +4,9 @@
 // other, and one launch orders any number of keys of any size.  Each reads every key twice, from L2; a sort by digits reads them fewer times but has a chain of launches, or of one workgroup's
 // rounds (us, digits / this: 2048 keys below 32000 10.3 / 5.2, 9999 27.8 / 7.6, 131072 below 128, three launches, 32 / 15).
 // Its sixteen waves have a part of the keys each.  First they count, by index and wave, with atomics in LDS whose order does not matter; sums over the counts are places.  Then every wave goes
-// through its part again, sixty-four keys at a time, in order: lanes with the same index are found by a ballot for each of its bits, and take consecutive places.
+// through its part again, sixty-four keys at a time, in order: lanes with the same index are found, and take consecutive places.  Of sixty-four keys a range has hardly any but for an index that many keys
+// have: the first lane's index, those that have it, the next lane's that is left ..., and for what is left after kLeaders of them a ballot for each bit (ballots alone, us: 9999 keys below 32000,
+// a tenth of them one, 12.9; 32768, 30.1).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -17,6 +19,7 @@
 
 namespace gspmd {
 
+constexpr int kLeaders = 4;
 struct OrderWork {
   OrderKeys in;
   OrderOut out;
@@ -69,7 +72,7 @@ __global__ __launch_bounds__(kOrderThreads) void order_kernel(const OrderWork w)
   if (in.shards > 1 && t < in.shards) from[t] = first_kernel_argument<OrderWork>()->in.shard[t];
   for (int i = t; i < entries; i += kOrderThreads) counts[i] = 0;
   __syncthreads();
-  constexpr int kAhead = 8;
+  constexpr int kAhead = 4;
   int key[kAhead];
   // this lane's of 64 x kAhead keys from `base` on, INT32_MAX behind the wave's last; what is no key is `keys`.  (No branch: a load in one is waited for there.)
   auto load = [&](int base) {
@@ -125,24 +128,36 @@ __global__ __launch_bounds__(kOrderThreads) void order_kernel(const OrderWork w)
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int index = key[u] - lo;
-      const bool here = key[u] >= lo && index < range;
-      uint64_t same = __builtin_amdgcn_ballot_w64(here);
-      if (same == 0) continue;
+      uint64_t left = __builtin_amdgcn_ballot_w64(key[u] >= lo && index < range);
+      auto place_of = [&](bool mine, uint64_t same) {              // the lanes `same`, those of this lane's index, if it is `mine`
+        if (mine) {
+          int32_t* const next = counts + index * kOrderWaves + wave;
+          const int place = *next + __builtin_popcountll(same & before);
+          staged_in_order();                    // all have read before the first of each counts them
+          if ((same & before) == 0) *next += __builtin_popcountll(same);
+          w.out.order[place] = base + u * 64 + lane;
+          w.out.entries[place] = key[u];
+        }
+        staged_in_order();
+      };
 #pragma unroll 1
-      for (int b = 0; b < log_range; ++b) {
-        const bool on = (index >> b) & 1;
-        const uint64_t with = __builtin_amdgcn_ballot_w64(here && on);
-        same &= on ? with : ~with;
+      for (int turn = 0; left != 0 && turn < kLeaders; ++turn) {
+        const int leader = __builtin_amdgcn_readlane(index, __builtin_ctzll(left));
+        const uint64_t same = __builtin_amdgcn_ballot_w64(index == leader);
+        place_of(index == leader, same);
+        left &= ~same;
       }
-      if (here) {
-        int32_t* const next = counts + index * kOrderWaves + wave;
-        const int place = *next + __builtin_popcountll(same & before);
-        staged_in_order();                      // all have read before the first of each counts them
-        if ((same & before) == 0) *next += __builtin_popcountll(same);
-        w.out.order[place] = base + u * 64 + lane;
-        w.out.entries[place] = key[u];
+      if (left != 0) {
+        const bool here = (left >> lane) & 1;
+        uint64_t same = left;
+#pragma unroll 1
+        for (int b = 0; b < log_range; ++b) {
+          const bool on = (index >> b) & 1;
+          const uint64_t with = __builtin_amdgcn_ballot_w64(here && on);
+          same &= on ? with : ~with;
+        }
+        place_of(here, same);
       }
-      staged_in_order();
     }
   }
 }

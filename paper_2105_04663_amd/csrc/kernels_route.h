@@ -395,139 +395,135 @@ __device__ __forceinline__ int expert_shard(const ExchangeArgs& a, int o) {
 
 // rows[slot] = x[token of the slot]: a wave has a piece of a row, or a few short rows.
 constexpr int kExchangeUnroll = 4;
-template <typename T>
+template <typename T, int LINES>
 __global__ __launch_bounds__(256) void dispatch_kernel(const ExchangeArgs a, int log_lanes, int pieces) {
   constexpr int n = Sixteen<T>::n;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lanes = 1 << log_lanes;
+  const int log = LINES == kWide ? 6 : log_lanes, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = blockIdx.x / pieces, piece = blockIdx.x - group * pieces;       // (neighbouring pieces of rows together)
-  const int slot = ((group * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);
+  const int slot = of_row<LINES>(((group * 4 + wave) << (6 - log)) + (lane >> log));
   if (slot >= a.T * a.k) return;
-  const int o = ((GSPMD_GLOBAL const int32_t*)a.order)[slot];
+  const int o = of_row<LINES>(((GSPMD_GLOBAL const int32_t*)a.order)[slot]);
   if (static_cast<uint32_t>(o) >= static_cast<uint32_t>(a.T * a.k)) return;
-  const int part = expert_shard(a, o);
+  const int part = of_row<LINES>(expert_shard(a, o));
   if (part < 0) return;
-  T* const to = static_cast<T*>(exchange_arguments()->rows[part]);
+  T* to = static_cast<T*>(exchange_arguments()->rows[part]);
   if (to == nullptr) return;
-  const int token = static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(a.k)), shard = embed_shard(token, a.ts, a.token_shards);
+  const int token = of_row<LINES>(static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(a.k))), shard = of_row<LINES>(embed_shard(token, a.ts, a.token_shards));
   const T* const x = static_cast<const T*>(exchange_arguments()->tokens[shard]) + (token - shard * a.ts) * a.ld_tokens;
-  const int col0 = ((piece * kExchangeUnroll) << log_lanes) * n + (lane & (lanes - 1)) * n, step = n << log_lanes;
+  to += slot * a.ld_rows;
+  const int col0 = (((piece * kExchangeUnroll) << log) + (lane & ((1 << log) - 1))) * n, step = n << log;
   u32x4_t v[kExchangeUnroll];
 #pragma unroll
-  for (int u = 0; u < kExchangeUnroll; ++u)
-    if (col0 + u * step < a.M) v[u] = load_up_to(x + col0 + u * step, a.M - col0 - u * step);
+  for (int u = 0; u < kExchangeUnroll; ++u) v[u] = load_line<LINES, T>(x, line_at<LINES, T>(col0 + u * step, a.M), a.M);
 #pragma unroll
   for (int u = 0; u < kExchangeUnroll; ++u)
-    if (col0 + u * step < a.M) store_up_to(to + slot * a.ld_rows + col0 + u * step, v[u], a.M - col0 - u * step);
+    if (col0 + u * step < a.M) store_line<LINES, T>(to, line_at<LINES, T>(col0 + u * step, a.M), a.M, v[u]);
 }
 
 // y[t] = sum over t's choices of weight * rows[slot], in float32, in their order; what has no slot adds nothing.
 constexpr int kCombineAhead = 4, kCombineUnroll = 2;
-template <typename T>
+template <typename T, int LINES>
 __global__ __launch_bounds__(256) void combine_kernel(const ExchangeArgs a, int log_lanes, int pieces) {
   constexpr int n = Sixteen<T>::n;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lanes = 1 << log_lanes;
+  const int log = LINES == kWide ? 6 : log_lanes, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = blockIdx.x / pieces, piece = blockIdx.x - group * pieces;
-  const int token = ((group * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);
+  const int token = of_row<LINES>(((group * 4 + wave) << (6 - log)) + (lane >> log));
   if (token >= a.ts * a.token_shards) return;
-  const int shard = embed_shard(token, a.ts, a.token_shards), col0 = (((piece * kCombineUnroll) << log_lanes) + (lane & (lanes - 1))) * n, step = n << log_lanes;
-  T* const y = static_cast<T*>(exchange_arguments()->tokens[shard]);
+  const int shard = of_row<LINES>(embed_shard(token, a.ts, a.token_shards)), col0 = (((piece * kCombineUnroll) << log) + (lane & ((1 << log) - 1))) * n, step = n << log;
+  T* y = static_cast<T*>(exchange_arguments()->tokens[shard]);
   if (y == nullptr || col0 >= a.M) return;
+  y += (token - shard * a.ts) * a.ld_tokens;
   float sum[kCombineUnroll][n];
 #pragma unroll
   for (int p = 0; p < kCombineUnroll; ++p)
 #pragma unroll
     for (int e = 0; e < n; ++e) sum[p][e] = 0.f;
   if (token < a.T) {
+#pragma unroll 1
     for (int i = 0; i < a.k; i += kCombineAhead) {
       u32x4_t v[kCombineAhead][kCombineUnroll];
       float w[kCombineAhead];
-      const T* from[kCombineAhead];
-      // choices beyond the last are the last again, those without a slot the first row, with a weight of 0 and zeros for a row: no branch, a load under one is waited for there
+      // choices beyond the last are the last again, those without a slot the first row, with a weight of 0 and zeros for a row: no branch, a load in one is waited for there
       int slot[kCombineAhead], part[kCombineAhead];
 #pragma unroll
       for (int u = 0; u < kCombineAhead; ++u) {
         const int o = token * a.k + min(i + u, a.k - 1);
-        slot[u] = ((GSPMD_GLOBAL const int32_t*)a.slots)[o];
-        part[u] = a.expert_shards == 1 ? 0 : ((GSPMD_GLOBAL const int32_t*)a.experts)[o];
+        slot[u] = of_row<LINES>(((GSPMD_GLOBAL const int32_t*)a.slots)[o]);
+        part[u] = a.expert_shards == 1 ? 0 : of_row<LINES>(((GSPMD_GLOBAL const int32_t*)a.experts)[o]);
         w[u] = a.weights ? ((GSPMD_GLOBAL const float*)a.weights)[o] : 1.f;
       }
       bool there[kCombineAhead];
 #pragma unroll
       for (int u = 0; u < kCombineAhead; ++u) {
         there[u] = i + u < a.k && static_cast<uint32_t>(slot[u]) < static_cast<uint32_t>(a.T * a.k) && (a.expert_shards == 1 || static_cast<uint32_t>(part[u]) < static_cast<uint32_t>(a.E));
-        const int of = there[u] && a.expert_shards != 1 ? static_cast<int>(static_cast<uint32_t>(part[u]) / static_cast<uint32_t>(a.es)) : 0;
-        from[u] = static_cast<const T*>(exchange_arguments()->rows[of]) + (there[u] ? slot[u] : 0) * a.ld_rows;
-      }
-      if (col0 + (kCombineUnroll - 1) * step + n <= a.M) {
+        const int of = there[u] && a.expert_shards != 1 ? of_row<LINES>(static_cast<int>(static_cast<uint32_t>(part[u]) / static_cast<uint32_t>(a.es))) : 0;
+        const T* const from = static_cast<const T*>(exchange_arguments()->rows[of]) + (there[u] ? slot[u] : 0) * a.ld_rows;
 #pragma unroll
-        for (int u = 0; u < kCombineAhead; ++u)
-#pragma unroll
-          for (int p = 0; p < kCombineUnroll; ++p) v[u][p] = load16(from[u] + col0 + p * step);
-      } else {
-#pragma unroll
-        for (int u = 0; u < kCombineAhead; ++u)
-#pragma unroll
-          for (int p = 0; p < kCombineUnroll; ++p) {
-            v[u][p] = u32x4_t{0u, 0u, 0u, 0u};
-            if (col0 + p * step < a.M) v[u][p] = load_up_to(from[u] + col0 + p * step, a.M - col0 - p * step);
-          }
+        for (int p = 0; p < kCombineUnroll; ++p) v[u][p] = load_line<LINES, T>(from, line_at<LINES, T>(col0 + p * step, a.M), a.M);
       }
 #pragma unroll
-      for (int u = 0; u < kCombineAhead; ++u)
+      for (int u = 0; u < kCombineAhead; ++u) {
+        if (!there[u]) continue;
 #pragma unroll
         for (int p = 0; p < kCombineUnroll; ++p) {
           float f[n];
           Sixteen<T>::open(v[u][p], f);
-          const float wu = there[u] ? w[u] : 0.f;
 #pragma unroll
-          for (int e = 0; e < n; ++e) sum[p][e] = fmaf(wu, there[u] ? f[e] : 0.f, sum[p][e]);
+          for (int e = 0; e < n; ++e) sum[p][e] = fmaf(w[u], f[e], sum[p][e]);
         }
+      }
     }
   }
 #pragma unroll
   for (int p = 0; p < kCombineUnroll; ++p)
-    if (col0 + p * step < a.M) store_up_to(y + (token - shard * a.ts) * a.ld_tokens + col0 + p * step, Sixteen<T>::close(sum[p]), a.M - col0 - p * step);
+    if (col0 + p * step < a.M) store_line<LINES, T>(y, line_at<LINES, T>(col0 + p * step, a.M), a.M, Sixteen<T>::close(sum[p]));
 }
 
 // drows[slot] = weight * dy[t] and dweight = the product of dy[t] and rows[slot], a wave for a choice (or a few with short rows).
-template <typename T>
+template <typename T, int LINES>
 __global__ __launch_bounds__(256) void combine_grad_kernel(const ExchangeArgs a, int log_lanes) {
   constexpr int n = Sixteen<T>::n, kAhead = 2;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lanes = 1 << log_lanes;
-  const int o = ((blockIdx.x * 4 + wave) << (6 - log_lanes)) + (lane >> log_lanes);
+  const int log = LINES == kWide ? 6 : log_lanes, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lanes = 1 << log;
+  const int o = of_row<LINES>(((blockIdx.x * 4 + wave) << (6 - log)) + (lane >> log));
   const bool in = o < a.T * a.k;
-  const int slot = in ? ((GSPMD_GLOBAL const int32_t*)a.slots)[o] : -1, part = in ? expert_shard(a, o) : -1;
+  const int slot = in ? of_row<LINES>(((GSPMD_GLOBAL const int32_t*)a.slots)[o]) : -1, part = in ? of_row<LINES>(expert_shard(a, o)) : -1;
   const bool there = static_cast<uint32_t>(slot) < static_cast<uint32_t>(a.T * a.k) && part >= 0;
   float dot = 0.f;
   if (there) {
-    const int token = static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(a.k)), shard = embed_shard(token, a.ts, a.token_shards);
+    const int token = of_row<LINES>(static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(a.k))), shard = of_row<LINES>(embed_shard(token, a.ts, a.token_shards));
     const T* const dy = static_cast<const T*>(exchange_arguments()->tokens[shard]) + (token - shard * a.ts) * a.ld_tokens;
     const T* const row = static_cast<const T*>(exchange_arguments()->rows[part]) + slot * a.ld_rows;
     T* drow = static_cast<T*>(exchange_arguments()->drows[part]);
-    if (drow != nullptr) drow += slot * a.ld_drows;
+    const bool wanted = drow != nullptr;
+    if (wanted) drow += slot * a.ld_drows;
     const float w = ((GSPMD_GLOBAL const float*)a.weights)[o];
-    const int step = n << log_lanes;
+    const int step = n << log;
+#pragma unroll 1
     for (int col0 = (lane & (lanes - 1)) * n; col0 < a.M; col0 += kAhead * step) {
       u32x4_t g[kAhead], v[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int col = col0 + u * step;
-        g[u] = v[u] = u32x4_t{0u, 0u, 0u, 0u};
-        if (col >= a.M) continue;
-        g[u] = load_up_to(dy + col, a.M - col);
-        v[u] = load_up_to(row + col, a.M - col);
+        const int at = line_at<LINES, T>(col0 + u * step, a.M);
+        g[u] = load_line<LINES, T>(dy, at, a.M);
+        v[u] = load_line<LINES, T>(row, at, a.M);
       }
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int col = col0 + u * step;
-        float p[n], q[n];
+        const int col = col0 + u * step, at = line_at<LINES, T>(col, a.M);
+        if (col >= a.M) continue;
+        float p[n], q[n], r[n];
         Sixteen<T>::open(g[u], p);
         Sixteen<T>::open(v[u], q);
 #pragma unroll
-        for (int e = 0; e < n; ++e) dot = fmaf(p[e], q[e], dot);
+        for (int e = 0; e < n; ++e) r[e] = p[e] * w;
+        if (wanted) store_line<LINES, T>(drow, at, a.M, Sixteen<T>::close(r));
+        if (LINES != kExact && at < col) {      // what the neighbour has of the product
 #pragma unroll
-        for (int e = 0; e < n; ++e) p[e] *= w;
-        if (drow != nullptr && col < a.M) store_up_to(drow + col, Sixteen<T>::close(p), a.M - col);
+          for (int e = 0; e < n; ++e)
+            if (at + e < col) p[e] = q[e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < n; ++e) dot = fmaf(p[e], q[e], dot);
       }
     }
   }

@@ -11,8 +11,11 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "kernels_basic.h"
 #include "mfma_common.h"
+#include "tokens.h"
 
 namespace gspmd {
 
@@ -148,6 +151,16 @@ __host__ __device__ __forceinline__ int row_lanes_log(int elements, int per_lane
   return log;
 }
 template <typename T> inline Lines lines_of(int64_t M) { return M < Sixteen<T>::n ? kExact : row_lanes_log(static_cast<int>(M), Sixteen<T>::n) < 6 ? kNarrow : kWide; }
+// a launch by them: go(lines), a compile-time constant
+template <typename Go>
+inline int32_t by_lines(Lines lines, Go go) {
+  switch (lines) {
+    case kExact: go(std::integral_constant<int, kExact>{}); break;
+    case kNarrow: go(std::integral_constant<int, kNarrow>{}); break;
+    default: go(std::integral_constant<int, kWide>{});
+  }
+  return launched();
+}
 // a value that all lanes have when a wave has one row
 template <int LINES> __device__ __forceinline__ int of_row(int v) { return LINES == kWide ? __builtin_amdgcn_readfirstlane(v) : v; }
 

@@ -179,10 +179,12 @@ int32_t launch_exchange(Exchanged what, const ExchangeArgs& a, hipStream_t strea
   const int64_t pieces = what == kCombineGrad ? 1 : (a.M + piece - 1) / piece, groups = (rows + side - 1) / side * pieces;
   if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(groups));
-  if (what == kDispatch) hipLaunchKernelGGL((dispatch_kernel<T>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
-  else if (what == kCombine) hipLaunchKernelGGL((combine_kernel<T>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
-  else hipLaunchKernelGGL((combine_grad_kernel<T>), grid, dim3(256), 0, stream, a, log);
-  return launched();
+  return by_lines(lines_of<T>(a.M), [&](auto lines) {
+    constexpr int L = decltype(lines)::value;
+    if (what == kDispatch) hipLaunchKernelGGL((dispatch_kernel<T, L>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
+    else if (what == kCombine) hipLaunchKernelGGL((combine_kernel<T, L>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
+    else hipLaunchKernelGGL((combine_grad_kernel<T, L>), grid, dim3(256), 0, stream, a, log);
+  });
 }
 int32_t run_exchange(Exchanged what, int32_t dtype, ExchangeArgs a, void* stream) {
   one_buffer(&a, what == kCombineGrad);
