@@ -385,6 +385,9 @@ struct ExchangeArgs {
   float* dweights;
 };
 __device__ __forceinline__ const GSPMD_KERNARG ExchangeArgs* exchange_arguments() { return first_kernel_argument<ExchangeArgs>(); }
+// (one shard: an address that is read with the other arguments, not once its number is known)
+__device__ __forceinline__ void* tokens_of(const ExchangeArgs& a, int shard) { return a.token_shards == 1 ? a.tokens[0] : exchange_arguments()->tokens[shard]; }
+__device__ __forceinline__ void* rows_of(const ExchangeArgs& a, int part) { return a.expert_shards == 1 ? a.rows[0] : exchange_arguments()->rows[part]; }
 
 // The shard of choice `o`'s expert, or -1 if it has none.
 __device__ __forceinline__ int expert_shard(const ExchangeArgs& a, int o) {
@@ -406,10 +409,10 @@ __global__ __launch_bounds__(256) void dispatch_kernel(const ExchangeArgs a, int
   if (static_cast<uint32_t>(o) >= static_cast<uint32_t>(a.T * a.k)) return;
   const int part = of_row<LINES>(expert_shard(a, o));
   if (part < 0) return;
-  T* to = static_cast<T*>(exchange_arguments()->rows[part]);
+  T* to = static_cast<T*>(rows_of(a, part));
   if (to == nullptr) return;
   const int token = of_row<LINES>(static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(a.k))), shard = of_row<LINES>(embed_shard(token, a.ts, a.token_shards));
-  const T* const x = static_cast<const T*>(exchange_arguments()->tokens[shard]) + (token - shard * a.ts) * a.ld_tokens;
+  const T* const x = static_cast<const T*>(tokens_of(a, shard)) + (token - shard * a.ts) * a.ld_tokens;
   to += slot * a.ld_rows;
   const int col0 = (((piece * kExchangeUnroll) << log) + (lane & ((1 << log) - 1))) * n, step = n << log;
   u32x4_t v[kExchangeUnroll];
@@ -430,7 +433,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const ExchangeArgs a, int 
   const int token = of_row<LINES>(((group * 4 + wave) << (6 - log)) + (lane >> log));
   if (token >= a.ts * a.token_shards) return;
   const int shard = of_row<LINES>(embed_shard(token, a.ts, a.token_shards)), col0 = (((piece * kCombineUnroll) << log) + (lane & ((1 << log) - 1))) * n, step = n << log;
-  T* y = static_cast<T*>(exchange_arguments()->tokens[shard]);
+  T* y = static_cast<T*>(tokens_of(a, shard));
   if (y == nullptr || col0 >= a.M) return;
   y += (token - shard * a.ts) * a.ld_tokens;
   float sum[kCombineUnroll][n];
@@ -457,7 +460,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const ExchangeArgs a, int 
       for (int u = 0; u < kCombineAhead; ++u) {
         there[u] = i + u < a.k && static_cast<uint32_t>(slot[u]) < static_cast<uint32_t>(a.T * a.k) && (a.expert_shards == 1 || static_cast<uint32_t>(part[u]) < static_cast<uint32_t>(a.E));
         const int of = there[u] && a.expert_shards != 1 ? of_row<LINES>(static_cast<int>(static_cast<uint32_t>(part[u]) / static_cast<uint32_t>(a.es))) : 0;
-        const T* const from = static_cast<const T*>(exchange_arguments()->rows[of]) + (there[u] ? slot[u] : 0) * a.ld_rows;
+        const T* const from = static_cast<const T*>(rows_of(a, of)) + (there[u] ? slot[u] : 0) * a.ld_rows;
 #pragma unroll
         for (int p = 0; p < kCombineUnroll; ++p) v[u][p] = load_line<LINES, T>(from, line_at<LINES, T>(col0 + p * step, a.M), a.M);
       }
@@ -491,8 +494,8 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(const ExchangeArgs a,
   float dot = 0.f;
   if (there) {
     const int token = of_row<LINES>(static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(a.k))), shard = of_row<LINES>(embed_shard(token, a.ts, a.token_shards));
-    const T* const dy = static_cast<const T*>(exchange_arguments()->tokens[shard]) + (token - shard * a.ts) * a.ld_tokens;
-    const T* const row = static_cast<const T*>(exchange_arguments()->rows[part]) + slot * a.ld_rows;
+    const T* const dy = static_cast<const T*>(tokens_of(a, shard)) + (token - shard * a.ts) * a.ld_tokens;
+    const T* const row = static_cast<const T*>(rows_of(a, part)) + slot * a.ld_rows;
     T* drow = static_cast<T*>(exchange_arguments()->drows[part]);
     const bool wanted = drow != nullptr;
     if (wanted) drow += slot * a.ld_drows;
