@@ -423,11 +423,11 @@ int32_t gspmd_softmax_distill(const gspmd_mesh* mesh,
  * All buffers of a call have one type, bf16 or f32; products and sums are fp32, in one fixed order, rounded once (a scale of 1 copies bits).  Equal calls give equal bits.
  * accumulate: dw holds a gradient already, to which this one is added (the losses', of a matrix that serves both): entries without tokens keep their bits.  0: dw is written whole, zeros where there
  * are no tokens.  Padding of the static shapes is written as 0 either way.  All shards of one tensor have one row stride; distinct buffers of the same data are each written.
- * At most 64 shards of tokens and of the vocabulary, 2^24 tokens.  Kernels only: both may be recorded into a HIP graph. */
+ * At most 64 shards of tokens and of the vocabulary, 2^24 tokens, rows of 2^21 elements.  Kernels only: both may be recorded into a HIP graph. */
 int32_t gspmd_embed(const gspmd_mesh* mesh, const int32_t* const* ids,
                     const gspmd_shard_buf* w_shards, const gspmd_sharding* w_sh, int32_t vocab_dim, float scale,
                     const gspmd_shard_buf* y_shards, const gspmd_sharding* y_sh, void* hip_stream);
-/* Bytes of device workspace gspmd_embed_grad needs (the tokens sorted by entry).  dtype: of the gradients.  Pure host work. */
+/* Bytes of device workspace gspmd_embed_grad needs (the tokens ordered by entry, and sums of parts of an entry's).  dtype: of the gradients.  Pure host work. */
 int32_t gspmd_embed_grad_workspace_bytes(const gspmd_mesh* mesh, const gspmd_sharding* dy_sh, const gspmd_sharding* dw_sh, int32_t vocab_dim, int32_t dtype, int64_t* bytes);
 int32_t gspmd_embed_grad(const gspmd_mesh* mesh, const int32_t* const* ids,
                          const gspmd_shard_buf* dy_shards, const gspmd_sharding* dy_sh,
@@ -456,7 +456,7 @@ int32_t gspmd_route_workspace_bytes(const gspmd_mesh* mesh, const gspmd_sharding
 int32_t gspmd_route(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_shards, const gspmd_sharding* logits_sh, int32_t choices, int32_t normalise,
                     const gspmd_route_buf* route, void* workspace, int64_t workspace_bytes, void* hip_stream);
 /* The gradient with respect to the logits of sum of dweights * weights, dweights [T, k] f32 (ignored where there is no expert): p (g - sum of p g) over the softmax's experts, g an expert's
- * dweight or 0.  Reads route's experts and weights.  dlogits: shards like logits, written whole (zeros for a token without experts and in the padding). */
+ * dweight or 0 (a token's choices of one expert, which gspmd_route never makes, add up).  Reads route's experts and weights.  dlogits: shards like logits, written whole (zeros for a token without experts and in the padding). */
 int32_t gspmd_route_grad(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_shards, const gspmd_sharding* logits_sh, int32_t choices, int32_t normalise,
                          const gspmd_route_buf* route, const float* dweights, const gspmd_shard_buf* dlogits_shards, void* hip_stream);
 

@@ -119,27 +119,31 @@ int32_t launch_embed(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
 }
 
 // Sums over the runs of the order: rows of dw [V, M], or what embed_grad_columns_kernel reads.
-template <typename T, bool COLUMNS, int CHUNK>
+template <typename T, int TO, int CHUNK>
 int32_t launch_chunks(const EmbedArgs& a, hipStream_t stream) {
   constexpr int n = Sixteen<T>::n;
   const int64_t chunks = (static_cast<int64_t>(a.T) + CHUNK - 1) / CHUNK;
-  const Lines lines = a.accumulate && !COLUMNS ? kExact : lines_of<T>(a.M);
+  const Lines lines = TO == kAddedRows && a.M % n != 0 ? kExact : lines_of<T>(a.M);        // (nothing may be added twice)
   const int log = row_lanes_log(a.M, n);
   int across = 0;
   while (across < 2 && (static_cast<int64_t>(n) << (log + across)) < a.M) ++across;
   const int64_t piece = static_cast<int64_t>(n) << (log + across), units = int64_t(4) >> across << (6 - log);
   const dim3 grid(static_cast<unsigned>((chunks + units - 1) / units), static_cast<unsigned>((a.M + piece - 1) / piece));
-  const int32_t st = by_lines(lines, [&](auto l) { hipLaunchKernelGGL((embed_runs_kernel<T, decltype(l)::value, COLUMNS, CHUNK>), grid, dim3(256), 0, stream, a, log, across); });
+  const int32_t st = by_lines(lines, [&](auto l) { hipLaunchKernelGGL((embed_runs_kernel<T, decltype(l)::value, TO, CHUNK>), grid, dim3(256), 0, stream, a, log, across); });
   if (st != GSPMD_OK || chunks < 2) return st;
   const dim3 joins(static_cast<unsigned>(chunks - 1), static_cast<unsigned>((a.M + 64 * n - 1) / (64 * n)));
-  if (lines == kExact) hipLaunchKernelGGL((embed_joins_kernel<T, kExact, COLUMNS, CHUNK>), joins, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((embed_joins_kernel<T, kWide, COLUMNS, CHUNK>), joins, dim3(256), 0, stream, a);
+  if (lines == kExact) hipLaunchKernelGGL((embed_joins_kernel<T, kExact, TO, CHUNK>), joins, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((embed_joins_kernel<T, kWide, TO, CHUNK>), joins, dim3(256), 0, stream, a);
   return launched();
 }
 template <typename T>
 int32_t launch_runs(const Embed& e, const EmbedArgs& a, hipStream_t stream) {
-  if (e.vocab_dim == 0) return e.chunk() == kSmallChunk ? launch_chunks<T, false, kSmallChunk>(a, stream) : launch_chunks<T, false, kLargeChunk>(a, stream);
-  return e.chunk() == kSmallChunk ? launch_chunks<T, true, kSmallChunk>(a, stream) : launch_chunks<T, true, kLargeChunk>(a, stream);
+  auto of_chunk = [&](auto to) {
+    constexpr int TO = decltype(to)::value;
+    return e.chunk() == kSmallChunk ? launch_chunks<T, TO, kSmallChunk>(a, stream) : launch_chunks<T, TO, kLargeChunk>(a, stream);
+  };
+  if (e.vocab_dim == 1) return of_chunk(std::integral_constant<int, kSums>{});
+  return a.accumulate ? of_chunk(std::integral_constant<int, kAddedRows>{}) : of_chunk(std::integral_constant<int, kRows>{});
 }
 
 template <typename T>

@@ -143,8 +143,10 @@ __device__ __forceinline__ const T* token_row(const EmbedArgs& a, int token) {
   return static_cast<const T*>(embed_arguments()->tokens[shard].rows) + static_cast<int64_t>(token - shard * a.ts) * a.ld_rows;
 }
 
-// dw's row of an entry [V, M] from its sum.  (Added to what is there: LINES exact.)
-template <typename T, int LINES>
+enum RunsTo { kRows, kAddedRows, kSums };        // what becomes of a run's sum: dw's row [V, M], the same added to what is there, or it is put by for dw [M, V]
+
+// dw's row of an entry [V, M] from its sum.
+template <typename T, int LINES, int TO>
 __device__ __forceinline__ void finish_row(const EmbedArgs& a, int entry, int at, float (&sum)[Sixteen<T>::n]) {
   constexpr int n = Sixteen<T>::n;
   const int shard = of_row<LINES>(embed_shard(entry, a.vs, a.vocab_shards));
@@ -153,20 +155,18 @@ __device__ __forceinline__ void finish_row(const EmbedArgs& a, int entry, int at
   dw += static_cast<int64_t>(entry - shard * a.vs) * a.ld_vocab;
 #pragma unroll
   for (int e = 0; e < n; ++e) sum[e] *= a.scale;
-  if constexpr (LINES == kExact) {
-    if (a.accumulate) {
-      float f[n];
-      Sixteen<T>::open(load_line<LINES, T>(dw, at, a.M), f);
+  if constexpr (TO == kAddedRows) {
+    float f[n];
+    Sixteen<T>::open(load_line<LINES, T>(dw, at, a.M), f);
 #pragma unroll
-      for (int e = 0; e < n; ++e) sum[e] += f[e];
-    }
+    for (int e = 0; e < n; ++e) sum[e] += f[e];
   }
   store_line<LINES, T>(dw, at, a.M, Sixteen<T>::close(sum));
 }
 
 // Chunks of the order: a wave (or a few lanes of one, with short rows) has a chunk and 16 bytes a lane of its tokens' rows, all on their way together.
-// COLUMNS: dw is [M, V]; runs of several tokens are put by for embed_grad_columns_kernel, those of one it reads itself.
-template <typename T, int LINES, bool COLUMNS, int CHUNK>
+// kSums: runs of several tokens are put by for embed_grad_columns_kernel, those of one it reads itself.
+template <typename T, int LINES, int TO, int CHUNK>
 __global__ __launch_bounds__(256) void embed_runs_kernel(const EmbedArgs a, int log_lanes, int log_across) {
   constexpr int n = Sixteen<T>::n;
   const int log = LINES == kWide ? 6 : log_lanes, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -203,11 +203,11 @@ __global__ __launch_bounds__(256) void embed_runs_kernel(const EmbedArgs a, int 
       const bool ends = place + 1 == total || entry[u + 1] != entry[u];
       if (ends || place + 1 == end) {
         const bool part = open || !ends;
-        if (part || COLUMNS) {
+        if (part || TO == kSums) {
           float* const to = open ? a.heads + static_cast<int64_t>(chunk) * a.M : part ? a.tails + static_cast<int64_t>(chunk) * a.M : a.sums + static_cast<int64_t>(first >> 1) * a.M;
           if (part || first != place) store_sums<LINES, n>(to, at, a.M, sum);
         } else {
-          finish_row<T, LINES>(a, entry[u], at, sum);
+          finish_row<T, LINES, TO>(a, entry[u], at, sum);
         }
         open = false;
         first = place + 1;
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(256) void embed_runs_kernel(const EmbedArgs a, int 
 }
 
 // Runs of several chunks: a workgroup for the chunk that one begins in (blockIdx.x) and 64 x 16 bytes of the row (blockIdx.y), a wave every fourth of the chunks behind it.
-template <typename T, int LINES, bool COLUMNS, int CHUNK>
+template <typename T, int LINES, int TO, int CHUNK>
 __global__ __launch_bounds__(256) void embed_joins_kernel(const EmbedArgs a) {
   constexpr int n = Sixteen<T>::n, kAhead = 4;
   const int chunk = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -253,8 +253,8 @@ __global__ __launch_bounds__(256) void embed_joins_kernel(const EmbedArgs a) {
   for (int w = 0; w < 4; ++w)
 #pragma unroll
     for (int e = 0; e < n; ++e) sum[e] += sums[w][e][lane];
-  if constexpr (COLUMNS) store_sums<LINES, n>(a.sums + static_cast<int64_t>(begins[entry] >> 1) * a.M, at, a.M, sum);
-  else finish_row<T, LINES>(a, entry, at, sum);
+  if constexpr (TO == kSums) store_sums<LINES, n>(a.sums + static_cast<int64_t>(begins[entry] >> 1) * a.M, at, a.M, sum);
+  else finish_row<T, LINES, TO>(a, entry, at, sum);
 }
 
 // dw [M, V]: 64 entries x 16 lanes' 16 bytes of dw's rows a workgroup.  Sixteen lanes have an entry, four of them one after the other, on their way together: the row of its token, or the sum of its

@@ -95,47 +95,68 @@ __device__ __forceinline__ float route_total(const float (&v)[R], float most, bo
   return strange ? NAN : sum;
 }
 
-// The sixteen lanes' choices: lane i of them has the i-th, its expert (-1: none) and weight.
+// Logits as whole numbers in the same order (a zero has one sign; -infinity, which is never chosen, the lowest of all), and back: the same steps.
+constexpr int32_t kNoLogit = INT32_MIN;
+__device__ __forceinline__ int32_t order_of_logit(float f) {
+  const int32_t i = __float_as_int(f + 0.f);
+  return f == -INFINITY ? kNoLogit : i ^ ((i >> 31) & INT32_MAX);
+}
+__device__ __forceinline__ float logit_of_order(int32_t i) { return i == kNoLogit ? -INFINITY : __int_as_float(i ^ ((i >> 31) & INT32_MAX)); }
+__device__ __forceinline__ int32_t row_most(int32_t v) {
+  auto turned = [](int32_t x, auto ctrl) { return __builtin_amdgcn_update_dpp(0, x, decltype(ctrl)::value, 0xf, 0xf, true); };
+  v = max(v, turned(v, std::integral_constant<int, 0x128>{}));      // row_ror:8
+  v = max(v, turned(v, std::integral_constant<int, 0x124>{}));
+  v = max(v, turned(v, std::integral_constant<int, 0x122>{}));
+  return max(v, turned(v, std::integral_constant<int, 0x121>{}));
+}
+
+// The sixteen lanes' choices: lane i of them has the i-th, its expert (-1: none) and weight.  `chosen`: LDS, a word for each lane of the wave.
 template <typename T, int R>
-__device__ __forceinline__ void route_choose(const RouteArgs& a, int token, int lane, int* chosen_expert, float* weight) {
+__device__ __forceinline__ void route_choose(const RouteArgs& a, int token, int lane, int32_t* chosen, int* chosen_expert, float* weight) {
   const int of_row = lane & 15;
   const T* z = nullptr;
   if (token < a.T) {
     const int shard = embed_shard(token, a.ts, a.shards);
-    z = static_cast<const T*>(first_kernel_argument<RouteArgs>()->shard[shard].logits) + static_cast<int64_t>(token - shard * a.ts) * a.ld;
+    z = static_cast<const T*>(a.shards == 1 ? a.shard[0].logits : first_kernel_argument<RouteArgs>()->shard[shard].logits) + static_cast<int64_t>(token - shard * a.ts) * a.ld;
   }
   float v[R];
   const bool strange = route_load<T, R>(z, a.E, of_row, lane, v);
-  float best = v[0];
+  int32_t order[R];
 #pragma unroll
-  for (int r = 1; r < R; ++r) best = fmaxf(best, v[r]);
-  const float most = row_max(best);
+  for (int r = 0; r < R; ++r) order[r] = order_of_logit(v[r]);
+  auto lanes_most = [&] {
+    int32_t best = order[0];
+#pragma unroll
+    for (int r = 1; r < R; ++r) best = max(best, order[r]);
+    return best;
+  };
+  chosen[lane] = -1;
+  staged_in_order();
+  int32_t best = lanes_most(), here = row_most(best), mine = kNoLogit;
+  const float most = logit_of_order(here);
   float total = a.normalise ? 0.f : route_total<R>(v, most, strange);
-  int expert = -1;
-  float logit = -INFINITY;
-  for (int i = 0; i < a.k; ++i) {
+  for (int i = 0;;) {
+    // the lowest lane of each row of sixteen that has the largest (one has), and the lowest of its experts that do
+    const uint64_t having = __builtin_amdgcn_ballot_w64(best == here), lowest = having & ~(having - 0x0001000100010001ull);
+    bool looking = ((lowest >> lane) & 1) != 0 && here != kNoLogit;
+    const bool winner = looking;
     int at = 0;
-    best = v[0];
 #pragma unroll
-    for (int r = 1; r < R; ++r)
-      if (v[r] > best) {
-        best = v[r];
-        at = r;
-      }
-    const float here = row_max(best);
-    const uint32_t those = row_ballot(best == here && here > -INFINITY, lane);
-    if (those != 0) {                            // (alike for the sixteen lanes)
-      const int winner = __builtin_ctz(those), chosen = __shfl(of_row * R + at, (lane & 48) + winner);
-      if (of_row == i) {
-        expert = chosen;
-        logit = here;
-      }
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-        if (of_row * R + r == chosen) v[r] = -INFINITY;
+    for (int r = 0; r < R; ++r) {
+      const bool it = looking && order[r] == here;
+      looking = looking && !it;
+      order[r] = it ? kNoLogit : order[r];
+      at = it ? r : at;
     }
+    if (winner) chosen[(lane & 48) + i] = of_row * R + at;
+    mine = of_row == i ? here : mine;
+    if (++i == a.k) break;
+    best = lanes_most();
+    here = row_most(best);
   }
-  const float share = expert >= 0 ? expf(logit - most) : 0.f;
+  staged_in_order();
+  const int expert = chosen[lane];
+  const float share = expert >= 0 ? expf(logit_of_order(mine) - most) : 0.f;
   if (a.normalise) total = row_sum(share);
   *chosen_expert = expert;
   *weight = expert >= 0 ? share / total : 0.f;
@@ -145,12 +166,12 @@ __device__ __forceinline__ void route_choose(const RouteArgs& a, int token, int 
 constexpr int kFewRouted = kOrderThreads / kRouteLanes, kTileTokens = kFewRouted;
 template <typename T, int R>
 __global__ __launch_bounds__(kOrderThreads) void route_kernel(const RouteArgs a, int32_t* counts) {
-  __shared__ int32_t here[kMostExperts];
+  __shared__ int32_t here[kMostExperts], chosen[kOrderThreads];
   const int t = threadIdx.x, lane = t & 63, of_row = lane & 15, token = blockIdx.x * kTileTokens + t / kRouteLanes;
   if (t < a.E) here[t] = 0;
   int expert;
   float weight;
-  route_choose<T, R>(a, token, lane, &expert, &weight);
+  route_choose<T, R>(a, token, lane, chosen + (t & ~63), &expert, &weight);
   __syncthreads();
   if (token < a.T && of_row < a.k) {
     a.experts[static_cast<int64_t>(token) * a.k + of_row] = expert;
@@ -294,10 +315,11 @@ template <typename T, int R>
 __global__ __launch_bounds__(kOrderThreads) void route_few_kernel(const RouteArgs a, int bits, int32_t* slots, int32_t* order, int32_t* sizes) {
   __shared__ uint16_t counts[kOrderWaves << kMostRange];
   __shared__ uint32_t keys[kOrderThreads], sums[kOrderWaves];
+  __shared__ int32_t chosen[kOrderThreads];
   const int t = threadIdx.x, lane = t & 63, of_row = lane & 15, token = t / kRouteLanes, n = a.T * a.k;
   int expert;
   float weight;
-  route_choose<T, R>(a, token, lane, &expert, &weight);
+  route_choose<T, R>(a, token, lane, chosen + (t & ~63), &expert, &weight);
   if (token < a.T && of_row < a.k) {
     a.experts[token * a.k + of_row] = expert;
     a.weights[token * a.k + of_row] = weight;
@@ -314,14 +336,21 @@ __global__ __launch_bounds__(kOrderThreads) void route_few_kernel(const RouteArg
   for (int e = t; e < a.E; e += kOrderThreads) sizes[e] = counts[(e + 1) * kOrderWaves] - counts[e * kOrderWaves];
 }
 
-// dlogits: of weights from all experts p (g - sum p g), g zero where not chosen; from the chosen ones the same among them, zeros elsewhere.
+// dlogits: of weights from all experts p (g - sum p g), g zero where not chosen; from the chosen ones the same among them, zeros elsewhere.  What the choices add is put where their experts are in LDS.
 template <typename T, int R>
 __global__ __launch_bounds__(256) void route_grad_kernel(const RouteArgs a) {
+  __shared__ __attribute__((aligned(16))) float added[256 / kRouteLanes][kRouteLanes * R];
   const int lane = threadIdx.x & 63, of_row = lane & 15, token = (blockIdx.x * 256 + threadIdx.x) / kRouteLanes;
+  float* const add = added[threadIdx.x / kRouteLanes];
   const bool in = token < a.ts * a.shards, live = token < a.T;
   const int shard = in ? embed_shard(token, a.ts, a.shards) : 0, within = token - shard * a.ts;
   const T* z = live && !a.normalise ? static_cast<const T*>(first_kernel_argument<RouteArgs>()->shard[shard].logits) + static_cast<int64_t>(within) * a.ld : nullptr;
   T* const d = in ? static_cast<T*>(first_kernel_argument<RouteArgs>()->shard[shard].dlogits) : nullptr;
+  const int64_t at = static_cast<int64_t>(token) * a.k + of_row;
+  const bool mine = live && of_row < a.k;
+  const int expert = mine ? a.experts[at] : -1;
+  const bool chosen = expert >= 0 && expert < a.E;
+  const float w = chosen ? a.weights[at] : 0.f, g = chosen ? a.dweights[at] : 0.f;
   float v[R];
   if (a.normalise) {
 #pragma unroll
@@ -331,27 +360,32 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteArgs a) {
     float best = v[0];
 #pragma unroll
     for (int r = 1; r < R; ++r) best = fmaxf(best, v[r]);
-    const float most = row_max(best), total = route_total<R>(v, most, strange);
+    const float most = row_max(best), each = 1.f / route_total<R>(v, most, strange);
     const bool none = most == -INFINITY && !strange;        // no expert at all
 #pragma unroll
-    for (int r = 0; r < R; ++r) v[r] = none ? 0.f : expf(v[r] - most) / total;
+    for (int r = 0; r < R; ++r) v[r] = none ? 0.f : expf(v[r] - most) * each;
   }
-  const int64_t at = static_cast<int64_t>(token) * a.k + of_row;
-  const bool mine = live && of_row < a.k;
-  const int expert = mine ? a.experts[at] : -1;
-  const bool chosen = expert >= 0 && expert < a.E;
-  const float w = chosen ? a.weights[at] : 0.f, g = chosen ? a.dweights[at] : 0.f;
-  const float mean = row_sum(w * g);
+  const float mean = row_sum(w * g), own = a.normalise ? w * (g - mean) : w * g;
 #pragma unroll
-  for (int r = 0; r < R; ++r) v[r] *= -mean;
-  const float own = a.normalise ? w * (g - mean) : w * g;
-  for (int i = 0; i < a.k; ++i) {
-    const int e = __shfl(chosen ? expert : -1, (lane & 48) + i);
-    const float add = __shfl(own, (lane & 48) + i);
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-      if (of_row * R + r == e) v[r] += add;
+  for (int r = 0; r < R; ++r) add[of_row * R + r] = 0.f;
+  staged_in_order();
+  if (chosen) add[expert] = __int_as_float(of_row);
+  staged_in_order();
+  const bool alone = !chosen || __float_as_int(add[expert]) == of_row;
+  staged_in_order();
+  if (__builtin_amdgcn_ballot_w64(!alone) == 0) {
+    if (chosen) add[expert] = own;
+  } else {                                       // an expert twice (no routing of gspmd_route's): one choice after the other
+    if (chosen) add[expert] = 0.f;
+    staged_in_order();
+    for (int i = 0; i < a.k; ++i) {
+      if (chosen && of_row == i) add[expert] += own;
+      staged_in_order();
+    }
   }
+  staged_in_order();
+#pragma unroll
+  for (int r = 0; r < R; ++r) v[r] = fmaf(v[r], -mean, add[of_row * R + r]);
   if (d == nullptr) return;
   constexpr int n = Sixteen<T>::n;
   if constexpr (R % n == 0) {

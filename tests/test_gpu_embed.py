@@ -151,3 +151,62 @@ def test_after_the_loss():
     e.w = e.dwc.whole()[:90].clone()
     e.gradient()
     e.check_gradient()
+
+
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("ids", sorted(IDS))
+@pytest.mark.parametrize("T", [8192, 8193, 16399])
+def test_gradient_of_many_tokens(order, ids, T):
+    """Chunks of either size; runs that begin and end in them, at their ends and beyond them; rows shorter than 16 bytes, that divide by them or not, written or added to."""
+    for M, kw in ((5, dict()), (40, dict(accumulate=True)), (515, dict(pad=False, scale=0.5)), (515, dict(accumulate=True, pad=False, shift=1))):
+        e = Embed(T, M, 333, order=order, ids=IDS[ids](T, 333) if IDS[ids] else None, seed=9, **kw).stage_gradient()
+        e.gradient()
+        e.check_gradient()
+
+
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("V", [131072, 131073, 600000])
+def test_gradient_of_large_vocabularies(order, V):
+    """Ranges of up to 1024 entries for a workgroup, and more workgroups than there are compute units."""
+    for T in (100, 9000):
+        ids = torch.randint(0, V, (T,), generator=torch.Generator().manual_seed(V))
+        ids[::7], ids[3], ids[5] = V - 1, V, -1
+        for accumulate in (False, True):
+            e = Embed(T, 8, V, y=3, order=order, ids=ids, accumulate=accumulate, seed=10).stage_gradient()
+            e.gradient()
+            e.check_gradient()
+
+
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [2, 3, 4, 6, 7, 9, 127, 128, 129, 255, 256, 257, 264, 511, 512, 520, 1023, 2047, 2049])
+def test_ends_of_rows(order, dtype, M):
+    for kw in (dict(pad=False), dict(pad=True, accumulate=True), dict(pad=False, shift=1, accumulate=True, x=2, y=2)):
+        e = Embed(37, M, 23, order=order, dtype=dtype, seed=11, scale=1.5, **kw).stage_lookup().stage_gradient()
+        e.lookup()
+        e.check_lookup()
+        e.gradient()
+        e.check_gradient()
+
+
+@pytest.mark.parametrize("order", ORDERS)
+def test_two_streams_at_once(order):
+    """Two gradients with workspaces of their own, side by side, many times over: the bits of one alone."""
+    both = [Embed(3000, 264, 900, order=order, seed=s, y=2).stage_gradient() for s in (12, 13)]
+    alone = []
+    for e in both:
+        e.gradient()
+        torch.cuda.synchronize()
+        e.check_gradient()
+        alone.append([t.clone() for t in e.dwc.t[0]])
+        for t in e.dwc.t[0]:
+            t[:, :e.dwc.cols] = 55.0
+    streams = [torch.cuda.Stream() for _ in both]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for e, s in zip(both, streams):
+            with torch.cuda.stream(s):
+                e.gradient()
+    torch.cuda.synchronize()
+    for e, want in zip(both, alone):
+        assert all(torch.equal(a, b) for a, b in zip(e.dwc.t[0], want))

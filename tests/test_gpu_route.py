@@ -280,3 +280,52 @@ def test_a_layer_in_a_graph():
         run()
         torch.cuda.synchronize()
         assert torch.equal(got[0], rows) and torch.equal(got[1], y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [2, 3, 7, 9, 127, 129, 256, 257, 264, 511, 1023, 2049, 4103])
+def test_ends_of_rows(M, dtype):
+    for case in (dict(T=21, E=6, k=3, M=M, dtype=dtype, pad=False), dict(T=10, E=5, k=5, M=M, dtype=dtype, x=2, y=2, share=False, shift=1, pad=False)):
+        test_dispatch_and_combine(case)
+        test_combine_gradient(case)
+
+
+@pytest.mark.parametrize("E, k", [(3, 3), (16, 4), (100, 8), (512, 16)])
+def test_equal_logits_go_to_the_lowest(E, k):
+    """Zeros of both signs are equal, as are infinities; numbers below normal are not."""
+    r = Routed(70, E, k, masked=0.0, seed=21)
+    gen = torch.Generator().manual_seed(22)
+    values = torch.tensor([0.0, -0.0, 1e-40, -1e-40, 2e-40, -float("inf"), -3.0e38, 3.0e38])
+    r.z = values[torch.randint(0, 8, (70, E), generator=gen)]
+    r.stage().call()
+    torch.cuda.synchronize()
+    experts, _, slots, order, sizes = r.expected()
+    assert torch.equal(r.experts.cpu().long(), experts) and torch.equal(r.slots.cpu().long(), slots)
+    assert torch.equal(r.order.cpu().long(), order) and torch.equal(r.sizes.cpu().long(), sizes)
+
+
+@pytest.mark.parametrize("normalise", [False, True])
+def test_gradient_of_an_expert_twice(normalise):
+    """A routing that a program made by itself may name an expert more than once: its choices' gradients add up, in their order."""
+    r = Routed(40, 24, 4, masked=0.0, normalise=normalise, seed=23).stage()
+    r.z[20] = 0.0
+    r.stage().call()
+    experts = r.experts.cpu().long()
+    experts[::3, 2] = experts[::3, 0]
+    experts[5, :] = experts[5, 1]
+    r.experts.copy_(experts.int())
+    dw = torch.randn(40, 4, generator=torch.Generator().manual_seed(24))
+    d, given = Cut(torch.zeros(40, 24), 1), dw.cuda()
+    outs = []
+    for _ in range(2):
+        g.route_grad(r.mesh, r.z_bufs, r.sh, 4, r.buf, given.data_ptr(), [d.buf(0)], normalise=normalise, stream=stream())
+        outs.append(d.whole())
+    assert torch.equal(outs[0], outs[1])
+    # p (all experts') or nothing minus the mean of w g over the choices, and what each choice adds, from the weights that the call was given
+    w = r.weights.cpu().double() * dw.double()
+    mean = w.sum(dim=1, keepdim=True)
+    p = torch.softmax(r.z.double(), dim=1)
+    want = torch.zeros(40, 24, dtype=torch.float64) if normalise else -p * mean
+    want.scatter_add_(1, experts, w - r.weights.cpu().double() * mean if normalise else w)
+    mag = (p + 1) * (w.abs().sum(dim=1, keepdim=True) + (r.weights.cpu().double().sum(dim=1, keepdim=True) + 1) * mean.abs())
+    assert ((d.whole().double() - want).abs() <= (24 + 80) * 2.0 ** -23 * mag).all()

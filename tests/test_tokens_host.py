@@ -155,3 +155,16 @@ def test_exchange_refusals(which):
         assert status(call, ok, weighted=False, route=g.RouteBuf(fields[0], 0, fields[2], 0, 0)) == 0
     if which == "combine_grad":
         assert status(call, ok, dweights=0) == NULL and status(call, ok, dweights=2) == BUFFER
+
+
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("vocab_dim", [0, 1])
+def test_rows_of_the_embedding_are_bounded(grad, vocab_dim):
+    call = g.embed_grad if grad else g.embed
+    ok = embed_args(grad=grad, vocab_dim=vocab_dim, M=1 << 21)
+    more = dict(workspace_bytes=1 << 40) if grad else {}
+    rows = "dy_shards" if grad else "y_shards"
+    w = "dw_shards" if grad else "w_shards"
+    dense = {name: [g.ShardBuf(b.data, b.dtype, 0) for b in ok[name]] for name in (rows, w)}
+    assert status(call, ok, **dense, **more) == 0
+    assert status(call, embed_args(grad=grad, vocab_dim=vocab_dim, M=(1 << 21) + 1), **dense, **more) == UNSUPPORTED
