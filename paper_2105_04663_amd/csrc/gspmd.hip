@@ -744,10 +744,32 @@ int32_t run_dots(std::vector<Problem>& ps, int32_t layout, int32_t in_dtype, int
   return launch_problems(ps, layout, in_dtype, out_dtype, GSPMD_EPILOGUE_NONE, false, tables, table_bytes, stream);
 }
 
+// Experts' packed rows differ in two ways from the problems that choose_mfma's lines were measured on: experts are of any size about the mean, so that a row tile of 256 is often nearly empty, and all their
+// matrices are read for however few rows.  dot_mid_kernel's tiles then do better (us, by the lines / this):
+//   up to kMidExpertRows rows an expert, from dot_mfma_kernel: 89 experts of 118, 320 x 1344 35 / 26; 18 of 105, 1255 x 3329 53 / 41; 64 of 9, 2048 x 704 34 / 25; 25 of 98, 960 x 2240 25.6 / 27.9; beyond it
+//     41 of 540, 1600 x 4096 276 / 342
+//   where its tiles take most compute units, from dot_split_kernel: 31 of 2, 1460 x 2500 54 / 27; 8 of 3, 3154 x 2373 33 / 21; 51 of 20, 1152 x 320 15 / 11; of 45 rows 14 of 3200 x 896 35 / 22; with fewer, or a
+//     short K, 5 of 13, 704 x 2944 6.2 / 8.2; 25 of 9, 5632 x 384 23 / 27; 36 of 1, 4800 x 384 17 / 23; 4 of 189, 6400 x 896 34 / 39
+// and of dot_split_kernel with K-contiguous matrices half the columns a workgroup, for a handful of rows (36 of 1, 4800 x 384 16.8 / 12.6; 16 of 8, 7744 x 448 25 / 20.5; 8 of 14, 5440 x 768 19.6 / 22.8).
+constexpr int64_t kMidExpertRows = 224, kMidExpertTiles = 150, kMidExpertTilesOfRows = 90, kMidExpertK = 1024, kHandful = 10;
+MfmaChoice for_experts(MfmaChoice m, const std::vector<Problem>& ps, KernelPath path, int32_t layout) {
+  if (t_pin.kernel != GSPMD_TESTING_BY_RULE || (layout & GSPMD_LAYOUT_LHS_K_MAJOR) || path == kPathMfmaStaged || ps.empty()) return m;
+  int64_t rows = 0, tiles = 0;
+  for (const auto& p : ps) {
+    rows += p.Mv;
+    tiles += tiles_of(p, kMidTile, kMidTile);
+  }
+  const int64_t mean = rows / static_cast<int64_t>(ps.size());
+  if (m.kernel == kMfmaBig && mean <= kMidExpertRows) return MfmaChoice{kMfmaMid, 0};
+  if (m.kernel == kMfmaSplit && path == kPathMfmaDirect && (tiles >= kMidExpertTiles || (m.row_blocks > 1 && tiles >= kMidExpertTilesOfRows && ps[0].Kv >= kMidExpertK))) return MfmaChoice{kMfmaMid, 0};
+  if (m.kernel == kMfmaSplit && m.row_blocks == 1 && (layout & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) && mean <= kHandful) m.col_blocks = 2;
+  return m;
+}
+
 DotChoice choose_dot(const std::vector<Problem>& ps, int32_t layout, int32_t in_dtype) {
   DotChoice c;
   const KernelPath path = kernel_path(ps, in_dtype, layout);
-  MfmaChoice m = pick_kernel(ps, path, layout, false);
+  MfmaChoice m = for_experts(pick_kernel(ps, path, layout, false), ps, path, layout);
   const LaunchSize size = launch_size(ps, layout);
   if (m.kernel == kMfmaBig && big_staged(size, path, layout))
     m = path != kPathMfmaStaged || mid_stages_whole(size, layout) ? MfmaChoice{kMfmaMid, 0} : MfmaChoice{kMfmaSplit, 4, 4};
