@@ -1,8 +1,10 @@
 // The choice of experts and the exchange of rows with them (gspmd_route, gspmd_dispatch, gspmd_combine and their gradients).
 //
 // Routing: sixteen lanes have a token, each R neighbouring experts in registers.  The largest logit is found k times over: every lane's own, a maximum over the sixteen by rotations
-// within their row of the wave, and of those that have it the lowest lane, whose experts are the lowest.  It is bound by that chain, 8 + 3 R instructions a choice, not by the logits.
-// Exchange: bound by memory, rows copied or added up 16 bytes a lane.  Every row has one writer; a token's rows are added in the order of its choices.
+// within their row of the wave, and of those that have it the lowest lane, whose experts are the lowest.  It is bound by those instructions, some 20 + 3 R a choice, not by the logits (16384 tokens of 128 experts, 8 chosen: 8.4 us,
+// of which the 8.4 MB would take 2).  Logits are compared as whole numbers: a maximum of floats is two instructions where a NaN may be about.
+// Exchange: bound by memory, rows copied or added up 16 bytes a lane.  Every row has one writer (or two with the same bits, kernels_rows.h); a token's rows are added in the order of its choices.
+// 8192 tokens of 4096, 4 choices: combine_kernel 79 us (336 MB, 4.2 TB/s), combine_grad_kernel 109 (604 MB, 5.5 TB/s); 2048 of 2048, 2 choices: dispatch_kernel 10.3, combine_kernel 6.6.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -162,7 +164,7 @@ __device__ __forceinline__ void route_choose(const RouteArgs& a, int token, int 
   *weight = expert >= 0 ? share / total : 0.f;
 }
 
-// The choices of sixty-four tokens, and how many of them each expert has: counts [tile][E].
+// The choices of sixty-four tokens, and how many of them each expert has: counts [tile][E].  (With them a routing takes two launches; ordering the choices as order_kernel does takes three.)
 constexpr int kFewRouted = kOrderThreads / kRouteLanes, kTileTokens = kFewRouted;
 template <typename T, int R>
 __global__ __launch_bounds__(kOrderThreads) void route_kernel(const RouteArgs a, int32_t* counts) {
@@ -240,7 +242,7 @@ __device__ __forceinline__ int place_of_mine(uint32_t key, int bits, uint16_t* c
   return rank + *mine;
 }
 
-// Slots of a tile's choices, a choice a thread.  `totals`: null where counts are the tiles' own (kTilesSummed).
+// Slots of a tile's choices, a choice a thread.  Bound by waits: 256 tiles' counts of 128 experts come in four rounds (7.4 us).  `totals`: null where counts are the tiles' own (kTilesSummed).
 __global__ __launch_bounds__(kOrderThreads) static void route_places_kernel(const int32_t* experts, const int32_t* counts, const int32_t* totals, int n, int each, int E, int tiles, int bits, int32_t* slots,
                                                                          int32_t* order, int32_t* sizes) {
   __shared__ uint16_t of_tile[kOrderWaves << kMostRange];
