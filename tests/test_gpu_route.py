@@ -4,7 +4,7 @@ import torch
 
 import paper_2105_04663_amd as g
 from tests.ragged import DIMS, BACK, FORWARD, WEIGHT
-from tests.tokens import HALF, KEPT, NAN, TYPES, Cut, Routed, stream
+from tests.tokens import HALF, KEPT, NAN, TYPES, Cut, Embed, Routed, stream
 
 pytestmark = pytest.mark.gpu
 
@@ -329,3 +329,15 @@ def test_gradient_of_an_expert_twice(normalise):
     want.scatter_add_(1, experts, w - r.weights.cpu().double() * mean if normalise else w)
     mag = (p + 1) * (w.abs().sum(dim=1, keepdim=True) + (r.weights.cpu().double().sum(dim=1, keepdim=True) + 1) * mean.abs())
     assert ((d.whole().double() - want).abs() <= (24 + 80) * 2.0 ** -23 * mag).all()
+
+
+def test_the_same_through_ctypes(monkeypatch):
+    from paper_2105_04663_amd import binding
+    monkeypatch.setattr(binding, "_CALL", None)
+    test_a_layer_and_its_gradients(3, "bf16")
+    test_route_gradient(True, "f32", 70, 100, 2, 3, 1)
+    e = Embed(150, 56, 37, x=2, y=3, copies=2, accumulate=True).stage_lookup().stage_gradient()
+    e.lookup()
+    e.check_lookup()
+    e.gradient()
+    e.check_gradient()

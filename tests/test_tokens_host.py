@@ -168,3 +168,17 @@ def test_rows_of_the_embedding_are_bounded(grad, vocab_dim):
     dense = {name: [g.ShardBuf(b.data, b.dtype, 0) for b in ok[name]] for name in (rows, w)}
     assert status(call, ok, **dense, **more) == 0
     assert status(call, embed_args(grad=grad, vocab_dim=vocab_dim, M=(1 << 21) + 1), **dense, **more) == UNSUPPORTED
+
+
+def test_the_same_through_ctypes(monkeypatch):
+    """Refusals do not depend on which way a call takes into the library."""
+    from paper_2105_04663_amd import binding
+    g.load_library()
+    monkeypatch.setattr(binding, "_CALL", None)
+    for grad in (False, True):
+        test_route_refusals(grad)
+        for vocab_dim in (0, 1):
+            test_embed_refusals(grad, vocab_dim)
+            test_rows_of_the_embedding_are_bounded(grad, vocab_dim)
+    for which in ("dispatch", "combine", "combine_grad"):
+        test_exchange_refusals(which)
