@@ -9,6 +9,7 @@
 #include "dots.h"
 #include "kernels_basic.h"
 #include "kernels_f32.h"
+#include "kernels_f32_experts.h"
 #include "launch.h"
 #include "plan.h"
 #include "ragged.h"
@@ -91,6 +92,17 @@ void launch_f32(const InlineProblems& inl, int n, unsigned tiles, int32_t layout
   }
 }
 
+// Whether experts' float32 rows are few enough for dot_f32_experts_kernel (us, dot_f32_kernel / it): K-major matrices 52 experts of 14 rows, 1216 x 4800 311 / 257; 18 of 20, 1024 x 7040 152 / 132; 23 of 29, 416 x 1142
+// 17 / 28; K-contiguous ones 27 of 8, 576 x 896 21 / 15; 12 of 12, 576 x 1088 12.6 / 14.6; 18 of 20, 7040 x 1024 202 / 233.
+constexpr int64_t kFewF32Rows = 20, kFewF32RowsKContiguous = 10;
+bool few_f32_rows(const Ragged& g, const std::vector<Problem>& parts) {
+  if (g.contracting || g.E == 0) return false;
+  for (const auto& p : parts)
+    if (std::max(p.lda, p.ldb) > kF32ExpertsStride) return false;
+  const int64_t rows = g.S / std::max<int64_t>(1, std::min(g.E, g.S));       // of an expert that has any
+  return rows <= (g.layout & GSPMD_LAYOUT_RHS_K_CONTIGUOUS ? kFewF32RowsKContiguous : kFewF32Rows);
+}
+
 int32_t launch_parts(const Ragged& g, std::vector<Problem>& parts, const int32_t* sizes, int32_t first, int32_t last, int32_t in_dtype, int32_t out_dtype, int32_t epilogue, hipStream_t stream) {
   if (parts.empty()) return GSPMD_OK;
   int64_t experts = last - first;
@@ -105,6 +117,11 @@ int32_t launch_parts(const Ragged& g, std::vector<Problem>& parts, const int32_t
   if (c.moves_back)
     for (auto& p : parts)
       if ((reinterpret_cast<uintptr_t>(p.B) & 15) || (p.ldb & 7)) p.flags |= kProblemMovesBack;
+  const bool few = in_dtype == GSPMD_F32 && few_f32_rows(g, parts);
+  if (few) {
+    c.bm = kF32ExpertsRows;
+    c.bn = kF32ExpertsCols;
+  }
   const int64_t tiles_n = (g.N + c.bn - 1) / c.bn;
   const int64_t row_tiles = g.contracting ? experts * ((g.M + c.bm - 1) / c.bm) : g.S / c.bm + std::min(experts, g.S);
   if (row_tiles * tiles_n > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
@@ -140,7 +157,9 @@ int32_t launch_parts(const Ragged& g, std::vector<Problem>& parts, const int32_t
     case GSPMD_TESTING_PAIR: ok = by_layout([&](auto layout) { return launch_ragged_pair_layout<decltype(layout)::value>(l, out_dtype, stream); }); break;
     case GSPMD_TESTING_MFMA: ok = by_layout([&](auto layout) { return launch_ragged_mfma_layout<decltype(layout)::value>(l, out_dtype, stream); }); break;
     default:
-      if (c.f32_wide) launch_f32<false, true>(inl, n, tiles, g.layout, epilogue, stream);
+      if (few && g.layout == 0) hipLaunchKernelGGL((dot_f32_experts_kernel<0>), dim3(tiles), dim3(256), 0, stream, inl, n, epilogue);
+      else if (few) hipLaunchKernelGGL((dot_f32_experts_kernel<GSPMD_LAYOUT_RHS_K_CONTIGUOUS>), dim3(tiles), dim3(256), 0, stream, inl, n, epilogue);
+      else if (c.f32_wide) launch_f32<false, true>(inl, n, tiles, g.layout, epilogue, stream);
       else if (c.f32_lean) launch_f32<true, false>(inl, n, tiles, g.layout, epilogue, stream);
       else launch_f32<false, false>(inl, n, tiles, g.layout, epilogue, stream);
       ok = hipGetLastError() == hipSuccess;

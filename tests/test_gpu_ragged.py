@@ -183,3 +183,28 @@ def test_the_gradients_against_differences():
     d_rows, d_w = back.outs[0][1][:, :M].cpu().double(), weight.outs[0][1][..., :H].cpu().double()
     for along, got in ((lambda s: forward(lhs + s * d_lhs, rhs), (d_rows * d_lhs).sum()), (lambda s: forward(lhs, rhs + s * d_rhs), (d_w * d_rhs).sum())):
         assert (((along(1) - along(-1)) / 2) * c).sum() == got
+
+
+FEW = [[1], [0, 3, 0, 1, 0, 0, 16, 0], [17, 2, 0, 5, 1, 33, 0, 4], [1] * 70, [0] * 63 + [5, 20, 1]]
+
+
+@pytest.mark.parametrize("way", [FORWARD, BACK])
+@pytest.mark.parametrize("sizes", range(len(FEW)))
+@pytest.mark.parametrize("M", [1, 3, 15, 16, 17, 64, 79, 128, 300, 1031])
+def test_few_float32_rows(way, sizes, M):
+    """K below a step, of whole steps for some waves and not for others, and what is left of it; columns that end inside a lane's four, at a tile's end, and fewer than four."""
+    for H, kw in ((1, dict()), (3, dict(pad=False, shift=1)), (63, dict(pad=False)), (64, dict(relu=True)), (66, dict(pad=False, shift=3)), (130, dict(y=2, share=False)), (257, dict(slots=sum(FEW[sizes]) + 7))):
+        r = Ragged(way, FEW[sizes], M=M, H=H, dtype="f32", seed=31, **kw).stage()
+        r.call()
+        r.check()
+
+
+@pytest.mark.parametrize("way", [FORWARD, BACK])
+def test_few_float32_rows_are_exact_in_whole_numbers(way):
+    r = Ragged(way, [3, 0, 20, 1, 9], M=515, H=131, dtype="f32", seed=32, whole_numbers=True, pad=False, shift=1).stage()
+    for _ in range(3):
+        r.call()
+    r.check()
+    want, _, _ = r.expected(0)
+    got = r.outs[0][1][:, :131].cpu().double()
+    assert torch.equal(got[:r.used], want[:r.used])
