@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256) void embed_columns_kernel(const EmbedArgs a, i
     float f[n];
 #pragma unroll
     for (int e = 0; e < n; ++e) f[e] = a.scale == 1.f ? tile[r][c + e] : tile[r][c + e] * a.scale;
-    store_up_to(y + static_cast<int64_t>(row - shard * a.ts) * a.ld_rows + col, Sixteen<T>::close(f), a.M - col);
+    store_up_to(y + static_cast<int64_t>(row - shard * a.ts) * a.ld_rows + col, a.scale == 1.f ? Sixteen<T>::bits(f) : Sixteen<T>::close(f), a.M - col);
   }
 }
 

@@ -21,7 +21,7 @@ namespace gspmd {
 
 enum Lines { kExact, kNarrow, kWide };
 
-template <typename T> struct Sixteen;          // 16 bytes as float32, and back with one rounding
+template <typename T> struct Sixteen;          // 16 bytes as float32, back with one rounding, and back the very bits of opened ones
 template <> struct Sixteen<bf16_bits> {
   static constexpr int n = 8;
   static __device__ __forceinline__ void open(u32x4_t v, float (&f)[8]) {
@@ -34,6 +34,12 @@ template <> struct Sixteen<bf16_bits> {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = f[i];
     return __builtin_bit_cast(u32x4_t, __builtin_convertvector(v, bf16x8_t));
+  }
+  static __device__ __forceinline__ u32x4_t bits(const float (&f)[8]) {
+    u32x4_t v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(f[2 * i]) >> 16 | (__float_as_uint(f[2 * i + 1]) & 0xffff0000u);
+    return v;
   }
 };
 template <> struct Sixteen<float> {
@@ -48,6 +54,7 @@ template <> struct Sixteen<float> {
     for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(f[i]);
     return v;
   }
+  static __device__ __forceinline__ u32x4_t bits(const float (&f)[4]) { return close(f); }
 };
 template <typename T> struct AnyAligned;
 template <> struct AnyAligned<bf16_bits> {

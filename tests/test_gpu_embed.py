@@ -210,3 +210,18 @@ def test_two_streams_at_once(order):
     torch.cuda.synchronize()
     for e, want in zip(both, alone):
         assert all(torch.equal(a, b) for a, b in zip(e.dwc.t[0], want))
+
+
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_scale_of_one_copies_any_bits(order, dtype):
+    """Every pattern of 16 bits, and float32 ones of each kind: signalling NaN with their payloads among them."""
+    if dtype == "bf16":
+        w = torch.arange(-2 ** 15, 2 ** 15, dtype=torch.int32).to(torch.int16).view(64, 1024)
+    else:
+        w = (torch.arange(2 ** 16, dtype=torch.int64) * 65537 + 2 ** 23 * 255 - 7).to(torch.int32).view(64, 1024)
+    e = Embed(64, 1024, 64, order=order, dtype=dtype, ids=torch.arange(64) * 37 % 64)
+    e.w = w.view(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    e.stage_lookup().lookup()
+    got = e.yc.whole()[:64]
+    assert torch.equal(got.view(w.dtype), w[e.ids])
