@@ -19,7 +19,7 @@ struct Embed {
   int64_t P = 0, T = 0, M = 0, V = 0;
   int64_t na = 1, nb = 1, ts = 0, vs = 0;       // shards of tokens and of the vocabulary, their static extents
   int axis_t = -1, axis_v = -1, vocab_dim = 0;
-  int64_t chunk() const { return T <= kFewTokens ? kSmallChunk : kLargeChunk; }
+  int64_t chunk() const { return T > kLargeChunk && T <= kFewTokens ? kSmallChunk : kLargeChunk; }       // (one chunk: nothing to join, a launch less)
   int64_t chunks() const { return (T + chunk() - 1) / chunk(); }
   // the workspace: the tokens' order and their entries in it, up to a chunk's end; where an entry's begin; chunks' sums, two of each; with dw [M, V] the sums of runs of two tokens and more
   int64_t order_bytes() const { return round_up(chunks() * chunk() * 4, kWsAlign); }

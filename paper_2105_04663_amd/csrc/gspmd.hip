@@ -751,9 +751,16 @@ int32_t run_dots(std::vector<Problem>& ps, int32_t layout, int32_t in_dtype, int
 //   where its tiles take most compute units, from dot_split_kernel: 31 of 2, 1460 x 2500 54 / 27; 8 of 3, 3154 x 2373 33 / 21; 51 of 20, 1152 x 320 15 / 11; of 45 rows 14 of 3200 x 896 35 / 22; with fewer, or a
 //     short K, 5 of 13, 704 x 2944 6.2 / 8.2; 25 of 9, 5632 x 384 23 / 27; 36 of 1, 4800 x 384 17 / 23; 4 of 189, 6400 x 896 34 / 39
 // and of dot_split_kernel with K-contiguous matrices half the columns a workgroup, for a handful of rows (36 of 1, 4800 x 384 16.8 / 12.6; 16 of 8, 7744 x 448 25 / 20.5; 8 of 14, 5440 x 768 19.6 / 22.8).
+// Sums over the slots (dw) come out more even in smaller tiles than dot_mfma_kernel's, experts' K being of any size, too: dot_pair_kernel's (8 of 1024 slots, 4096 x 8192 464 / 431; 6 of 2346, 1295 x 2083 95 / 81; 22
+// of 3985, 1900 x 922 320 / 354; thirteen cases 0.93 in the geometric mean), dot_mid_kernel's for matrices of up to kMidExpertMatrix elements (72 of 749, 704 x 512 88 / 60; 17 of 1502, 1344 x 384 53 / 38).
+constexpr int64_t kMidExpertMatrix = 1 << 20;
 constexpr int64_t kMidExpertRows = 224, kMidExpertTiles = 150, kMidExpertTilesOfRows = 90, kMidExpertK = 1024, kHandful = 10;
 MfmaChoice for_experts(MfmaChoice m, const std::vector<Problem>& ps, KernelPath path, int32_t layout) {
-  if (t_pin.kernel != GSPMD_TESTING_BY_RULE || (layout & GSPMD_LAYOUT_LHS_K_MAJOR) || path == kPathMfmaStaged || ps.empty()) return m;
+  if (t_pin.kernel != GSPMD_TESTING_BY_RULE || path == kPathMfmaStaged || ps.empty()) return m;
+  if (layout & GSPMD_LAYOUT_LHS_K_MAJOR) {
+    if (m.kernel != kMfmaBig || !pair_takes(launch_size(ps, layout), path, layout)) return m;
+    return static_cast<int64_t>(ps[0].Mv) * ps[0].Nv <= kMidExpertMatrix ? MfmaChoice{kMfmaMid, 0} : MfmaChoice{kMfmaPair, 0, 0, false, path == kPathMfmaWords};
+  }
   int64_t rows = 0, tiles = 0;
   for (const auto& p : ps) {
     rows += p.Mv;
