@@ -19,7 +19,7 @@ struct Embed {
   int64_t P = 0, T = 0, M = 0, V = 0;
   int64_t na = 1, nb = 1, ts = 0, vs = 0;       // shards of tokens and of the vocabulary, their static extents
   int axis_t = -1, axis_v = -1, vocab_dim = 0;
-  int64_t chunk() const { return T > kLargeChunk && T <= kFewTokens ? kSmallChunk : kLargeChunk; }       // (one chunk: nothing to join, a launch less)
+  int64_t chunk() const { return T <= kFewTokens ? kSmallChunk : kLargeChunk; }
   int64_t chunks() const { return (T + chunk() - 1) / chunk(); }
   // the workspace: the tokens' order and their entries in it, up to a chunk's end; where an entry's begin; chunks' sums, two of each; with dw [M, V] the sums of runs of two tokens and more
   int64_t order_bytes() const { return round_up(chunks() * chunk() * 4, kWsAlign); }
@@ -119,7 +119,7 @@ int32_t launch_embed(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
 }
 
 // Sums over the runs of the order: rows of dw [V, M], or what embed_grad_columns_kernel reads.
-template <typename T, int TO, int CHUNK>
+template <typename T, int TO, int CHUNK, bool ALONE>
 int32_t launch_chunks(const EmbedArgs& a, hipStream_t stream) {
   constexpr int n = Sixteen<T>::n;
   const int64_t chunks = (static_cast<int64_t>(a.T) + CHUNK - 1) / CHUNK;
@@ -129,8 +129,8 @@ int32_t launch_chunks(const EmbedArgs& a, hipStream_t stream) {
   while (across < 2 && (static_cast<int64_t>(n) << (log + across)) < a.M) ++across;
   const int64_t piece = static_cast<int64_t>(n) << (log + across), units = int64_t(4) >> across << (6 - log);
   const dim3 grid(static_cast<unsigned>((chunks + units - 1) / units), static_cast<unsigned>((a.M + piece - 1) / piece));
-  const int32_t st = by_lines(lines, [&](auto l) { hipLaunchKernelGGL((embed_runs_kernel<T, decltype(l)::value, TO, CHUNK>), grid, dim3(256), 0, stream, a, log, across); });
-  if (st != GSPMD_OK || chunks < 2) return st;
+  const int32_t st = by_lines(lines, [&](auto l) { hipLaunchKernelGGL((embed_runs_kernel<T, decltype(l)::value, TO, CHUNK, ALONE>), grid, dim3(256), 0, stream, a, log, across); });
+  if (ALONE || st != GSPMD_OK || chunks < 2) return st;
   const dim3 joins(static_cast<unsigned>(chunks - 1), static_cast<unsigned>((a.M + 64 * n - 1) / (64 * n)));
   if (lines == kExact) hipLaunchKernelGGL((embed_joins_kernel<T, kExact, TO, CHUNK>), joins, dim3(256), 0, stream, a);
   else hipLaunchKernelGGL((embed_joins_kernel<T, kWide, TO, CHUNK>), joins, dim3(256), 0, stream, a);
@@ -140,7 +140,8 @@ template <typename T>
 int32_t launch_runs(const Embed& e, const EmbedArgs& a, hipStream_t stream) {
   auto of_chunk = [&](auto to) {
     constexpr int TO = decltype(to)::value;
-    return e.chunk() == kSmallChunk ? launch_chunks<T, TO, kSmallChunk>(a, stream) : launch_chunks<T, TO, kLargeChunk>(a, stream);
+    if (e.T <= kAloneTokens) return launch_chunks<T, TO, kSmallChunk, true>(a, stream);
+    return e.chunk() == kSmallChunk ? launch_chunks<T, TO, kSmallChunk, false>(a, stream) : launch_chunks<T, TO, kLargeChunk, false>(a, stream);
   };
   if (e.vocab_dim == 1) return of_chunk(std::integral_constant<int, kSums>{});
   return a.accumulate ? of_chunk(std::integral_constant<int, kAddedRows>{}) : of_chunk(std::integral_constant<int, kRows>{});

@@ -41,6 +41,9 @@ struct EmbedArgs {
 // Tokens of a chunk: few where there are few chunks, as a chunk's tokens wait for each other; more where there are many, as their sums are read again (us, 8 / 16: 2048 tokens of 2048 29.3 / 30.9,
 // 8192 of 1024 25.1 / 25.5, 32768 of 4096 172 / 159).
 constexpr int kSmallChunk = 8, kLargeChunk = 16, kFewTokens = 8192;
+// Up to so many tokens nothing is joined: a launch less, but a run of all of them is a chain of their loads (us, joined / alone, texts: 100 tokens of 832, 1152 entries 13.2 / 10.4, 512 13.1 / 16.1; beside
+// the 131 MB of 32000 entries of 2048, where the host is ahead, 100 tokens 26.6 / 28.1).
+constexpr int kAloneTokens = 128;
 
 typedef __attribute__((address_space(4))) const EmbedArgs embed_args;
 __device__ __forceinline__ embed_args* embed_arguments() { return first_kernel_argument<EmbedArgs>(); }
@@ -166,8 +169,9 @@ __device__ __forceinline__ void finish_row(const EmbedArgs& a, int entry, int at
 }
 
 // Chunks of the order: a wave (or a few lanes of one, with short rows) has a chunk and 16 bytes a lane of its tokens' rows, all on their way together (2048 tokens of 2048: 6.8 us, 9999 of 1001 9.3).
-// kSums: runs of several tokens are put by for embed_grad_columns_kernel, those of one it reads itself.
-template <typename T, int LINES, int TO, int CHUNK>
+// kSums: runs of several tokens are put by for embed_grad_columns_kernel, those of one it reads itself.  ALONE: of few tokens a run is added up by the chunk that it begins in, to its end, and there
+// is nothing to join.
+template <typename T, int LINES, int TO, int CHUNK, bool ALONE>
 __global__ __launch_bounds__(256) void embed_runs_kernel(const EmbedArgs a, int log_lanes, int log_across) {
   constexpr int n = Sixteen<T>::n;
   const int log = LINES == kWide ? 6 : log_lanes, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -179,43 +183,51 @@ __global__ __launch_bounds__(256) void embed_runs_kernel(const EmbedArgs a, int 
   GSPMD_GLOBAL const int32_t* const order = (GSPMD_GLOBAL const int32_t*)a.order;
   GSPMD_GLOBAL const int32_t* const entries = (GSPMD_GLOBAL const int32_t*)a.entries;
   const int at = line_at<LINES, T>(col, a.M);
-  int entry[CHUNK + 1];
-  u32x4_t v[CHUNK];
-#pragma unroll
-  for (int u = 0; u < CHUNK; ++u) {             // (places up to the chunk's end exist; those behind the last token hold anything)
-    const int token = of_row<LINES>(order[begin + u]);
-    entry[u] = of_row<LINES>(entries[begin + u]);
-    v[u] = load_line<LINES, T>(token_row<T>(a, begin + u < end ? token : 0), at, a.M);
-  }
-  entry[CHUNK] = begin + CHUNK < total ? of_row<LINES>(entries[begin + CHUNK]) : a.V;
-  bool open = begin > 0 && of_row<LINES>(entries[max(begin - 1, 0)]) == entry[0];          // the run began before the chunk
   int first = begin;                                                                       // the run's first place here
+  bool open = false;                                                                       // it began before the chunk
   float sum[n];
 #pragma unroll
   for (int e = 0; e < n; ++e) sum[e] = 0.f;
+#pragma unroll 1
+  for (int base = begin; base < total; base += CHUNK) {
+    int entry[CHUNK + 1];
+    u32x4_t v[CHUNK];
 #pragma unroll
-  for (int u = 0; u < CHUNK; ++u) {
-    const int place = begin + u;
-    if (place < end) {
-      float f[n];
-      Sixteen<T>::open(v[u], f);
+    for (int u = 0; u < CHUNK; ++u) {           // (places up to the chunk's end exist; those behind the last token hold anything)
+      const int token = of_row<LINES>(order[base + u]);
+      entry[u] = of_row<LINES>(entries[base + u]);
+      v[u] = load_line<LINES, T>(token_row<T>(a, base + u < total ? token : 0), at, a.M);
+    }
+    entry[CHUNK] = base + CHUNK < total ? of_row<LINES>(entries[base + CHUNK]) : a.V;
+    if (base == begin) open = begin > 0 && of_row<LINES>(entries[max(begin - 1, 0)]) == entry[0];
+    bool done = !ALONE;
 #pragma unroll
-      for (int e = 0; e < n; ++e) sum[e] += f[e];
-      const bool ends = place + 1 == total || entry[u + 1] != entry[u];
-      if (ends || place + 1 == end) {
-        const bool part = open || !ends;
-        if (part || TO == kSums) {
-          float* const to = open ? a.heads + static_cast<int64_t>(chunk) * a.M : part ? a.tails + static_cast<int64_t>(chunk) * a.M : a.sums + static_cast<int64_t>(first >> 1) * a.M;
-          if (part || first != place) store_sums<LINES, n>(to, at, a.M, sum);
-        } else {
-          finish_row<T, LINES, TO>(a, entry[u], at, sum);
+    for (int u = 0; u < CHUNK; ++u) {
+      const int place = base + u;
+      if (place < total && (!ALONE || !done)) {
+        float f[n];
+        Sixteen<T>::open(v[u], f);
+#pragma unroll
+        for (int e = 0; e < n; ++e) sum[e] += f[e];
+        const bool ends = place + 1 == total || entry[u + 1] != entry[u];
+        if (ends || (!ALONE && place + 1 == end)) {
+          const bool part = open || !ends;
+          if (ALONE && open) {                  // another chunk's
+          } else if (part || TO == kSums) {
+            float* const to = open ? a.heads + static_cast<int64_t>(chunk) * a.M : part ? a.tails + static_cast<int64_t>(chunk) * a.M : a.sums + static_cast<int64_t>(first >> 1) * a.M;
+            if (part || first != place) store_sums<LINES, n>(to, at, a.M, sum);
+          } else {
+            finish_row<T, LINES, TO>(a, entry[u], at, sum);
+          }
+          open = false;
+          first = place + 1;
+          done = !ALONE || first >= end;        // the next run begins in another chunk
+#pragma unroll
+          for (int e = 0; e < n; ++e) sum[e] = 0.f;
         }
-        open = false;
-        first = place + 1;
-#pragma unroll
-        for (int e = 0; e < n; ++e) sum[e] = 0.f;
       }
     }
+    if (done || open) break;                    // (open: all of the chunk belongs to a run of an earlier one)
   }
 }
 

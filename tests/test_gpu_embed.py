@@ -225,3 +225,14 @@ def test_a_scale_of_one_copies_any_bits(order, dtype):
     e.stage_lookup().lookup()
     got = e.yc.whole()[:64]
     assert torch.equal(got.view(w.dtype), w[e.ids])
+
+
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("ids", sorted(IDS))
+@pytest.mark.parametrize("T", [7, 8, 9, 15, 16, 17, 24, 33, 100, 127, 128, 136])
+def test_gradient_of_few_tokens(order, ids, T):
+    """Runs that are added up by the chunk they begin in, over several others, in rows of each kind."""
+    for M, kw in ((5, dict()), (40, dict(accumulate=True)), (515, dict(pad=False, scale=0.5)), (515, dict(accumulate=True, pad=False, shift=1)), (1024, dict(x=3, y=2))):
+        e = Embed(T, M, 29, order=order, ids=IDS[ids](T, 29) if IDS[ids] else None, seed=14, **kw).stage_gradient()
+        e.gradient()
+        e.check_gradient()
