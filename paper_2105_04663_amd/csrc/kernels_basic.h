@@ -65,6 +65,18 @@ __device__ __forceinline__ int find_problem(const Problem* __restrict__ tab, int
 constexpr int kInlineProblems = 32;
 constexpr int kInlineRects = 2 * kInlineProblems;
 struct InlineProblems { Problem p[kInlineProblems]; };
+// The table of a launch over experts' packed rows (ragged.h): its first entries.  Smaller, as what a launch costs the host goes by the arguments that it copies (us a call, 32 entries / 9: 6.6 / 6.3).
+constexpr int kRaggedParts = 8;
+struct RaggedParts { Problem p[kRaggedParts + 1]; };
+template <bool RAGGED> struct InlineTableOf { typedef InlineProblems type; };
+template <> struct InlineTableOf<true> { typedef RaggedParts type; };
+template <bool RAGGED> using inline_table = typename InlineTableOf<RAGGED>::type;
+static_assert(kRaggedParts < kInlineProblems, "the first of the other");
+// what a launch passes of it
+template <bool RAGGED> inline const inline_table<RAGGED>& table_of(const InlineProblems& inl) {
+  if constexpr (RAGGED) return reinterpret_cast<const RaggedParts&>(inl);
+  else return inl;
+}
 struct InlineRects { ZeroRect r[kInlineRects]; };
 
 // The kernel-argument segment, read in place: loads from it with a wave-uniform index are scalar loads.  (A by-value

@@ -40,7 +40,7 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 // LEAN: LDS for four workgroups on a compute unit (f32_four).  WIDE: rows beyond 32-bit offsets (512 MiB and more), a lane's offsets in 64 bits and one
 // addition per load.
 template <int LAYOUT, bool LEAN, bool WIDE = false, bool RAGGED = false>
-__global__ __launch_bounds__(kF32Threads, LEAN ? 4 : 3) void dot_f32_kernel(const InlineProblems inl, const Problem* __restrict__ tab, int n_prob, int epilogue) {
+__global__ __launch_bounds__(kF32Threads, LEAN ? 4 : 3) void dot_f32_kernel(const inline_table<RAGGED> inl, const Problem* __restrict__ tab, int n_prob, int epilogue) {
   constexpr bool AKM = (LAYOUT & GSPMD_LAYOUT_LHS_K_MAJOR) != 0, BKC = (LAYOUT & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) != 0;
   constexpr int R = f32_stages<LEAN>();
   __shared__ __attribute__((aligned(1024))) unsigned char lds[R * 2 * kF32Part];        // [stage][operand]

@@ -21,7 +21,7 @@ constexpr int kF32ExpertsRows = 16, kF32ExpertsCols = 64, kF32ExpertsStep = 16, 
 constexpr int64_t kF32ExpertsStride = 1 << 23;           // elements: a tile's rows stay within 32-bit offsets (of bytes)
 
 template <int LAYOUT>
-__global__ __launch_bounds__(256, 4) void dot_f32_experts_kernel(const InlineProblems inl, int n_prob, int epilogue) {
+__global__ __launch_bounds__(256, 4) void dot_f32_experts_kernel(const RaggedParts inl, int n_prob, int epilogue) {
   constexpr bool BKC = (LAYOUT & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) != 0;
   static_assert(!(LAYOUT & GSPMD_LAYOUT_LHS_K_MAJOR), "experts' rows");
   typedef GSPMD_GLOBAL const float* gfloats;

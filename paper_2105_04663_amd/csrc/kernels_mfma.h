@@ -89,7 +89,7 @@ constexpr int kMfmaCodeAlign = 16384;
 // `finish`: what becomes of a tile's accumulators instead of the epilogue, in a launch without joined problems.
 struct NoFinish {};
 template <typename TOut, int LAYOUT, bool STAGED, typename Finish, bool RAGGED = false>
-__global__ __attribute__((aligned(kMfmaCodeAlign))) __launch_bounds__(kMfmaThreads) void dot_mfma_kernel(const InlineProblems inl, const Problem* __restrict__ tab, int n_prob, int epilogue,
+__global__ __attribute__((aligned(kMfmaCodeAlign))) __launch_bounds__(kMfmaThreads) void dot_mfma_kernel(const inline_table<RAGGED> inl, const Problem* __restrict__ tab, int n_prob, int epilogue,
                                                                 float* __restrict__ join_partials, uint32_t* __restrict__ join_counters,
                                                                 unsigned long long* __restrict__ timeline, int timeline_records, const Finish finish) {
   constexpr bool AKM = (LAYOUT & GSPMD_LAYOUT_LHS_K_MAJOR) != 0, BKC = (LAYOUT & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) != 0;
@@ -757,7 +757,7 @@ inline bool launch_dot_mfma_as(const MfmaLaunch& l, hipStream_t stream) {
   });
   if (!ok[dev]) return false;
   const dim3 grid(static_cast<unsigned>(l.tiles)), block(kMfmaThreads);
-  hipLaunchKernelGGL((dot_mfma_kernel<TOut, LAYOUT, STAGED, NoFinish, RAGGED>), grid, block, kMfmaLds, stream, *l.inl, l.tab, l.n_prob, l.epilogue, l.join_partials,
+  hipLaunchKernelGGL((dot_mfma_kernel<TOut, LAYOUT, STAGED, NoFinish, RAGGED>), grid, block, kMfmaLds, stream, table_of<RAGGED>(*l.inl), l.tab, l.n_prob, l.epilogue, l.join_partials,
                      l.join_counters, l.timeline, l.timeline_records, NoFinish{});
   return hipGetLastError() == hipSuccess;
 }

@@ -47,7 +47,7 @@ constexpr int kMidUnroll = 5;                         // K steps after which the
 // RAGGED: where the table holds parts of experts whose rows only the device counts (ragged.h).
 template <typename TOut, int LAYOUT, bool CHAIN, int PER_CU, bool STAGED, bool RAGGED>
 __global__ __launch_bounds__(kMidThreads, CHAIN && PER_CU == 1 ? 1 : 2)   // (one: the sums' accumulators take the other half of the registers)
- void dot_mid_kernel(const InlineProblems inl, const Problem* __restrict__ tab, int n_prob, int epilogue) {
+ void dot_mid_kernel(const inline_table<RAGGED> inl, const Problem* __restrict__ tab, int n_prob, int epilogue) {
   constexpr bool AKM = (LAYOUT & GSPMD_LAYOUT_LHS_K_MAJOR) != 0, BKC = (LAYOUT & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) != 0;
   static_assert(!(STAGED && CHAIN) && (!STAGED || PER_CU == 2), "");
   constexpr int R = mid_stages<PER_CU>(), L = mid_ahead<PER_CU>();
@@ -477,7 +477,7 @@ inline bool launch_dot_mid_as(const MfmaLaunch& l, hipStream_t stream) {
                                   hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
   });
   if (!ok[dev]) return false;
-  hipLaunchKernelGGL((dot_mid_kernel<TOut, LAYOUT, CHAIN, PER_CU, STAGED, RAGGED>), dim3(static_cast<unsigned>(l.tiles)), dim3(kMidThreads), lds, stream, *l.inl, l.tab,
+  hipLaunchKernelGGL((dot_mid_kernel<TOut, LAYOUT, CHAIN, PER_CU, STAGED, RAGGED>), dim3(static_cast<unsigned>(l.tiles)), dim3(kMidThreads), lds, stream, table_of<RAGGED>(*l.inl), l.tab,
                      l.n_prob, !STAGED && sizeof(TOut) == 2 && l.past ? l.epilogue | kStorePast : l.epilogue);
   return hipGetLastError() == hipSuccess;
 }

@@ -40,7 +40,7 @@ constexpr int kPairLds = kPairStages * kPairStage;
 
 // PAST: bf16 outputs past all caches (pair_stores_past in gspmd.hip)
 template <typename TOut, int LAYOUT, bool PAST, bool RAGGED>
-__global__ __launch_bounds__(kPairThreads, 2) void dot_pair_kernel(const InlineProblems inl, const Problem* __restrict__ tab, int n_prob, int epilogue) {
+__global__ __launch_bounds__(kPairThreads, 2) void dot_pair_kernel(const inline_table<RAGGED> inl, const Problem* __restrict__ tab, int n_prob, int epilogue) {
   constexpr bool AKM = (LAYOUT & GSPMD_LAYOUT_LHS_K_MAJOR) != 0, BKC = (LAYOUT & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) != 0;
   constexpr int R = kPairStages, kLoads = 6;     // a wave's load instructions of a tile: four of the lhs's part, two of the rhs's
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -224,7 +224,7 @@ inline bool launch_dot_pair_as(const MfmaLaunch& l, hipStream_t stream) {
     ok[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&dot_pair_kernel<TOut, LAYOUT, PAST, RAGGED>), hipFuncAttributeMaxDynamicSharedMemorySize, kPairLds) == hipSuccess;
   });
   if (!ok[dev]) return false;
-  hipLaunchKernelGGL((dot_pair_kernel<TOut, LAYOUT, PAST, RAGGED>), dim3(static_cast<unsigned>(l.tiles)), dim3(kPairThreads), kPairLds, stream, *l.inl, l.tab, l.n_prob, l.epilogue);
+  hipLaunchKernelGGL((dot_pair_kernel<TOut, LAYOUT, PAST, RAGGED>), dim3(static_cast<unsigned>(l.tiles)), dim3(kPairThreads), kPairLds, stream, table_of<RAGGED>(*l.inl), l.tab, l.n_prob, l.epilogue);
   return hipGetLastError() == hipSuccess;
 }
 

@@ -70,7 +70,7 @@ template <int W> __device__ __forceinline__ int split_pair(int block, int krow) 
 }
 
 template <typename TOut, int LAYOUT, int RB, int CB, bool RAGGED>
-__global__ __launch_bounds__(kSplitThreads) void dot_split_kernel(const InlineProblems inl, const Problem* __restrict__ tab, int n_prob, int epilogue, int spread,
+__global__ __launch_bounds__(kSplitThreads) void dot_split_kernel(const inline_table<RAGGED> inl, const Problem* __restrict__ tab, int n_prob, int epilogue, int spread,
                                                                   unsigned long long* __restrict__ timeline, int timeline_records) {
   constexpr bool AKM = (LAYOUT & GSPMD_LAYOUT_LHS_K_MAJOR) != 0, BKC = (LAYOUT & GSPMD_LAYOUT_RHS_K_CONTIGUOUS) != 0;
   constexpr int BM = 16 * RB, BN = 16 * CB, D = split_depth<RB, CB>();
@@ -354,7 +354,7 @@ inline bool launch_dot_split_as(const MfmaLaunch& l, hipStream_t stream) {
                                   hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
   });
   if (!ok[dev]) return false;
-  hipLaunchKernelGGL((dot_split_kernel<TOut, LAYOUT, RB, CB, RAGGED>), dim3(static_cast<unsigned>(l.tiles)), dim3(kSplitThreads), lds, stream, *l.inl, l.tab,
+  hipLaunchKernelGGL((dot_split_kernel<TOut, LAYOUT, RB, CB, RAGGED>), dim3(static_cast<unsigned>(l.tiles)), dim3(kSplitThreads), lds, stream, table_of<RAGGED>(*l.inl), l.tab,
                      l.n_prob, l.epilogue, l.spread ? 1 : 0, l.timeline, l.timeline_records);
   return hipGetLastError() == hipSuccess;
 }

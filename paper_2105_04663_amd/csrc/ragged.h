@@ -35,7 +35,6 @@ struct RaggedSizes {           // of experts base .. base + 63, this lane's
 
 // The table in the kernel arguments holds up to kRaggedParts parts -- A, B, C of the first of the part's experts (of packed rows: of slot 0), the leading dimensions, the extents that
 // are the same for all experts, and join_first, join_count: the first expert and how many -- and in its last entry's place what is the same for all of them.
-constexpr int kRaggedParts = kInlineProblems - 1;
 struct RaggedRows {
   const int32_t* sizes;        // [experts], device
   int32_t experts, slots;      // slots at most kMostSlots

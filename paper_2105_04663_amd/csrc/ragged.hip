@@ -86,9 +86,9 @@ template <bool LEAN, bool WIDE>
 void launch_f32(const InlineProblems& inl, int n, unsigned tiles, int32_t layout, int32_t epilogue, hipStream_t stream) {
   const dim3 grid(tiles), block(kF32Threads);
   switch (layout) {
-    case 0: hipLaunchKernelGGL((dot_f32_kernel<0, LEAN, WIDE, true>), grid, block, 0, stream, inl, nullptr, n, epilogue); break;
-    case 1: hipLaunchKernelGGL((dot_f32_kernel<1, LEAN, WIDE, true>), grid, block, 0, stream, inl, nullptr, n, epilogue); break;
-    default: hipLaunchKernelGGL((dot_f32_kernel<2, LEAN, WIDE, true>), grid, block, 0, stream, inl, nullptr, n, epilogue);
+    case 0: hipLaunchKernelGGL((dot_f32_kernel<0, LEAN, WIDE, true>), grid, block, 0, stream, table_of<true>(inl), nullptr, n, epilogue); break;
+    case 1: hipLaunchKernelGGL((dot_f32_kernel<1, LEAN, WIDE, true>), grid, block, 0, stream, table_of<true>(inl), nullptr, n, epilogue); break;
+    default: hipLaunchKernelGGL((dot_f32_kernel<2, LEAN, WIDE, true>), grid, block, 0, stream, table_of<true>(inl), nullptr, n, epilogue);
   }
 }
 
@@ -157,8 +157,8 @@ int32_t launch_parts(const Ragged& g, std::vector<Problem>& parts, const int32_t
     case GSPMD_TESTING_PAIR: ok = by_layout([&](auto layout) { return launch_ragged_pair_layout<decltype(layout)::value>(l, out_dtype, stream); }); break;
     case GSPMD_TESTING_MFMA: ok = by_layout([&](auto layout) { return launch_ragged_mfma_layout<decltype(layout)::value>(l, out_dtype, stream); }); break;
     default:
-      if (few && g.layout == 0) hipLaunchKernelGGL((dot_f32_experts_kernel<0>), dim3(tiles), dim3(256), 0, stream, inl, n, epilogue);
-      else if (few) hipLaunchKernelGGL((dot_f32_experts_kernel<GSPMD_LAYOUT_RHS_K_CONTIGUOUS>), dim3(tiles), dim3(256), 0, stream, inl, n, epilogue);
+      if (few && g.layout == 0) hipLaunchKernelGGL((dot_f32_experts_kernel<0>), dim3(tiles), dim3(256), 0, stream, table_of<true>(inl), n, epilogue);
+      else if (few) hipLaunchKernelGGL((dot_f32_experts_kernel<GSPMD_LAYOUT_RHS_K_CONTIGUOUS>), dim3(tiles), dim3(256), 0, stream, table_of<true>(inl), n, epilogue);
       else if (c.f32_wide) launch_f32<false, true>(inl, n, tiles, g.layout, epilogue, stream);
       else if (c.f32_lean) launch_f32<true, false>(inl, n, tiles, g.layout, epilogue, stream);
       else launch_f32<false, false>(inl, n, tiles, g.layout, epilogue, stream);
