@@ -95,8 +95,19 @@ EmbedArgs arguments(const Embed& e, const Shards& s, float scale) {
   return a;
 }
 
-template <typename T>
-int32_t launch_embed(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
+// Launches with a table of as few shards as will do.
+template <typename Go>
+int32_t with_few_shards(const EmbedArgs& a, Go go) {
+  if (std::max(a.token_shards, a.vocab_shards) > kFewShards) return go(a);
+  EmbedArgsOf<kFewShards> few{};
+  static_cast<EmbedSizes&>(few) = a;
+  std::copy_n(a.tokens, kFewShards, few.tokens);
+  std::copy_n(a.vocab, kFewShards, few.vocab);
+  return go(few);
+}
+
+template <typename T, typename A>
+int32_t launch_embed(const A& a, int vocab_dim, hipStream_t stream) {
   const int64_t rows = static_cast<int64_t>(a.ts) * a.token_shards;
   constexpr int n = Sixteen<T>::n;
   if (vocab_dim == 0) {
@@ -107,20 +118,20 @@ int32_t launch_embed(const EmbedArgs& a, int vocab_dim, hipStream_t stream) {
     const dim3 grid(static_cast<unsigned>(groups));
     return by_lines(lines_of<T>(a.M), [&](auto lines) {
       constexpr int L = decltype(lines)::value;
-      if (a.scale == 1.f) hipLaunchKernelGGL((embed_rows_kernel<T, L, false>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
-      else hipLaunchKernelGGL((embed_rows_kernel<T, L, true>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
+      if (a.scale == 1.f) hipLaunchKernelGGL((embed_rows_kernel<T, L, false, A>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
+      else hipLaunchKernelGGL((embed_rows_kernel<T, L, true, A>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
     });
   }
   const int64_t token_blocks = (rows + kColumnTokens - 1) / kColumnTokens, col_blocks = (a.M + kColumnCols - 1) / kColumnCols;
   const int64_t groups = 8 * token_blocks * ((col_blocks + 7) / 8);
   if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL((embed_columns_kernel<T>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, stream, a, static_cast<int>(token_blocks), static_cast<int>(col_blocks));
+  hipLaunchKernelGGL((embed_columns_kernel<T, A>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, stream, a, static_cast<int>(token_blocks), static_cast<int>(col_blocks));
   return launched();
 }
 
 // Sums over the runs of the order: rows of dw [V, M], or what embed_grad_columns_kernel reads.
-template <typename T, int TO, int CHUNK, bool ALONE>
-int32_t launch_chunks(const EmbedArgs& a, hipStream_t stream) {
+template <typename T, int TO, int CHUNK, bool ALONE, typename A>
+int32_t launch_chunks(const A& a, hipStream_t stream) {
   constexpr int n = Sixteen<T>::n;
   const int64_t chunks = (static_cast<int64_t>(a.T) + CHUNK - 1) / CHUNK;
   const Lines lines = TO == kAddedRows && a.M % n != 0 ? kExact : lines_of<T>(a.M);        // (nothing may be added twice)
@@ -129,15 +140,15 @@ int32_t launch_chunks(const EmbedArgs& a, hipStream_t stream) {
   while (across < 2 && (static_cast<int64_t>(n) << (log + across)) < a.M) ++across;
   const int64_t piece = static_cast<int64_t>(n) << (log + across), units = int64_t(4) >> across << (6 - log);
   const dim3 grid(static_cast<unsigned>((chunks + units - 1) / units), static_cast<unsigned>((a.M + piece - 1) / piece));
-  const int32_t st = by_lines(lines, [&](auto l) { hipLaunchKernelGGL((embed_runs_kernel<T, decltype(l)::value, TO, CHUNK, ALONE>), grid, dim3(256), 0, stream, a, log, across); });
+  const int32_t st = by_lines(lines, [&](auto l) { hipLaunchKernelGGL((embed_runs_kernel<T, decltype(l)::value, TO, CHUNK, ALONE, A>), grid, dim3(256), 0, stream, a, log, across); });
   if (ALONE || st != GSPMD_OK || chunks < 2) return st;
   const dim3 joins(static_cast<unsigned>(chunks - 1), static_cast<unsigned>((a.M + 64 * n - 1) / (64 * n)));
-  if (lines == kExact) hipLaunchKernelGGL((embed_joins_kernel<T, kExact, TO, CHUNK>), joins, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((embed_joins_kernel<T, kWide, TO, CHUNK>), joins, dim3(256), 0, stream, a);
+  if (lines == kExact) hipLaunchKernelGGL((embed_joins_kernel<T, kExact, TO, CHUNK, A>), joins, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((embed_joins_kernel<T, kWide, TO, CHUNK, A>), joins, dim3(256), 0, stream, a);
   return launched();
 }
-template <typename T>
-int32_t launch_runs(const Embed& e, const EmbedArgs& a, hipStream_t stream) {
+template <typename T, typename A>
+int32_t launch_runs(const Embed& e, const A& a, hipStream_t stream) {
   auto of_chunk = [&](auto to) {
     constexpr int TO = decltype(to)::value;
     if (e.T <= kAloneTokens) return launch_chunks<T, TO, kSmallChunk, true>(a, stream);
@@ -147,19 +158,19 @@ int32_t launch_runs(const Embed& e, const EmbedArgs& a, hipStream_t stream) {
   return a.accumulate ? of_chunk(std::integral_constant<int, kAddedRows>{}) : of_chunk(std::integral_constant<int, kRows>{});
 }
 
-template <typename T>
-int32_t launch_turn(const EmbedArgs& a, hipStream_t stream) {
+template <typename T, typename A>
+int32_t launch_turn(const A& a, hipStream_t stream) {
   constexpr int n = Sixteen<T>::n, kRows = kTurnLanes * n;
   const int64_t across = (a.vs + kTurnEntries - 1) / kTurnEntries * static_cast<int64_t>(a.vocab_shards), tiles = across * ((a.M + kRows - 1) / kRows);
   if (tiles > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(tiles)), block(256);
   const int x = static_cast<int>(across);
   if (a.M < n) {
-    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, kExact, float>), grid, block, 0, stream, a, x);
-    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, kExact, T>), grid, block, 0, stream, a, x);
+    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, kExact, float, A>), grid, block, 0, stream, a, x);
+    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, kExact, T, A>), grid, block, 0, stream, a, x);
   } else {
-    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, kNarrow, float>), grid, block, 0, stream, a, x);
-    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, kNarrow, T>), grid, block, 0, stream, a, x);
+    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, kNarrow, float, A>), grid, block, 0, stream, a, x);
+    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, kNarrow, T, A>), grid, block, 0, stream, a, x);
   }
   return launched();
 }
@@ -200,9 +211,9 @@ int32_t gradient(const Embed& e, const Shards& s, EmbedArgs a, char* workspace, 
       zero.stride = a.ld_vocab * static_cast<int64_t>(sizeof(T) / 2);
     }
     if ((st = run_order(in, out, zero, stream)) != GSPMD_OK) return st;
-    if (e.T > 0 && (e.vocab_dim == 0 || in.count > 0) && (st = launch_runs<T>(e, a, stream)) != GSPMD_OK) return st;
+    if (e.T > 0 && (e.vocab_dim == 0 || in.count > 0) && (st = with_few_shards(a, [&](const auto& b) { return launch_runs<T>(e, b, stream); })) != GSPMD_OK) return st;
     in.count = 0;                               // (ordered, for the next replicas; columns' sums are there, too)
-    if (e.vocab_dim == 1 && (st = launch_turn<T>(a, stream)) != GSPMD_OK) return st;
+    if (e.vocab_dim == 1 && (st = with_few_shards(a, [&](const auto& b) { return launch_turn<T>(b, stream); })) != GSPMD_OK) return st;
   }
   return st;
 }
@@ -226,7 +237,9 @@ int32_t gspmd_embed(const gspmd_mesh* mesh, const int32_t* const* ids, const gsp
   EmbedArgs a = arguments(e, s, scale);
   for (const auto& level : s.rows.which) {
     for (int64_t i = 0; i < e.na; ++i) a.tokens[i].rows = level[static_cast<size_t>(i)];
-    st = y_shards[0].dtype == GSPMD_BF16 ? launch_embed<bf16_bits>(a, vocab_dim, static_cast<hipStream_t>(hip_stream)) : launch_embed<float>(a, vocab_dim, static_cast<hipStream_t>(hip_stream));
+    st = with_few_shards(a, [&](const auto& b) {
+      return y_shards[0].dtype == GSPMD_BF16 ? launch_embed<bf16_bits>(b, vocab_dim, static_cast<hipStream_t>(hip_stream)) : launch_embed<float>(b, vocab_dim, static_cast<hipStream_t>(hip_stream));
+    });
     if (st != GSPMD_OK) return st;
   }
   return GSPMD_OK;

@@ -17,16 +17,13 @@
 
 namespace gspmd {
 
-constexpr int kTokenShards = 64, kVocabShards = 64;
+constexpr int kTokenShards = 64, kVocabShards = 64, kFewShards = 8;
 
 struct TokenShard {
   const int32_t* ids;
   void* rows;                  // y or dy; null: none to be written
 };
-// The first thing in a kernel's arguments (its shards are read there with run-time indexes).
-struct EmbedArgs {
-  TokenShard tokens[kTokenShards];
-  void* vocab[kVocabShards];   // null: none to be written
+struct EmbedSizes {
   int32_t T, ts, token_shards; // tokens, of a shard, shards
   int32_t V, vs, vocab_shards;
   int32_t M, ld_rows;
@@ -38,6 +35,15 @@ struct EmbedArgs {
   const int32_t *order, *entries, *begins;
   float *heads, *tails, *sums;
 };
+// The first of a kernel's arguments (its shards are read there with run-time indexes).  A table of few shards where that is enough: what a launch costs the host goes by the arguments that it copies (us a
+// call, one token, 64 / 8: 6.7 / 6.3).
+template <int SHARDS>
+struct EmbedArgsOf : EmbedSizes {
+  TokenShard tokens[SHARDS];
+  void* vocab[SHARDS];         // null: none to be written
+};
+typedef EmbedArgsOf<kTokenShards> EmbedArgs;
+static_assert(kTokenShards == kVocabShards, "one size of table");
 // Tokens of a chunk: few where there are few chunks, as a chunk's tokens wait for each other; more where there are many, as their sums are read again (us, 8 / 16: 2048 tokens of 2048 29.3 / 30.9,
 // 8192 of 1024 25.1 / 25.5, 32768 of 4096 172 / 159).
 constexpr int kSmallChunk = 8, kLargeChunk = 16, kFewTokens = 8192;
@@ -45,28 +51,26 @@ constexpr int kSmallChunk = 8, kLargeChunk = 16, kFewTokens = 8192;
 // the 131 MB of 32000 entries of 2048, where the host is ahead, 100 tokens 26.6 / 28.1).
 constexpr int kAloneTokens = 128;
 
-typedef __attribute__((address_space(4))) const EmbedArgs embed_args;
-__device__ __forceinline__ embed_args* embed_arguments() { return first_kernel_argument<EmbedArgs>(); }
 // (one shard: no division)
 __device__ __forceinline__ int embed_shard(int i, int per, int shards) { return shards == 1 ? 0 : static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(per)); }
 
 // y from [V, M]: a wave has a piece of a row (or a few short rows), kEmbedUnroll x 16 bytes a lane (16384 tokens of 8192 from 32000 entries: 74 us, 268 MB written at 3.6 TB/s).
 constexpr int kEmbedUnroll = 4;
-template <typename T, int LINES, bool SCALED>
-__global__ __launch_bounds__(256) void embed_rows_kernel(const EmbedArgs a, int log_lanes, int pieces) {
+template <typename T, int LINES, bool SCALED, typename A>
+__global__ __launch_bounds__(256) void embed_rows_kernel(const A a, int log_lanes, int pieces) {
   constexpr int n = Sixteen<T>::n;
   const int log = LINES == kWide ? 6 : log_lanes, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = blockIdx.x / pieces, piece = blockIdx.x - group * pieces;              // (neighbouring pieces of rows together)
   const int row = of_row<LINES>(((group * 4 + wave) << (6 - log)) + (lane >> log));        // static rows of all shards, one after the other
   if (row >= a.ts * a.token_shards) return;
   const int shard = of_row<LINES>(embed_shard(row, a.ts, a.token_shards)), within = row - shard * a.ts;
-  const TokenShard to = {embed_arguments()->tokens[shard].ids, embed_arguments()->tokens[shard].rows};
+  const TokenShard to = {first_kernel_argument<A>()->tokens[shard].ids, first_kernel_argument<A>()->tokens[shard].rows};
   if (to.rows == nullptr) return;
   const int id = row < a.T ? of_row<LINES>(((GSPMD_GLOBAL const int32_t*)to.ids)[within]) : -1;
   const bool there = static_cast<uint32_t>(id) < static_cast<uint32_t>(a.V);
   T* const y = static_cast<T*>(to.rows) + static_cast<int64_t>(within) * a.ld_rows;
   const int of = there ? of_row<LINES>(embed_shard(id, a.vs, a.vocab_shards)) : 0;
-  const T* const w = static_cast<const T*>(embed_arguments()->vocab[of]) + (there ? static_cast<int64_t>(id - of * a.vs) * a.ld_vocab : 0);
+  const T* const w = static_cast<const T*>(first_kernel_argument<A>()->vocab[of]) + (there ? static_cast<int64_t>(id - of * a.vs) * a.ld_vocab : 0);
   const int col0 = (((piece * kEmbedUnroll) << log) + (lane & ((1 << log) - 1))) * n, step = n << log;
   u32x4_t v[kEmbedUnroll];
   if (there) {
@@ -94,8 +98,8 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(const EmbedArgs a, int 
 // has to be near is the row.  Workgroups of one XCD take the same 32 rows of w for all tokens, one after the other, out of its L2.  Bound by
 // one line a cycle from the caches for every lane (19870 tokens of 1792 from 5248 entries: 87 us).
 constexpr int kColumnTokens = 64, kColumnCols = 32;
-template <typename T>
-__global__ __launch_bounds__(256) void embed_columns_kernel(const EmbedArgs a, int token_blocks, int col_blocks) {
+template <typename T, typename A>
+__global__ __launch_bounds__(256) void embed_columns_kernel(const A a, int token_blocks, int col_blocks) {
   __shared__ float tile[kColumnTokens][kColumnCols + 1];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, block = xcd + 8 * (turn / token_blocks);
@@ -106,11 +110,11 @@ __global__ __launch_bounds__(256) void embed_columns_kernel(const EmbedArgs a, i
     int id = -1;
     if (row < a.T) {
       const int shard = embed_shard(row, a.ts, a.token_shards);
-      id = ((GSPMD_GLOBAL const int32_t*)embed_arguments()->tokens[shard].ids)[row - shard * a.ts];
+      id = ((GSPMD_GLOBAL const int32_t*)first_kernel_argument<A>()->tokens[shard].ids)[row - shard * a.ts];
     }
     const bool there = static_cast<uint32_t>(id) < static_cast<uint32_t>(a.V);
     const int of = there ? embed_shard(id, a.vs, a.vocab_shards) : 0;
-    GSPMD_GLOBAL const T* const w = (GSPMD_GLOBAL const T*)embed_arguments()->vocab[of] + (there ? id - of * a.vs : 0);
+    GSPMD_GLOBAL const T* const w = (GSPMD_GLOBAL const T*)first_kernel_argument<A>()->vocab[of] + (there ? id - of * a.vs : 0);
     float v[kColumnCols / 4];
 #pragma unroll
     for (int i = 0; i < kColumnCols / 4; ++i) {
@@ -130,7 +134,7 @@ __global__ __launch_bounds__(256) void embed_columns_kernel(const EmbedArgs a, i
     const int r = i / per_row, c = (i - r * per_row) * n, row = row0 + r, col = col0 + c;
     if (row >= rows || col >= a.M) continue;
     const int shard = embed_shard(row, a.ts, a.token_shards);
-    T* const y = static_cast<T*>(embed_arguments()->tokens[shard].rows);
+    T* const y = static_cast<T*>(first_kernel_argument<A>()->tokens[shard].rows);
     if (y == nullptr) continue;
     float f[n];
 #pragma unroll
@@ -141,20 +145,20 @@ __global__ __launch_bounds__(256) void embed_columns_kernel(const EmbedArgs a, i
 
 // ---- the gradient
 // dy's row of a token
-template <typename T>
-__device__ __forceinline__ const T* token_row(const EmbedArgs& a, int token) {
+template <typename T, typename A>
+__device__ __forceinline__ const T* token_row(const A& a, int token) {
   const int shard = embed_shard(token, a.ts, a.token_shards);
-  return static_cast<const T*>(embed_arguments()->tokens[shard].rows) + static_cast<int64_t>(token - shard * a.ts) * a.ld_rows;
+  return static_cast<const T*>(first_kernel_argument<A>()->tokens[shard].rows) + static_cast<int64_t>(token - shard * a.ts) * a.ld_rows;
 }
 
 enum RunsTo { kRows, kAddedRows, kSums };        // what becomes of a run's sum: dw's row [V, M], the same added to what is there, or it is put by for dw [M, V]
 
 // dw's row of an entry [V, M] from its sum.
-template <typename T, int LINES, int TO>
-__device__ __forceinline__ void finish_row(const EmbedArgs& a, int entry, int at, float (&sum)[Sixteen<T>::n]) {
+template <typename T, int LINES, int TO, typename A>
+__device__ __forceinline__ void finish_row(const A& a, int entry, int at, float (&sum)[Sixteen<T>::n]) {
   constexpr int n = Sixteen<T>::n;
   const int shard = of_row<LINES>(embed_shard(entry, a.vs, a.vocab_shards));
-  T* dw = static_cast<T*>(embed_arguments()->vocab[shard]);
+  T* dw = static_cast<T*>(first_kernel_argument<A>()->vocab[shard]);
   if (dw == nullptr) return;
   dw += static_cast<int64_t>(entry - shard * a.vs) * a.ld_vocab;
 #pragma unroll
@@ -171,8 +175,8 @@ __device__ __forceinline__ void finish_row(const EmbedArgs& a, int entry, int at
 // Chunks of the order: a wave (or a few lanes of one, with short rows) has a chunk and 16 bytes a lane of its tokens' rows, all on their way together (2048 tokens of 2048: 6.8 us, 9999 of 1001 9.3).
 // kSums: runs of several tokens are put by for embed_grad_columns_kernel, those of one it reads itself.  ALONE: of few tokens a run is added up by the chunk that it begins in, to its end, and there
 // is nothing to join.
-template <typename T, int LINES, int TO, int CHUNK, bool ALONE>
-__global__ __launch_bounds__(256) void embed_runs_kernel(const EmbedArgs a, int log_lanes, int log_across) {
+template <typename T, int LINES, int TO, int CHUNK, bool ALONE, typename A>
+__global__ __launch_bounds__(256) void embed_runs_kernel(const A a, int log_lanes, int log_across) {
   constexpr int n = Sixteen<T>::n;
   const int log = LINES == kWide ? 6 : log_lanes, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int across = 1 << log_across, units = (4 >> log_across) << (6 - log);              // waves along a row; chunks of a workgroup
@@ -233,8 +237,8 @@ __global__ __launch_bounds__(256) void embed_runs_kernel(const EmbedArgs a, int 
 
 // Runs of several chunks: a workgroup for the chunk that one begins in (blockIdx.x) and 64 x 16 bytes of the row (blockIdx.y), a wave every fourth of the chunks behind it.  (4 us where there are
 // hardly any, and the launch is all.)
-template <typename T, int LINES, int TO, int CHUNK>
-__global__ __launch_bounds__(256) void embed_joins_kernel(const EmbedArgs a) {
+template <typename T, int LINES, int TO, int CHUNK, typename A>
+__global__ __launch_bounds__(256) void embed_joins_kernel(const A a) {
   constexpr int n = Sixteen<T>::n, kAhead = 4;
   const int chunk = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   GSPMD_GLOBAL const int32_t* const entries = (GSPMD_GLOBAL const int32_t*)a.entries;
@@ -275,8 +279,8 @@ __global__ __launch_bounds__(256) void embed_joins_kernel(const EmbedArgs a) {
 // tokens'.  They turn in LDS, rounded but for what is still to be added to (TTile float).  Bound by waits, for where runs begin, their tokens and the rows (9999 tokens, 1001 x 32003: 22 us, 64 MB of
 // dw at 2.9 TB/s; 48 in all with neighbouring tiles on different XCDs, 44 with one).
 constexpr int kTurnEntries = 64, kTurnLanes = 16;
-template <typename T, int LINES, typename TTile>
-__global__ __launch_bounds__(256) void embed_grad_columns_kernel(const EmbedArgs a, int blocks_x) {
+template <typename T, int LINES, typename TTile, typename A>
+__global__ __launch_bounds__(256) void embed_grad_columns_kernel(const A a, int blocks_x) {
   constexpr int n = Sixteen<T>::n, kRows = kTurnLanes * n, side = 64 / kTurnLanes, kEach = kTurnEntries / (4 * side), kPitch = kTurnEntries + (sizeof(TTile) == 2 ? 2 : 1);
   __shared__ __attribute__((aligned(4))) TTile tile[n + kRows][kPitch];        // (n rows before the tile's: what the lane at the row's end has of its neighbours' may begin there)
   __shared__ int begins[kTurnEntries + 1];
@@ -286,7 +290,7 @@ __global__ __launch_bounds__(256) void embed_grad_columns_kernel(const EmbedArgs
   // entries of one shard: block_x counts blocks of every shard
   const int per_shard = (a.vs + kTurnEntries - 1) / kTurnEntries, shard = block_x / per_shard, c0 = (block_x - shard * per_shard) * kTurnEntries;
   const int row0 = shard * a.vs + c0, m0 = block_m * kRows, entries = min(kTurnEntries, a.vs - c0);
-  T* const dw = static_cast<T*>(embed_arguments()->vocab[shard]);
+  T* const dw = static_cast<T*>(first_kernel_argument<A>()->vocab[shard]);
   if (dw == nullptr) return;
   if (t <= kTurnEntries) begins[t] = a.T > 0 ? ((GSPMD_GLOBAL const int32_t*)a.begins)[min(row0 + t, a.V)] : 0;
   __syncthreads();

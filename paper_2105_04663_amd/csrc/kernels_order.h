@@ -20,20 +20,22 @@
 namespace gspmd {
 
 constexpr int kLeaders = 4;
+template <int SHARDS>
 struct OrderWork {
-  OrderKeys in;
+  OrderKeysOf<SHARDS> in;
   OrderOut out;
-  ZeroRows zero;
+  ZeroRowsOf<SHARDS> zero;
   int32_t log_range, groups;                    // of workgroups that order; those behind them zero rows
   int32_t zero_log, zero_pieces;                // lanes of a row, as a power of two; pieces of kZeroUnroll x 16 bytes a lane
 };
 
 // Rows zeroed, beside the order, whose time it hides (131 MB with the order of 2048 tokens 20 us, 6.5 TB/s): a workgroup has a piece of every so-many-th row, a wave one row (or a few short ones) at a time.
 constexpr int kZeroUnroll = 4;
-__device__ __forceinline__ void zero_rows(const OrderWork& w) {
+template <int SHARDS>
+__device__ __forceinline__ void zero_rows(const OrderWork<SHARDS>& w) {
   typedef bf16_bits half;
   constexpr int n = Sixteen<half>::n;
-  const ZeroRows& z = w.zero;
+  const ZeroRowsOf<SHARDS>& z = w.zero;
   const int block = blockIdx.x - w.groups, of = gridDim.x - w.groups, piece = block % w.zero_pieces, log = w.zero_log, side = 6 - log;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), count = z.per * z.shards - z.from;
   const int col0 = (((piece * kZeroUnroll) << log) + (lane & ((1 << log) - 1))) * n, turn = (of / w.zero_pieces * kOrderWaves) << side;
@@ -42,7 +44,7 @@ __device__ __forceinline__ void zero_rows(const OrderWork& w) {
     if (row - z.from >= count) break;
     int shard = z.shards == 1 ? 0 : static_cast<int>(static_cast<uint32_t>(row) / static_cast<uint32_t>(z.per));
     if (log == 6) shard = __builtin_amdgcn_readfirstlane(shard);
-    half* const to = static_cast<half*>(z.shards == 1 ? z.shard[0] : first_kernel_argument<OrderWork>()->zero.shard[shard]);
+    half* const to = static_cast<half*>(z.shards == 1 ? z.shard[0] : first_kernel_argument<OrderWork<SHARDS>>()->zero.shard[shard]);
     if (to == nullptr) continue;
     half* const at = to + static_cast<int64_t>(row - shard * z.per) * z.stride;
     const u32x4_t zeros = {0u, 0u, 0u, 0u};
@@ -57,19 +59,20 @@ __device__ __forceinline__ void zero_rows(const OrderWork& w) {
   }
 }
 
-__global__ __launch_bounds__(kOrderThreads) void order_kernel(const OrderWork w) {
+template <int SHARDS>
+__global__ __launch_bounds__(kOrderThreads) void order_kernel(const OrderWork<SHARDS> w) {
   extern __shared__ __attribute__((aligned(16))) int32_t counts[];      // [range][waves]
   __shared__ int32_t sums[kOrderWaves], below[kOrderWaves];
-  __shared__ const int32_t* from[kKeyShards];
+  __shared__ const int32_t* from[SHARDS];
   if (static_cast<int>(blockIdx.x) >= w.groups) {
     zero_rows(w);
     return;
   }
-  const OrderKeys& in = w.in;
+  const OrderKeysOf<SHARDS>& in = w.in;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), log_range = w.log_range, entries = kOrderWaves << log_range;
   const int lo = blockIdx.x << log_range, range = min(1 << log_range, in.keys - lo);
   const int part = ((in.count + kOrderWaves - 1) / kOrderWaves + 63) & ~63, first = min(wave * part, in.count), end = min(first + part, in.count);
-  if (in.shards > 1 && t < in.shards) from[t] = first_kernel_argument<OrderWork>()->in.shard[t];
+  if (in.shards > 1 && t < in.shards) from[t] = first_kernel_argument<OrderWork<SHARDS>>()->in.shard[t];
   for (int i = t; i < entries; i += kOrderThreads) counts[i] = 0;
   __syncthreads();
   constexpr int kAhead = 4;

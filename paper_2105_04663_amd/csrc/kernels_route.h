@@ -21,17 +21,22 @@ namespace gspmd {
 constexpr int kRouteLanes = 16, kMostExperts = GSPMD_MAX_EXPERTS, kMostChoices = GSPMD_MAX_CHOICES;
 static_assert(kMostChoices <= kRouteLanes, "a lane for every choice");
 
-struct RouteArgs {
-  struct Shard {
-    const void* logits;
-    void* dlogits;                 // null: none to be written
-  } shard[kTokenShards];           // (first in the kernel's arguments: read there)
+struct RouteSizes {
   int32_t T, ts, shards, E, k, ld, ld_d;
   int32_t normalise;
   int32_t* experts;                // [T][k]
   float* weights;                  // [T][k]
   const float* dweights;           // the gradient's
 };
+struct RouteShard {
+  const void* logits;
+  void* dlogits;                   // null: none to be written
+};
+template <int SHARDS>
+struct RouteArgsOf : RouteSizes {  // (the first of a kernel's arguments: shards are read there)
+  RouteShard shard[SHARDS];
+};
+typedef RouteArgsOf<kTokenShards> RouteArgs;
 
 // v combined over the sixteen lanes of a row, in all of them.  (Rotations: every lane adds in another order, but of max and of the two-by-two sums the bits are the same.)
 template <typename Op>
@@ -113,13 +118,13 @@ __device__ __forceinline__ int32_t row_most(int32_t v) {
 }
 
 // The sixteen lanes' choices: lane i of them has the i-th, its expert (-1: none) and weight.  `chosen`: LDS, a word for each lane of the wave.
-template <typename T, int R>
-__device__ __forceinline__ void route_choose(const RouteArgs& a, int token, int lane, int32_t* chosen, int* chosen_expert, float* weight) {
+template <typename T, int R, typename A>
+__device__ __forceinline__ void route_choose(const A& a, int token, int lane, int32_t* chosen, int* chosen_expert, float* weight) {
   const int of_row = lane & 15;
   const T* z = nullptr;
   if (token < a.T) {
     const int shard = embed_shard(token, a.ts, a.shards);
-    z = static_cast<const T*>(a.shards == 1 ? a.shard[0].logits : first_kernel_argument<RouteArgs>()->shard[shard].logits) + static_cast<int64_t>(token - shard * a.ts) * a.ld;
+    z = static_cast<const T*>(a.shards == 1 ? a.shard[0].logits : first_kernel_argument<A>()->shard[shard].logits) + static_cast<int64_t>(token - shard * a.ts) * a.ld;
   }
   float v[R];
   const bool strange = route_load<T, R>(z, a.E, of_row, lane, v);
@@ -166,8 +171,8 @@ __device__ __forceinline__ void route_choose(const RouteArgs& a, int token, int 
 
 // The choices of sixty-four tokens, and how many of them each expert has: counts [tile][E].  (With them a routing takes two launches; ordering the choices as order_kernel does takes three.)
 constexpr int kFewRouted = kOrderThreads / kRouteLanes, kTileTokens = kFewRouted;
-template <typename T, int R>
-__global__ __launch_bounds__(kOrderThreads) void route_kernel(const RouteArgs a, int32_t* counts) {
+template <typename T, int R, typename A>
+__global__ __launch_bounds__(kOrderThreads) void route_kernel(const A a, int32_t* counts) {
   __shared__ int32_t here[kMostExperts], chosen[kOrderThreads];
   const int t = threadIdx.x, lane = t & 63, of_row = lane & 15, token = blockIdx.x * kTileTokens + t / kRouteLanes;
   if (t < a.E) here[t] = 0;
@@ -313,8 +318,8 @@ __global__ __launch_bounds__(kOrderThreads) static void route_places_kernel(cons
 }
 
 // A routing of a few tokens, with its order, by one workgroup.
-template <typename T, int R>
-__global__ __launch_bounds__(kOrderThreads) void route_few_kernel(const RouteArgs a, int bits, int32_t* slots, int32_t* order, int32_t* sizes) {
+template <typename T, int R, typename A>
+__global__ __launch_bounds__(kOrderThreads) void route_few_kernel(const A a, int bits, int32_t* slots, int32_t* order, int32_t* sizes) {
   __shared__ uint16_t counts[kOrderWaves << kMostRange];
   __shared__ uint32_t keys[kOrderThreads], sums[kOrderWaves];
   __shared__ int32_t chosen[kOrderThreads];
@@ -339,15 +344,15 @@ __global__ __launch_bounds__(kOrderThreads) void route_few_kernel(const RouteArg
 }
 
 // dlogits: of weights from all experts p (g - sum p g), g zero where not chosen; from the chosen ones the same among them, zeros elsewhere.  What the choices add is put where their experts are in LDS.
-template <typename T, int R>
-__global__ __launch_bounds__(256) void route_grad_kernel(const RouteArgs a) {
+template <typename T, int R, typename A>
+__global__ __launch_bounds__(256) void route_grad_kernel(const A a) {
   __shared__ __attribute__((aligned(16))) float added[256 / kRouteLanes][kRouteLanes * R];
   const int lane = threadIdx.x & 63, of_row = lane & 15, token = (blockIdx.x * 256 + threadIdx.x) / kRouteLanes;
   float* const add = added[threadIdx.x / kRouteLanes];
   const bool in = token < a.ts * a.shards, live = token < a.T;
   const int shard = in ? embed_shard(token, a.ts, a.shards) : 0, within = token - shard * a.ts;
-  const T* z = live && !a.normalise ? static_cast<const T*>(first_kernel_argument<RouteArgs>()->shard[shard].logits) + static_cast<int64_t>(within) * a.ld : nullptr;
-  T* const d = in ? static_cast<T*>(first_kernel_argument<RouteArgs>()->shard[shard].dlogits) : nullptr;
+  const T* z = live && !a.normalise ? static_cast<const T*>(first_kernel_argument<A>()->shard[shard].logits) + static_cast<int64_t>(within) * a.ld : nullptr;
+  T* const d = in ? static_cast<T*>(first_kernel_argument<A>()->shard[shard].dlogits) : nullptr;
   const int64_t at = static_cast<int64_t>(token) * a.k + of_row;
   const bool mine = live && of_row < a.k;
   const int expert = mine ? a.experts[at] : -1;

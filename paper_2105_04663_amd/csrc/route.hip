@@ -99,6 +99,24 @@ RouteArgs arguments(const Route& r, const Replicas& logits, int64_t ld, const gs
   return a;
 }
 
+// Launches with a table of as few shards as will do (kernels_embed.h).
+template <typename Go>
+int32_t with_few_shards(const RouteArgs& a, Go go) {
+  if (a.shards > kFewShards) return go(a);
+  RouteArgsOf<kFewShards> few{};
+  static_cast<RouteSizes&>(few) = a;
+  std::copy_n(a.shard, kFewShards, few.shard);
+  return go(few);
+}
+// go(a lane's experts, the arguments): launches.
+template <typename Go>
+int32_t launch_route(int64_t E, const RouteArgs& a, Go go) {
+  return with_few_shards(a, [&](const auto& b) {
+    by_experts(E, [&](auto each) { go(each, b); });
+    return launched();
+  });
+}
+
 dim3 token_grid(int64_t tokens) { return dim3(static_cast<unsigned>((tokens * kRouteLanes + 255) / 256)); }
 
 // ---- the exchange
@@ -164,10 +182,10 @@ void one_buffer(ExchangeArgs* a, bool with_drows) {
   if (one) a->expert_shards = 1;
 }
 
+static_assert(kTokenShards == kExpertShards, "one kind of table");
 void set(void* (&table)[kTokenShards], const std::vector<void*>& level) {
   for (size_t i = 0; i < level.size(); ++i) table[i] = level[i];
 }
-static_assert(kTokenShards == kExpertShards, "one kind of table");
 
 enum Exchanged { kDispatch, kCombine, kCombineGrad };
 template <typename T>
@@ -227,21 +245,22 @@ int32_t gspmd_route(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_shards
   int bits = 1;
   while ((int64_t(1) << bits) <= r.E) ++bits;               // of the numbers 0 .. E
   if (r.few()) {
-    by_experts(r.E, [&](auto each) {
+    return launch_route(r.E, a, [&](auto each, const auto& b) {
       constexpr int R = decltype(each)::value;
-      if (dtype == GSPMD_BF16) hipLaunchKernelGGL((route_few_kernel<bf16_bits, R>), dim3(1), dim3(kOrderThreads), 0, stream, a, bits, route->slots, route->order, route->sizes);
-      else hipLaunchKernelGGL((route_few_kernel<float, R>), dim3(1), dim3(kOrderThreads), 0, stream, a, bits, route->slots, route->order, route->sizes);
+      typedef std::decay_t<decltype(b)> A;
+      if (dtype == GSPMD_BF16) hipLaunchKernelGGL((route_few_kernel<bf16_bits, R, A>), dim3(1), dim3(kOrderThreads), 0, stream, b, bits, route->slots, route->order, route->sizes);
+      else hipLaunchKernelGGL((route_few_kernel<float, R, A>), dim3(1), dim3(kOrderThreads), 0, stream, b, bits, route->slots, route->order, route->sizes);
     });
-    return launched();
   }
   int32_t* const counts = static_cast<int32_t*>(workspace);
   const unsigned tiles = static_cast<unsigned>(r.tiles());
-  by_experts(r.E, [&](auto each) {
+  st = launch_route(r.E, a, [&](auto each, const auto& b) {
     constexpr int R = decltype(each)::value;
-    if (dtype == GSPMD_BF16) hipLaunchKernelGGL((route_kernel<bf16_bits, R>), dim3(tiles), dim3(kOrderThreads), 0, stream, a, counts);
-    else hipLaunchKernelGGL((route_kernel<float, R>), dim3(tiles), dim3(kOrderThreads), 0, stream, a, counts);
+    typedef std::decay_t<decltype(b)> A;
+    if (dtype == GSPMD_BF16) hipLaunchKernelGGL((route_kernel<bf16_bits, R, A>), dim3(tiles), dim3(kOrderThreads), 0, stream, b, counts);
+    else hipLaunchKernelGGL((route_kernel<float, R, A>), dim3(tiles), dim3(kOrderThreads), 0, stream, b, counts);
   });
-  if ((st = launched()) != GSPMD_OK) return st;
+  if (st != GSPMD_OK) return st;
   int32_t* totals = nullptr;
   if (tiles > kTilesSummed) {
     totals = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + r.counts_bytes());
@@ -274,12 +293,13 @@ int32_t gspmd_route_grad(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_s
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   for (const auto& level : dlogits.which) {
     for (int64_t i = 0; i < r.na; ++i) a.shard[i].dlogits = level[static_cast<size_t>(i)];
-    by_experts(r.E, [&](auto each) {
+    st = launch_route(r.E, a, [&](auto each, const auto& b) {
       constexpr int R = decltype(each)::value;
-      if (dtype == GSPMD_BF16) hipLaunchKernelGGL((route_grad_kernel<bf16_bits, R>), token_grid(r.ts * r.na), dim3(256), 0, stream, a);
-      else hipLaunchKernelGGL((route_grad_kernel<float, R>), token_grid(r.ts * r.na), dim3(256), 0, stream, a);
+      typedef std::decay_t<decltype(b)> A;
+      if (dtype == GSPMD_BF16) hipLaunchKernelGGL((route_grad_kernel<bf16_bits, R, A>), token_grid(r.ts * r.na), dim3(256), 0, stream, b);
+      else hipLaunchKernelGGL((route_grad_kernel<float, R, A>), token_grid(r.ts * r.na), dim3(256), 0, stream, b);
     });
-    if ((st = launched()) != GSPMD_OK) return st;
+    if (st != GSPMD_OK) return st;
   }
   return GSPMD_OK;
 } catch (...) { return GSPMD_ERR_HOST_MEMORY; }

@@ -341,3 +341,15 @@ def test_the_same_through_ctypes(monkeypatch):
     e.check_lookup()
     e.gradient()
     e.check_gradient()
+
+
+@pytest.mark.parametrize("T, x", [(70, 8), (70, 9), (300, 64), (10, 64)])
+def test_route_over_many_shards(T, x):
+    """Tables of few shards and of many; shards that lie behind the last token."""
+    r = Routed(T, 40, 3, x=x, seed=25).stage()
+    r.call()
+    r.check()
+    dw = torch.randn(T, 3, generator=torch.Generator().manual_seed(26))
+    d, given = Cut(torch.full((T, 40), KEPT), x, fill=KEPT), dw.cuda()
+    g.route_grad(r.mesh, r.z_bufs, r.sh, 3, r.buf, given.data_ptr(), [d.buf(i) for i, _ in r.places], stream=stream())
+    r.check_gradient(dw, d)
