@@ -87,3 +87,39 @@ def test_exchange_and_products():
     for e in range(E):
         for a, b in (((ends[e - 1] if e else 0), (ends[e - 1] if e else 0) + 300), (ends[e] - 300, ends[e])):
             assert torch.equal(out[a:b], rows[a:b].float() @ w[e].float())                          # whole numbers below 2^24
+
+
+def test_as_many_choices_as_there_may_be():
+    """2^24 tokens with a choice each: the routing's order, and the gradient of an embedding of as many."""
+    T, E = 1 << 24, 6
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    logits = torch.randint(-4, 5, (T, E), generator=gen, device="cuda").float()
+    logits[5::1001] = -float("inf")
+    ints = lambda *s: torch.full(s, -7, dtype=torch.int32, device="cuda")
+    experts, slots, order, sizes, weights = ints(T, 1), ints(T, 1), ints(T), ints(E), torch.zeros(T, 1, device="cuda")
+    buf = g.RouteBuf(experts.data_ptr(), weights.data_ptr(), slots.data_ptr(), order.data_ptr(), sizes.data_ptr())
+    sh = g.Sharding((T, E), (-1, -1))
+    n = g.route_workspace_bytes(ONE, sh, 1)
+    keep, at = space(n)
+    g.route(ONE, [g.ShardBuf.of(logits, E)], sh, 1, buf, normalise=True, workspace=at, workspace_bytes=n, stream=stream())
+    most, there = logits.amax(dim=1), logits[:, 0] != -float("inf")
+    want = torch.where(there, (logits == most[:, None]).int().argmax(dim=1), torch.full((T,), E, device="cuda"))
+    assert torch.equal(experts[:, 0].long(), torch.where(there, want, torch.full_like(want, -1)))
+    by_expert = torch.argsort(want, stable=True)
+    total = int(there.sum())
+    assert torch.equal(order[:total].long(), by_expert[:total]) and (order[total:] == -1).all()
+    assert torch.equal(sizes.long(), torch.bincount(want, minlength=E + 1)[:E])
+    assert torch.equal(slots[by_expert[:total], 0].long(), torch.arange(total, device="cuda")) and (slots[~there] == -1).all()
+    assert (weights[there] == 1).all() and (weights[~there] == 0).all()
+    del by_expert, want, logits
+    V, M = 50, 2
+    ids = torch.randint(-1, V + 1, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    dy = torch.ones(T, M, device="cuda")
+    dy[:, 1] = -0.5
+    dw = torch.full((V, M), KEPT, device="cuda")
+    rows_sh, w_sh = g.Sharding((T, M), (-1, -1)), g.Sharding((V, M), (-1, -1))
+    n = g.embed_grad_workspace_bytes(ONE, rows_sh, w_sh, 0, g.F32)
+    keep, at = space(n)
+    g.embed_grad(ONE, [ids.data_ptr()], [g.ShardBuf.of(dy, M)], rows_sh, [g.ShardBuf.of(dw, M)], w_sh, workspace=at, workspace_bytes=n, stream=stream())
+    count = torch.bincount(ids[(ids >= 0) & (ids < V)].long(), minlength=V).float()
+    assert torch.equal(dw[:, 0], count) and torch.equal(dw[:, 1], -0.5 * count)                      # whole numbers below 2^24
