@@ -463,7 +463,7 @@ int32_t gspmd_route_grad(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_s
 /* Between tokens' rows [T, M] (dimension 0 split or whole) and experts' packed rows, a tensor [E, S, M] held as gspmd_ragged_dot holds it (dimension 0 split or whole, S at least T k): the AllToAlls around
  * the experts.  Arrays of `route` that a call names have to be there, others may be NULL; values that are no slot or choice count as none, and so
  * do those that are no expert where experts tell buffers apart (partitions that all share one buffer of rows need none).  One type, bf16 or f32; sums in fp32.
- *   gspmd_dispatch      rows[s, :] = x[token of s, :]                        reads order, experts; its gradient is gspmd_combine of the rows' gradient, not weighted
+ *   gspmd_dispatch      rows[slot, :] = x[t, :] for t's choices              reads slots, experts; its gradient is gspmd_combine of the rows' gradient, not weighted
  *   gspmd_combine       y[t, :] = sum over t's choices of weight * rows[slot, :], in their order; not `weighted`: weights of 1.  Reads slots, experts, weights
  *   gspmd_combine_grad  drows[slot, :] = weight * dy[t, :], dweights[t, i] = sum over M of dy[t, :] rows[slot, :] (0 where there is no slot)     reads slots, experts, weights
  * A partition's rows are those of its own experts, in their places: others, and those behind the last slot, are left as they were and never read.  The rows of y's padding are zeros.

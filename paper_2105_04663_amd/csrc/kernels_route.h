@@ -4,7 +4,8 @@
 // within their row of the wave, and of those that have it the lowest lane, whose experts are the lowest.  It is bound by those instructions, some 20 + 3 R a choice, not by the logits (16384 tokens of 128 experts, 8 chosen: 8.4 us,
 // of which the 8.4 MB would take 2).  Logits are compared as whole numbers: a maximum of floats is two instructions where a NaN may be about.
 // Exchange: bound by memory, rows copied or added up 16 bytes a lane.  Every row has one writer (or two with the same bits, kernels_rows.h); a token's rows are added in the order of its choices.
-// 8192 tokens of 4096, 4 choices: combine_kernel 79 us (336 MB, 4.2 TB/s), combine_grad_kernel 109 (604 MB, 5.5 TB/s); 2048 of 2048, 2 choices: dispatch_kernel 10.3, combine_kernel 6.6.
+// 8192 tokens of 4096, 4 choices: combine_kernel 79 us (336 MB, 4.2 TB/s), combine_grad_kernel 109 (604 MB, 5.5 TB/s); 2048 of 2048, 2 choices: dispatch_kernel 10.0,
+// combine_kernel 6.1.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -421,7 +422,7 @@ struct ExchangeArgs {
   void* drows[kExpertShards];
   int32_t T, ts, token_shards, k, E, es, expert_shards, M;
   int64_t ld_tokens, ld_rows, ld_drows;
-  const int32_t *experts, *slots, *order;
+  const int32_t *experts, *slots;
   const float* weights;            // null: all 1
   float* dweights;
 };
@@ -437,31 +438,47 @@ __device__ __forceinline__ int expert_shard(const ExchangeArgs& a, int o) {
   return e < static_cast<uint32_t>(a.E) ? static_cast<int>(e / static_cast<uint32_t>(a.es)) : -1;
 }
 
-// rows[slot] = x[token of the slot]: a wave has a piece of a row, or a few short rows.
+// rows[slot] = x[token of the slot]: a wave has a piece of a token's row, or a few tokens' short rows, which it reads once and writes to each of their slots.  (Slot by slot, a row read
+// for each of them: 16384 tokens of 1024, 8 choices, with combine_kernel 127 us, so 113.)
 constexpr int kExchangeUnroll = 4;
 template <typename T, int LINES>
 __global__ __launch_bounds__(256) void dispatch_kernel(const ExchangeArgs a, int log_lanes, int pieces) {
   constexpr int n = Sixteen<T>::n;
   const int log = LINES == kWide ? 6 : log_lanes, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = blockIdx.x / pieces, piece = blockIdx.x - group * pieces;       // (neighbouring pieces of rows together)
-  const int slot = of_row<LINES>(((group * 4 + wave) << (6 - log)) + (lane >> log));
-  if (slot >= a.T * a.k) return;
-  const int o = of_row<LINES>(((GSPMD_GLOBAL const int32_t*)a.order)[slot]);
-  if (static_cast<uint32_t>(o) >= static_cast<uint32_t>(a.T * a.k)) return;
-  const int part = of_row<LINES>(expert_shard(a, o));
-  if (part < 0) return;
-  T* to = static_cast<T*>(rows_of(a, part));
-  if (to == nullptr) return;
-  const int token = of_row<LINES>(static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(a.k))), shard = of_row<LINES>(embed_shard(token, a.ts, a.token_shards));
+  const int token = of_row<LINES>(((group * 4 + wave) << (6 - log)) + (lane >> log));
+  if (token >= a.T) return;
+  const int shard = of_row<LINES>(embed_shard(token, a.ts, a.token_shards));
   const T* const x = static_cast<const T*>(tokens_of(a, shard)) + (token - shard * a.ts) * a.ld_tokens;
-  to += slot * a.ld_rows;
   const int col0 = (((piece * kExchangeUnroll) << log) + (lane & ((1 << log) - 1))) * n, step = n << log;
+  // its slot, or -1, and where that lies
+  auto slot_of = [&](int o, int* part) {
+    const int slot = ((GSPMD_GLOBAL const int32_t*)a.slots)[o];
+    *part = expert_shard(a, o);
+    return static_cast<uint32_t>(slot) < static_cast<uint32_t>(a.T * a.k) && *part >= 0 ? slot : -1;
+  };
+  int part = 0;
+  static_assert(kMostChoices <= 64, "a lane for every choice");
+  const int slots = LINES == kWide ? slot_of(token * a.k + min(lane, a.k - 1), &part) : 0, parts = part;      // (of a wave's one token: a choice a lane)
   u32x4_t v[kExchangeUnroll];
 #pragma unroll
   for (int u = 0; u < kExchangeUnroll; ++u) v[u] = load_line<LINES, T>(x, line_at<LINES, T>(col0 + u * step, a.M), a.M);
+  for (int i = 0; i < a.k; ++i) {
+    int slot;
+    if constexpr (LINES == kWide) {
+      slot = __builtin_amdgcn_readlane(slots, i);
+      part = __builtin_amdgcn_readlane(parts, i);
+    } else {
+      slot = slot_of(token * a.k + i, &part);
+    }
+    if (slot < 0) continue;
+    T* to = static_cast<T*>(rows_of(a, part));
+    if (to == nullptr) continue;
+    to += slot * a.ld_rows;
 #pragma unroll
-  for (int u = 0; u < kExchangeUnroll; ++u)
-    if (col0 + u * step < a.M) store_line<LINES, T>(to, line_at<LINES, T>(col0 + u * step, a.M), a.M, v[u]);
+    for (int u = 0; u < kExchangeUnroll; ++u)
+      if (col0 + u * step < a.M) store_line<LINES, T>(to, line_at<LINES, T>(col0 + u * step, a.M), a.M, v[u]);
+  }
 }
 
 // y[t] = sum over t's choices of weight * rows[slot], in float32, in their order; what has no slot adds nothing.

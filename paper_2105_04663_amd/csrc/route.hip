@@ -171,7 +171,6 @@ ExchangeArgs arguments(const Exchange& g, const gspmd_route_buf& b) {
   a.M = static_cast<int32_t>(g.M);
   a.experts = b.experts;
   a.slots = b.slots;
-  a.order = b.order;
   return a;
 }
 
@@ -192,7 +191,7 @@ template <typename T>
 int32_t launch_exchange(Exchanged what, const ExchangeArgs& a, hipStream_t stream) {
   constexpr int n = Sixteen<T>::n;
   const int log = row_lanes_log(a.M, n);
-  const int64_t side = int64_t(4) << (6 - log), rows = what == kCombine ? static_cast<int64_t>(a.ts) * a.token_shards : static_cast<int64_t>(a.T) * a.k;
+  const int64_t side = int64_t(4) << (6 - log), rows = what == kCombine ? static_cast<int64_t>(a.ts) * a.token_shards : what == kDispatch ? a.T : static_cast<int64_t>(a.T) * a.k;
   const int64_t piece = (static_cast<int64_t>(n) << log) * (what == kDispatch ? kExchangeUnroll : kCombineUnroll);
   const int64_t pieces = what == kCombineGrad ? 1 : (a.M + piece - 1) / piece, groups = (rows + side - 1) / side * pieces;
   if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
@@ -310,7 +309,7 @@ int32_t gspmd_dispatch(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, 
   Exchange g;
   int32_t st = analyse_exchange(mesh, x_sh, rows_sh, choices, &g);
   if (st != GSPMD_OK) return st;
-  if ((st = check_route(route, kExperts | kOrder, g.T > 0)) != GSPMD_OK) return st;
+  if ((st = check_route(route, kExperts | kSlots, g.T > 0)) != GSPMD_OK) return st;
   Replicas x(g.na), rows(g.nb);
   int64_t ld_x = -1, ld_rows = -1;
   const int32_t dtype = x_shards[0].dtype;

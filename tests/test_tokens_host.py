@@ -146,7 +146,7 @@ def test_exchange_refusals(which):
             assert status(call, ok, **{name: ok[name][:3] + [wrong]}) == expect, (name, wrong)
         with pytest.raises(ValueError):
             call(**{**ok, name: ok[name][:3]})
-    needed = {"dispatch": (0, 3), "combine": (0, 1, 2), "combine_grad": (0, 1, 2)}[which]
+    needed = {"dispatch": (0, 2), "combine": (0, 1, 2), "combine_grad": (0, 1, 2)}[which]
     fields = [(1 << 21) + 64 * j for j in range(5)]
     for i in range(5):
         assert status(call, ok, route=g.RouteBuf(*(fields[:i] + [0] + fields[i + 1:]))) == (NULL if i in needed else 0), i
