@@ -25,6 +25,7 @@ struct Embed {
   int64_t order_bytes() const { return round_up(chunks() * chunk() * 4, kWsAlign); }
   int64_t begins_bytes() const { return round_up((V + 1) * 4, kWsAlign); }
   int64_t chunks_bytes() const { return round_up(chunks() * M * 4, kWsAlign); }
+  bool columns_alone() const { return vocab_dim == 1 && T <= kAloneTokens; }        // (embed_grad_columns_kernel adds runs up itself)
   int64_t sums_bytes() const { return vocab_dim == 1 ? round_up(T / 2 * M * 4, kWsAlign) : 0; }
   int64_t bytes() const { return T == 0 ? 0 : 2 * order_bytes() + begins_bytes() + 2 * chunks_bytes() + sums_bytes(); }
 };
@@ -151,7 +152,8 @@ template <typename T, typename A>
 int32_t launch_runs(const Embed& e, const A& a, hipStream_t stream) {
   auto of_chunk = [&](auto to) {
     constexpr int TO = decltype(to)::value;
-    if (e.T <= kAloneTokens) return launch_chunks<T, TO, kSmallChunk, true>(a, stream);
+    if constexpr (TO != kSums)
+      if (e.T <= kAloneTokens) return launch_chunks<T, TO, kSmallChunk, true>(a, stream);
     return e.chunk() == kSmallChunk ? launch_chunks<T, TO, kSmallChunk, false>(a, stream) : launch_chunks<T, TO, kLargeChunk, false>(a, stream);
   };
   if (e.vocab_dim == 1) return of_chunk(std::integral_constant<int, kSums>{});
@@ -159,20 +161,22 @@ int32_t launch_runs(const Embed& e, const A& a, hipStream_t stream) {
 }
 
 template <typename T, typename A>
-int32_t launch_turn(const A& a, hipStream_t stream) {
+int32_t launch_turn(const Embed& e, const A& a, hipStream_t stream) {
   constexpr int n = Sixteen<T>::n, kRows = kTurnLanes * n;
   const int64_t across = (a.vs + kTurnEntries - 1) / kTurnEntries * static_cast<int64_t>(a.vocab_shards), tiles = across * ((a.M + kRows - 1) / kRows);
   if (tiles > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(tiles)), block(256);
   const int x = static_cast<int>(across);
-  if (a.M < n) {
-    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, kExact, float, A>), grid, block, 0, stream, a, x);
-    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, kExact, T, A>), grid, block, 0, stream, a, x);
-  } else {
-    if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, kNarrow, float, A>), grid, block, 0, stream, a, x);
-    else hipLaunchKernelGGL((embed_grad_columns_kernel<T, kNarrow, T, A>), grid, block, 0, stream, a, x);
-  }
-  return launched();
+  return by_lines(a.M < n ? kExact : kNarrow, [&](auto lines) {
+    constexpr int L = decltype(lines)::value == kExact ? kExact : kNarrow;
+    if (e.columns_alone()) {
+      if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, L, float, true, A>), grid, block, 0, stream, a, x);
+      else hipLaunchKernelGGL((embed_grad_columns_kernel<T, L, T, true, A>), grid, block, 0, stream, a, x);
+    } else {
+      if (a.accumulate) hipLaunchKernelGGL((embed_grad_columns_kernel<T, L, float, false, A>), grid, block, 0, stream, a, x);
+      else hipLaunchKernelGGL((embed_grad_columns_kernel<T, L, T, false, A>), grid, block, 0, stream, a, x);
+    }
+  });
 }
 
 // The gradient: the tokens' order and zeros, the runs' sums, dw's columns.
@@ -189,7 +193,7 @@ int32_t gradient(const Embed& e, const Shards& s, EmbedArgs a, char* workspace, 
     out.begins = reinterpret_cast<int32_t*>(take(e.begins_bytes()));
     a.heads = reinterpret_cast<float*>(take(e.chunks_bytes()));
     a.tails = reinterpret_cast<float*>(take(e.chunks_bytes()));
-    a.sums = reinterpret_cast<float*>(take(e.sums_bytes()));
+    a.sums = e.columns_alone() ? nullptr : reinterpret_cast<float*>(take(e.sums_bytes()));
     a.order = out.order;
     a.entries = out.entries;
     a.begins = out.begins;
@@ -211,9 +215,9 @@ int32_t gradient(const Embed& e, const Shards& s, EmbedArgs a, char* workspace, 
       zero.stride = a.ld_vocab * static_cast<int64_t>(sizeof(T) / 2);
     }
     if ((st = run_order(in, out, zero, stream)) != GSPMD_OK) return st;
-    if (e.T > 0 && (e.vocab_dim == 0 || in.count > 0) && (st = with_few_shards(a, [&](const auto& b) { return launch_runs<T>(e, b, stream); })) != GSPMD_OK) return st;
+    if (e.T > 0 && !e.columns_alone() && (e.vocab_dim == 0 || in.count > 0) && (st = with_few_shards(a, [&](const auto& b) { return launch_runs<T>(e, b, stream); })) != GSPMD_OK) return st;
     in.count = 0;                               // (ordered, for the next replicas; columns' sums are there, too)
-    if (e.vocab_dim == 1 && (st = with_few_shards(a, [&](const auto& b) { return launch_turn<T>(b, stream); })) != GSPMD_OK) return st;
+    if (e.vocab_dim == 1 && (st = with_few_shards(a, [&](const auto& b) { return launch_turn<T>(e, b, stream); })) != GSPMD_OK) return st;
   }
   return st;
 }

@@ -275,11 +275,31 @@ __global__ __launch_bounds__(256) void embed_joins_kernel(const A a) {
   else finish_row<T, LINES, TO>(a, entry, at, sum);
 }
 
+// sum += the rows of `count` tokens from place `begin` of the order on, eight on their way at a time.
+template <typename T, int LINES, typename A>
+__device__ __forceinline__ void add_run(const A& a, int begin, int count, int at, float (&sum)[Sixteen<T>::n]) {
+  constexpr int n = Sixteen<T>::n, kAhead = 8;
+  GSPMD_GLOBAL const int32_t* const order = (GSPMD_GLOBAL const int32_t*)a.order + begin;
+#pragma unroll 1
+  for (int i = 0; i < count; i += kAhead) {
+    u32x4_t v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) v[u] = load_line<LINES, T>(token_row<T>(a, order[min(i + u, count - 1)]), at, a.M);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      float f[n];
+      Sixteen<T>::open(v[u], f);
+#pragma unroll
+      for (int e = 0; e < n; ++e) sum[e] += i + u < count ? f[e] : 0.f;
+    }
+  }
+}
+
 // dw [M, V]: 64 entries x 16 lanes' 16 bytes of dw's rows a workgroup.  Sixteen lanes have an entry, four of them one after the other, on their way together: the row of its token, or the sum of its
-// tokens'.  They turn in LDS, rounded but for what is still to be added to (TTile float).  Bound by waits, for where runs begin, their tokens and the rows (9999 tokens, 1001 x 32003: 22 us, 64 MB of
+// tokens' (ALONE: added up here, of few tokens; 100 of 896, 2560 entries, in two launches 14.7 -> 11.5 us).  They turn in LDS, rounded but for what is still to be added to (TTile float).  Bound by waits, for where runs begin, their tokens and the rows (9999 tokens, 1001 x 32003: 22 us, 64 MB of
 // dw at 2.9 TB/s; 48 in all with neighbouring tiles on different XCDs, 44 with one).
 constexpr int kTurnEntries = 64, kTurnLanes = 16;
-template <typename T, int LINES, typename TTile, typename A>
+template <typename T, int LINES, typename TTile, bool ALONE, typename A>
 __global__ __launch_bounds__(256) void embed_grad_columns_kernel(const A a, int blocks_x) {
   constexpr int n = Sixteen<T>::n, kRows = kTurnLanes * n, side = 64 / kTurnLanes, kEach = kTurnEntries / (4 * side), kPitch = kTurnEntries + (sizeof(TTile) == 2 ? 2 : 1);
   __shared__ __attribute__((aligned(4))) TTile tile[n + kRows][kPitch];        // (n rows before the tile's: what the lane at the row's end has of its neighbours' may begin there)
@@ -317,7 +337,10 @@ __global__ __launch_bounds__(256) void embed_grad_columns_kernel(const A a, int 
   for (int u = 0; u < kEach; ++u) {
     float sum[n];
     Sixteen<T>::open(v[u], sum);
-    if (count[u] > 1 && col < a.M) load_sums<LINES, n>(a.sums + static_cast<int64_t>(begin[u] >> 1) * a.M, at, a.M, sum);
+    if (count[u] > 1 && col < a.M) {
+      if constexpr (ALONE) add_run<T, LINES>(a, begin[u] + 1, count[u] - 1, at, sum);
+      else load_sums<LINES, n>(a.sums + static_cast<int64_t>(begin[u] >> 1) * a.M, at, a.M, sum);
+    }
 #pragma unroll
     for (int e = 0; e < n; ++e)
       if (col < a.M) store_from_float<TTile>(&tile[n + at - m0 + e][r0 + u * 4 * side], count[u] > 0 ? sum[e] * a.scale : 0.f);
