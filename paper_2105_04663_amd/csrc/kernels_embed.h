@@ -359,14 +359,21 @@ __global__ __launch_bounds__(256) void embed_grad_columns_kernel(const A a, int 
       float f[n];
 #pragma unroll
       for (int e = 0; e < n; ++e) f[e] = tile[n + m][c + e];
-      if (a.accumulate) {                       // entries without tokens keep what they have
+      if (a.accumulate) {
+        const u32x4_t held = load_up_to(to, keep);
         float before[n];
-        Sixteen<T>::open(load_up_to(to, keep), before);
+        Sixteen<T>::open(held, before);
+        u32x4_t same = {0u, 0u, 0u, 0u};        // entries without tokens keep the bits they have, which float32 and back would change (a signalling NaN's)
 #pragma unroll
-        for (int e = 0; e < n; ++e)
-          if (e < keep && row0 + c + e < a.V) f[e] = begins[c + e] == begins[c + e + 1] ? before[e] : before[e] + f[e];
+        for (int e = 0; e < n; ++e) {
+          const bool there = e < keep && row0 + c + e < a.V, none = begins[c + e] == begins[c + e + 1];
+          f[e] = there ? before[e] + f[e] : f[e];
+          same[e * 4 / n] |= there && none ? (sizeof(T) == 2 ? 0xffffu << (e & 1) * 16 : ~0u) : 0u;
+        }
+        store_up_to(to, (held & same) | (Sixteen<T>::close(f) & ~same), keep);
+      } else {
+        store_up_to(to, Sixteen<T>::close(f), keep);
       }
-      store_up_to(to, Sixteen<T>::close(f), keep);
     }
   }
 }
