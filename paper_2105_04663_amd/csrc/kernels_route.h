@@ -369,7 +369,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const A a) {
 #pragma unroll
     for (int r = 1; r < R; ++r) best = fmaxf(best, v[r]);
     const float most = row_max(best), each = 1.f / route_total<R>(v, most, strange);
-    const bool none = most == -INFINITY && !strange;        // no expert at all
+    const bool none = row_ballot(chosen, lane) == 0 || (most == -INFINITY && !strange);        // a token without experts has no gradient, whatever its logits hold
 #pragma unroll
     for (int r = 0; r < R; ++r) v[r] = none ? 0.f : expf(v[r] - most) * each;
   }
