@@ -457,7 +457,8 @@ int32_t gspmd_route(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_shards
                     const gspmd_route_buf* route, void* workspace, int64_t workspace_bytes, void* hip_stream);
 /* The gradient with respect to the logits of sum of dweights * weights, dweights [T, k] f32 (ignored where there is no expert): p (g - sum of p g) over the softmax's experts, g an expert's
  * dweight or 0 (a token's choices of one expert, which gspmd_route never makes, add up).  Reads route's experts and weights.  dlogits: shards like logits, written whole (zeros for a token without experts, whatever its
- * logits hold, and in the padding).  Over all experts a NaN among the logits of a token that has experts makes its whole row NaN, as its weights are; over the chosen ones it takes no part. */
+ * logits hold, and in the padding).  Over all experts a NaN among the logits of a token that has experts makes its whole row NaN, as its weights are; over the chosen ones it takes no part, and
+ * experts that are not chosen have zeros, whatever the weights and their gradients are. */
 int32_t gspmd_route_grad(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_shards, const gspmd_sharding* logits_sh, int32_t choices, int32_t normalise,
                          const gspmd_route_buf* route, const float* dweights, const gspmd_shard_buf* dlogits_shards, void* hip_stream);
 

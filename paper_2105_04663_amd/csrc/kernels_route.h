@@ -373,7 +373,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const A a) {
 #pragma unroll
     for (int r = 0; r < R; ++r) v[r] = none ? 0.f : expf(v[r] - most) * each;
   }
-  const float mean = row_sum(w * g), own = a.normalise ? w * (g - mean) : w * g;
+  const float mean = row_sum(w * g), own = a.normalise ? w * (g - mean) : w * g, all = a.normalise ? 0.f : -mean;      // (what is not chosen: zeros, also where the mean is not finite)
 #pragma unroll
   for (int r = 0; r < R; ++r) add[of_row * R + r] = 0.f;
   staged_in_order();
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const A a) {
   }
   staged_in_order();
 #pragma unroll
-  for (int r = 0; r < R; ++r) v[r] = fmaf(v[r], -mean, add[of_row * R + r]);
+  for (int r = 0; r < R; ++r) v[r] = fmaf(v[r], all, add[of_row * R + r]);
   if (d == nullptr) return;
   constexpr int n = Sixteen<T>::n;
   if constexpr (R % n == 0) {

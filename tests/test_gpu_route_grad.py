@@ -58,3 +58,25 @@ def test_a_token_without_experts_has_no_gradient(normalise, dtype, E, k, x):
     else:
         assert got[13].isnan().all()
     check_ordinary(r, torch.tensor([i for i in range(T) if i not in (1, 4, 9, 12, 13, 15)]), got, dw)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("E, k, x", [(7, 3, 2), (16, 4, 1), (40, 2, 1), (64, 8, 3), (200, 5, 1), (512, 15, 1)])
+def test_experts_outside_the_softmax_have_no_gradient(dtype, E, k, x):
+    """Weights over the chosen experts: a NaN or an infinity among a token's weights or their gradients stays with those experts."""
+    T = 19
+    r = Routed(T, E, k, x=x, dtype=dtype, normalise=True, masked=0.0, seed=32)
+    r.z[T // 2] = 1.0
+    r.z[2, E // 2], r.z[5, 0], r.z[5, E - 1] = INF, INF, INF
+    r.stage().call()
+    experts = r.experts.cpu().long()
+    assert r.weights.cpu()[[2, 5]].isnan().any(dim=1).all()
+    dw = torch.randn(T, k, generator=torch.Generator().manual_seed(E))
+    dw[7, 0], dw[8, k - 1], dw[11, k // 2] = INF, NAN, -INF
+    got = gradient(r, dw)
+    strange = [2, 5, 7, 8, 11]
+    chosen = torch.zeros(T, E, dtype=torch.bool).scatter_(1, experts, True)
+    assert (got[~chosen] == 0).all()
+    for t in strange:
+        assert not got[t][chosen[t]].isfinite().all()
+    check_ordinary(r, torch.tensor([i for i in range(T) if i not in strange]), got, dw)
