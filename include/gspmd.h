@@ -423,7 +423,7 @@ int32_t gspmd_softmax_distill(const gspmd_mesh* mesh,
  * All buffers of a call have one type, bf16 or f32; products and sums are fp32, in one fixed order, rounded once (a scale of 1 copies bits).  Equal calls give equal bits.
  * accumulate: dw holds a gradient already, to which this one is added (the losses', of a matrix that serves both): entries without tokens keep their bits.  0: dw is written whole, zeros where there
  * are no tokens.  Padding of the static shapes is written as 0 either way.  All shards of one tensor have one row stride; distinct buffers of the same data are each written.
- * At most 64 shards of tokens and of the vocabulary, 2^24 tokens, rows of 2^21 elements.  Kernels only: both may be recorded into a HIP graph. */
+ * At most 64 shards of tokens and of the vocabulary, 2^24 tokens, rows of 2^21 elements; y from [V, M] of 2^37 bytes and more may be GSPMD_ERR_UNSUPPORTED.  Kernels only: both may be recorded into a HIP graph. */
 int32_t gspmd_embed(const gspmd_mesh* mesh, const int32_t* const* ids,
                     const gspmd_shard_buf* w_shards, const gspmd_sharding* w_sh, int32_t vocab_dim, float scale,
                     const gspmd_shard_buf* y_shards, const gspmd_sharding* y_sh, void* hip_stream);
@@ -469,7 +469,7 @@ int32_t gspmd_route_grad(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_s
  *   gspmd_combine       y[t, :] = sum over t's choices of weight * rows[slot, :], in their order; not `weighted`: weights of 1.  Reads slots, experts, weights
  *   gspmd_combine_grad  drows[slot, :] = weight * dy[t, :], dweights[t, i] = sum over M of dy[t, :] rows[slot, :] (0 where there is no slot)     reads slots, experts, weights
  * A partition's rows are those of its own experts, in their places: others, and those behind the last slot, are left as they were and never read.  The rows of y's padding are zeros.
- * Distinct buffers of the same data are each written; outputs must not overlap inputs.  Kernels only. */
+ * Distinct buffers of the same data are each written; outputs must not overlap inputs.  Tokens' rows of 2^36 bytes and more in all may be GSPMD_ERR_UNSUPPORTED.  Kernels only. */
 int32_t gspmd_dispatch(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const gspmd_sharding* x_sh, int32_t choices, const gspmd_route_buf* route,
                        const gspmd_shard_buf* rows_shards, const gspmd_sharding* rows_sh, void* hip_stream);
 int32_t gspmd_combine(const gspmd_mesh* mesh, const gspmd_shard_buf* rows_shards, const gspmd_sharding* rows_sh, int32_t choices, const gspmd_route_buf* route, int32_t weighted,

@@ -115,7 +115,7 @@ int32_t launch_embed(const A& a, int vocab_dim, hipStream_t stream) {
     const int log = row_lanes_log(a.M, n);
     const int64_t piece = static_cast<int64_t>(kEmbedUnroll) * n << log, per_group = int64_t(4) << (6 - log);
     const int64_t pieces = (a.M + piece - 1) / piece, groups = (rows + per_group - 1) / per_group * pieces;
-    if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
+    if (groups > kMostGroups) return GSPMD_ERR_UNSUPPORTED;
     const dim3 grid(static_cast<unsigned>(groups));
     return by_lines(lines_of<T>(a.M), [&](auto lines) {
       constexpr int L = decltype(lines)::value;
@@ -123,10 +123,10 @@ int32_t launch_embed(const A& a, int vocab_dim, hipStream_t stream) {
       else hipLaunchKernelGGL((embed_rows_kernel<T, L, true, A>), grid, dim3(256), 0, stream, a, log, static_cast<int>(pieces));
     });
   }
+  // blocks of tokens for eight XCDs along x (of 2^24 tokens 2^29 threads; a launch counts them in 32 bits along each dimension), and what each XCD takes one after the other along y
   const int64_t token_blocks = (rows + kColumnTokens - 1) / kColumnTokens, col_blocks = (a.M + kColumnCols - 1) / kColumnCols;
-  const int64_t groups = 8 * token_blocks * ((col_blocks + 7) / 8);
-  if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL((embed_columns_kernel<T, A>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, stream, a, static_cast<int>(token_blocks), static_cast<int>(col_blocks));
+  const dim3 grid(static_cast<unsigned>(8 * token_blocks), static_cast<unsigned>((col_blocks + 7) / 8));
+  hipLaunchKernelGGL((embed_columns_kernel<T, A>), grid, dim3(256), 0, stream, a, static_cast<int>(col_blocks));
   return launched();
 }
 
@@ -164,7 +164,7 @@ template <typename T, typename A>
 int32_t launch_turn(const Embed& e, const A& a, hipStream_t stream) {
   constexpr int n = Sixteen<T>::n, kRows = kTurnLanes * n;
   const int64_t across = (a.vs + kTurnEntries - 1) / kTurnEntries * static_cast<int64_t>(a.vocab_shards), tiles = across * ((a.M + kRows - 1) / kRows);
-  if (tiles > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
+  if (tiles > kMostGroups) return GSPMD_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(tiles)), block(256);
   const int x = static_cast<int>(across);
   return by_lines(a.M < n ? kExact : kNarrow, [&](auto lines) {

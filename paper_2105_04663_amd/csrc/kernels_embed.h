@@ -99,12 +99,12 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(const A a, int log_lane
 // one line a cycle from the caches for every lane (19870 tokens of 1792 from 5248 entries: 87 us).
 constexpr int kColumnTokens = 64, kColumnCols = 32;
 template <typename T, typename A>
-__global__ __launch_bounds__(256) void embed_columns_kernel(const A a, int token_blocks, int col_blocks) {
+__global__ __launch_bounds__(256) void embed_columns_kernel(const A a, int col_blocks) {
   __shared__ float tile[kColumnTokens][kColumnCols + 1];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, block = xcd + 8 * (turn / token_blocks);
+  const int xcd = blockIdx.x & 7, block = xcd + 8 * blockIdx.y;         // (eight divides gridDim.x)
   if (block >= col_blocks) return;
-  const int row0 = (turn % token_blocks) * kColumnTokens, col0 = block * kColumnCols, rows = a.ts * a.token_shards;
+  const int row0 = (blockIdx.x >> 3) * kColumnTokens, col0 = block * kColumnCols, rows = a.ts * a.token_shards;
   {
     const int row = row0 + lane;
     int id = -1;

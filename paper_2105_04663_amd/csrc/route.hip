@@ -194,7 +194,7 @@ int32_t launch_exchange(Exchanged what, const ExchangeArgs& a, hipStream_t strea
   const int64_t side = int64_t(4) << (6 - log), rows = what == kCombine ? static_cast<int64_t>(a.ts) * a.token_shards : what == kDispatch ? a.T : static_cast<int64_t>(a.T) * a.k;
   const int64_t piece = (static_cast<int64_t>(n) << log) * (what == kDispatch ? kExchangeUnroll : kCombineUnroll);
   const int64_t pieces = what == kCombineGrad ? 1 : (a.M + piece - 1) / piece, groups = (rows + side - 1) / side * pieces;
-  if (groups > INT32_MAX) return GSPMD_ERR_UNSUPPORTED;
+  if (groups > kMostGroups) return GSPMD_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(groups));
   return by_lines(lines_of<T>(a.M), [&](auto lines) {
     constexpr int L = decltype(lines)::value;

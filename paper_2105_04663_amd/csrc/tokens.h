@@ -11,6 +11,8 @@
 
 namespace gspmd {
 
+constexpr int64_t kMostGroups = UINT32_MAX / 256;      // workgroups of 256 along one dimension of a launch, whose threads are counted in 32 bits
+
 inline int32_t launched() { return hipGetLastError() == hipSuccess ? GSPMD_OK : GSPMD_ERR_DEVICE; }
 
 // The mesh dimension that splits a tensor's dimension (one of size 1 splits nothing), or -1.
