@@ -304,6 +304,9 @@ __global__ __launch_bounds__(256) void embed_grad_columns_kernel(const A a, int 
   constexpr int n = Sixteen<T>::n, kRows = kTurnLanes * n, side = 64 / kTurnLanes, kEach = kTurnEntries / (4 * side), kPitch = kTurnEntries + (sizeof(TTile) == 2 ? 2 : 1);
   __shared__ __attribute__((aligned(4))) TTile tile[n + kRows][kPitch];        // (n rows before the tile's: what the lane at the row's end has of its neighbours' may begin there)
   __shared__ int begins[kTurnEntries + 1];
+  // Of a row of the tile as words of dw, what is added to what is there, and what keeps its bits: entries without tokens, which float32 and back would change (a signalling NaN).  Padding is neither, and 0.
+  constexpr int kWords = sizeof(TTile) == 4 ? kTurnEntries * sizeof(T) / 4 : 0;
+  __shared__ __attribute__((aligned(16))) uint32_t added[kWords > 0 ? kWords : 1], kept[kWords > 0 ? kWords : 1];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   // neighbouring entries' tiles, whose lines of dw are shared where rows are not aligned, on one XCD
   const int logical = logical_tile(blockIdx.x, gridDim.x), block_m = logical / blocks_x, block_x = logical - block_m * blocks_x;
@@ -314,6 +317,19 @@ __global__ __launch_bounds__(256) void embed_grad_columns_kernel(const A a, int 
   if (dw == nullptr) return;
   if (t <= kTurnEntries) begins[t] = a.T > 0 ? ((GSPMD_GLOBAL const int32_t*)a.begins)[min(row0 + t, a.V)] : 0;
   __syncthreads();
+  if (a.accumulate && t < kWords) {
+    constexpr int each = 4 / sizeof(T);
+    uint32_t sums = 0u, same = 0u;
+#pragma unroll
+    for (int i = 0; i < each; ++i) {
+      const int r = t * each + i;
+      const uint32_t bits = each == 1 ? ~0u : 0xffffu << 16 * i;
+      if (begins[r] != begins[r + 1]) sums |= bits;
+      else if (row0 + r < a.V) same |= bits;
+    }
+    added[t] = sums;
+    kept[t] = same;
+  }
   const int col = m0 + (lane & (kTurnLanes - 1)) * n, at = line_at<LINES, T>(col, a.M), r0 = wave * side + lane / kTurnLanes;
   int begin[kEach], count[kEach], token[kEach];
   u32x4_t v[kEach];
@@ -363,14 +379,10 @@ __global__ __launch_bounds__(256) void embed_grad_columns_kernel(const A a, int 
         const u32x4_t held = load_up_to(to, keep);
         float before[n];
         Sixteen<T>::open(held, before);
-        u32x4_t same = {0u, 0u, 0u, 0u};        // entries without tokens keep the bits they have, which float32 and back would change (a signalling NaN's)
 #pragma unroll
-        for (int e = 0; e < n; ++e) {
-          const bool there = e < keep && row0 + c + e < a.V, none = begins[c + e] == begins[c + e + 1];
-          f[e] = there ? before[e] + f[e] : f[e];
-          same[e * 4 / n] |= there && none ? (sizeof(T) == 2 ? 0xffffu << (e & 1) * 16 : ~0u) : 0u;
-        }
-        store_up_to(to, (held & same) | (Sixteen<T>::close(f) & ~same), keep);
+        for (int e = 0; e < n; ++e) f[e] += before[e];
+        const int at = c / n * 4;
+        store_up_to(to, (held & *reinterpret_cast<const u32x4_t*>(kept + at)) | (Sixteen<T>::close(f) & *reinterpret_cast<const u32x4_t*>(added + at)), keep);
       } else {
         store_up_to(to, Sixteen<T>::close(f), keep);
       }
