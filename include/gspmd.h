@@ -282,7 +282,8 @@ int32_t gspmd_grouped_dot_noalloc(const gspmd_mesh* mesh, const gspmd_dot_dims* 
  * lead out of the buffers.  Of a packed out the rows behind the last slot are left as they were; an expert without slots has a matrix of zeros.
  * Only dimension 0 may be split, alike in all three (else GSPMD_ERR_NEEDS_RESHARD): a partition reads and writes its own experts' slots, in their places in the whole array, and no others; of partitions
  * that share one out buffer that is the whole array.  lhs_shards, rhs_shards, out_shards: P entries by partition id; partitions of the same experts may share
- * buffers, distinct out buffers are each written.  Matrices of padded experts are written as zeros.  Types, row strides, epilogue and accumulation as gspmd_grouped_dot; out must not overlap the operands.
+ * buffers, distinct out buffers are each written.  Matrices of padded experts are written as zeros.  Types, row strides, epilogue and accumulation as gspmd_grouped_dot, but for
+ * bfloat16 operands' longest rows: strides of up to 2^22 elements where K is contiguous (lhs, and rhs [E, H, M], of the first form), else 2^24; longer ones are GSPMD_ERR_UNSUPPORTED.  out must not overlap the operands.
  * No workspace; kernels only, so the call may be recorded into a HIP graph, whose replays read the sizes anew.  Equal sizes, values and alignments give equal bits; one row's
  * may differ with how many the others are (within fp32 accumulation). */
 int32_t gspmd_ragged_dot(const gspmd_mesh* mesh, const gspmd_dot_dims* dims,
