@@ -469,7 +469,7 @@ int32_t gspmd_route_grad(const gspmd_mesh* mesh, const gspmd_shard_buf* logits_s
  *   gspmd_dispatch      rows[slot, :] = x[t, :] for t's choices              reads slots, experts; its gradient is gspmd_combine of the rows' gradient, not weighted
  *   gspmd_combine       y[t, :] = sum over t's choices of weight * rows[slot, :], in their order; not `weighted`: weights of 1.  Reads slots, experts, weights
  *   gspmd_combine_grad  drows[slot, :] = weight * dy[t, :], dweights[t, i] = sum over M of dy[t, :] rows[slot, :] (0 where there is no slot)     reads slots, experts, weights
- * A partition's rows are those of its own experts, in their places: others, and those behind the last slot, are left as they were and never read.  The rows of y's padding are zeros.
+ * A partition's rows are those of its own experts, in their places: others, and those behind the last slot, are left as they were and take no part, whatever they hold.  The rows of y's padding are zeros.
  * Distinct buffers of the same data are each written; outputs must not overlap inputs.  Tokens' rows of 2^36 bytes and more in all may be GSPMD_ERR_UNSUPPORTED.  Kernels only. */
 int32_t gspmd_dispatch(const gspmd_mesh* mesh, const gspmd_shard_buf* x_shards, const gspmd_sharding* x_sh, int32_t choices, const gspmd_route_buf* route,
                        const gspmd_shard_buf* rows_shards, const gspmd_sharding* rows_sh, void* hip_stream);

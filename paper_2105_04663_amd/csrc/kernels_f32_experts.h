@@ -2,7 +2,8 @@
 //
 // Operands go from memory into registers, where v_mfma_f32_16x16x4_f32 takes them as they lie, 16 bytes a lane along whatever is contiguous.  A K-contiguous operand gives a lane four k of a row, one for
 // each of four MFMAs; a K-major one four neighbouring columns of a k, one for each of four blocks of sixteen, whose columns are then every fourth.  No LDS and no barrier in the loop: each of the four waves has 16
-// of every 64 k, kF32ExpertsAhead such steps on their way, and their sums meet in LDS once, in the order of the waves.  Sums are folded by 32 products, as dot_f32_kernel's by 64.
+// of every 64 k, kF32ExpertsAhead such steps on their way, and their sums meet in LDS once, in the order of the waves.  Sums are folded by 32 products, as dot_f32_kernel's by 96
+// or 64 (relative to float64, rows of 2240 1.4e-7, of 4096 1.5e-7).
 // Bound by the matrices, read once where an expert has up to 16 rows (us, dot_f32_kernel / this: 35 experts of 3 rows, 3378 x 2950 286 / 247; 77 of
 // 1.5, 320 x 4096 60 / 41; 5 of 6, 1024 x 640 18.4 / 10.2).  Two steps ahead and four workgroups on a compute unit: with four and three 45 for the second, 6 and two 50.
 #pragma once

@@ -192,7 +192,9 @@ __global__ __launch_bounds__(kOrderThreads) void route_kernel(const A a, int32_t
 static_assert(kMostExperts <= kOrderThreads, "a thread for every expert");
 
 // Where a tile's choices begin, of every expert: the choices of lower experts, and those of its own in earlier tiles.  With few tiles a workgroup adds them up itself (route_places_kernel); with many, one
-// for every expert turns the tiles' counts into sums of the earlier ones, and its total.
+// for every expert turns the tiles' counts into sums of the earlier ones, and its total.  What the first reads grows with the square of the tiles, the second is a launch more (the whole routing, us, first /
+// second; tokens x experts, choices: 8192 x 64, 2 9.2 / 11.4; 16384 x 16, 2 8.9 / 11.7, x 128, 8 14.6 / 15.2, x 256, 2 16.3 / 15.6, x 512, 2 27.8 / 25.1; 32768 x 8, 2 9.6 / 11.2, x 64, 2 13.7 / 13.2, x 128, 8
+// 23.9 / 21.0, x 256, 2 29.1 / 21.7; 65536 x 8, 2 16.3 / 16.1, x 64, 2 27.5 / 20.6).  512 tiles, of 64 tokens, are where they cross with 64 experts; with more of them it is earlier, which the rule does not follow.
 constexpr int kTilesSummed = 512;
 __global__ __launch_bounds__(kOrderThreads) static void route_sums_kernel(int32_t* counts, int tiles, int E, int32_t* totals) {
   __shared__ uint32_t sums[kOrderWaves];

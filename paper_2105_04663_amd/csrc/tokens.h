@@ -21,12 +21,6 @@ inline int split_axis(const gspmd_mesh* mesh, const gspmd_sharding* sh, int dim)
   return a >= 0 && mesh->shape[a] > 1 ? a : -1;
 }
 
-inline int64_t partitions(const gspmd_mesh* mesh) {
-  int64_t n = 1;
-  for (int i = 0; i < mesh->rank; ++i) n *= mesh->shape[i];
-  return n;
-}
-
 // Type, row stride (the same for all of a tensor's shards) and alignment of a shard buffer.
 inline int32_t check_rows(const gspmd_shard_buf& b, int32_t dtype, int64_t cols, bool elements, int64_t* ld) {
   if (b.dtype != dtype) return GSPMD_ERR_UNSUPPORTED;
