@@ -298,6 +298,7 @@ __device__ __forceinline__ void add_run(const A& a, int begin, int count, int at
 // dw [M, V]: 64 entries x 16 lanes' 16 bytes of dw's rows a workgroup.  Sixteen lanes have an entry, four of them one after the other, on their way together: the row of its token, or the sum of its
 // tokens' (ALONE: added up here, of few tokens; 100 of 896, 2560 entries, in two launches 14.7 -> 11.5 us).  They turn in LDS, rounded but for what is still to be added to (TTile float).  Bound by waits, for where runs begin, their tokens and the rows (9999 tokens, 1001 x 32003: 22 us, 64 MB of
 // dw at 2.9 TB/s; 48 in all with neighbouring tiles on different XCDs, 44 with one).
+// Added to what is there every tile reads its part of dw, too: 53 in all; 100 tokens, 2048 x 32000 51, written whole 36.
 constexpr int kTurnEntries = 64, kTurnLanes = 16;
 template <typename T, int LINES, typename TTile, bool ALONE, typename A>
 __global__ __launch_bounds__(256) void embed_grad_columns_kernel(const A a, int blocks_x) {
